@@ -593,6 +593,51 @@ int32_t mz_attention_auto_splits_keys(int32_t m, int32_t max_pos, int64_t keys, 
                                       int32_t chunk_tokens, int32_t n_q_heads, int32_t n_kv_heads,
                                       int32_t head_dim, int64_t workspace_bytes);
 
+/* ---- a decode step of many sequences ----------------------------------- */
+/* The calls below carry one step of several requests at once over one set of
+ * weights and one slab of chunk slots, each sequence with its own row of a
+ * chunk table: after the step's projections (mz_q4_gemm_ex, with
+ * mz_lora_add), mz_kv_append puts the new keys and values into the chunks,
+ * mz_attention_batch reads them, and mz_logits_rules picks the tokens.
+ * Lengths, positions and tables are read on the device, so one captured
+ * graph serves steps of any lengths.  Each call allocates nothing and
+ * enqueues on stream, which must belong to the current device (EINVAL). */
+
+typedef struct {
+  const void *q, *k, *v;     /* device: rows of query, key and value heads before rotation, [m][n_q_heads *
+                                head_dim], [m][n_kv_heads * head_dim] twice; q may be NULL with n_q_heads 0 */
+  int64_t q_stride, k_stride, v_stride;   /* elements from a row to the next (0: rows follow each other), so
+                                that the three may be parts of one fused projection's rows */
+  int32_t f32;               /* 1: q, k and v are fp32 (a projection's output); 0: f16 */
+  int32_t head_dim;          /* 32, 64 or 128 */
+  int32_t n_q_heads, n_kv_heads;
+  const int32_t *seq;        /* device int32 [m]: sequence of the row */
+  const int32_t *pos;        /* device int32 [m]: its position */
+  const void *rope_cs;       /* device float2 [n_rope][head_dim / 2], as in mz_q4_gemm_args */
+  int32_t n_rope;
+  int32_t n_slots;           /* chunk slots in slab */
+  void *slab;                /* device: slots laid out as in mz_attention */
+  const int32_t *table;      /* device int32 [n_seq][n_table]: slot of each sequence's chunks */
+  int32_t n_seq, n_table;
+  int32_t chunk_tokens;      /* a power of two >= 8 */
+  void *q_out;               /* device f16 [m][n_q_heads * head_dim]: the rotated queries */
+} mz_kv_append_args;
+
+/* Rotate the keys of m rows of any sequences to their positions (rotate-half
+ * pairs i, i + head_dim/2, as the rotary epilogues of mz_q4_gemm_ex, the same
+ * bits) and write them with the values into the chunks (paper Sec. 4.2) that
+ * the sequences' tables name; rotate the rows' queries into q_out.  Rows may
+ * come in any order, a whole prompt or one row per sequence.  A row whose seq
+ * is outside 0..n_seq-1 (padding), or whose pos is outside 0..n_rope-1 or the
+ * table, writes nothing, its row of q_out included; one whose chunk's entry is
+ * outside 0..n_slots-1 writes its query only.  The caller sees that no two
+ * rows name the same position of a sequence and that no two sequences share
+ * a chunk that is written.  m may be 0.  Errors: EINVAL for a NULL pointer,
+ * sizes or heads out of range, a stride below the row, n_table * chunk_tokens
+ * above 2^31 - 1, or rows (pointers, strides), rope_cs, slab or q_out off
+ * 16-byte boundaries. */
+mz_status mz_kv_append(const mz_kv_append_args *args, int32_t m, void *stream);
+
 /* x = h / sqrt(mean(h^2) + eps) per row: h float [m][d] -> x f16 [m][d]. */
 mz_status mz_rmsnorm(const void *h_f32, int32_t m, int32_t d, float eps, void *x_f16,
                      void *stream);

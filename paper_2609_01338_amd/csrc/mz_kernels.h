@@ -153,6 +153,25 @@ void launch_rope_kv(const float* qkv, int qkv_stride, int m, const int32_t* pos,
                     const int64_t* kv_off, const float2* rope_cs, int nq, int nkv, int hd, int C,
                     void* q_out, void* slab, hipStream_t s);
 
+// Keys and values of m rows of many sequences, rotated and written through
+// the sequences' chunk tables, and the rows' queries rotated (see mz.h,
+// mz_kv_append).  q, k, v: rows of fp32 or f16, strides in elements; C = 1 <<
+// cshift; hd 32, 64 or 128; nq 0 leaves the queries out.  Every pointer and
+// row 16-byte aligned.  Only for kv_append_fits(m, ...).
+struct KvAppend {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t *seq, *pos;
+  const float2* rope_cs;
+  uint8_t* slab;
+  int64_t slot_bytes;
+  const int32_t* table;
+  _Float16* q_out;
+  int n_rope, n_slots, n_seq, n_table, C, cshift, nq, nkv, hd;
+};
+bool kv_append_fits(int m, int nq, int nkv, int hd);
+void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s);
+
 // h float [m][d] = dequant(E[tok[i]]) with E split into nibbles [V][d/2] and
 // fp16 scales [V][d/32]; with last_tok (device) row m - 1 takes *last_tok.
 void launch_embed(const uint8_t* e_nib, const uint16_t* e_scale, const int32_t* tok, int m, int d,

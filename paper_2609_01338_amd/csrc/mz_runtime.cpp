@@ -2062,6 +2062,75 @@ mz_status mz_attention_split(const void* q, const int32_t* qpos, int32_t m, int3
   });
 }
 
+// ---- a decode step of many sequences
+
+static void check_stream(void* stream) {
+  if (!stream) return;
+  int cur = -1;
+  hipDevice_t dev = -1;
+  if (hipGetDevice(&cur) != hipSuccess || hipStreamGetDevice((hipStream_t)stream, &dev) != hipSuccess || dev != cur)
+    fail(MZ_EINVAL, "the stream must belong to the current device");
+}
+
+static void check_chunks(int32_t n_seq, int32_t n_slots, int32_t n_table, int32_t chunk_tokens) {
+  if (n_seq < 1 || n_slots < 1 || n_table < 1) fail(MZ_EINVAL, "n_seq, n_slots and n_table must be positive");
+  if (chunk_tokens < 8 || (chunk_tokens & (chunk_tokens - 1)))
+    fail(MZ_EINVAL, "chunk_tokens must be a power of two >= 8");
+  if ((int64_t)n_table * chunk_tokens > INT32_MAX) fail(MZ_EINVAL, "n_table * chunk_tokens exceeds 2^31 - 1");
+}
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!args) fail(MZ_EINVAL, "args is NULL");
+    const mz_kv_append_args& a = *args;
+    if (m < 0) fail(MZ_EINVAL, "m is negative");
+    if (!a.k || !a.v || !a.seq || !a.pos || !a.rope_cs || !a.slab || !a.table) fail(MZ_EINVAL, "NULL pointer");
+    if (a.head_dim != 32 && a.head_dim != 64 && a.head_dim != 128) fail(MZ_EINVAL, "head_dim must be 32, 64 or 128");
+    if (a.n_kv_heads < 1 || a.n_kv_heads > 1024 || a.n_q_heads < 0 || a.n_q_heads > 1024)
+      fail(MZ_EINVAL, "bad head counts");
+    if (a.n_q_heads > 0 && (!a.q || !a.q_out)) fail(MZ_EINVAL, "n_q_heads without q or q_out");
+    if (a.f32 != 0 && a.f32 != 1) fail(MZ_EINVAL, "f32 must be 0 or 1");
+    if (a.n_rope < 1) fail(MZ_EINVAL, "n_rope must be positive");
+    check_chunks(a.n_seq, a.n_slots, a.n_table, a.chunk_tokens);
+    const int64_t dkv = (int64_t)a.n_kv_heads * a.head_dim, dq = (int64_t)a.n_q_heads * a.head_dim;
+    mzk::KvAppend k{};
+    k.k_stride = a.k_stride ? a.k_stride : dkv;
+    k.v_stride = a.v_stride ? a.v_stride : dkv;
+    k.q_stride = a.q_stride ? a.q_stride : dq;
+    const int64_t step = a.f32 ? 4 : 8;   // elements of 16 bytes
+    if (k.k_stride < dkv || k.v_stride < dkv || k.q_stride < dq) fail(MZ_EINVAL, "a row stride is below the row");
+    if (k.k_stride % step || k.v_stride % step || k.q_stride % step || !aligned16(a.k) || !aligned16(a.v) ||
+        !aligned16(a.rope_cs) || !aligned16(a.slab) || (a.n_q_heads && (!aligned16(a.q) || !aligned16(a.q_out))))
+      fail(MZ_EINVAL, "rows, rope_cs, slab and q_out must lie on 16-byte boundaries");
+    if (!mzk::kv_append_fits(m, a.n_q_heads, a.n_kv_heads, a.head_dim)) fail(MZ_EINVAL, "too many rows");
+    check_stream(stream);
+    if (m == 0) return;
+    k.q = a.q;
+    k.k = a.k;
+    k.v = a.v;
+    k.seq = a.seq;
+    k.pos = a.pos;
+    k.rope_cs = reinterpret_cast<const float2*>(a.rope_cs);
+    k.slab = reinterpret_cast<uint8_t*>(a.slab);
+    k.slot_bytes = a.chunk_tokens * dkv * 4;
+    k.table = a.table;
+    k.q_out = reinterpret_cast<_Float16*>(a.q_out);
+    k.n_rope = a.n_rope;
+    k.n_slots = a.n_slots;
+    k.n_seq = a.n_seq;
+    k.n_table = a.n_table;
+    k.C = a.chunk_tokens;
+    k.cshift = __builtin_ctz((unsigned)a.chunk_tokens);
+    k.nq = a.n_q_heads;
+    k.nkv = a.n_kv_heads;
+    k.hd = a.head_dim;
+    mzk::launch_kv_append(k, m, a.f32 != 0, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
 mz_status mz_rmsnorm(const void* h, int32_t m, int32_t d, float eps, void* x, void* stream) {
   return guarded(nullptr, [&] {
     if (!h || !x) fail(MZ_EINVAL, "NULL pointer");

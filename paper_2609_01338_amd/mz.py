@@ -63,6 +63,16 @@ class mz_q4_gemm_args(ctypes.Structure):
                 ("n_valid", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32)]
 
 
+class mz_kv_append_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("f32", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("seq", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("rope_cs", ctypes.c_void_p), ("n_rope", ctypes.c_int32), ("n_slots", ctypes.c_int32),
+                ("slab", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_seq", ctypes.c_int32),
+                ("n_table", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32), ("q_out", ctypes.c_void_p)]
+
+
 SIZE_RULES = {"paper": 0, "total": 1}
 STAGES = ("kv-only", "kv-and-w", "w-only", "exhausted")
 _INFO_KEYS = ("released", "T", "stage", "link_s", "recompute_s", "n_kv", "n_w", "reached")
@@ -116,6 +126,7 @@ def lib() -> ctypes.CDLL:
         "mz_q4_gemm_queued": ([vp, i32, i32, i32, vp, i32, vp, vp, vp], i32),
         "mz_q4_gemm_ex": ([vp, i32, i32, i32, vp, i32, ctypes.POINTER(mz_q4_gemm_args), vp, vp], i32),
         "mz_q4_gemv": ([vp, i32, vp, i32, i32, ctypes.POINTER(mz_q4_gemm_args), vp, ctypes.c_float, vp, vp], i32),
+        "mz_kv_append": ([ctypes.POINTER(mz_kv_append_args), i32, vp], i32),
         "mz_rmsnorm": ([vp, i32, i32, ctypes.c_float, vp, vp], i32),
         "mz_probe_ceilings": ([i32, ctypes.c_char_p, sz], i32),
         "mz_plan_evict": ([ctypes.POINTER(mz_model_cfg), ctypes.POINTER(mz_evict_request), vp, vp, vp], i32),
@@ -438,6 +449,16 @@ def mz_attention_auto_splits_keys(m: int, max_pos: int, keys: int, n_table: int,
                                   head_dim: int, ws_bytes: int) -> int:
     return int(lib().mz_attention_auto_splits_keys(m, max_pos, keys, n_table, chunk_tokens, n_q, n_kv, head_dim,
                                                    ws_bytes))
+
+
+def mz_kv_append(m: int, k_ptr: int, v_ptr: int, seq_ptr: int, pos_ptr: int, rope_cs_ptr: int, n_rope: int,
+                 slab_ptr: int, n_slots: int, table_ptr: int, n_seq: int, n_table: int, chunk_tokens: int, n_kv: int,
+                 head_dim: int, stream: Optional[int] = None, q_ptr: int = 0, n_q: int = 0, q_out_ptr: int = 0,
+                 k_stride: int = 0, v_stride: int = 0, q_stride: int = 0, f32: bool = True) -> None:
+    """Rows of many sequences into their chunks; strides in elements (0: rows follow each other)."""
+    a = mz_kv_append_args(q_ptr, k_ptr, v_ptr, q_stride, k_stride, v_stride, f32, head_dim, n_q, n_kv, seq_ptr, pos_ptr,
+                          rope_cs_ptr, n_rope, n_slots, slab_ptr, table_ptr, n_seq, n_table, chunk_tokens, q_out_ptr)
+    _check(lib().mz_kv_append(ctypes.byref(a), m, stream), None)
 
 
 def mz_rmsnorm(h_ptr: int, m: int, d: int, eps: float, x_ptr: int, stream: Optional[int] = None) -> None:

@@ -1,0 +1,56 @@
+"""Refusals of the calls that carry a decode step of many sequences: every one
+is found on the host before anything is enqueued, so they need no GPU.  The
+device pointers are never followed."""
+
+import os
+
+import pytest
+
+from paper_2609_01338_amd import mz
+
+P = 4096          # stands for a device pointer on a 16-byte boundary
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not os.path.exists(mz.LIB_PATH):
+        from paper_2609_01338_amd import build
+        build.build_all()
+    mz.lib()
+
+
+def refused(fn, *args, match=None, **kw):
+    with pytest.raises(mz.MzError) as e:
+        fn(*args, **kw)
+    assert e.value.status == mz.MZ_EINVAL
+    if match:
+        assert match in str(e.value), str(e.value)
+
+
+APPEND = dict(m=3, k_ptr=P, v_ptr=P, seq_ptr=P, pos_ptr=P, rope_cs_ptr=P, n_rope=64, slab_ptr=P, n_slots=4, table_ptr=P,
+              n_seq=2, n_table=4, chunk_tokens=16, n_kv=2, head_dim=64, q_ptr=P, n_q=4, q_out_ptr=P)
+
+
+@pytest.mark.parametrize("bad,match", [
+    (dict(m=-1), "negative"),
+    (dict(k_ptr=0), "NULL"), (dict(v_ptr=0), "NULL"), (dict(seq_ptr=0), "NULL"), (dict(pos_ptr=0), "NULL"),
+    (dict(rope_cs_ptr=0), "NULL"), (dict(slab_ptr=0), "NULL"), (dict(table_ptr=0), "NULL"),
+    (dict(q_ptr=0), "q_out"), (dict(q_out_ptr=0), "q_out"),
+    (dict(head_dim=48), "head_dim"), (dict(head_dim=256), "head_dim"),
+    (dict(n_kv=0), "head"), (dict(n_q=-1), "head"), (dict(n_kv=1025), "head"),
+    (dict(n_rope=0), "n_rope"), (dict(n_slots=0), "positive"), (dict(n_seq=0), "positive"), (dict(n_table=0), "positive"),
+    (dict(chunk_tokens=4), "chunk_tokens"), (dict(chunk_tokens=24), "chunk_tokens"), (dict(chunk_tokens=-8), "chunk_tokens"),
+    (dict(n_table=1 << 27), "2^31"),
+    (dict(k_stride=124), "stride"), (dict(v_stride=64), "stride"), (dict(q_stride=-256), "stride"),
+    (dict(k_stride=130), "16-byte"), (dict(v_stride=129), "16-byte"), (dict(q_stride=258), "16-byte"),
+    (dict(f32=False, k_stride=132), "16-byte"),
+    (dict(k_ptr=P + 4), "16-byte"), (dict(v_ptr=P + 8), "16-byte"), (dict(q_ptr=P + 2), "16-byte"),
+    (dict(slab_ptr=P + 8), "16-byte"), (dict(rope_cs_ptr=P + 8), "16-byte"), (dict(q_out_ptr=P + 8), "16-byte"),
+    (dict(f32=2), "f32"), (dict(m=(1 << 31) - 1, n_q=1024, n_kv=1024, head_dim=128), "too many"),
+])
+def test_kv_append_refusals(bad, match):
+    refused(mz.mz_kv_append, **{**APPEND, **bad}, match=match)
+
+
+def test_kv_append_no_rows():
+    mz.mz_kv_append(**{**APPEND, "m": 0})     # nothing to do, nothing enqueued

@@ -1,0 +1,242 @@
+"""The calls that carry a decode step of many sequences -- the append to the
+chunked caches, the attention over them, the adapters beside a projection and
+the rules on the logits -- against plain implementations in 64 bits.
+
+Roundings: u16 = 2^-11 is half a step of f16 relative to the value (2^-25
+below its normal range), u32 = 2^-24 half a step of fp32.
+"""
+
+import numpy as np
+import pytest
+
+from paper_2609_01338_amd import mz
+from gpu_util import report, stream, torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+U16, U32, TINY16 = 2.0 ** -11, 2.0 ** -24, 2.0 ** -25
+
+
+def dev(a):
+    return torch_cuda().from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def close(got, ref, bound, what):
+    """got (device or host) within bound of ref everywhere; NaN and infinities at the same places."""
+    got = got.double().cpu().numpy() if hasattr(got, "cpu") else np.asarray(got, np.float64)
+    ref, bound = np.broadcast_arrays(np.asarray(ref, np.float64), np.asarray(bound, np.float64))
+    fine = np.isfinite(ref)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), what + ": NaN"
+    assert np.array_equal(got[~fine & ~np.isnan(ref)], ref[~fine & ~np.isnan(ref)]), what + ": infinities"
+    err = np.abs(got[fine] - ref[fine])
+    worst = float((err / np.maximum(bound[fine], 1e-300)).max()) if err.size else 0.0
+    report("  " + what, worst_of_bound=round(worst, 4), max_err=float(err.max()) if err.size else 0.0)
+    assert np.all(err <= bound[fine]), what
+
+
+def rope_table(n, hd, theta=1e4):
+    a = np.arange(n)[:, None] * theta ** (-2.0 * np.arange(hd // 2) / hd)
+    return np.stack([np.cos(a), np.sin(a)], 2).astype(np.float32)
+
+
+# ----------------------------------------------------------------------------- append
+
+def append_oracle(k, v, q, seq, pos, rope, slab, table, C, nkv, hd):
+    """What the rows leave: (slab, its bound, q, its bound, rows of q that are written)."""
+    m, n_slots = len(seq), slab.shape[0]
+    dkv, h2 = nkv * hd, hd // 2
+
+    def turn(x, p):
+        c, s = rope[p, :, 0].astype(np.float64), rope[p, :, 1].astype(np.float64)
+        a, b = x[:, :h2], x[:, h2:]
+        y = np.concatenate([a * c - b * s, b * c + a * s], 1)
+        part = np.concatenate([np.abs(a * c) + np.abs(b * s), np.abs(b * c) + np.abs(a * s)], 1)
+        # two fp32 roundings, then one to f16
+        return y, U16 * np.abs(y) + TINY16 + 2 * U32 * part * (1 + U16)
+
+    out, bound = slab.astype(np.float64), np.zeros(slab.shape)
+    kh, vh = out[:, :C * dkv].reshape(n_slots, C, nkv, hd), out[:, C * dkv:].reshape(n_slots, dkv, C)
+    kb = bound[:, :C * dkv].reshape(n_slots, C, nkv, hd)
+    qo, qb, wrote = None, None, np.zeros(m, bool)
+    if q is not None:
+        qo, qb = np.zeros(q.shape), np.zeros(q.shape)
+    for r in range(m):
+        s, p = int(seq[r]), int(pos[r])
+        if not (0 <= s < table.shape[0] and 0 <= p < rope.shape[0] and p // C < table.shape[1]):
+            continue
+        if q is not None:
+            y, b = turn(q[r].reshape(-1, hd).astype(np.float64), p)
+            qo[r], qb[r], wrote[r] = y.reshape(-1), b.reshape(-1), True
+        slot = int(table[s, p // C])
+        if 0 <= slot < n_slots:
+            kh[slot, p % C], kb[slot, p % C] = turn(k[r].reshape(nkv, hd).astype(np.float64), p)
+            vh[slot, :, p % C] = v[r].astype(np.float16).astype(np.float64)
+    return out, bound, qo, qb, wrote
+
+
+def append_run(k, v, q, seq, pos, rope, slab, table, C, nkv, hd, f32, fused, st=None):
+    torch = torch_cuda()
+    m, dkv = len(seq), nkv * hd
+    dt, size = (np.float32, 4) if f32 else (np.float16, 2)
+    d_slab, d_rope, d_seq, d_pos, d_table = dev(slab), dev(rope), dev(seq), dev(pos), dev(table)
+    nq = 0 if q is None else q.shape[1] // hd
+    q_out = torch.full((m, max(nq, 1) * hd), 7.0, device="cuda", dtype=torch.float16)
+    kw = {}
+    if fused:      # one buffer of rows, as a projection leaves them, with a tail behind each row
+        parts = ([q] if q is not None else []) + [k, v, np.full((m, 16), np.nan)]
+        rows = dev(np.concatenate(parts, 1).astype(dt))
+        base = rows.data_ptr()
+        kp, vp = base + nq * hd * size, base + (nq * hd + dkv) * size
+        kw = dict(k_stride=rows.shape[1], v_stride=rows.shape[1], q_stride=rows.shape[1])
+        if q is not None:
+            kw.update(q_ptr=base, n_q=nq, q_out_ptr=q_out.data_ptr())
+    else:
+        dk, dv = dev(k.astype(dt)), dev(v.astype(dt))
+        kp, vp = dk.data_ptr(), dv.data_ptr()
+        if q is not None:
+            dq = dev(q.astype(dt))
+            kw.update(q_ptr=dq.data_ptr(), n_q=nq, q_out_ptr=q_out.data_ptr())
+    mz.mz_kv_append(m, kp, vp, d_seq.data_ptr(), d_pos.data_ptr(), d_rope.data_ptr(), rope.shape[0], d_slab.data_ptr(),
+                    slab.shape[0], d_table.data_ptr(), table.shape[0], table.shape[1], C, nkv, hd,
+                    stream() if st is None else st, f32=f32, **kw)
+    torch.cuda.synchronize()
+    return d_slab, q_out
+
+
+def append_case(spans, C, nq, nkv, hd, f32, seed, shuffle=False, extra=(), fused=True, bad_slots=()):
+    """spans: (first position, rows) per sequence; extra: (seq, pos) rows that must write nothing;
+    bad_slots: (sequence, chunk, entry) written over the table."""
+    rng = np.random.default_rng(seed)
+    rows = [(s, p + i) for s, (p, n) in enumerate(spans) for i in range(n)] + list(extra)
+    if shuffle:
+        rng.shuffle(rows)
+    seq, pos = (np.array([r[i] for r in rows], np.int32) for i in (0, 1))
+    m, n_table = len(rows), max(p + n for p, n in spans) // C + 1
+    n_slots = len(spans) * n_table + 3
+    table = rng.permutation(n_slots)[:len(spans) * n_table].reshape(len(spans), n_table).astype(np.int32)
+    for s, c, e in bad_slots:
+        table[s, c] = e
+    rope = rope_table(max(p + n for p, n in spans), hd)
+    dt = np.float32 if f32 else np.float16
+    draw = lambda h: rng.standard_normal((m, h * hd)).astype(dt)  # noqa: E731
+    q, k, v = (draw(nq) if nq else None), draw(nkv), draw(nkv)
+    for r, (s, p) in enumerate(rows):      # rows that write nothing hold no numbers
+        if (s, p) in extra:
+            k[r], v[r] = np.nan, np.inf
+    slab = rng.standard_normal((n_slots, 2 * C * nkv * hd)).astype(np.float16)
+    report("append", spans=spans, C=C, nq=nq, nkv=nkv, hd=hd, f32=f32, m=m, seed=seed)
+    got, q_got = append_run(k, v, q, seq, pos, rope, slab, table, C, nkv, hd, f32, fused)
+    ref, bound, q_ref, q_bound, wrote = append_oracle(k, v, q, seq, pos, rope, slab, table, C, nkv, hd)
+    close(got, ref, bound, "slab")
+    if nq:
+        close(q_got[dev(wrote)], q_ref[wrote], q_bound[wrote], "q")
+        assert bool((q_got[dev(~wrote)] == 7).all()), "a row that writes nothing"
+
+
+@pytest.mark.parametrize("nq,nkv,hd", [(4, 2, 64), (32, 8, 64), (12, 2, 128), (8, 8, 128), (0, 1, 64), (5, 1, 32), (3, 3, 32)])
+@pytest.mark.parametrize("f32", [True, False])
+def test_append_one_row_each(nq, nkv, hd, f32):
+    append_case([(p, 1) for p in (0, 1, 15, 16, 77, 255, 256, 300)], 16, nq, nkv, hd, f32, seed=nq + hd)
+
+
+@pytest.mark.parametrize("C", [8, 16, 64, 256])
+@pytest.mark.parametrize("f32", [True, False])
+@pytest.mark.parametrize("spans", [[(0, 1)], [(0, 64)], [(0, 200)], [(3, 71), (0, 8), (250, 140), (9, 7)],
+                                   [(511, 1), (8, 57), (0, 63), (1, 129)]])
+def test_append_prompts(spans, C, f32):
+    append_case(spans, C, 4, 2, 64, f32, seed=C + len(spans))
+
+
+def test_append_rows_in_any_order():
+    append_case([(3, 71), (0, 40), (250, 33)], 16, 6, 2, 128, True, seed=5, shuffle=True)
+
+
+def test_append_separate_rows_without_queries():
+    append_case([(3, 71), (0, 40)], 32, 0, 4, 64, True, seed=6, fused=False)
+    append_case([(3, 71), (0, 40)], 32, 4, 4, 64, False, seed=7, fused=False)
+
+
+LOW, TOP = -(1 << 31), (1 << 31) - 1
+
+
+@pytest.mark.parametrize("f32", [True, False])
+def test_append_rows_and_chunks_that_write_nothing(f32):
+    """Padding rows, positions outside the rotary table or the chunk table, chunks without a slot."""
+    extra = [(-1, 3), (2, 3), (LOW, 0), (TOP, 0), (0, -1), (0, LOW), (1, TOP), (0, 400), (1, 303)]
+    bad = [(0, 1, -1), (1, 0, LOW), (1, 18, TOP)]
+    append_case([(10, 60), (0, 303)], 16, 4, 2, 64, f32, seed=8, shuffle=True, extra=extra, bad_slots=bad)
+    append_case([(10, 60), (0, 303)], 16, 4, 2, 64, f32, seed=9, extra=extra, bad_slots=bad + [(0, 2, 41)])
+
+
+def test_append_not_numbers_and_large_values():
+    """Infinities and NaN go where the formula sends them; values beyond f16 become infinite."""
+    nkv, hd, C = 1, 64, 16
+    rng = np.random.default_rng(10)
+    k, v = (rng.standard_normal((16, hd)).astype(np.float32) for _ in range(2))
+    k[3, 5], k[4, 40], v[2, 7], v[9, 0], v[11, 1] = np.inf, np.nan, np.nan, -np.inf, 1e6
+    slab, table = np.zeros((1, 2 * C * hd), np.float16), np.zeros((1, 1), np.int32)
+    seq, pos, rope = np.zeros(16, np.int32), np.arange(16, dtype=np.int32), rope_table(16, hd)
+    with np.errstate(over="ignore", invalid="ignore"):
+        ref, bound, *_ = append_oracle(k, v, None, seq, pos, rope, slab, table, C, nkv, hd)
+    got, _ = append_run(k, v, None, seq, pos, rope, slab, table, C, nkv, hd, True, False)
+    close(got, ref, bound, "slab")
+
+
+def test_append_offsets_past_32_bits():
+    """A slab of more than 4 GiB: slots at its end."""
+    torch = torch_cuda()
+    nkv, hd, C = 8, 128, 256
+    n_slots = 4200                                  # 1 MiB each
+    slab = torch.zeros(n_slots, 2 * C * nkv * hd, device="cuda", dtype=torch.float16)
+    rng = np.random.default_rng(11)
+    pos = np.arange(250, 262, dtype=np.int32)
+    k, v = (rng.standard_normal((12, nkv * hd)).astype(np.float32) for _ in range(2))
+    rope, table = rope_table(300, hd), np.array([[n_slots - 1, n_slots - 2]], np.int32)
+    dk, dv, ds, dp, dr, dt = dev(k), dev(v), dev(np.zeros(12, np.int32)), dev(pos), dev(rope), dev(table)
+    mz.mz_kv_append(12, dk.data_ptr(), dv.data_ptr(), ds.data_ptr(), dp.data_ptr(), dr.data_ptr(), 300, slab.data_ptr(),
+                    n_slots, dt.data_ptr(), 1, 2, C, nkv, hd, stream())
+    torch.cuda.synchronize()
+    small = np.zeros((2, 2 * C * nkv * hd), np.float16)
+    ref, bound, *_ = append_oracle(k, v, None, np.zeros(12), pos, rope, small, np.array([[1, 0]]), C, nkv, hd)
+    close(slab[-2:], ref, bound, "last slots")
+    assert int(slab[:-2].count_nonzero()) == 0
+
+
+def test_append_captured_on_another_stream():
+    """One graph serves every step: sequences, positions and rows change between its replays."""
+    torch = torch_cuda()
+    nq, nkv, hd, C, m, n_seq = 4, 2, 64, 16, 6, 6
+    rng = np.random.default_rng(12)
+    table = rng.permutation(n_seq * 8).reshape(n_seq, 8).astype(np.int32)
+    rope, slab0 = rope_table(128, hd), np.zeros((n_seq * 8, 2 * C * nkv * hd), np.float16)
+    slab, d_rope, d_table = dev(slab0), dev(rope), dev(table)
+    rows = torch.zeros(m, (nq + 2 * nkv) * hd, device="cuda")
+    seq, pos = torch.zeros(m, device="cuda", dtype=torch.int32), torch.zeros(m, device="cuda", dtype=torch.int32)
+    q_out = torch.zeros(m, nq * hd, device="cuda", dtype=torch.float16)
+    wide = rows.shape[1]
+
+    def call():
+        b = rows.data_ptr()
+        mz.mz_kv_append(m, b + nq * hd * 4, b + (nq + nkv) * hd * 4, seq.data_ptr(), pos.data_ptr(), d_rope.data_ptr(), 128,
+                        slab.data_ptr(), n_seq * 8, d_table.data_ptr(), n_seq, 8, C, nkv, hd, stream(), q_ptr=b, n_q=nq,
+                        q_out_ptr=q_out.data_ptr(), k_stride=wide, v_stride=wide, q_stride=wide)
+
+    call()
+    torch.cuda.synchronize()
+    slab.zero_()
+    g = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=side):
+        call()
+    ref = slab0
+    for step in range(4):
+        x = rng.standard_normal((m, wide)).astype(np.float32)
+        s, p = rng.permutation(n_seq).astype(np.int32), rng.integers(0, 128, m).astype(np.int32)
+        rows.copy_(dev(x)), seq.copy_(dev(s)), pos.copy_(dev(p))
+        before = slab.cpu().numpy()
+        g.replay()
+        torch.cuda.synchronize()
+        q, k, v = np.split(x, [nq * hd, (nq + nkv) * hd], 1)
+        ref, bound, qr, qb, _ = append_oracle(k, v, q, s, p, rope, before, table, C, nkv, hd)
+        close(slab, ref, bound, f"slab of step {step}")
+        close(q_out, qr, qb, f"q of step {step}")
