@@ -634,9 +634,40 @@ typedef struct {
  * rows name the same position of a sequence and that no two sequences share
  * a chunk that is written.  m may be 0.  Errors: EINVAL for a NULL pointer,
  * sizes or heads out of range, a stride below the row, n_table * chunk_tokens
- * above 2^31 - 1, or rows (pointers, strides), rope_cs, slab or q_out off
+ * above 2^30, or rows (pointers, strides), rope_cs, slab or q_out off
  * 16-byte boundaries. */
 mz_status mz_kv_append(const mz_kv_append_args *args, int32_t m, void *stream);
+
+/* Attention of one new token of each of n_seq sequences over its cached
+ * chunks (paper Sec. 2.1 and 4.2, for many contexts at once).  q: device f16
+ * [n_seq][n_q_heads][head_dim], rotated; lens: device int32 [n_seq], the keys
+ * that the sequence's token sees, its own among them (positions 0..len-1);
+ * table: device int32 [n_seq][n_table], slots of the sequence's chunks, laid
+ * out as in mz_attention.  out: device f16 [n_seq][n_q_heads * head_dim].
+ * Lengths may differ freely: the kernel shares the keys of all sequences
+ * evenly among its workgroups and joins what several of them summed, in a
+ * fixed order, so results do not change from run to run.  A length below 0
+ * counts as 0, one beyond the table as n_table * chunk_tokens; a chunk whose
+ * entry is outside 0..n_slots-1 is left out, as if its keys were not there; a
+ * token that sees no key gets zeros.  What slots hold past the last key is
+ * never used.  Scores, sums and joins are fp32; the softmax weights are
+ * rounded to f16 for the product with the values.  head_dim 64 or 128,
+ * n_q_heads a multiple of n_kv_heads with a group of at most 16, chunk_tokens
+ * a power of two >= 8, n_table * chunk_tokens at most 2^30, a slot below 2^31
+ * bytes.  workspace: device,
+ * caller-owned, at least mz_attention_batch_workspace_bytes(...) bytes, any
+ * content, not shared by calls in flight together (two graphs that may run at
+ * once need two).  Errors: EINVAL for the above, a NULL pointer, q, slab,
+ * workspace or out off 16-byte boundaries, or a short workspace. */
+mz_status mz_attention_batch(const void *q_f16, const int32_t *lens, int32_t n_seq, const void *slab,
+                             int32_t n_slots, const int32_t *table, int32_t n_table,
+                             int32_t chunk_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                             int32_t head_dim, void *workspace, int64_t workspace_bytes,
+                             void *out_f16, void *stream);
+
+/* Workspace bytes of mz_attention_batch (-1 for invalid arguments). */
+int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
+                                           int32_t head_dim);
 
 /* x = h / sqrt(mean(h^2) + eps) per row: h float [m][d] -> x f16 [m][d]. */
 mz_status mz_rmsnorm(const void *h_f32, int32_t m, int32_t d, float eps, void *x_f16,

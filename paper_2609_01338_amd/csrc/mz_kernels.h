@@ -172,6 +172,28 @@ struct KvAppend {
 bool kv_append_fits(int m, int nq, int nkv, int hd);
 void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s);
 
+// Attention of one token of every sequence over its chunks (see mz.h,
+// mz_attention_batch); hd 64 or 128, group = nq / nkv <= 16, C = 1 << cshift,
+// slot_bytes and attention_batch_units below 2^31.  The fields after slot_bytes'
+// line are the launcher's own, in ws (attention_batch_ws_bytes bytes).
+struct AttnBatch {
+  const _Float16* q;
+  const int32_t *lens, *table;
+  const uint8_t* slab;
+  _Float16* out;
+  int n_seq, n_slots, n_table, C, cshift, nq, nkv, group;
+  int64_t slot_bytes;
+  int32_t* base;      // [n_seq + 1] units of 128 keys of the sequences before
+  float2* ml;         // [2 kAttnBatchWgs][group] running max and sum of a partial
+  float* part;        // [2 kAttnBatchWgs][group][hd]
+  int wgs;            // most workgroups that share the units
+  float scale_log2;
+};
+constexpr int kAttnBatchWgs = 1024;
+int64_t attention_batch_units(int n_seq, int n_table, int chunk_tokens, int n_kv);
+int64_t attention_batch_ws_bytes(int n_seq, int group, int hd);
+void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
+
 // h float [m][d] = dequant(E[tok[i]]) with E split into nibbles [V][d/2] and
 // fp16 scales [V][d/32]; with last_tok (device) row m - 1 takes *last_tok.
 void launch_embed(const uint8_t* e_nib, const uint16_t* e_scale, const int32_t* tok, int m, int d,

@@ -2076,7 +2076,7 @@ static void check_chunks(int32_t n_seq, int32_t n_slots, int32_t n_table, int32_
   if (n_seq < 1 || n_slots < 1 || n_table < 1) fail(MZ_EINVAL, "n_seq, n_slots and n_table must be positive");
   if (chunk_tokens < 8 || (chunk_tokens & (chunk_tokens - 1)))
     fail(MZ_EINVAL, "chunk_tokens must be a power of two >= 8");
-  if ((int64_t)n_table * chunk_tokens > INT32_MAX) fail(MZ_EINVAL, "n_table * chunk_tokens exceeds 2^31 - 1");
+  if ((int64_t)n_table * chunk_tokens > (1 << 30)) fail(MZ_EINVAL, "n_table * chunk_tokens exceeds 2^30");
 }
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -2127,6 +2127,50 @@ mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
     k.nkv = a.n_kv_heads;
     k.hd = a.head_dim;
     mzk::launch_kv_append(k, m, a.f32 != 0, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
+int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t head_dim) {
+  if (n_seq < 1 || n_kv < 1 || n_q < n_kv || n_q % n_kv || n_q / n_kv > 16 || (head_dim != 64 && head_dim != 128))
+    return -1;
+  return mzk::attention_batch_ws_bytes(n_seq, n_q / n_kv, head_dim);
+}
+
+mz_status mz_attention_batch(const void* q, const int32_t* lens, int32_t n_seq, const void* slab, int32_t n_slots,
+                             const int32_t* table, int32_t n_table, int32_t chunk_tokens, int32_t n_q, int32_t n_kv,
+                             int32_t head_dim, void* workspace, int64_t workspace_bytes, void* out, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!q || !lens || !slab || !table || !workspace || !out) fail(MZ_EINVAL, "NULL pointer");
+    check_chunks(n_seq, n_slots, n_table, chunk_tokens);
+    if (head_dim != 64 && head_dim != 128) fail(MZ_EINVAL, "head_dim must be 64 or 128");
+    if (n_kv < 1 || n_q < n_kv || n_q % n_kv || n_q / n_kv > 16) fail(MZ_EINVAL, "bad head counts");
+    const int64_t slot_bytes = (int64_t)chunk_tokens * n_kv * head_dim * 4;
+    if (slot_bytes > INT32_MAX) fail(MZ_EINVAL, "a chunk slot exceeds 2^31 - 1 bytes");
+    if (mzk::attention_batch_units(n_seq, n_table, chunk_tokens, n_kv) > INT32_MAX ||
+        (int64_t)n_seq * n_q > INT32_MAX)
+      fail(MZ_EINVAL, "n_seq sequences of n_table chunks are too many");
+    if (workspace_bytes < mzk::attention_batch_ws_bytes(n_seq, n_q / n_kv, head_dim))
+      fail(MZ_EINVAL, "workspace too small");
+    if (!aligned16(q) || !aligned16(slab) || !aligned16(out) || !aligned16(workspace))
+      fail(MZ_EINVAL, "q, slab, workspace and out must lie on 16-byte boundaries");
+    check_stream(stream);
+    mzk::AttnBatch a{};
+    a.q = reinterpret_cast<const _Float16*>(q);
+    a.lens = lens;
+    a.table = table;
+    a.slab = reinterpret_cast<const uint8_t*>(slab);
+    a.out = reinterpret_cast<_Float16*>(out);
+    a.n_seq = n_seq;
+    a.n_slots = n_slots;
+    a.n_table = n_table;
+    a.C = chunk_tokens;
+    a.cshift = __builtin_ctz((unsigned)chunk_tokens);
+    a.nq = n_q;
+    a.nkv = n_kv;
+    a.group = n_q / n_kv;
+    a.slot_bytes = slot_bytes;
+    mzk::launch_attention_batch(a, head_dim, workspace, (hipStream_t)stream);
     HIPCHK(hipGetLastError());
   });
 }

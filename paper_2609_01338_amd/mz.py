@@ -127,6 +127,8 @@ def lib() -> ctypes.CDLL:
         "mz_q4_gemm_ex": ([vp, i32, i32, i32, vp, i32, ctypes.POINTER(mz_q4_gemm_args), vp, vp], i32),
         "mz_q4_gemv": ([vp, i32, vp, i32, i32, ctypes.POINTER(mz_q4_gemm_args), vp, ctypes.c_float, vp, vp], i32),
         "mz_kv_append": ([ctypes.POINTER(mz_kv_append_args), i32, vp], i32),
+        "mz_attention_batch": ([vp, vp, i32, vp, i32, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp], i32),
+        "mz_attention_batch_workspace_bytes": ([i32, i32, i32, i32], i64),
         "mz_rmsnorm": ([vp, i32, i32, ctypes.c_float, vp, vp], i32),
         "mz_probe_ceilings": ([i32, ctypes.c_char_p, sz], i32),
         "mz_plan_evict": ([ctypes.POINTER(mz_model_cfg), ctypes.POINTER(mz_evict_request), vp, vp, vp], i32),
@@ -459,6 +461,17 @@ def mz_kv_append(m: int, k_ptr: int, v_ptr: int, seq_ptr: int, pos_ptr: int, rop
     a = mz_kv_append_args(q_ptr, k_ptr, v_ptr, q_stride, k_stride, v_stride, f32, head_dim, n_q, n_kv, seq_ptr, pos_ptr,
                           rope_cs_ptr, n_rope, n_slots, slab_ptr, table_ptr, n_seq, n_table, chunk_tokens, q_out_ptr)
     _check(lib().mz_kv_append(ctypes.byref(a), m, stream), None)
+
+
+def mz_attention_batch(q_ptr: int, lens_ptr: int, n_seq: int, slab_ptr: int, n_slots: int, table_ptr: int, n_table: int,
+                       chunk_tokens: int, n_q: int, n_kv: int, head_dim: int, ws_ptr: int, ws_bytes: int, out_ptr: int,
+                       stream: Optional[int] = None) -> None:
+    _check(lib().mz_attention_batch(q_ptr, lens_ptr, n_seq, slab_ptr, n_slots, table_ptr, n_table, chunk_tokens, n_q,
+                                    n_kv, head_dim, ws_ptr, ws_bytes, out_ptr, stream), None)
+
+
+def mz_attention_batch_workspace_bytes(n_seq: int, n_q: int, n_kv: int, head_dim: int) -> int:
+    return int(lib().mz_attention_batch_workspace_bytes(n_seq, n_q, n_kv, head_dim))
 
 
 def mz_rmsnorm(h_ptr: int, m: int, d: int, eps: float, x_ptr: int, stream: Optional[int] = None) -> None:

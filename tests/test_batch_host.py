@@ -40,7 +40,7 @@ APPEND = dict(m=3, k_ptr=P, v_ptr=P, seq_ptr=P, pos_ptr=P, rope_cs_ptr=P, n_rope
     (dict(n_kv=0), "head"), (dict(n_q=-1), "head"), (dict(n_kv=1025), "head"),
     (dict(n_rope=0), "n_rope"), (dict(n_slots=0), "positive"), (dict(n_seq=0), "positive"), (dict(n_table=0), "positive"),
     (dict(chunk_tokens=4), "chunk_tokens"), (dict(chunk_tokens=24), "chunk_tokens"), (dict(chunk_tokens=-8), "chunk_tokens"),
-    (dict(n_table=1 << 27), "2^31"),
+    (dict(n_table=1 << 27), "2^30"),
     (dict(k_stride=124), "stride"), (dict(v_stride=64), "stride"), (dict(q_stride=-256), "stride"),
     (dict(k_stride=130), "16-byte"), (dict(v_stride=129), "16-byte"), (dict(q_stride=258), "16-byte"),
     (dict(f32=False, k_stride=132), "16-byte"),
@@ -54,3 +54,30 @@ def test_kv_append_refusals(bad, match):
 
 def test_kv_append_no_rows():
     mz.mz_kv_append(**{**APPEND, "m": 0})     # nothing to do, nothing enqueued
+
+
+ATTENTION = dict(q_ptr=P, lens_ptr=P, n_seq=3, slab_ptr=P, n_slots=8, table_ptr=P, n_table=4, chunk_tokens=16, n_q=8, n_kv=2,
+                 head_dim=64, ws_ptr=P, ws_bytes=1 << 30, out_ptr=P)
+
+
+@pytest.mark.parametrize("bad,match", [
+    (dict(q_ptr=0), "NULL"), (dict(lens_ptr=0), "NULL"), (dict(slab_ptr=0), "NULL"), (dict(table_ptr=0), "NULL"),
+    (dict(ws_ptr=0), "NULL"), (dict(out_ptr=0), "NULL"),
+    (dict(n_seq=0), "positive"), (dict(n_slots=-1), "positive"), (dict(n_table=0), "positive"),
+    (dict(chunk_tokens=4), "chunk_tokens"), (dict(chunk_tokens=48), "chunk_tokens"), (dict(n_table=1 << 27), "2^30"),
+    (dict(head_dim=32), "head_dim"), (dict(n_kv=0), "head"), (dict(n_q=7), "head"), (dict(n_q=34), "head"), (dict(n_q=0), "head"),
+    (dict(chunk_tokens=1 << 24), "slot"), (dict(n_seq=1 << 30, n_table=1 << 20), "too many"),
+    (dict(n_seq=(1 << 31) - 1, n_table=1, n_q=2), "too many"),
+    (dict(ws_bytes=0), "workspace"), (dict(ws_bytes=-1), "workspace"),
+    (dict(q_ptr=P + 2), "16-byte"), (dict(slab_ptr=P + 8), "16-byte"), (dict(out_ptr=P + 4), "16-byte"), (dict(ws_ptr=P + 8), "16-byte"),
+])
+def test_attention_batch_refusals(bad, match):
+    refused(mz.mz_attention_batch, **{**ATTENTION, **bad}, match=match)
+
+
+def test_attention_batch_workspace():
+    need = mz.mz_attention_batch_workspace_bytes(3, 8, 2, 64)
+    assert need > 0
+    refused(mz.mz_attention_batch, **{**ATTENTION, "ws_bytes": need - 1}, match="workspace")
+    for bad in [(0, 8, 2, 64), (3, 7, 2, 64), (3, 8, 0, 64), (3, 8, 2, 32), (3, 0, 2, 64), (3, 34, 2, 64)]:
+        assert mz.mz_attention_batch_workspace_bytes(*bad) == -1

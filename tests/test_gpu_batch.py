@@ -240,3 +240,233 @@ def test_append_captured_on_another_stream():
         ref, bound, qr, qb, _ = append_oracle(k, v, q, s, p, rope, before, table, C, nkv, hd)
         close(slab, ref, bound, f"slab of step {step}")
         close(q_out, qr, qb, f"q of step {step}")
+
+
+# ----------------------------------------------------------------------------- attention
+
+def attention_oracle(q, lens, slab, table, C, nq, nkv, hd):
+    """(out, bound): weights rounded to f16 (u16 relative, the sums with them) from fp32 scores, f16 outputs."""
+    n_seq, n_slots, dkv, group = len(lens), slab.shape[0], nkv * hd, nq // nkv
+    out, bound = np.zeros((n_seq, nq * hd)), np.zeros((n_seq, nq * hd))
+    halves = slab.reshape(n_slots, 2, C * dkv)
+    ks, vs = halves[:, 0].reshape(n_slots, C, dkv), halves[:, 1].reshape(n_slots, dkv, C)
+    for b in range(n_seq):
+        n = min(max(int(lens[b]), 0), table.shape[1] * C)
+        keep = [c for c in range((n + C - 1) // C) if 0 <= int(table[b, c]) < n_slots]
+        at = np.concatenate([np.arange(c * C, min(n, (c + 1) * C)) for c in keep]) if keep else np.zeros(0, int)
+        if at.size == 0:
+            continue
+        slots = table[b, at // C]
+        k, v = ks[slots, at % C], vs[slots, :, at % C]
+        k, v = k.astype(np.float64).reshape(-1, nkv, hd), v.astype(np.float64).reshape(-1, nkv, hd)
+        for h in range(nq):
+            x = q[b, h * hd:(h + 1) * hd].astype(np.float64)
+            kk, vv = k[:, h // group], v[:, h // group]
+            with np.errstate(invalid="ignore", over="ignore"):
+                s = kk @ x / np.sqrt(hd)
+                w = np.exp(s - s.max())
+                p = w / w.sum()
+                o = p @ vv
+                # fp32 sums of hd exact products, the scale's and the exponent's roundings; a score of -inf is a
+                # weight of exactly 0 on both sides, so its key adds no error (and no finite product to bound it by)
+                on = np.isfinite(s)
+                if on.any():
+                    part = (np.abs(kk[on]) @ np.abs(x)).max() / np.sqrt(hd)
+                    e = (hd + 4) * U32 * part + 4 * U32 * np.abs(s[on] - s[on].max()).max() + 4 * U32
+                    bound[b, h * hd:(h + 1) * hd] = 2.1 * (U16 + e) * (p[on] @ np.abs(vv[on])) + U16 * np.abs(o) + TINY16 + \
+                        len(s) * 2.0 ** -39 * np.abs(vv[on]).max(0)
+                out[b, h * hd:(h + 1) * hd] = o
+    return out, bound
+
+
+def attention_run(q, lens, slab, table, C, nq, nkv, hd, ws=None):
+    torch = torch_cuda()
+    n_seq = len(lens)
+    need = mz.mz_attention_batch_workspace_bytes(n_seq, nq, nkv, hd)
+    if ws is None:
+        ws = torch.full((need // 4 + 1,), float("nan"), device="cuda")      # what it held must not show
+    out = torch.full((n_seq, nq * hd), 7.0, device="cuda", dtype=torch.float16)
+    a = [dev(x) if isinstance(x, np.ndarray) else x for x in (q, lens, slab, table)]
+    mz.mz_attention_batch(a[0].data_ptr(), a[1].data_ptr(), n_seq, a[2].data_ptr(), slab.shape[0], a[3].data_ptr(),
+                          table.shape[1], C, nq, nkv, hd, ws.data_ptr(), need, out.data_ptr(), stream())
+    torch.cuda.synchronize()
+    return out
+
+
+def attention_inputs(lens, C, nq, nkv, hd, seed, spread=1.0, extra_table=2):
+    rng = np.random.default_rng(seed)
+    lens = np.array(lens, np.int32)
+    n_table = max(int(lens.max()), 1) // C + 1 + extra_table
+    n_slots = int(sum((max(int(n), 0) + C - 1) // C for n in lens)) + 2
+    order, at = rng.permutation(n_slots), 0
+    table = rng.integers(-(1 << 31), 1 << 31, (len(lens), n_table)).astype(np.int32)   # entries past a length are never followed
+    slab = np.full((n_slots, 2, C * nkv * hd), np.nan, np.float16)                     # nor what slots hold past it
+    for b, n in enumerate(lens):
+        for c in range((max(int(n), 0) + C - 1) // C):
+            slot, held = order[at], min(C, n - c * C)
+            at += 1
+            table[b, c] = slot
+            slab[slot, 0].reshape(C, -1)[:held] = rng.standard_normal((held, nkv * hd)) * spread
+            slab[slot, 1].reshape(-1, C)[:, :held] = rng.standard_normal((nkv * hd, held))
+    q = (rng.standard_normal((len(lens), nq * hd)) * spread).astype(np.float16)
+    return q, lens, slab.reshape(n_slots, -1), table
+
+
+def attention_case(lens, C, nq, nkv, hd, seed, spread=1.0):
+    report("attention", lens=list(lens)[:12], n_seq=len(lens), C=C, nq=nq, nkv=nkv, hd=hd, seed=seed)
+    a = attention_inputs(lens, C, nq, nkv, hd, seed, spread)
+    out = attention_run(*a, C, nq, nkv, hd)
+    ref, bound = attention_oracle(*a, C, nq, nkv, hd)
+    close(out, ref, bound, "out")
+    assert torch_cuda().equal(out, attention_run(*a, C, nq, nkv, hd)), "another run, other bits"
+    return a, out
+
+
+RAGGED = [0, 1, 2, 7, 8, 9, 31, 32, 33, 63, 127, 128, 129, 255, 300, 1000, 0, 5]
+
+
+@pytest.mark.parametrize("nq,nkv,hd", [(4, 2, 64), (32, 8, 64), (12, 2, 128), (32, 8, 128), (16, 1, 128), (8, 8, 64),
+                                       (3, 1, 64), (7, 1, 128), (33, 3, 64)])
+@pytest.mark.parametrize("C", [8, 16, 32, 256])
+def test_attention_ragged(nq, nkv, hd, C):
+    attention_case(RAGGED, C, nq, nkv, hd, seed=nq * C + hd)
+
+
+@pytest.mark.parametrize("lens,C,nq,nkv,hd", [
+    ([1], 16, 4, 2, 64), ([5000], 64, 8, 2, 128), ([20000], 256, 6, 1, 128), ([3333, 1], 128, 2, 2, 64),
+    ([0, 0, 9000, 0], 8, 5, 1, 64)])
+def test_attention_few_long(lens, C, nq, nkv, hd):
+    attention_case(lens, C, nq, nkv, hd, seed=sum(lens))
+
+
+def test_attention_many_sequences():
+    """More sequences than a workgroup has threads, some of them empty, more pairs than workgroups."""
+    rng = np.random.default_rng(3)
+    attention_case([int(n) for n in rng.integers(0, 200, 700)], 16, 4, 2, 64, seed=4)
+    attention_case([0] * 600 + [77] + [0] * 300, 16, 4, 2, 64, seed=5)
+    attention_case([0, 0, 0], 16, 4, 2, 64, seed=6)
+
+
+def test_attention_sharp_and_flat():
+    attention_case([700, 64, 3], 64, 8, 2, 128, seed=7, spread=4.0)
+    attention_case([9000], 64, 4, 1, 64, seed=8, spread=0.01)
+
+
+def test_attention_lengths_outside_the_table():
+    a = list(attention_inputs([64, 40, 16], 16, 4, 2, 64, seed=9, extra_table=-1))
+    assert a[3].shape[1] == 4
+    a[1] = np.array([1 << 30, -5, 16], np.int32)
+    out = attention_run(*a, 16, 4, 2, 64)
+    ref, bound = attention_oracle(*a, 16, 4, 2, 64)
+    close(out, ref, bound, "out")
+    assert int(out[1].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("C", [8, 16, 32, 64])
+def test_attention_chunks_without_a_slot(C):
+    """Their keys are left out; a sequence of none but such chunks gives zeros."""
+    a = attention_inputs([500, 130, 100, 64], C, 4, 2, 64, seed=10)
+    low, top = -(1 << 31), (1 << 31) - 1
+    a[3][0, 0], a[3][0, 3], a[3][0, 500 // C] = -1, a[2].shape[0], low
+    a[3][1, 1] = top
+    a[3][2, :] = -1
+    out = attention_run(*a, C, 4, 2, 64)
+    ref, bound = attention_oracle(*a, C, 4, 2, 64)
+    close(out, ref, bound, "out")
+    assert int(out[2].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("C", [16, 64])
+def test_attention_not_numbers(C):
+    """NaN, infinities and lowest values among the keys and values that count."""
+    nq, nkv, hd = 4, 1, 64
+    q, lens, slab, table = attention_inputs([90, 90, 90, 90, 90, 90, 90], C, nq, nkv, hd, seed=11)
+    k = lambda b, j: slab[table[b, j // C], :C * hd].reshape(C, hd)[j % C]       # noqa: E731
+    v = lambda b, j: slab[table[b, j // C], C * hd:].reshape(hd, C)[:, j % C]    # noqa: E731
+    k(0, 50)[3] = np.nan
+    v(1, 20)[5] = np.nan
+    v(2, 33)[6] = np.inf
+    v(2, 34)[6] = -np.inf
+    v(2, 35)[7] = -np.inf
+    k(3, 10)[:] = 65504.0                        # scores of either sign, far beyond the others
+    k(4, 11)[:] = -65504.0
+    q[5] = 1.0
+    for j in range(90):                          # a row that sees nothing above -inf
+        k(5, j)[0] = -np.inf
+    q[6] = 1.0
+    k(6, 77)[0] = -np.inf                        # one such key counts for nothing
+    out = attention_run(q, lens, slab, table, C, nq, nkv, hd)
+    ref, bound = attention_oracle(q, lens, slab, table, C, nq, nkv, hd)
+    close(out, ref, bound, "out")
+
+
+def test_attention_against_the_single_sequence_call():
+    torch = torch_cuda()
+    nq, nkv, hd, C, n = 8, 2, 128, 64, 3000
+    q, lens, slab, table = attention_inputs([n], C, nq, nkv, hd, seed=12)
+    slab = np.nan_to_num(slab)
+    out = attention_run(q, lens, slab, table, C, nq, nkv, hd)
+    d = [dev(x) for x in (q, np.array([n - 1], np.int32), slab, table)]
+    other = torch.zeros_like(out)
+    mz.mz_attention(d[0].data_ptr(), d[1].data_ptr(), 1, d[2].data_ptr(), d[3].data_ptr(), (n + C - 1) // C, C, nq, nkv, hd,
+                    other.data_ptr(), stream())
+    torch.cuda.synchronize()
+    ref, bound = attention_oracle(q, lens, slab, table, C, nq, nkv, hd)
+    close(out, ref, bound, "batch")
+    close(out, other.double().cpu().numpy(), 2 * bound, "batch against mz_attention")
+
+
+def test_attention_offsets_past_32_bits():
+    torch = torch_cuda()
+    nq, nkv, hd, C, n = 8, 8, 128, 256, 700
+    n_slots = 4200                                  # 1 MiB each
+    slab = torch.zeros(n_slots, 2 * C * nkv * hd, device="cuda", dtype=torch.float16)
+    q, lens, small, table = attention_inputs([n], C, nq, nkv, hd, seed=13)
+    slab[n_slots - small.shape[0]:] = dev(small)
+    far = table.copy()
+    far[0, :3] += n_slots - small.shape[0]
+    out = attention_run(q, lens, slab, far, C, nq, nkv, hd)
+    ref, bound = attention_oracle(q, lens, small, table, C, nq, nkv, hd)
+    close(out, ref, bound, "out")
+
+
+def test_attention_captured_on_another_stream():
+    """One graph over changing lengths; its workspace holds the last replay's partials."""
+    torch = torch_cuda()
+    nq, nkv, hd, C = 4, 2, 64, 16
+    q, lens, slab, table = attention_inputs([800, 650, 513, 77], C, nq, nkv, hd, seed=14)
+    need = mz.mz_attention_batch_workspace_bytes(4, nq, nkv, hd)
+    ws = torch.full((need // 4,), float("nan"), device="cuda")
+    d = [dev(x) for x in (q, lens, slab, table)]
+    out = torch.zeros(4, nq * hd, device="cuda", dtype=torch.float16)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        mz.mz_attention_batch(d[0].data_ptr(), d[1].data_ptr(), 4, d[2].data_ptr(), slab.shape[0], d[3].data_ptr(),
+                              table.shape[1], C, nq, nkv, hd, ws.data_ptr(), need, out.data_ptr(), stream())
+    for now in ([800, 650, 513, 77], [1, 0, 300, 77], [0, 0, 0, 0], [128, 129, 1, 64]):
+        now = np.array(now, np.int32)
+        d[1].copy_(dev(now))
+        out.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        ref, bound = attention_oracle(q, now, slab, table, C, nq, nkv, hd)
+        close(out, ref, bound, f"lengths {now.tolist()}")
+
+
+def test_attention_on_two_streams_at_once():
+    torch = torch_cuda()
+    nq, nkv, hd, C = 8, 2, 128, 64
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    args = [attention_inputs([4000 + 900 * i, 50, 3100], C, nq, nkv, hd, seed=15 + i) for i in range(2)]
+    need = mz.mz_attention_batch_workspace_bytes(3, nq, nkv, hd)
+    held = [[dev(x) for x in a] + [torch.full((need // 4,), float("nan"), device="cuda"),
+                                   torch.zeros(3, nq * hd, device="cuda", dtype=torch.float16)] for a in args]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for side, a, d in zip(sides, args, held):
+            mz.mz_attention_batch(d[0].data_ptr(), d[1].data_ptr(), 3, d[2].data_ptr(), a[2].shape[0], d[3].data_ptr(),
+                                  a[3].shape[1], C, nq, nkv, hd, d[4].data_ptr(), need, d[5].data_ptr(), side.cuda_stream)
+    torch.cuda.synchronize()
+    for i, (a, d) in enumerate(zip(args, held)):
+        ref, bound = attention_oracle(*a, C, nq, nkv, hd)
+        close(d[5], ref, bound, f"stream {i}")
