@@ -669,6 +669,32 @@ mz_status mz_attention_batch(const void *q_f16, const int32_t *lens, int32_t n_s
 int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
                                            int32_t head_dim);
 
+/* Low-rank adapters of many requests beside a shared projection:
+ *   y[r] = base[r] + scale[a] * (x[r] A_a^T) B_a^T,  a = adapter[r],
+ * for the first n columns of rows of y_stride floats.  x: device f16 [m][k],
+ * the projection's input; base: its output (mz_q4_gemm epilogue 0 or 1), y
+ * may be base itself.  a: device f16 [n_adapters][max_rank][k], b: device f16
+ * [n_adapters][n][max_rank]; of adapter a the first rank[a] ranks count
+ * (device int32 [n_adapters], clamped to 0..max_rank; NULL: all), whatever
+ * the others hold.  scale: device float [n_adapters] (NULL: 1).  adapter:
+ * device int32 [m], in any order; a row whose entry is outside
+ * 0..n_adapters-1 has none: its y is the base's (in place it is not
+ * touched).  Rows do not affect each other.  Nothing is rounded to f16 on the
+ * way: x A^T and its product with B are fp32.  k a multiple of 8, max_rank a
+ * multiple of 8 in 8..128, y_stride a multiple of 4, m may be 0.  workspace:
+ * device, caller-owned, at least mz_lora_workspace_bytes(m, k, max_rank)
+ * bytes, any content, not shared by calls in flight together (two graphs that
+ * may run at once need two).  Results do not change from run to run.  Errors:
+ * EINVAL for the above, a NULL pointer, pointers off 16-byte boundaries, or a
+ * short workspace. */
+mz_status mz_lora_add(const void *x_f16, int32_t m, int32_t k, const int32_t *adapter,
+                      int32_t n_adapters, const void *a_f16, const void *b_f16, const float *scale,
+                      const int32_t *rank, int32_t max_rank, int32_t n, const float *base, float *y,
+                      int64_t y_stride, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Workspace bytes of mz_lora_add (-1 for invalid arguments). */
+int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank);
+
 /* x = h / sqrt(mean(h^2) + eps) per row: h float [m][d] -> x f16 [m][d]. */
 mz_status mz_rmsnorm(const void *h_f32, int32_t m, int32_t d, float eps, void *x_f16,
                      void *stream);

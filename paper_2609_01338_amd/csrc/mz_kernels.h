@@ -194,6 +194,23 @@ int64_t attention_batch_units(int n_seq, int n_table, int chunk_tokens, int n_kv
 int64_t attention_batch_ws_bytes(int n_seq, int group, int hd);
 void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
 
+// y = base + scale (x A^T) B^T with each row's adapter (see mz.h,
+// mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8, y_stride of 4,
+// every pointer 16-byte aligned.  t and n_split are the launcher's own, in ws
+// (lora_ws_bytes bytes).
+struct Lora {
+  const _Float16 *x, *a, *b;
+  const int32_t *adapter, *rank;
+  const float *scale, *base;
+  float* y;
+  int64_t y_stride;
+  int m, k, n, R, n_adapters;
+  float* t;          // [n_split][m][R rounded up] partials of x A^T
+  int n_split;
+};
+int64_t lora_ws_bytes(int m, int k, int R);
+void launch_lora(Lora p, void* ws, hipStream_t s);
+
 // h float [m][d] = dequant(E[tok[i]]) with E split into nibbles [V][d/2] and
 // fp16 scales [V][d/32]; with last_tok (device) row m - 1 takes *last_tok.
 void launch_embed(const uint8_t* e_nib, const uint16_t* e_scale, const int32_t* tok, int m, int d,

@@ -2175,6 +2175,47 @@ mz_status mz_attention_batch(const void* q, const int32_t* lens, int32_t n_seq, 
   });
 }
 
+int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank) {
+  if (m < 1 || k < 8 || max_rank < 8 || max_rank > 128) return -1;
+  return mzk::lora_ws_bytes(m, k, max_rank);
+}
+
+mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapter, int32_t n_adapters, const void* a,
+                      const void* b, const float* scale, const int32_t* rank, int32_t max_rank, int32_t n,
+                      const float* base, float* y, int64_t y_stride, void* workspace, int64_t workspace_bytes,
+                      void* stream) {
+  return guarded(nullptr, [&] {
+    if (!x || !adapter || !a || !b || !base || !y || !workspace) fail(MZ_EINVAL, "NULL pointer");
+    if (m < 0 || n < 1 || n_adapters < 1) fail(MZ_EINVAL, "n and n_adapters must be positive, m at least 0");
+    if (k < 8 || k % 8) fail(MZ_EINVAL, "k must be a positive multiple of 8");
+    if (max_rank < 8 || max_rank > 128 || max_rank % 8) fail(MZ_EINVAL, "max_rank must be a multiple of 8 in 8..128");
+    if (y_stride < n || y_stride % 4) fail(MZ_EINVAL, "y_stride must be a multiple of 4 and at least n");
+    if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(base) || !aligned16(y) || !aligned16(workspace))
+      fail(MZ_EINVAL, "x, a, b, base, y and workspace must lie on 16-byte boundaries");
+    if ((int64_t)n > 65535 * 256) fail(MZ_EINVAL, "n exceeds 65535 * 256");
+    check_stream(stream);
+    if (m == 0) return;
+    if (workspace_bytes < mzk::lora_ws_bytes(m, k, max_rank)) fail(MZ_EINVAL, "workspace too small");
+    mzk::Lora p{};
+    p.x = reinterpret_cast<const _Float16*>(x);
+    p.a = reinterpret_cast<const _Float16*>(a);
+    p.b = reinterpret_cast<const _Float16*>(b);
+    p.adapter = adapter;
+    p.rank = rank;
+    p.scale = scale;
+    p.base = base;
+    p.y = y;
+    p.y_stride = y_stride;
+    p.m = m;
+    p.k = k;
+    p.n = n;
+    p.R = max_rank;
+    p.n_adapters = n_adapters;
+    mzk::launch_lora(p, workspace, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
 mz_status mz_rmsnorm(const void* h, int32_t m, int32_t d, float eps, void* x, void* stream) {
   return guarded(nullptr, [&] {
     if (!h || !x) fail(MZ_EINVAL, "NULL pointer");

@@ -129,6 +129,8 @@ def lib() -> ctypes.CDLL:
         "mz_kv_append": ([ctypes.POINTER(mz_kv_append_args), i32, vp], i32),
         "mz_attention_batch": ([vp, vp, i32, vp, i32, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp], i32),
         "mz_attention_batch_workspace_bytes": ([i32, i32, i32, i32], i64),
+        "mz_lora_add": ([vp, i32, i32, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp, i64, vp], i32),
+        "mz_lora_workspace_bytes": ([i32, i32, i32], i64),
         "mz_rmsnorm": ([vp, i32, i32, ctypes.c_float, vp, vp], i32),
         "mz_probe_ceilings": ([i32, ctypes.c_char_p, sz], i32),
         "mz_plan_evict": ([ctypes.POINTER(mz_model_cfg), ctypes.POINTER(mz_evict_request), vp, vp, vp], i32),
@@ -472,6 +474,17 @@ def mz_attention_batch(q_ptr: int, lens_ptr: int, n_seq: int, slab_ptr: int, n_s
 
 def mz_attention_batch_workspace_bytes(n_seq: int, n_q: int, n_kv: int, head_dim: int) -> int:
     return int(lib().mz_attention_batch_workspace_bytes(n_seq, n_q, n_kv, head_dim))
+
+
+def mz_lora_add(x_ptr: int, m: int, k: int, adapter_ptr: int, n_adapters: int, a_ptr: int, b_ptr: int, max_rank: int,
+                n: int, base_ptr: int, y_ptr: int, y_stride: int, ws_ptr: int, ws_bytes: int,
+                stream: Optional[int] = None, scale_ptr: int = 0, rank_ptr: int = 0) -> None:
+    _check(lib().mz_lora_add(x_ptr, m, k, adapter_ptr, n_adapters, a_ptr, b_ptr, scale_ptr, rank_ptr, max_rank, n,
+                             base_ptr, y_ptr, y_stride, ws_ptr, ws_bytes, stream), None)
+
+
+def mz_lora_workspace_bytes(m: int, k: int, max_rank: int) -> int:
+    return int(lib().mz_lora_workspace_bytes(m, k, max_rank))
 
 
 def mz_rmsnorm(h_ptr: int, m: int, d: int, eps: float, x_ptr: int, stream: Optional[int] = None) -> None:

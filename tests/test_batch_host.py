@@ -81,3 +81,31 @@ def test_attention_batch_workspace():
     refused(mz.mz_attention_batch, **{**ATTENTION, "ws_bytes": need - 1}, match="workspace")
     for bad in [(0, 8, 2, 64), (3, 7, 2, 64), (3, 8, 0, 64), (3, 8, 2, 32), (3, 0, 2, 64), (3, 34, 2, 64)]:
         assert mz.mz_attention_batch_workspace_bytes(*bad) == -1
+
+
+LORA = dict(x_ptr=P, m=3, k=64, adapter_ptr=P, n_adapters=2, a_ptr=P, b_ptr=P, max_rank=16, n=100, base_ptr=P, y_ptr=P,
+            y_stride=256, ws_ptr=P, ws_bytes=1 << 30)
+
+
+@pytest.mark.parametrize("bad,match", [
+    (dict(x_ptr=0), "NULL"), (dict(adapter_ptr=0), "NULL"), (dict(a_ptr=0), "NULL"), (dict(b_ptr=0), "NULL"),
+    (dict(base_ptr=0), "NULL"), (dict(y_ptr=0), "NULL"), (dict(ws_ptr=0), "NULL"),
+    (dict(m=-1), "positive"), (dict(n=0), "positive"), (dict(n_adapters=0), "positive"),
+    (dict(k=0), "k must"), (dict(k=60), "k must"), (dict(k=-8), "k must"),
+    (dict(max_rank=0), "max_rank"), (dict(max_rank=12), "max_rank"), (dict(max_rank=136), "max_rank"),
+    (dict(y_stride=96), "y_stride"), (dict(y_stride=102), "y_stride"), (dict(y_stride=-4), "y_stride"),
+    (dict(x_ptr=P + 2), "16-byte"), (dict(a_ptr=P + 8), "16-byte"), (dict(b_ptr=P + 8), "16-byte"),
+    (dict(base_ptr=P + 4), "16-byte"), (dict(y_ptr=P + 4), "16-byte"), (dict(ws_ptr=P + 4), "16-byte"),
+    (dict(n=1 << 30, y_stride=1 << 30), "65535"), (dict(ws_bytes=0), "workspace"), (dict(ws_bytes=-1), "workspace"),
+])
+def test_lora_add_refusals(bad, match):
+    refused(mz.mz_lora_add, **{**LORA, **bad}, match=match)
+
+
+def test_lora_workspace_and_no_rows():
+    need = mz.mz_lora_workspace_bytes(3, 64, 16)
+    assert need > 0
+    refused(mz.mz_lora_add, **{**LORA, "ws_bytes": need - 1}, match="workspace")
+    for bad in [(0, 64, 16), (3, 4, 16), (3, 64, 4), (3, 64, 129)]:
+        assert mz.mz_lora_workspace_bytes(*bad) == -1
+    mz.mz_lora_add(**{**LORA, "m": 0, "ws_bytes": 0})

@@ -470,3 +470,177 @@ def test_attention_on_two_streams_at_once():
     for i, (a, d) in enumerate(zip(args, held)):
         ref, bound = attention_oracle(*a, C, nq, nkv, hd)
         close(d[5], ref, bound, f"stream {i}")
+
+
+# ----------------------------------------------------------------------------- adapters
+
+def lora_oracle(x, adapter, a, b, scale, rank, base, n):
+    """(y, bound): fp32 sums of k and of the ranks' products, nothing rounded to f16."""
+    y, bound = base.astype(np.float64), np.zeros(base.shape)
+    na, R, k = a.shape
+    with np.errstate(invalid="ignore", over="ignore"):
+        for i in range(na):
+            rows, r = np.nonzero(adapter == i)[0], R if rank is None else min(max(int(rank[i]), 0), R)
+            s = 1.0 if scale is None else float(scale[i])
+            xs, ai, bi = x[rows].astype(np.float64), a[i, :r].astype(np.float64), b[i, :, :r].astype(np.float64)
+            y[rows, :n] += s * ((xs @ ai.T) @ bi.T)
+            size = abs(s) * ((np.abs(xs) @ np.abs(ai).T) @ np.abs(bi).T)
+            bound[rows, :n] = 2 * (k + R + 20) * U32 * size + 2 * U32 * np.abs(y[rows, :n])
+    return y, bound
+
+
+def lora_run(x, adapter, a, b, scale, rank, base, n, in_place=False, ws=None):
+    torch = torch_cuda()
+    m, k = x.shape
+    na, R, _ = a.shape
+    need = mz.mz_lora_workspace_bytes(m, k, R)
+    if ws is None:
+        ws = torch.full((need // 4,), float("nan"), device="cuda")
+    d = [None if v is None else dev(v) for v in (x, adapter, a, b, scale, rank, base)]
+    y = d[6] if in_place else torch.full(base.shape, 7.0, device="cuda")
+    mz.mz_lora_add(d[0].data_ptr(), m, k, d[1].data_ptr(), na, d[2].data_ptr(), d[3].data_ptr(), R, n, d[6].data_ptr(),
+                   y.data_ptr(), base.shape[1], ws.data_ptr(), need, stream(),
+                   scale_ptr=0 if scale is None else d[4].data_ptr(), rank_ptr=0 if rank is None else d[5].data_ptr())
+    torch.cuda.synchronize()
+    return y
+
+
+def lora_inputs(adapter, k, n, R, na, seed, stride=None, ranks=None):
+    rng = np.random.default_rng(seed)
+    adapter = np.array(adapter, np.int32)
+    m = len(adapter)
+    x = rng.standard_normal((m, k)).astype(np.float16)
+    a = (rng.standard_normal((na, R, k)) / np.sqrt(k)).astype(np.float16)
+    b = (rng.standard_normal((na, n, R)) * 0.3).astype(np.float16)
+    scale = (rng.random(na) + 0.5).astype(np.float32)
+    rank = np.array([int(rng.integers(0, R + 1)) for _ in range(na)] if ranks is None else ranks, np.int32)
+    for i in range(na):                  # what lies past a rank is not data
+        a[i, rank[i]:], b[i, :, rank[i]:] = np.nan, np.inf
+    base = rng.standard_normal((m, stride or (n + 3) // 4 * 4)).astype(np.float32)
+    return x, adapter, a, b, scale, rank, base, n
+
+
+def lora_case(adapter, k, n, R, na, seed, **kw):
+    torch = torch_cuda()
+    a = lora_inputs(adapter, k, n, R, na, seed, **kw)
+    report("lora", m=len(adapter), k=k, n=n, R=R, adapters=na, ranks=a[5].tolist()[:8], seed=seed)
+    ref, bound = lora_oracle(*a)
+    y = lora_run(*a)
+    close(y[:, :n], ref[:, :n], bound[:, :n], "y")
+    assert bool((y[:, n:] == 7).all()), "columns past n"
+    bits = lambda t: t[:, :n].contiguous().view(torch.int32)  # noqa: E731
+    assert torch.equal(bits(lora_run(*a)), bits(y)), "another run, other bits"
+    there = lora_run(*a, in_place=True)
+    assert torch.equal(bits(there), bits(y)), "in place"
+    assert torch.equal(there[:, n:], dev(a[6])[:, n:]), "columns past n in place"
+    none = dev((a[1] < 0) | (a[1] >= na))
+    assert torch.equal(bits(y)[none], bits(dev(a[6]))[none]), "rows without an adapter"
+
+
+@pytest.mark.parametrize("m", [1, 2, 15, 16, 17, 33, 64, 65, 200])
+@pytest.mark.parametrize("k,n,R", [(64, 256, 16), (264, 100, 8), (2048, 515, 32)])
+def test_lora_mixed_rows(m, k, n, R):
+    rng = np.random.default_rng(m)
+    lora_case(rng.integers(-1, 6, m), k, n, R, 5, seed=m + k)      # -1 and 5: none
+
+
+@pytest.mark.parametrize("R", [8, 16, 24, 32, 40, 64, 72, 128])
+def test_lora_ranks(R):
+    rng = np.random.default_rng(R)
+    ranks = [0, 1, R // 2, R - 1, R, min(R, 15), min(R, 17)]
+    lora_case(rng.integers(-1, 7, 40), 136, 77, R, 7, seed=R, ranks=ranks)
+    lora_case(rng.integers(0, 7, 600), 136, 77, R, 7, seed=R + 1, ranks=ranks)
+
+
+def test_lora_one_adapter_for_all():
+    lora_case([0] * 1, 8, 1, 8, 1, seed=20)
+    lora_case([0] * 47, 512, 256, 16, 1, seed=21)
+    lora_case([1] * 512, 512, 256, 16, 2, seed=22)
+    lora_case([1] * 1100, 512, 256, 16, 2, seed=23)
+
+
+def test_lora_no_adapters_used():
+    lora_case([-1] * 5, 64, 60, 16, 2, seed=24)
+    lora_case([-1] * 700, 64, 60, 16, 2, seed=25)
+    lora_case([7] * 5 + [-(1 << 31), (1 << 31) - 1], 64, 60, 16, 2, seed=26)
+
+
+@pytest.mark.parametrize("m", [511, 512, 513, 576, 1025, 2000])
+def test_lora_runs_of_rows(m):
+    """Requests one after the other: a tile may hold the end of one and the beginning of the next."""
+    rng = np.random.default_rng(m)
+    cuts = np.sort(rng.integers(0, m, 6))
+    lora_case(np.searchsorted(cuts, np.arange(m), side="right") - 1, 320, 300, 32, 7, seed=m, stride=512)
+    lora_case(rng.integers(-1, 4, m), 320, 300, 16, 4, seed=m + 1)
+
+
+def test_lora_without_scales_and_ranks():
+    x, adapter, a, b, scale, rank, base, n = lora_inputs([1, 0, -1, 1, 1], 96, 48, 16, 2, seed=27, ranks=[16, 16])
+    ref, bound = lora_oracle(x, adapter, a, b, None, None, base, n)
+    close(lora_run(x, adapter, a, b, None, None, base, n), ref, bound, "y")
+
+
+@pytest.mark.parametrize("m", [40, 700])
+def test_lora_rows_do_not_touch_each_other(m):
+    """Rows of NaN, infinities and large values among others, and an adapter that holds them."""
+    rng = np.random.default_rng(28)
+    x, adapter, a, b, scale, rank, base, n = lora_inputs(rng.integers(0, 4, m), 256, 128, 16, 4, seed=28, ranks=[16] * 4)
+    a[3, 2, 5], b[3, 7, 1] = np.inf, np.nan
+    adapter[:9] = [0, 0, 1, 1, 2, -1, 2, 0, 3]
+    x[1], x[3, 4], x[5], x[6, 1] = np.nan, np.inf, np.nan, 65504.0
+    base[7, 3] = np.inf
+    ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+    close(lora_run(x, adapter, a, b, scale, rank, base, n), ref, bound, "y")
+
+
+def test_lora_large_and_small_values():
+    """x A^T far beyond f16 and below its normal range keeps fp32 precision."""
+    x, adapter, a, b, scale, rank, base, n = lora_inputs([0, 1, 0, 1], 512, 64, 16, 2, seed=29, ranks=[16, 16])
+    x[0], x[2] = np.float16(3000) * x[0], np.float16(2.0 ** -12) * x[2]
+    a[0] = a[0] * np.float16(200)
+    base[2] = 0
+    scale[1] = -1e-20
+    base[1] = 0
+    ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+    close(lora_run(x, adapter, a, b, scale, rank, base, n), ref, bound, "y")
+
+
+def test_lora_captured_on_another_stream():
+    torch = torch_cuda()
+    rng = np.random.default_rng(30)
+    x, adapter, a, b, scale, rank, base, n = lora_inputs([0] * 30, 256, 200, 16, 3, seed=30, ranks=[16, 9, 4])
+    need = mz.mz_lora_workspace_bytes(30, 256, 16)
+    ws = torch.full((need // 4,), float("nan"), device="cuda")
+    d = [dev(v) for v in (x, adapter, a, b, scale, rank, base)]
+    y = torch.zeros(base.shape, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        mz.mz_lora_add(d[0].data_ptr(), 30, 256, d[1].data_ptr(), 3, d[2].data_ptr(), d[3].data_ptr(), 16, n,
+                       d[6].data_ptr(), y.data_ptr(), base.shape[1], ws.data_ptr(), need, stream(),
+                       scale_ptr=d[4].data_ptr(), rank_ptr=d[5].data_ptr())
+    for step in range(4):
+        adapter = rng.integers(-1, 4, 30).astype(np.int32)
+        x = rng.standard_normal(x.shape).astype(np.float16)
+        d[0].copy_(dev(x)), d[1].copy_(dev(adapter))
+        g.replay()
+        torch.cuda.synchronize()
+        ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+        close(y, ref, bound, f"step {step}")
+
+
+def test_lora_offsets_past_32_bits():
+    """Adapters and rows beyond 4 GiB from their bases."""
+    torch = torch_cuda()
+    k, n, R, na = 16384, 64, 128, 1200
+    a = torch.zeros(na, R, k, device="cuda", dtype=torch.float16)       # 4 MiB each
+    b = torch.zeros(na, n, R, device="cuda", dtype=torch.float16)
+    x, adapter, a1, b1, scale, rank, base, _ = lora_inputs([0, 0, -1], k, n, R, 1, seed=31, ranks=[R])
+    a[-1], b[-1] = dev(a1[0]), dev(b1[0])
+    need = mz.mz_lora_workspace_bytes(3, k, R)
+    ws, y = torch.full((need // 4,), float("nan"), device="cuda"), torch.zeros(base.shape, device="cuda")
+    d = [dev(v) for v in (x, np.where(adapter < 0, -1, na - 1).astype(np.int32), base)]
+    mz.mz_lora_add(d[0].data_ptr(), 3, k, d[1].data_ptr(), na, a.data_ptr(), b.data_ptr(), R, n, d[2].data_ptr(),
+                   y.data_ptr(), base.shape[1], ws.data_ptr(), need, stream())
+    torch.cuda.synchronize()
+    ref, bound = lora_oracle(x, adapter, a1, b1, None, None, base, n)
+    close(y, ref, bound, "y")
