@@ -695,6 +695,43 @@ mz_status mz_lora_add(const void *x_f16, int32_t m, int32_t k, const int32_t *ad
 /* Workspace bytes of mz_lora_add (-1 for invalid arguments). */
 int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank);
 
+/* Rules on m rows of logits; a zeroed struct means none of them. */
+typedef struct {
+  const float *penalty;        /* device float [m][3]: repetition, frequency and presence penalty of the row */
+  const int32_t *history;      /* device: the tokens that the rows' requests hold, row after row */
+  const int64_t *history_off;  /* device int64 [m + 1]: row i's are history[history_off[i] .. history_off[i + 1]) */
+  const int32_t *bias_token;   /* device: tokens with a bias, row after row */
+  const float *bias_value;     /* device: their biases */
+  const int64_t *bias_off;     /* device int64 [m + 1], as history_off */
+  const uint32_t *mask;        /* device uint32 [n_masks][mask_words]: bit v % 32 of word v / 32 is 1 where a
+                                  grammar allows token v */
+  const int32_t *mask_row;     /* device int32 [m]: the row's mask; outside 0..n_masks-1: none */
+  int32_t n_masks, mask_words;
+} mz_logits_rules_args;
+
+/* Apply the rules to rows of vocab logits, stride floats apart (a product's
+ * n_pad, say), and pick each row's token.  For token v with c occurrences in
+ * the row's history and logit x: where c > 0, x = (x > 0 ? x / repetition : x *
+ * repetition) - frequency * c - presence; then the bias of v is added, of
+ * several entries for v the last; then x = -inf where the mask forbids v.
+ * Each operation is rounded to fp32, in this order.  Tokens outside 0..vocab-1
+ * in a history or a bias list are passed over.  out: device float, rows stride
+ * floats apart, may be logits itself or NULL; columns past vocab are not
+ * touched.  token: device int32 [m] or NULL: the lowest token of the largest
+ * value, NaN aside; -1 where no value is above -inf (a mask that allows
+ * nothing).  rules NULL: none.  The caller sees that the offsets ascend and
+ * stay inside their lists.  workspace: device, caller-owned, needed for token
+ * only, at least mz_logits_rules_workspace_bytes(m, vocab) bytes, any content,
+ * not shared by calls in flight together.  m may be 0, vocab is at most 2^30.
+ * Errors: EINVAL for sizes out of range, a list without its offsets, values or penalties, a mask
+ * of too few words, neither out nor token, or a short workspace. */
+mz_status mz_logits_rules(const float *logits, int32_t m, int32_t vocab, int64_t stride,
+                          const mz_logits_rules_args *rules, float *out, int32_t *token,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Workspace bytes of mz_logits_rules (-1 for invalid arguments). */
+int64_t mz_logits_rules_workspace_bytes(int32_t m, int32_t vocab);
+
 /* x = h / sqrt(mean(h^2) + eps) per row: h float [m][d] -> x f16 [m][d]. */
 mz_status mz_rmsnorm(const void *h_f32, int32_t m, int32_t d, float eps, void *x_f16,
                      void *stream);

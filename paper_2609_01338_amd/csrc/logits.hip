@@ -1,0 +1,194 @@
+// Rules on the logits of a batch of requests, and the token each row takes
+// (gfx950).  For value x of token v in row i, with c occurrences of v in the
+// row's history:
+//   c > 0:  x = (x > 0 ? x / rep : x rep) - freq c - pres
+//   v named by the row's biases:  x += the last of its entries
+//   v's bit of the row's grammar mask is 0:  x = -inf
+// then token = lowest index of the largest x, -1 where nothing is above -inf
+// (NaN is never taken).  Each step is rounded to fp32 by itself.
+//
+// Memory-bound: the logits are read and written once.  A workgroup owns a
+// slice of one row's vocabulary; it reads the row's whole history and bias
+// list and keeps what falls into its slice in LDS, as counts (integer adds)
+// and as the highest entry index per token (integer max), so neither needs
+// vocabulary-sized memory, and the order in which lanes arrive changes
+// nothing.  The slices' largest values meet in a second, small kernel.
+#include "mz_kernels.h"
+
+namespace mzk {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// (value, index) of the larger value, of the lower index where they are equal.
+__device__ __forceinline__ void take(float& bv, int& bi, float ov, int oi) {
+  if (ov > bv || (ov == bv && oi < bi)) {
+    bv = ov;
+    bi = oi;
+  }
+}
+
+__device__ __forceinline__ void wave_best(float& bv, int& bi) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float ov = __shfl_xor(bv, o);
+    const int oi = __shfl_xor(bi, o);
+    take(bv, bi, ov, oi);
+  }
+}
+
+__device__ __forceinline__ float penalised(float x, float count, float rep, float freq, float pres) {
+#pragma clang fp contract(off)
+  const float held = x > 0.f ? x / rep : x * rep;
+  const float f = count * freq;
+  const float y = held - f;
+  return y - pres;
+}
+
+template <int SLICE, int VEC>
+__global__ __launch_bounds__(256) void logits_rules_kernel(LogitsRules p) {
+  constexpr int GROUPS = SLICE / (256 * VEC);
+  __shared__ __attribute__((aligned(16))) int s_count[SLICE];
+  __shared__ __attribute__((aligned(16))) int s_last[SLICE];
+  __shared__ float s_val[4];
+  __shared__ int s_idx[4];
+  const int row = blockIdx.x / p.slices, v0 = (blockIdx.x % p.slices) * SLICE, tid = threadIdx.x;
+  const float* x = p.logits + (int64_t)row * p.stride;
+  // value e of group i: token at(i) + e
+  auto at = [&](int i) { return v0 + (i * 256 + tid) * VEC; };
+  float val[GROUPS][VEC];
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const int v = at(i);
+    if (VEC == 4 && v + 4 <= p.vocab) {
+      const f32x4 u = *reinterpret_cast<const f32x4*>(x + v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) val[i][e] = u[e & 3];
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) val[i][e] = v + e < p.vocab ? x[v + e] : -INFINITY;
+    }
+  }
+  const int mask_row = p.mask ? p.mask_row[row] : -1;
+  uint32_t bits[GROUPS];
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    bits[i] = ~0u;
+    if ((unsigned)mask_row < (unsigned)p.n_masks && at(i) < p.vocab)
+      bits[i] = p.mask[(int64_t)mask_row * p.mask_words + at(i) / 32] >> (at(i) & 31);
+  }
+  const int64_t h0 = p.history ? p.history_off[row] : 0, h1 = p.history ? p.history_off[row + 1] : 0;
+  const int64_t b0 = p.bias_token ? p.bias_off[row] : 0, b1 = p.bias_token ? p.bias_off[row + 1] : 0;
+  const bool hist = h1 > h0, bias = b1 > b0;
+  if (hist || bias) {
+    for (int i = tid * 4; i < SLICE; i += 1024) {
+      *reinterpret_cast<int4*>(&s_count[i]) = make_int4(0, 0, 0, 0);
+      *reinterpret_cast<int4*>(&s_last[i]) = make_int4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    const unsigned here = (unsigned)min(SLICE, p.vocab - v0);
+#pragma unroll 4
+    for (int64_t i = h0 + tid; i < h1; i += 256) {
+      const unsigned t = (unsigned)p.history[i] - (unsigned)v0;
+      if (t < here) atomicAdd(&s_count[t], 1);
+    }
+    for (int64_t i = b0 + tid; i < b1; i += 256) {
+      const unsigned t = (unsigned)p.bias_token[i] - (unsigned)v0;
+      if (t < here) atomicMax(&s_last[t], (int)(i - b0) + 1);
+    }
+    __syncthreads();
+    const float* pen = p.penalty + (int64_t)row * 3;
+    const float rep = hist ? pen[0] : 1.f, freq = hist ? pen[1] : 0.f, pres = hist ? pen[2] : 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const int t = at(i) + e - v0, c = s_count[t], last = s_last[t];
+        if (c > 0) val[i][e] = penalised(val[i][e], (float)c, rep, freq, pres);
+        if (last > 0) val[i][e] += p.bias_value[b0 + last - 1];
+      }
+  }
+  float bv = -INFINITY;
+  int bi = 0x7fffffff;
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const int v = at(i);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      if (!((bits[i] >> e) & 1)) val[i][e] = -INFINITY;
+      if (val[i][e] > bv && v + e < p.vocab) {       // a thread's tokens ascend
+        bv = val[i][e];
+        bi = v + e;
+      }
+    }
+    if (p.out) {
+      float* o = p.out + (int64_t)row * p.stride + v;
+      if (VEC == 4 && v + 4 <= p.vocab) {
+        f32x4 u;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[e & 3] = val[i][e];
+        *reinterpret_cast<f32x4*>(o) = u;
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (v + e < p.vocab) o[e] = val[i][e];
+      }
+    }
+  }
+  if (!p.token) return;
+  wave_best(bv, bi);
+  if ((tid & 63) == 0) {
+    s_val[tid >> 6] = bv;
+    s_idx[tid >> 6] = bi;
+  }
+  __syncthreads();
+  if (tid == 0) {
+#pragma unroll
+    for (int i = 1; i < 4; ++i) take(bv, bi, s_val[i], s_idx[i]);
+    p.part_val[blockIdx.x] = bv;
+    p.part_idx[blockIdx.x] = bi;
+  }
+}
+
+__global__ __launch_bounds__(64) void logits_token_kernel(LogitsRules p) {
+  float bv = -INFINITY;
+  int bi = 0x7fffffff;
+  const int64_t first = (int64_t)blockIdx.x * p.slices;
+  for (int i = threadIdx.x; i < p.slices; i += 64) take(bv, bi, p.part_val[first + i], p.part_idx[first + i]);
+  wave_best(bv, bi);
+  if (threadIdx.x == 0) p.token[blockIdx.x] = bi == 0x7fffffff ? -1 : bi;
+}
+
+constexpr int kSmallSlice = 1024, kSlice = 4096;
+
+int logits_slice(int m, int vocab) { return (int64_t)m * ((vocab + kSlice - 1) / kSlice) >= 512 ? kSlice : kSmallSlice; }
+
+}  // namespace
+
+int64_t logits_rules_blocks(int m, int vocab) {
+  const int slice = logits_slice(m, vocab);
+  return ((int64_t)vocab + slice - 1) / slice * m;
+}
+
+void launch_logits_rules(LogitsRules p, int m, void* ws, hipStream_t s) {
+  const int slice = logits_slice(m, p.vocab);
+  p.slices = (p.vocab + slice - 1) / slice;
+  p.part_val = reinterpret_cast<float*>(ws);
+  p.part_idx = reinterpret_cast<int32_t*>(p.part_val + (int64_t)m * p.slices);
+  const bool vec = p.stride % 4 == 0 && ((uintptr_t)p.logits & 15) == 0 && ((uintptr_t)p.out & 15) == 0;
+  const dim3 grid(m * p.slices), block(256);
+  if (slice == kSlice) {
+    if (vec)
+      hipLaunchKernelGGL((logits_rules_kernel<kSlice, 4>), grid, block, 0, s, p);
+    else
+      hipLaunchKernelGGL((logits_rules_kernel<kSlice, 1>), grid, block, 0, s, p);
+  } else {
+    if (vec)
+      hipLaunchKernelGGL((logits_rules_kernel<kSmallSlice, 4>), grid, block, 0, s, p);
+    else
+      hipLaunchKernelGGL((logits_rules_kernel<kSmallSlice, 1>), grid, block, 0, s, p);
+  }
+  if (p.token) hipLaunchKernelGGL(logits_token_kernel, dim3(m), dim3(64), 0, s, p);
+}
+
+}  // namespace mzk

@@ -211,6 +211,30 @@ struct Lora {
 int64_t lora_ws_bytes(int m, int k, int R);
 void launch_lora(Lora p, void* ws, hipStream_t s);
 
+// Penalties, biases and masks on m rows of logits and the token of each (see
+// mz.h, mz_logits_rules); out and token may be null, and each of history,
+// bias_token and mask.  The last line is the launcher's own, in ws (8 bytes
+// for each of logits_rules_blocks(m, vocab), which is below 2^31).
+struct LogitsRules {
+  const float* logits;
+  float* out;
+  int64_t stride;
+  int vocab;
+  const float* penalty;            // [m][3] repetition, frequency, presence
+  const int32_t* history;
+  const int64_t* history_off;      // [m + 1]
+  const int32_t* bias_token;
+  const float* bias_value;
+  const int64_t* bias_off;         // [m + 1]
+  const uint32_t* mask;            // [n_masks][mask_words]
+  const int32_t* mask_row;         // [m]
+  int n_masks, mask_words;
+  int32_t* token;
+  int slices; float* part_val; int32_t* part_idx;
+};
+int64_t logits_rules_blocks(int m, int vocab);
+void launch_logits_rules(LogitsRules p, int m, void* ws, hipStream_t s);
+
 // h float [m][d] = dequant(E[tok[i]]) with E split into nibbles [V][d/2] and
 // fp16 scales [V][d/32]; with last_tok (device) row m - 1 takes *last_tok.
 void launch_embed(const uint8_t* e_nib, const uint16_t* e_scale, const int32_t* tok, int m, int d,

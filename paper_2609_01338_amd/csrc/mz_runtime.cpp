@@ -2216,6 +2216,50 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
   });
 }
 
+int64_t mz_logits_rules_workspace_bytes(int32_t m, int32_t vocab) {
+  if (m < 1 || vocab < 1) return -1;
+  return mzk::logits_rules_blocks(m, vocab) * 8;
+}
+
+mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t stride, const mz_logits_rules_args* rules,
+                          float* out, int32_t* token, void* workspace, int64_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&] {
+    const mz_logits_rules_args r = rules ? *rules : mz_logits_rules_args{};
+    if (!logits || (!out && !token)) fail(MZ_EINVAL, "NULL pointer");
+    if (m < 0 || vocab < 1 || vocab > (1 << 30) || stride < vocab)
+      fail(MZ_EINVAL, "m must be at least 0, vocab in 1..2^30, stride at least vocab");
+    if (((uintptr_t)logits & 3) || ((uintptr_t)out & 3)) fail(MZ_EINVAL, "logits and out must lie on 4-byte boundaries");
+    if (r.history && (!r.history_off || !r.penalty)) fail(MZ_EINVAL, "history needs history_off and penalty");
+    if (r.bias_token && (!r.bias_value || !r.bias_off)) fail(MZ_EINVAL, "bias_token needs bias_value and bias_off");
+    if (r.mask && (!r.mask_row || r.n_masks < 1 || r.mask_words < ((int64_t)vocab + 31) / 32))
+      fail(MZ_EINVAL, "mask needs mask_row, n_masks, and mask_words that cover vocab");
+    check_stream(stream);
+    if (m == 0) return;
+    const int64_t blocks = mzk::logits_rules_blocks(m, vocab);
+    if (blocks > INT32_MAX) fail(MZ_EINVAL, "too many rows");
+    if (token && (!workspace || ((uintptr_t)workspace & 3) || workspace_bytes < blocks * 8))
+      fail(MZ_EINVAL, "workspace too small");
+    mzk::LogitsRules p{};
+    p.logits = logits;
+    p.out = out;
+    p.stride = stride;
+    p.vocab = vocab;
+    p.penalty = r.penalty;
+    p.history = r.history;
+    p.history_off = r.history_off;
+    p.bias_token = r.bias_token;
+    p.bias_value = r.bias_value;
+    p.bias_off = r.bias_off;
+    p.mask = r.mask;
+    p.mask_row = r.mask_row;
+    p.n_masks = r.n_masks;
+    p.mask_words = r.mask_words;
+    p.token = token;
+    mzk::launch_logits_rules(p, m, workspace, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
 mz_status mz_rmsnorm(const void* h, int32_t m, int32_t d, float eps, void* x, void* stream) {
   return guarded(nullptr, [&] {
     if (!h || !x) fail(MZ_EINVAL, "NULL pointer");

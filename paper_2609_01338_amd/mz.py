@@ -73,6 +73,13 @@ class mz_kv_append_args(ctypes.Structure):
                 ("n_table", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32), ("q_out", ctypes.c_void_p)]
 
 
+class mz_logits_rules_args(ctypes.Structure):
+    _fields_ = [("penalty", ctypes.c_void_p), ("history", ctypes.c_void_p), ("history_off", ctypes.c_void_p),
+                ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("bias_off", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p), ("mask_row", ctypes.c_void_p), ("n_masks", ctypes.c_int32),
+                ("mask_words", ctypes.c_int32)]
+
+
 SIZE_RULES = {"paper": 0, "total": 1}
 STAGES = ("kv-only", "kv-and-w", "w-only", "exhausted")
 _INFO_KEYS = ("released", "T", "stage", "link_s", "recompute_s", "n_kv", "n_w", "reached")
@@ -131,6 +138,8 @@ def lib() -> ctypes.CDLL:
         "mz_attention_batch_workspace_bytes": ([i32, i32, i32, i32], i64),
         "mz_lora_add": ([vp, i32, i32, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp, i64, vp], i32),
         "mz_lora_workspace_bytes": ([i32, i32, i32], i64),
+        "mz_logits_rules": ([vp, i32, i32, i64, ctypes.POINTER(mz_logits_rules_args), vp, vp, vp, i64, vp], i32),
+        "mz_logits_rules_workspace_bytes": ([i32, i32], i64),
         "mz_rmsnorm": ([vp, i32, i32, ctypes.c_float, vp, vp], i32),
         "mz_probe_ceilings": ([i32, ctypes.c_char_p, sz], i32),
         "mz_plan_evict": ([ctypes.POINTER(mz_model_cfg), ctypes.POINTER(mz_evict_request), vp, vp, vp], i32),
@@ -485,6 +494,22 @@ def mz_lora_add(x_ptr: int, m: int, k: int, adapter_ptr: int, n_adapters: int, a
 
 def mz_lora_workspace_bytes(m: int, k: int, max_rank: int) -> int:
     return int(lib().mz_lora_workspace_bytes(m, k, max_rank))
+
+
+def mz_logits_rules(logits_ptr: int, m: int, vocab: int, stride: int, out_ptr: Optional[int], token_ptr: Optional[int],
+                    ws_ptr: Optional[int], ws_bytes: int, stream: Optional[int] = None, penalty_ptr: int = 0,
+                    history_ptr: int = 0, history_off_ptr: int = 0, bias_token_ptr: int = 0, bias_value_ptr: int = 0,
+                    bias_off_ptr: int = 0, mask_ptr: int = 0, n_masks: int = 0, mask_words: int = 0,
+                    mask_row_ptr: int = 0) -> None:
+    """Device pointers as integers (0: absent)."""
+    r = mz_logits_rules_args(penalty_ptr, history_ptr, history_off_ptr, bias_token_ptr, bias_value_ptr, bias_off_ptr,
+                             mask_ptr, mask_row_ptr, n_masks, mask_words)
+    _check(lib().mz_logits_rules(logits_ptr, m, vocab, stride, ctypes.byref(r), out_ptr, token_ptr, ws_ptr, ws_bytes,
+                                 stream), None)
+
+
+def mz_logits_rules_workspace_bytes(m: int, vocab: int) -> int:
+    return int(lib().mz_logits_rules_workspace_bytes(m, vocab))
 
 
 def mz_rmsnorm(h_ptr: int, m: int, d: int, eps: float, x_ptr: int, stream: Optional[int] = None) -> None:

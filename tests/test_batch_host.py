@@ -109,3 +109,29 @@ def test_lora_workspace_and_no_rows():
     for bad in [(0, 64, 16), (3, 4, 16), (3, 64, 4), (3, 64, 129)]:
         assert mz.mz_lora_workspace_bytes(*bad) == -1
     mz.mz_lora_add(**{**LORA, "m": 0, "ws_bytes": 0})
+
+
+LOGITS = dict(logits_ptr=P, m=3, vocab=1000, stride=1024, out_ptr=P, token_ptr=P, ws_ptr=P, ws_bytes=1 << 20, penalty_ptr=P,
+              history_ptr=P, history_off_ptr=P, bias_token_ptr=P, bias_value_ptr=P, bias_off_ptr=P, mask_ptr=P, n_masks=1,
+              mask_words=32, mask_row_ptr=P)
+
+
+@pytest.mark.parametrize("bad,match", [
+    (dict(logits_ptr=0), "NULL"), (dict(out_ptr=0, token_ptr=0), "NULL"), (dict(logits_ptr=P + 2), "4-byte"),
+    (dict(out_ptr=P + 1), "4-byte"), (dict(m=-1), "stride"), (dict(vocab=0), "vocab"), (dict(vocab=(1 << 30) + 1), "vocab"),
+    (dict(stride=999), "stride"), (dict(stride=-1024), "stride"),
+    (dict(history_off_ptr=0), "history"), (dict(penalty_ptr=0), "history"), (dict(bias_value_ptr=0), "bias"),
+    (dict(bias_off_ptr=0), "bias"), (dict(mask_row_ptr=0), "mask"), (dict(n_masks=0), "mask"), (dict(mask_words=31), "mask"),
+    (dict(m=(1 << 31) - 1, vocab=1 << 20, stride=1 << 20, mask_words=1 << 20), "too many"),
+    (dict(ws_ptr=0), "workspace"), (dict(ws_bytes=0), "workspace"), (dict(ws_ptr=P + 2), "workspace"),
+])
+def test_logits_rules_refusals(bad, match):
+    refused(mz.mz_logits_rules, **{**LOGITS, **bad}, match=match)
+
+
+def test_logits_rules_workspace_and_no_rows():
+    need = mz.mz_logits_rules_workspace_bytes(3, 1000)
+    assert need > 0
+    refused(mz.mz_logits_rules, **{**LOGITS, "ws_bytes": need - 1}, match="workspace")
+    assert mz.mz_logits_rules_workspace_bytes(0, 1000) == -1 and mz.mz_logits_rules_workspace_bytes(3, 0) == -1
+    mz.mz_logits_rules(**{**LOGITS, "m": 0, "ws_ptr": 0, "ws_bytes": 0})

@@ -644,3 +644,189 @@ def test_lora_offsets_past_32_bits():
     torch.cuda.synchronize()
     ref, bound = lora_oracle(x, adapter, a1, b1, None, None, base, n)
     close(y, ref, bound, "y")
+
+
+# ----------------------------------------------------------------------------- rules on logits
+
+def logits_oracle(x, penalty, histories, biases, mask, mask_row):
+    """(out, bound): at most five fp32 roundings of values no larger than the parts."""
+    m, v = x.shape
+    out, bound = x.astype(np.float64), np.zeros(x.shape)
+    with np.errstate(all="ignore"):
+        for i in range(m):
+            rep, freq, pres = (float(t) for t in penalty[i])
+            h = np.array([t for t in histories[i] if 0 <= t < v], np.int64)
+            ids, c = np.unique(h, return_counts=True)
+            old = out[i, ids]
+            held = np.where(old > 0, old / rep, old * rep)
+            out[i, ids] = held - freq * c - pres
+            bound[i, ids] = 5 * U32 * (np.abs(held) + np.abs(freq * c) + abs(pres))
+            last = {t: b for t, b in biases[i] if 0 <= t < v}
+            for t, b in last.items():
+                out[i, t] += b
+                bound[i, t] += U32 * (abs(out[i, t]) + abs(b))
+            if mask is not None and 0 <= mask_row[i] < len(mask):
+                bits = np.unpackbits(mask[mask_row[i]].view(np.uint8), bitorder="little")[:v]
+                out[i, bits == 0] = -np.inf
+    return out, bound
+
+
+def rows_of(lists, dtype):
+    off = np.concatenate([[0], np.cumsum([len(t) for t in lists])]).astype(np.int64)
+    flat = np.array([t for one in lists for t in one] + [0], dtype)      # never an empty buffer
+    return flat, off
+
+
+def logits_run(x, penalty, histories, biases, mask, mask_row, stride=None, mode="new", shift=0):
+    """mode: "new" rows, "in place", or "token" only.  shift: floats before the first row (alignment)."""
+    torch = torch_cuda()
+    m, v = x.shape
+    stride = stride or v
+    rows = np.full((m, stride), 9.0, np.float32)
+    rows[:, :v] = x
+    buf = torch.full((shift + m * stride,), 5.0, device="cuda")
+    buf[shift:] = dev(rows).view(-1)
+    src = buf[shift:].view(m, stride)
+    dst = torch.full((shift + m * stride,), 7.0, device="cuda")[shift:].view(m, stride) if mode == "new" else src
+    need = mz.mz_logits_rules_workspace_bytes(m, v)
+    ws, token = torch.full((need // 4,), float("nan"), device="cuda"), torch.full((m,), -7, device="cuda", dtype=torch.int32)
+    kw, keep = {}, []
+    if histories is not None:
+        flat, off = rows_of(histories, np.int32)
+        keep += [dev(flat), dev(off), dev(np.asarray(penalty, np.float32))]
+        kw.update(history_ptr=keep[-3].data_ptr(), history_off_ptr=keep[-2].data_ptr(), penalty_ptr=keep[-1].data_ptr())
+    if biases is not None:
+        tok, off = rows_of([[t for t, _ in b] for b in biases], np.int32)
+        val, _ = rows_of([[u for _, u in b] for b in biases], np.float32)
+        keep += [dev(tok), dev(val), dev(off)]
+        kw.update(bias_token_ptr=keep[-3].data_ptr(), bias_value_ptr=keep[-2].data_ptr(), bias_off_ptr=keep[-1].data_ptr())
+    if mask is not None:
+        keep += [dev(mask.view(np.int32)), dev(np.asarray(mask_row, np.int32))]
+        kw.update(mask_ptr=keep[-2].data_ptr(), n_masks=mask.shape[0], mask_words=mask.shape[1], mask_row_ptr=keep[-1].data_ptr())
+    mz.mz_logits_rules(src.data_ptr(), m, v, stride, None if mode == "token" else dst.data_ptr(), token.data_ptr(),
+                       ws.data_ptr(), need, stream(), **kw)
+    torch.cuda.synchronize()
+    if mode == "token":
+        assert torch.equal(src.contiguous().view(torch.int32), dev(rows.view(np.int32))), "the logits are only read"
+    else:
+        assert bool((dst[:, v:] == (7.0 if mode == "new" else 9.0)).all()), "columns past vocab"
+    return dst[:, :v].cpu().numpy(), token.cpu().numpy()
+
+
+def picked(out):
+    """The lowest token of the largest value, NaN aside; -1 where nothing is above -inf."""
+    best = np.where(np.isnan(out), -np.inf, out)
+    return np.where(best.max(1) > -np.inf, best.argmax(1), -1)
+
+
+def logits_inputs(m, v, seed, n_hist=50, n_bias=9, n_masks=3, low=0):
+    rng = np.random.default_rng(seed)
+    x = (rng.standard_normal((m, v)) * 3).astype(np.float32)
+    penalty = np.stack([1 + rng.random(m), rng.random(m), rng.random(m) - 0.3], 1).astype(np.float32)
+    # repeats, tokens outside the vocabulary, some empty lists
+    histories = [[int(t) for t in (rng.random(int(rng.integers(0, n_hist + 1))) ** 3 * (v + 3) - low)] for _ in range(m)]
+    biases = [[(int(rng.integers(-2, v + 2)), float(np.float32(rng.standard_normal()))) for _ in range(int(rng.integers(0, n_bias + 1)))]
+              for _ in range(m)]
+    mask = rng.integers(0, 1 << 32, (n_masks, (v + 31) // 32 + 1), dtype=np.uint32)
+    mask_row = rng.integers(-1, n_masks + 1, m).astype(np.int32)
+    return x, penalty, histories, biases, mask, mask_row
+
+
+def logits_case(a, **kw):
+    report("logits", m=a[0].shape[0], vocab=a[0].shape[1], kw=kw)
+    none = [[] for _ in a[2] or a[0]]
+    ref, bound = logits_oracle(a[0], a[1], a[2] or none, a[3] or none, a[4], a[5])
+    out, token = logits_run(*a, **kw)
+    close(out, ref, bound, "logits")
+    assert np.array_equal(token, picked(out))
+    assert np.array_equal(logits_run(*a, **{**kw, "mode": "in place"})[0].view(np.int32), out.view(np.int32)), "in place"
+    assert np.array_equal(logits_run(*a, **{**kw, "mode": "token"})[1], token), "token only"
+    return out, token
+
+
+@pytest.mark.parametrize("m,v", [(1, 1), (1, 3), (2, 31), (3, 33), (1, 1000), (4, 1024), (2, 1025), (5, 4096), (3, 10007),
+                                 (1, 128256), (200, 12345)])
+def test_logits_rules(m, v):
+    logits_case(logits_inputs(m, v, seed=m + v, low=2))
+
+
+@pytest.mark.parametrize("v,stride,shift", [(1000, 1024, 0), (1001, 1024, 0), (1000, 1003, 0), (1000, 1024, 1), (4099, 4352, 4)])
+def test_logits_strides_and_alignment(v, stride, shift):
+    logits_case(logits_inputs(3, v, seed=v + stride), stride=stride, shift=shift)
+
+
+@pytest.mark.parametrize("use", range(8))
+def test_logits_rules_one_by_one(use):
+    x, penalty, histories, biases, mask, mask_row = logits_inputs(6, 3000, seed=30)
+    logits_case((x, penalty, histories if use & 1 else None, biases if use & 2 else None, mask if use & 4 else None,
+                 mask_row if use & 4 else None))
+
+
+def test_logits_long_histories():
+    rng = np.random.default_rng(31)
+    x, penalty, _, biases, mask, mask_row = logits_inputs(3, 5000, seed=31, n_bias=3000)
+    histories = [[7] * 70000, [int(t) for t in rng.integers(0, 5000, 40000)], []]
+    logits_case((x, penalty, histories, biases, mask, mask_row))
+
+
+def test_logits_many_rows():
+    """The larger slices, and rows enough for many workgroups."""
+    logits_case(logits_inputs(130, 20000, seed=32, n_hist=300))
+
+
+def test_logits_of_repeated_biases_the_last_counts():
+    x = np.zeros((2, 100), np.float32)
+    biases = [[(5, 1.0), (6, 2.0), (5, -3.0), (5, 0.5)], [(99, 4.0)] * 600 + [(99, -4.0)]]
+    out, token = logits_case((x, np.ones((2, 3)), None, biases, None, None))
+    assert out[0, 5] == 0.5 and out[0, 6] == 2.0 and out[1, 99] == -4.0 and token.tolist() == [6, 0]
+
+
+def test_logits_ties_masks_and_not_numbers():
+    v = 2500
+    x = np.full((8, v), -1.0, np.float32)
+    x[0, [3, 700, 2000]] = 5.0                       # the lowest of equal ones, across slices
+    x[1, :] = np.nan
+    x[2, :] = np.nan
+    x[2, 1234] = -8.0
+    x[3, :] = -np.inf
+    x[4, 17] = np.inf
+    x[4, 18] = np.nan
+    x[5, :] = -3.402823466e38
+    x[6, 4] = -0.0
+    x[6, 2] = 0.0
+    mask = np.zeros((2, (v + 31) // 32), np.uint32)
+    mask[1, 2400 // 32] = 1 << (2400 % 32)
+    mask_row = np.array([-1, -1, -1, -1, -1, -1, -1, 0], np.int32)
+    histories = [[]] * 6 + [[2, 4, 4], []]
+    pen = np.array([[1.5, 0.0, 0.0]] * 8)
+    out, token = logits_case((x, pen, histories, None, mask, mask_row))
+    assert token.tolist() == [3, -1, 1234, -1, 17, 0, 2, -1]
+    _, token = logits_case((x, pen, histories, None, mask, np.full(8, 1, np.int32)))
+    assert token.tolist() == [2400, -1, -1, -1, 2400, 2400, 2400, 2400]
+
+
+def test_logits_captured_on_another_stream():
+    torch = torch_cuda()
+    m, v = 3, 5000
+    x, penalty, _, _, mask, mask_row = logits_inputs(m, v, seed=33)
+    need = mz.mz_logits_rules_workspace_bytes(m, v)
+    ws = torch.full((need // 4,), float("nan"), device="cuda")
+    history, off = torch.zeros(1000, device="cuda", dtype=torch.int32), torch.zeros(m + 1, device="cuda", dtype=torch.int64)
+    d = [dev(x), dev(penalty), dev(mask.view(np.int32)), dev(mask_row)]
+    out, token = torch.zeros(m, v, device="cuda"), torch.zeros(m, device="cuda", dtype=torch.int32)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        mz.mz_logits_rules(d[0].data_ptr(), m, v, v, out.data_ptr(), token.data_ptr(), ws.data_ptr(), need, stream(),
+                           penalty_ptr=d[1].data_ptr(), history_ptr=history.data_ptr(), history_off_ptr=off.data_ptr(),
+                           mask_ptr=d[2].data_ptr(), n_masks=mask.shape[0], mask_words=mask.shape[1], mask_row_ptr=d[3].data_ptr())
+    rng = np.random.default_rng(34)
+    for step in range(4):
+        x = (rng.standard_normal((m, v)) * 3).astype(np.float32)
+        histories = [[int(t) for t in rng.integers(0, 60, 100 * step)] for _ in range(m)]
+        flat, offs = rows_of(histories, np.int32)
+        d[0].copy_(dev(x)), off.copy_(dev(offs)), history[:len(flat)].copy_(dev(flat))
+        g.replay()
+        torch.cuda.synchronize()
+        ref, bound = logits_oracle(x, penalty, histories, [[]] * m, mask, mask_row)
+        close(out, ref, bound, f"step {step}")
+        assert np.array_equal(token.cpu().numpy(), picked(out.cpu().numpy()))
