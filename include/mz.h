@@ -157,6 +157,29 @@ mz_status mz_first_token(mz_ctx *ctx, int32_t *token_out, float *logits_out);
  * holds the tokens of the steps that ran. */
 mz_status mz_generate(mz_ctx *ctx, int32_t token, int32_t n, int32_t *tokens_out);
 
+/* Rules on the tokens that mz_first_token and mz_generate choose (see
+ * mz_logits_rules for what they do to the logits).  The history of the
+ * penalties is the cached context, prompt included.  Arrays are host memory. */
+typedef struct {
+  float repetition, frequency, presence;   /* 1, 0, 0: no penalties */
+  const int32_t *bias_token;   /* [n_bias] tokens and what is added to their logits; of several entries */
+  const float *bias_value;     /* for a token the last counts */
+  int32_t n_bias;              /* 0..vocab */
+  const uint32_t *mask;        /* [ceil(vocab / 32)], bit v % 32 of word v / 32 is 1 where token v is
+                                  allowed, or NULL: all are */
+} mz_token_rules;
+
+/* Set the rules for the tokens chosen from now on (NULL: none, the default);
+ * they stay until the next call.  With rules, logits_out of mz_first_token
+ * holds the logits after them, and mz_generate takes its steps one by one.
+ * Where they leave no token above -inf (finite biases and a mask that allows
+ * something do, unless logits are not numbers), mz_first_token gives -1 and
+ * MZ_ESTATE, and mz_generate ends there.  Synchronizes; allocates device
+ * memory the first time.  Errors: EINVAL for a repetition that is not
+ * positive, penalties that are not finite, n_bias out of range, a bias token
+ * outside the vocabulary, a NaN bias or a mask without a token; ENOMEM. */
+mz_status mz_set_token_rules(mz_ctx *ctx, const mz_token_rules *rules);
+
 /* Engine options: "overlap" (1: swap-in overlapped with compute, default;
  * 0: every copy finishes before compute starts), "kernel_timing" (1: time
  * every kernel launch with HIP events on its stream; setting it clears the

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void logits_rules_kernel(LogitsRules p) {
       for (int e = 0; e < VEC; ++e) val[i][e] = v + e < p.vocab ? x[v + e] : -INFINITY;
     }
   }
-  const int mask_row = p.mask ? p.mask_row[row] : -1;
+  const int mask_row = !p.mask ? -1 : p.mask_row ? p.mask_row[row] : 0;
   uint32_t bits[GROUPS];
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
@@ -77,8 +77,9 @@ __global__ __launch_bounds__(256) void logits_rules_kernel(LogitsRules p) {
     if ((unsigned)mask_row < (unsigned)p.n_masks && at(i) < p.vocab)
       bits[i] = p.mask[(int64_t)mask_row * p.mask_words + at(i) / 32] >> (at(i) & 31);
   }
-  const int64_t h0 = p.history ? p.history_off[row] : 0, h1 = p.history ? p.history_off[row + 1] : 0;
-  const int64_t b0 = p.bias_token ? p.bias_off[row] : 0, b1 = p.bias_token ? p.bias_off[row + 1] : 0;
+  int64_t h0 = 0, h1 = p.n_history, b0 = 0, b1 = p.n_bias;
+  if (p.history_off) h0 = p.history_off[row], h1 = p.history_off[row + 1];
+  if (p.bias_off) b0 = p.bias_off[row], b1 = p.bias_off[row + 1];
   const bool hist = h1 > h0, bias = b1 > b0;
   if (hist || bias) {
     for (int i = tid * 4; i < SLICE; i += 1024) {

@@ -213,8 +213,10 @@ void launch_lora(Lora p, void* ws, hipStream_t s);
 
 // Penalties, biases and masks on m rows of logits and the token of each (see
 // mz.h, mz_logits_rules); out and token may be null, and each of history,
-// bias_token and mask.  The last line is the launcher's own, in ws (8 bytes
-// for each of logits_rules_blocks(m, vocab), which is below 2^31).
+// bias_token and mask.  A single row may leave out the offsets (its lists are
+// n_history and n_bias long) and mask_row (mask 0).  The last line is the
+// launcher's own, in ws (8 bytes for each of logits_rules_blocks(m, vocab),
+// which is below 2^31).
 struct LogitsRules {
   const float* logits;
   float* out;
@@ -228,7 +230,7 @@ struct LogitsRules {
   const int64_t* bias_off;         // [m + 1]
   const uint32_t* mask;            // [n_masks][mask_words]
   const int32_t* mask_row;         // [m]
-  int n_masks, mask_words;
+  int n_masks, mask_words, n_history, n_bias;
   int32_t* token;
   int slices; float* part_val; int32_t* part_idx;
 };

@@ -385,12 +385,13 @@ struct HostArena {
 
 enum KernelKind {
   kKEmbed, kKRmsnorm, kKGemmKV, kKRopeKV, kKGemmQ, kKRopeQ, kKGather, kKAttention, kKGemmO,
-  kKGemmGateUp, kKGemmDown, kKLmHead, kKAttentionSplit, kKGemmQKV1, kKCount
+  kKGemmGateUp, kKGemmDown, kKLmHead, kKAttentionSplit, kKGemmQKV1, kKLogitsRules,
+  kKCount
 };
 const char* kKindName[kKCount] = {"embed_q4", "rmsnorm", "gemm_q4_kv", "rope_kv", "gemm_q4_q",
                                   "rope_q", "gather_rows", "attention", "gemm_q4_o",
                                   "gemm_q4_gateup", "gemm_q4_down", "lm_head_argmax", "attention_split",
-                                  "gemm_q4_qkv_one_row"};
+                                  "gemm_q4_qkv_one_row", "logits_rules"};
 // HIP kernel symbols each kind launches, the epilogue as the first template
 // argument (to line up with profiler summaries).  Products that split over K
 // run as <3> and a gemm_splitk_reduce (_rope for Q and K/V), single rows as
@@ -401,7 +402,7 @@ const char* kKindKernel[kKCount] = {"embed_kernel", "rmsnorm_kernel", "gemm_q4_k
                                     "gemm_q4_kernel<2>|gemm_rows_kernel<2>", "gemm_q4_kernel<1>|gemm_rows_kernel<1>",
                                     "lm_head_kernel+argmax_kernel",
                                     "attn_kernel<split>|attn_few_kernel+attn_merge_wide_kernel|attn_merge_rows_kernel",
-                                    "gemv1_qkv_kernel"};
+                                    "gemv1_qkv_kernel", "logits_rules_kernel+logits_token_kernel"};
 
 struct KindStats {
   int64_t launches = 0;
@@ -464,6 +465,14 @@ struct mz_ctx {
   void* act = nullptr;     // f16 [max_ctx][ffp]
   float* part_val = nullptr;
   int32_t* part_idx = nullptr;
+  // rules on the first token's logits (mz_set_token_rules); the buffers exist
+  // from the first rules on
+  bool rules_on = false;
+  mzk::LogitsRules rules;
+  float* d_logits = nullptr;         // [V]
+  uint8_t* d_rules = nullptr;        // penalties, bias tokens and values, mask, the kernel's workspace
+  int32_t* d_hist = nullptr;         // [max_ctx] the context's tokens, the first hist_n of them up to date
+  int hist_n = 0;
   int32_t* d_gen = nullptr;          // [max_ctx] tokens chosen by the steps of mz_generate
 
   // restore metadata: a pinned staging block and its device mirror of the
@@ -654,6 +663,7 @@ struct mz_ctx {
       }
     arena.reset();
     tokens.clear();
+    hist_n = 0;
     have_last = false;
   }
 };
@@ -1376,7 +1386,7 @@ void mz_free(mz_ctx* x) {
   void* dptrs[] = {x->codec_stage, x->d_meta, x->split_ws, x->attn_wq, x->gemm_wq, x->w_slab, x->emb_nib, x->emb_sc, x->lm_nib, x->lm_sc,
                    x->rope_cs, x->kv_slab,
                    x->h[0], x->h[1], x->xb, x->qf, x->kvf, x->q16, x->act, x->part_val,
-                   x->part_idx, x->d_gen};
+                   x->part_idx, x->d_gen, x->d_logits, x->d_rules, x->d_hist};
   for (void* p : dptrs)
     if (p) (void)hipFree(p);
   if (x->w_image) (void)hipHostFree(x->w_image);
@@ -1489,6 +1499,7 @@ mz_status mz_truncate_context(mz_ctx* x, int32_t n) {
         t = -1;
       }
     x->tokens.resize(n);
+    x->hist_n = std::min(x->hist_n, (int)n);
     x->have_last = false;
   });
 }
@@ -1682,9 +1693,24 @@ mz_status mz_first_token(mz_ctx* x, int32_t* token_out, float* logits_out) {
     if (!x->have_last) fail(MZ_ESTATE, "no prefill since the last first token");
     hipStream_t cs = x->s_compute;
     x->timed(kKLmHead, 2.0 * x->d * x->V, (double)x->V * x->d * 0.5625 + x->V * 4.0, cs, [&] {
-      mzk::launch_lm_head(x->h_last, x->d, x->cfg.rms_eps, x->lm_nib, x->lm_sc, x->V,
-                          logits_out ? x->h_logits : nullptr, x->part_val, x->part_idx, x->h_token, cs);
+      float* logits = x->rules_on ? x->d_logits : logits_out ? x->h_logits : nullptr;
+      mzk::launch_lm_head(x->h_last, x->d, x->cfg.rms_eps, x->lm_nib, x->lm_sc, x->V, logits, x->part_val, x->part_idx,
+                          x->h_token, cs);
     });
+    if (x->rules_on) {
+      const int n = (int)x->tokens.size();
+      if (x->rules.history && n > x->hist_n) {
+        HIPCHK(hipMemcpyAsync(x->d_hist + x->hist_n, x->tokens.data() + x->hist_n, (size_t)(n - x->hist_n) * 4,
+                              hipMemcpyHostToDevice, cs));
+        x->hist_n = n;
+      }
+      x->timed(kKLogitsRules, 6.0 * x->V, x->V * (logits_out ? 8.0 : 4.0) + n * 4.0, cs, [&] {
+        mzk::LogitsRules r = x->rules;
+        r.out = logits_out ? x->h_logits : nullptr;
+        r.n_history = r.history ? n : 0;
+        mzk::launch_logits_rules(r, 1, x->d_rules, cs);
+      });
+    }
     HIPCHK(hipStreamSynchronize(cs));
     if (logits_out) memcpy(logits_out, x->h_logits, (size_t)x->V * 4);
     *token_out = *x->h_token;
@@ -1697,6 +1723,68 @@ mz_status mz_first_token(mz_ctx* x, int32_t* token_out, float* logits_out) {
       x->swap_timed = false;
     }
     x->collect_timing();
+    if (x->rules_on && *token_out < 0) fail(MZ_ESTATE, "the token rules leave no token");
+  });
+}
+
+mz_status mz_set_token_rules(mz_ctx* x, const mz_token_rules* rules) {
+  if (!x) return MZ_EINVAL;
+  return guarded(x, [&] {
+    if (!rules) {
+      x->rules_on = false;
+      return;
+    }
+    const mz_token_rules& t = *rules;
+    if (!(t.repetition > 0) || !std::isfinite(t.repetition) || !std::isfinite(t.frequency) || !std::isfinite(t.presence))
+      fail(MZ_EINVAL, "repetition must be positive, frequency and presence finite");
+    if (t.n_bias < 0 || t.n_bias > x->V) fail(MZ_EINVAL, "n_bias must be 0..vocab");
+    if (t.n_bias > 0 && (!t.bias_token || !t.bias_value)) fail(MZ_EINVAL, "bias_token or bias_value is NULL");
+    for (int i = 0; i < t.n_bias; ++i) {
+      if (t.bias_token[i] < 0 || t.bias_token[i] >= x->V) fail(MZ_EINVAL, "bias token %d out of range", t.bias_token[i]);
+      if (std::isnan(t.bias_value[i])) fail(MZ_EINVAL, "bias %d is NaN", i);
+    }
+    const int words = (x->V + 31) / 32;
+    if (t.mask) {
+      bool any = false;
+      for (int i = 0; i < words; ++i)
+        any |= (i + 1 < words || x->V % 32 == 0 ? t.mask[i] : t.mask[i] & ((1u << (x->V % 32)) - 1)) != 0;
+      if (!any) fail(MZ_EINVAL, "the mask allows no token");
+    }
+    HIPCHK(hipStreamSynchronize(x->s_compute));
+    // the kernel's workspace first, then penalties, bias tokens, bias values and mask
+    const int64_t b_ws = round_up(mzk::logits_rules_blocks(1, x->V) * 8, 256), b_bias = round_up((int64_t)x->V * 4, 256);
+    if (!x->d_logits) x->d_logits = (float*)dmalloc((size_t)x->V * 4);
+    if (!x->d_hist) x->d_hist = (int32_t*)dmalloc((size_t)x->max_ctx * 4);
+    if (!x->d_rules) x->d_rules = (uint8_t*)dmalloc((size_t)(b_ws + 256 + 2 * b_bias + words * 4));
+    uint8_t* p = x->d_rules + b_ws;
+    mzk::LogitsRules r{};
+    r.logits = x->d_logits;
+    r.stride = x->V;
+    r.vocab = x->V;
+    r.token = x->h_token;
+    // no rules, rather than half of them, should a copy fail
+    x->rules_on = false;
+    if (t.repetition != 1.f || t.frequency != 0.f || t.presence != 0.f) {
+      const float pen[3] = {t.repetition, t.frequency, t.presence};
+      HIPCHK(hipMemcpy(p, pen, sizeof pen, hipMemcpyHostToDevice));
+      r.penalty = (const float*)p;
+      r.history = x->d_hist;
+    }
+    if (t.n_bias > 0) {
+      HIPCHK(hipMemcpy(p + 256, t.bias_token, (size_t)t.n_bias * 4, hipMemcpyHostToDevice));
+      HIPCHK(hipMemcpy(p + 256 + b_bias, t.bias_value, (size_t)t.n_bias * 4, hipMemcpyHostToDevice));
+      r.bias_token = (const int32_t*)(p + 256);
+      r.bias_value = (const float*)(p + 256 + b_bias);
+      r.n_bias = t.n_bias;
+    }
+    if (t.mask) {
+      HIPCHK(hipMemcpy(p + 256 + 2 * b_bias, t.mask, (size_t)words * 4, hipMemcpyHostToDevice));
+      r.mask = (const uint32_t*)(p + 256 + 2 * b_bias);
+      r.n_masks = 1;
+      r.mask_words = words;
+    }
+    x->rules = r;
+    x->rules_on = true;
   });
 }
 
@@ -1710,6 +1798,13 @@ mz_status mz_generate(mz_ctx* x, int32_t token, int32_t n, int32_t* tokens_out) 
   if (st != MZ_OK) return st;
   st = mz_first_token(x, &tokens_out[0], nullptr);
   if (st != MZ_OK || n == 1) return st;
+  if (x->rules_on) {   // the host sees each token before it is appended: rules may leave none
+    for (int i = 1; i < n && st == MZ_OK; ++i) {
+      st = mz_restore_and_prefill(x, &tokens_out[i - 1], 1);
+      if (st == MZ_OK) st = mz_first_token(x, &tokens_out[i], nullptr);
+    }
+    return st;
+  }
   // the others back to back: each step's token stays on the device, where
   // the argmax leaves it (d_gen[i]) and the next step's embedding reads it;
   // the host plans the next step while the GPU runs this one and learns
@@ -2246,10 +2341,10 @@ mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t
     p.vocab = vocab;
     p.penalty = r.penalty;
     p.history = r.history;
-    p.history_off = r.history_off;
+    p.history_off = r.history ? r.history_off : nullptr;
     p.bias_token = r.bias_token;
     p.bias_value = r.bias_value;
-    p.bias_off = r.bias_off;
+    p.bias_off = r.bias_token ? r.bias_off : nullptr;
     p.mask = r.mask;
     p.mask_row = r.mask_row;
     p.n_masks = r.n_masks;

@@ -73,6 +73,12 @@ class mz_kv_append_args(ctypes.Structure):
                 ("n_table", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32), ("q_out", ctypes.c_void_p)]
 
 
+class mz_token_rules(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_float), ("frequency", ctypes.c_float), ("presence", ctypes.c_float),
+                ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
+                ("mask", ctypes.c_void_p)]
+
+
 class mz_logits_rules_args(ctypes.Structure):
     _fields_ = [("penalty", ctypes.c_void_p), ("history", ctypes.c_void_p), ("history_off", ctypes.c_void_p),
                 ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("bias_off", ctypes.c_void_p),
@@ -118,6 +124,7 @@ def lib() -> ctypes.CDLL:
         "mz_evict": ([vp, ctypes.POINTER(mz_evict_plan)], i32),
         "mz_restore_and_prefill": ([vp, vp, i32], i32),
         "mz_first_token": ([vp, vp, vp], i32),
+        "mz_set_token_rules": ([vp, ctypes.POINTER(mz_token_rules)], i32),
         "mz_set_option": ([vp, ctypes.c_char_p, i64], i32),
         "mz_generate": ([vp, i32, i32, vp], i32),
         "mz_stats": ([vp, ctypes.c_char_p, sz], i32),
@@ -268,6 +275,21 @@ def mz_generate(ctx, token: int, n: int) -> np.ndarray:
     out = np.zeros(max(n, 1), np.int32)
     _check(lib().mz_generate(ctx, int(token), int(n), out.ctypes.data), ctx)
     return out[:n]
+
+
+def mz_set_token_rules(ctx, repetition: float = 1.0, frequency: float = 0.0, presence: float = 0.0,
+                       bias: Optional[list] = None, mask: Optional[np.ndarray] = None) -> None:
+    """bias: (token, value) pairs; mask: uint32 words, bit v % 32 of word v / 32 set where token v is
+    allowed (one word per 32 tokens of the vocabulary)."""
+    tok = np.array([t for t, _ in bias or []], np.int32)
+    val = np.array([v for _, v in bias or []], np.float32)
+    words = None if mask is None else np.ascontiguousarray(mask, dtype=np.uint32)
+    r = mz_token_rules(repetition, frequency, presence, tok.ctypes.data, val.ctypes.data, tok.size, _ptr(words))
+    _check(lib().mz_set_token_rules(ctx, ctypes.byref(r)), ctx)
+
+
+def mz_clear_token_rules(ctx) -> None:
+    _check(lib().mz_set_token_rules(ctx, None), ctx)
 
 
 def mz_set_option(ctx, key: str, value: int) -> None:

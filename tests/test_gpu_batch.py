@@ -830,3 +830,233 @@ def test_logits_captured_on_another_stream():
         ref, bound = logits_oracle(x, penalty, histories, [[]] * m, mask, mask_row)
         close(out, ref, bound, f"step {step}")
         assert np.array_equal(token.cpu().numpy(), picked(out.cpu().numpy()))
+
+
+# ----------------------------------------------------------------------------- rules on a context's tokens
+
+def tiny_engine(extra=16):
+    from paper_2609_01338_amd import workloads as W
+    torch_cuda()
+    w = W.WORKLOADS["tiny"]
+    return w.model, W.make_tokens(w)[0], mz.Engine(w.model, W.make_blob(w), max_ctx=w.n_ctx + extra)
+
+
+def words_of(allowed, vocab):
+    bits = np.zeros((vocab + 31) // 32 * 32, np.uint8)
+    bits[list(allowed)] = 1
+    return np.packbits(bits, bitorder="little").view(np.uint32)
+
+
+def test_token_rules_of_a_context():
+    """The first token and its logits after the rules, from the logits without them and the context as history."""
+    m, ctx, eng = tiny_engine()
+    bias = [(5, 2.5), (17, -1.0), (5, 0.75)]
+    mask = words_of(set(range(0, m.vocab, 2)) | {5, 17}, m.vocab)
+    with eng:
+        e = eng.ctx
+        mz.mz_prefill_context(e, ctx)
+        plain, raw = mz.mz_first_token(e, m.vocab)
+        for rules in (dict(repetition=1.3, frequency=0.2, presence=0.1), dict(bias=bias), dict(mask=mask),
+                      dict(repetition=0.7, frequency=-0.1, bias=bias, mask=mask)):
+            mz.mz_set_token_rules(e, **rules)
+            mz.mz_prefill_context(e, ctx)
+            tok, logits = mz.mz_first_token(e, m.vocab)
+            pen = [[rules.get("repetition", 1.0), rules.get("frequency", 0.0), rules.get("presence", 0.0)]]
+            got_mask = rules.get("mask")
+            ref, bound = logits_oracle(raw[None], np.array(pen, np.float32), [ctx.tolist()],
+                                       [[(t, float(np.float32(v))) for t, v in rules.get("bias", [])]],
+                                       None if got_mask is None else got_mask[None], [0])
+            close(logits[None], ref, bound, "logits after " + ", ".join(rules))
+            assert tok == picked(logits[None])[0]
+            mz.mz_prefill_context(e, ctx)
+            assert mz.mz_first_token(e) == tok, "without the logits"
+        mz.mz_clear_token_rules(e)
+        mz.mz_prefill_context(e, ctx)
+        again, logits = mz.mz_first_token(e, m.vocab)
+        assert again == plain and logits.tobytes() == raw.tobytes()
+
+
+def test_token_rules_while_generating():
+    """The history grows with each token; mz_generate and single steps choose the same; a context cut back
+    and continued otherwise counts its own tokens only."""
+    m, ctx, eng = tiny_engine()
+    with eng:
+        e = eng.ctx
+        mz.mz_set_token_rules(e, presence=1000.0)
+        mz.mz_prefill_context(e, ctx)
+        first = mz.mz_first_token(e)
+        toks = mz.mz_generate(e, first, 10).tolist()
+        seen = ctx.tolist() + [first] + toks
+        assert len(set([first] + toks)) == 11 and not set([first] + toks) & set(ctx.tolist())
+        mz.mz_truncate_context(e, ctx.size)
+        t, steps = first, []
+        for _ in range(10):
+            mz.mz_restore_and_prefill(e, np.array([t], np.int32))
+            t = mz.mz_first_token(e)
+            steps.append(t)
+        assert steps == toks
+        # cut back, then on with a token that was not there before: those cut off may come again
+        mz.mz_truncate_context(e, ctx.size)
+        other = next(v for v in range(m.vocab) if v not in seen)
+        mz.mz_restore_and_prefill(e, np.array([other], np.int32))
+        _, logits = mz.mz_first_token(e, m.vocab)
+        low = np.nonzero(logits < -500)[0]
+        assert set(low.tolist()) == set(ctx.tolist()) | {other}
+        # a grammar of five tokens
+        allowed = [3, 77, 500, 777, m.vocab - 1]
+        mz.mz_set_token_rules(e, mask=words_of(allowed, m.vocab))
+        mz.mz_prefill_context(e, ctx)
+        toks = mz.mz_generate(e, mz.mz_first_token(e), 6)
+        assert set(toks.tolist()) <= set(allowed)
+
+
+def test_token_rules_that_leave_no_token():
+    m, ctx, eng = tiny_engine()
+    with eng:
+        e = eng.ctx
+        mz.mz_set_token_rules(e, mask=words_of([9], m.vocab), bias=[(9, float("-inf"))])
+        mz.mz_prefill_context(e, ctx)
+        with pytest.raises(mz.MzError) as err:
+            mz.mz_first_token(e)
+        assert err.value.status == mz.MZ_ESTATE and "rules" in str(err.value)
+        with pytest.raises(mz.MzError) as err:
+            mz.mz_generate(e, 1, 4)
+        assert err.value.status == mz.MZ_ESTATE
+        mz.mz_clear_token_rules(e)
+        mz.mz_restore_and_prefill(e, np.array([2], np.int32))
+        assert 0 <= mz.mz_first_token(e) < m.vocab
+
+
+def test_token_rules_refusals_keep_the_rules():
+    m, ctx, eng = tiny_engine()
+    nan, inf = float("nan"), float("inf")
+    with eng:
+        e = eng.ctx
+        mz.mz_set_token_rules(e, mask=words_of([9, 10], m.vocab))
+        past = words_of([9], m.vocab) * np.uint32(0)
+        for bad in (dict(repetition=0.0), dict(repetition=-1.0), dict(repetition=nan), dict(repetition=inf), dict(frequency=inf),
+                    dict(presence=nan), dict(bias=[(-1, 0.0)]), dict(bias=[(m.vocab, 0.0)]), dict(bias=[(0, nan)]),
+                    dict(bias=[(0, 0.0)] * (m.vocab + 1)), dict(mask=past)):
+            with pytest.raises(mz.MzError) as err:
+                mz.mz_set_token_rules(e, **bad)
+            assert err.value.status == mz.MZ_EINVAL, bad
+        mz.mz_prefill_context(e, ctx)
+        assert mz.mz_first_token(e) in (9, 10)
+
+
+# ----------------------------------------------------------------------------- the calls together
+
+def test_decode_steps_of_a_batch_in_one_graph():
+    """Prompts of five requests, then decode steps of all of them, captured once: shared Q4_0 projections with each
+    request's adapter, the append, the attention, the output projection, the head and the rules.  Every call's output
+    is checked from the buffers that it read; lengths, positions, histories and adapters change between replays."""
+    from paper_2609_01338_amd import workloads as W
+    torch = torch_cuda()
+    nq, nkv, hd, d, V, C, n_seq, R, na = 4, 2, 64, 256, 1024, 16, 5, 16, 3
+    dq, dkv, wide = nq * hd, nkv * hd, (nq + 2 * nkv) * hd
+    rng = np.random.default_rng(50)
+    pack = lambda n, k: dev(mz.mz_q4_gemm_pack(W.encode_q4_0((rng.standard_normal((n, k)) * 0.05).astype(np.float32)), n, k))  # noqa: E731
+    w_qkv, w_o, w_lm = pack(wide, d), pack(d, dq), pack(V, d)
+    lora = {k: [(rng.standard_normal(s) * 0.1).astype(np.float16) for s in ((na, R, i), (na, o, R))]
+            for k, i, o in (("qkv", d, wide), ("o", dq, d))}
+    d_lora = {k: [dev(t) for t in v] for k, v in lora.items()}
+    rank, scale = np.array([16, 5, 8], np.int32), np.array([1.0, 0.5, 2.0], np.float32)
+    d_rank, d_scale = dev(rank), dev(scale)
+    n_table, n_rope = 8, 128
+    table = rng.permutation(n_seq * n_table).reshape(n_seq, n_table).astype(np.int32)
+    rope = rope_table(n_rope, hd)
+    d_table, d_rope = dev(table), dev(rope)
+    slab = torch.full((n_seq * n_table, 2 * C * dkv), float("nan"), device="cuda", dtype=torch.float16)
+
+    def buffers(m):
+        z = lambda *s, dt=torch.float32: torch.zeros(*s, device="cuda", dtype=dt)  # noqa: E731
+        h16, i32 = torch.float16, torch.int32
+        return dict(m=m, h=z(m, d), x=z(m, d, dt=h16), qkv0=z(m, wide), qkv=z(m, wide), q=z(m, dq, dt=h16), o0=z(m, d), o=z(m, d),
+                    att=z(m, dq, dt=h16), logits=z(m, V), out=z(m, V), seq=z(m, dt=i32), pos=z(m, dt=i32), lens=z(m, dt=i32),
+                    adapter=z(m, dt=i32), token=z(m, dt=i32), history=z(2000, dt=i32), off=z(m + 1, dt=torch.int64),
+                    pen=dev(np.tile(np.array([1.2, 0.1, 0.3], np.float32), (m, 1))), ws=z(8 << 20, dt=torch.uint8))
+
+    def project(b, x, k, w, n, y):
+        mz.mz_q4_gemm_ex(x.data_ptr(), b["m"], n, k, w.data_ptr(), 0, y.data_ptr(), stream())
+
+    def adapt(b, name, x, k, n, base, y):
+        a, bb = d_lora[name]
+        mz.mz_lora_add(x.data_ptr(), b["m"], k, b["adapter"].data_ptr(), na, a.data_ptr(), bb.data_ptr(), R, n, base.data_ptr(),
+                       y.data_ptr(), y.shape[1], b["ws"].data_ptr(), b["ws"].numel(), stream(), scale_ptr=d_scale.data_ptr(),
+                       rank_ptr=d_rank.data_ptr())
+
+    def to_chunks(b):
+        mz.mz_rmsnorm(b["h"].data_ptr(), b["m"], d, 1e-5, b["x"].data_ptr(), stream())
+        project(b, b["x"], d, w_qkv, wide, b["qkv0"])
+        adapt(b, "qkv", b["x"], d, wide, b["qkv0"], b["qkv"])
+        p = b["qkv"].data_ptr()
+        mz.mz_kv_append(b["m"], p + dq * 4, p + (dq + dkv) * 4, b["seq"].data_ptr(), b["pos"].data_ptr(), d_rope.data_ptr(), n_rope,
+                        slab.data_ptr(), n_seq * n_table, d_table.data_ptr(), n_seq, n_table, C, nkv, hd, stream(), q_ptr=p, n_q=nq,
+                        q_out_ptr=b["q"].data_ptr(), k_stride=wide, v_stride=wide, q_stride=wide)
+
+    def step(b):
+        to_chunks(b)
+        mz.mz_attention_batch(b["q"].data_ptr(), b["lens"].data_ptr(), n_seq, slab.data_ptr(), n_seq * n_table, d_table.data_ptr(),
+                              n_table, C, nq, nkv, hd, b["ws"].data_ptr(), b["ws"].numel(), b["att"].data_ptr(), stream())
+        project(b, b["att"], dq, w_o, d, b["o0"])
+        adapt(b, "o", b["att"], dq, d, b["o0"], b["o"])
+        mz.mz_rmsnorm(b["o"].data_ptr(), b["m"], d, 1e-5, b["x"].data_ptr(), stream())
+        project(b, b["x"], d, w_lm, V, b["logits"])
+        mz.mz_logits_rules(b["logits"].data_ptr(), b["m"], V, V, b["out"].data_ptr(), b["token"].data_ptr(), b["ws"].data_ptr(),
+                           b["ws"].numel(), stream(), penalty_ptr=b["pen"].data_ptr(), history_ptr=b["history"].data_ptr(),
+                           history_off_ptr=b["off"].data_ptr())
+
+    host = lambda t: t.cpu().numpy()  # noqa: E731
+
+    def check_chunks(b, before, adapter, what):
+        base, x = host(b["qkv0"]), host(b["x_qkv"])
+        ref, bound = lora_oracle(x, adapter, *lora["qkv"], scale, rank, base, wide)
+        close(b["qkv"], ref, bound, what + ": adapters")
+        q, k, v = np.split(host(b["qkv"]), [dq, dq + dkv], 1)
+        ref, bound, qr, qb, wrote = append_oracle(k, v, q, host(b["seq"]), host(b["pos"]), rope, before, table, C, nkv, hd)
+        close(slab, ref, bound, what + ": chunks")
+        close(b["q"][dev(wrote)], qr[wrote], qb[wrote], what + ": queries")
+
+    # the prompts, of uneven lengths, and three rows of padding
+    lens = np.array([33, 1, 16, 90, 47], np.int32)
+    p = buffers(int(lens.sum()) + 3)
+    seq = np.concatenate([np.repeat(np.arange(n_seq), lens), [-1] * 3]).astype(np.int32)
+    pos = np.concatenate([np.arange(n) for n in lens] + [[0] * 3]).astype(np.int32)
+    adapter = np.where(seq >= 0, np.array([0, 1, -1, 2, 1])[seq], -1).astype(np.int32)
+    for name, t in (("h", rng.standard_normal((len(seq), d)).astype(np.float32)), ("seq", seq), ("pos", pos), ("adapter", adapter)):
+        p[name].copy_(dev(t))
+    before = host(slab)
+    to_chunks(p)
+    torch.cuda.synchronize()
+    p["x_qkv"] = p["x"]
+    check_chunks(p, before, adapter, "prompts")
+    # decode steps
+    b = buffers(n_seq)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        step(b)
+    histories = [[int(t) for t in rng.integers(0, V, n)] for n in lens]
+    for i in range(4):
+        lens = lens + 1
+        adapter = np.array([[0, 1, -1, 2, 1], [2, 2, 2, 2, 2], [-1] * 5, [1, 0, 2, 5, 0]][i], np.int32)
+        flat, off = rows_of(histories, np.int32)
+        for name, t in (("h", rng.standard_normal((n_seq, d)).astype(np.float32)), ("seq", np.arange(n_seq, dtype=np.int32)),
+                        ("pos", lens - 1), ("lens", lens), ("adapter", adapter), ("off", off)):
+            b[name].copy_(dev(t))
+        b["history"][:len(flat)].copy_(dev(flat))
+        before = host(slab)
+        g.replay()
+        torch.cuda.synchronize()
+        x = torch.zeros(n_seq, d, device="cuda", dtype=torch.float16)      # the step's x, which the head's took the place of
+        mz.mz_rmsnorm(b["h"].data_ptr(), n_seq, d, 1e-5, x.data_ptr(), stream())
+        b["x_qkv"] = x
+        check_chunks(b, before, adapter, f"step {i}")
+        ref, bound = attention_oracle(host(b["q"]), lens, host(slab), table, C, nq, nkv, hd)
+        close(b["att"], ref, bound, f"step {i}: attention")
+        ref, bound = lora_oracle(host(b["att"]), adapter, *lora["o"], scale, rank, host(b["o0"]), d)
+        close(b["o"], ref, bound, f"step {i}: output adapters")
+        ref, bound = logits_oracle(host(b["logits"]), host(b["pen"]), histories, [[]] * n_seq, None, None)
+        close(b["out"], ref, bound, f"step {i}: logits")
+        assert np.array_equal(host(b["token"]), picked(host(b["out"])))
+        for s, t in enumerate(host(b["token"]).tolist()):
+            histories[s].append(t)
