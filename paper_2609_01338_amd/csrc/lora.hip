@@ -15,7 +15,7 @@
 //    workgroup from the adapter list: row r begins a group when the rows
 //    before it with its adapter fill whole groups.  Each adapter is read once
 //    per 16 of its rows, however the rows are mixed.
-//  - Many rows: tiles of 64 neighbouring rows; a tile with several adapters
+//  - Many rows: tiles of 32 neighbouring rows; a tile with several adapters
 //    runs once for each of them and keeps each row's own result.
 // A row's results depend on no other row: a row is one column (or row) of an
 // MFMA operand, and what other adapters make of it is dropped, not masked by
@@ -30,7 +30,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kGatherRows = 512;     // rows up to which the adapter list is searched
-constexpr int kTileRows = 64;
+constexpr int kTileRows = 32;
 constexpr int kColsWg = 256;         // columns of a workgroup of the second product: 64 a wave
 
 __device__ __forceinline__ bool has_adapter(const Lora& p, int a) { return (unsigned)a < (unsigned)p.n_adapters; }
@@ -68,105 +68,132 @@ __device__ __forceinline__ int gather_group(const Lora& p, int r, int a, int* ro
   return min(seen - before, 16);
 }
 
-// acc += x A^T over the 32-wide K steps s0, s0 + ds, ... below s1: 16 rows x
-// NR tiles of 16 ranks.  xr: this lane's x row, ar: its A row of rank tile 0
-// (rank l % 16); the last step may pass k.
-template <int NR>
-__device__ __forceinline__ void shrink_steps(const Lora& p, const _Float16* xr, const _Float16* const (&ar)[NR], int s0,
-                                             int s1, int ds, int n_rt, f32x4 (&acc)[NR]) {
+// acc += x A^T over the 32-wide K steps s0 .. s1 - 1: NX tiles of 16 rows x
+// NT tiles of 16 ranks.  xr: this lane's x row of each tile, ar: its A row
+// (rank l % 16 of each tile).  No branch lies between the loads of a few
+// steps, so all of them are in flight together; the last step may pass k.
+template <int NX, int NT, int NR>
+__device__ __forceinline__ void shrink_steps(int k_all, const _Float16* const (&xr)[NX], const _Float16* const (&ar)[NR],
+                                             int s0, int s1, f32x4 (&acc)[NX][NR]) {
   const int lg = (threadIdx.x & 63) >> 4;
-#pragma unroll 4
-  for (int s = s0; s < s1; s += ds) {
+  const int full = min(s1, k_all / 32);
+  constexpr int U = NX + NT <= 4 ? 4 : 2;
+  int s = s0;
+  for (; s + U <= full; s += U) {
+    f16x8 xv[U][NX], av[U][NT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = (s + u) * 32 + lg * 8;
+#pragma unroll
+      for (int i = 0; i < NX; ++i) xv[u][i] = *reinterpret_cast<const f16x8*>(xr[i] + k);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) av[u][j] = *reinterpret_cast<const f16x8*>(ar[j] + k);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < NX; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[u][i], av[u][j], acc[i][j], 0, 0, 0);
+  }
+  for (; s < s1; ++s) {
     const int k = s * 32 + lg * 8;
-    const bool in = k < p.k;             // k is a multiple of 8
-    const int kc = in ? k : 0;
-    f16x8 xv = *reinterpret_cast<const f16x8*>(xr + kc);
-    f16x8 av[NR];
+    const bool in = k < k_all;             // k_all is a multiple of 8
+    f16x8 xv[NX], av[NT];
 #pragma unroll
-    for (int j = 0; j < NR; ++j)
-      if (j < n_rt) av[j] = *reinterpret_cast<const f16x8*>(ar[j] + kc);
-    if (!in) xv = f16x8{};
+    for (int i = 0; i < NX; ++i) xv[i] = *reinterpret_cast<const f16x8*>(xr[i] + (in ? k : 0));
 #pragma unroll
-    for (int j = 0; j < NR; ++j)
-      if (j < n_rt) {
-        if (!in) av[j] = f16x8{};
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av[j], acc[j], 0, 0, 0);
-      }
+    for (int j = 0; j < NT; ++j) av[j] = *reinterpret_cast<const f16x8*>(ar[j] + (in ? k : 0));
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(in ? xv[i] : f16x8{}, in ? av[j] : f16x8{}, acc[i][j], 0, 0, 0);
+  }
+}
+
+// The rows of a workgroup that share adapter a: bit i of members is row i of
+// its 16 NX; row_of(i) its index.  The four waves take a quarter of the
+// split's K range each and join through LDS.
+template <int NX, int NR, class RowOf>
+__device__ __forceinline__ void shrink_adapter(const Lora& p, float* t, int a, uint64_t members, int n_rows, RowOf row_of,
+                                               f32x4 (&s_acc)[4][NX][NR][64]) {
+  constexpr int RP = 16 * NR;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, lg = lane >> 4;
+  const int steps = (p.k + 31) / 32, ns = gridDim.y;
+  const int s0 = (int)((int64_t)blockIdx.y * steps / ns), s1 = (int)((int64_t)(blockIdx.y + 1) * steps / ns);
+  const int q0 = s0 + (s1 - s0) * w / 4, q1 = s0 + (s1 - s0) * (w + 1) / 4;
+  const int rank = rank_of(p, a), n_rt = (rank + 15) / 16;
+  const _Float16 *ar[NR], *xr[NX];
+  f32x4 acc[NX][NR];
+#pragma unroll
+  for (int j = 0; j < NR; ++j) ar[j] = p.a + ((int64_t)a * p.R + max(min(j * 16 + col, rank - 1), 0)) * p.k;
+#pragma unroll
+  for (int i = 0; i < NX; ++i) {
+    xr[i] = p.x + (int64_t)row_of(min(i * 16 + col, n_rows - 1)) * p.k;
+#pragma unroll
+    for (int j = 0; j < NR; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // rank tiles past the rank are left out, by powers of two
+  if (n_rt <= 1) shrink_steps<NX, 1>(p.k, xr, ar, q0, q1, acc);
+  else if (NR == 2 || (NR > 2 && n_rt <= 2)) shrink_steps<NX, NR >= 2 ? 2 : 1>(p.k, xr, ar, q0, q1, acc);
+  else if (NR == 4 || (NR > 4 && n_rt <= 4)) shrink_steps<NX, NR >= 4 ? 4 : 1>(p.k, xr, ar, q0, q1, acc);
+  else shrink_steps<NX, NR>(p.k, xr, ar, q0, q1, acc);
+#pragma unroll
+  for (int i = 0; i < NX; ++i)
+#pragma unroll
+    for (int j = 0; j < NR; ++j) s_acc[w][i][j][lane] = acc[i][j];
+  __syncthreads();
+  // element e of lane l is row 4 (l / 16) + e, rank l % 16
+  for (int ij = w; ij < NX * NR; ij += 4) {
+    const int i = ij / NR, j = ij % NR;
+    const f32x4 v = s_acc[0][i][j][lane] + s_acc[1][i][j][lane] + s_acc[2][i][j][lane] + s_acc[3][i][j][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = i * 16 + lg * 4 + e;
+      if ((members >> at) & 1) t[(int64_t)row_of(at) * RP + j * 16 + col] = j * 16 + col < rank ? v[e] : 0.f;
+    }
   }
 }
 
 // t [split][m][16 NR] of the K range of split blockIdx.y.
 template <int NR, bool GATHER>
 __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
-  constexpr int RP = 16 * NR;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, lg = lane >> 4;
-  const int steps = (p.k + 31) / 32, ns = gridDim.y;
-  const int s0 = (int)((int64_t)blockIdx.y * steps / ns), s1 = (int)((int64_t)(blockIdx.y + 1) * steps / ns);
+  constexpr int RP = 16 * NR, NX = GATHER ? 1 : kTileRows / 16;
+  __shared__ int s_rows[16];
+  __shared__ f32x4 s_acc[4][NX][NR][64];
   float* t = p.t + (int64_t)blockIdx.y * p.m * RP;
-  const _Float16* ar[NR];
-  f32x4 acc[NR];
-  auto begin = [&](int a) {              // A rows of this lane; how many rank tiles count
-#pragma unroll
-    for (int j = 0; j < NR; ++j) {
-      ar[j] = p.a + ((int64_t)a * p.R + min(j * 16 + col, p.R - 1)) * p.k;
-      acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-  };
   if constexpr (GATHER) {
-    __shared__ int s_rows[16];
-    __shared__ f32x4 s_acc[4][NR][64];
     const int r = blockIdx.x, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
     if (!has_adapter(p, a)) return;
     const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
     if (n == 0) return;
     __syncthreads();
-    const int rank = rank_of(p, a), n_rt = (rank + 15) / 16;
-    begin(a);
-    // a quarter of the split's steps for each wave, in one run
-    const int q0 = s0 + (s1 - s0) * w / 4, q1 = s0 + (s1 - s0) * (w + 1) / 4;
-    shrink_steps<NR>(p, p.x + (int64_t)s_rows[min(col, n - 1)] * p.k, ar, q0, q1, 1, n_rt, acc);
-#pragma unroll
-    for (int j = 0; j < NR; ++j) s_acc[w][j][lane] = acc[j];
-    __syncthreads();
-    // wave w: rank tiles w, w + 4, ...; element e of lane l is row 4 (l / 16) + e, rank l % 16
-    for (int j = w; j < NR; j += 4) {
-      const f32x4 v = s_acc[0][j][lane] + s_acc[1][j][lane] + s_acc[2][j][lane] + s_acc[3][j][lane];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (lg * 4 + e < n) t[(int64_t)s_rows[lg * 4 + e] * RP + j * 16 + col] = j * 16 + col < rank ? v[e] : 0.f;
-    }
+    shrink_adapter<NX, NR>(p, t, a, (1ull << n) - 1, n, [&](int i) { return s_rows[i]; }, s_acc);
   } else {
-    // wave w: rows 16 w .. 16 w + 15 of the tile, over the whole split
-    const int r0 = blockIdx.x * kTileRows + w * 16;
-    if (r0 >= p.m) return;
-    const int mine = r0 + col < p.m ? p.adapter[r0 + col] : -1;      // the same for the four lane groups
-    uint64_t todo = __ballot(has_adapter(p, mine)) & 0xFFFF;
+    const int r0 = blockIdx.x * kTileRows, lane = threadIdx.x & 63, n = min(kTileRows, p.m - r0);
+    const int mine = lane < n ? p.adapter[r0 + lane] : -1;
+    uint64_t todo = __ballot(has_adapter(p, mine));
     while (todo) {
       const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
-      const uint64_t members = __ballot(mine == a) & 0xFFFF;
+      const uint64_t members = __ballot(mine == a);
       todo &= ~members;
-      const int rank = rank_of(p, a), n_rt = (rank + 15) / 16;
-      begin(a);
-      shrink_steps<NR>(p, p.x + (int64_t)min(r0 + col, p.m - 1) * p.k, ar, s0, s1, 1, n_rt, acc);
-#pragma unroll
-      for (int j = 0; j < NR; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if ((members >> (lg * 4 + e)) & 1)
-            t[(int64_t)(r0 + lg * 4 + e) * RP + j * 16 + col] = j * 16 + col < rank ? acc[j][e] : 0.f;
+      shrink_adapter<NX, NR>(p, t, a, members, n, [&](int i) { return r0 + i; }, s_acc);
+      if (todo) __syncthreads();
     }
   }
 }
 
-// y of 16 NRT rows x 256 columns: wave w has columns 64 w .. 64 w + 63 of the
+// y of 16 NX rows x 256 columns: wave w has columns 64 w .. 64 w + 63 of the
 // range, as four tiles of 16.  The products run transposed, D[column][row], so
 // that a lane holds four neighbouring columns of one row.
 template <int NR, bool GATHER>
 __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
-  constexpr int RP = 16 * NR, PITCH = RP + 4, NRT = GATHER ? 1 : kTileRows / 16, ROWS = 16 * NRT;
+  constexpr int RP = 16 * NR, PITCH = RP + 4, NX = GATHER ? 1 : kTileRows / 16, ROWS = 16 * NX;
   __shared__ int s_rows[16];
-  __shared__ float s_t[ROWS][PITCH];
+  __shared__ __attribute__((aligned(16))) float s_t[ROWS][PITCH];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int c0 = blockIdx.y * kColsWg + w * 64;
@@ -187,25 +214,27 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
   }
   auto row_of = [&](int i) { return GATHER ? s_rows[i] : r0 + i; };
   // the base's values go out first; they are needed last
-  f32x4 y[NRT][4];
-  int rows[NRT], mine[NRT];
+  f32x4 y[NX][4];
+  int rows[NX], mine[NX];
 #pragma unroll
-  for (int i = 0; i < NRT; ++i) {
+  for (int i = 0; i < NX; ++i) {
     rows[i] = row_of(min(i * 16 + col, n_rows - 1));
     mine[i] = p.adapter[rows[i]];
+  }
+  const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
+#pragma unroll
+  for (int i = 0; i < NX; ++i)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int at = c0 + c * 16 + lg * 4;
       const float* b = p.base + (int64_t)rows[i] * p.y_stride + at;
-      y[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (at + 4 <= p.n)
+      if (whole) {
         y[i][c] = *reinterpret_cast<const f32x4*>(b);
-      else
+      } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (at + e < p.n) y[i][c][e] = b[e];
+        for (int e = 0; e < 4; ++e) y[i][c][e] = at + e < p.n ? b[e] : 0.f;
+      }
     }
-  }
   // t of the rows: the splits added in order, times the row's scale
   for (int idx = threadIdx.x; idx < n_rows * (RP / 4); idx += 256) {
     const int i = idx / (RP / 4), j = (idx % (RP / 4)) * 4, r = row_of(i), a = p.adapter[r];
@@ -220,11 +249,6 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
   }
   __syncthreads();
   if (c0 >= p.n) return;
-  f32x4 add[NRT][4];
-#pragma unroll
-  for (int i = 0; i < NRT; ++i)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) add[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int seen = GATHER ? mine[0] : (lane < n_rows ? p.adapter[r0 + lane] : -1);
   uint64_t todo = GATHER ? 1ull : __ballot(has_adapter(p, seen));
   while (todo) {
@@ -232,55 +256,50 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
     const uint64_t members = GATHER ? 1ull : __ballot(seen == a);
     todo &= ~members;
     const int rank = rank_of(p, a);
-    f32x4 d[NRT][4];
+    // B of columns c0 + 16 c + l % 16, ranks 16 j + 4 (l / 16) .. + 3; past the rank the last four that exist are
+    // read, and not used
+    f16x4 b[NR][4];
 #pragma unroll
-    for (int i = 0; i < NRT; ++i)
+    for (int j = 0; j < NR; ++j)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) d[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < 4; ++c)
+        b[j][c] = *reinterpret_cast<const f16x4*>(p.b + ((int64_t)a * p.n + min(c0 + c * 16 + col, p.n - 1)) * p.R +
+                                                  min(j * 16 + lg * 4, max(rank - 1, 0) & ~3));
 #pragma unroll
-    for (int j = 0; j < NR; ++j) {
-      if (j * 16 >= rank) break;
-      // B of columns c0 + 16 c + l % 16, ranks 16 j + 4 (l / 16) .. + 3; ranks that do not count are zero
-      const int k = j * 16 + lg * 4;
-      f32x4 b[4];
+    for (int i = 0; i < NX; ++i) {
+      if (!GATHER && !((members >> (i * 16)) & 0xFFFF)) continue;
+      f32x4 d[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int at = min(c0 + c * 16 + col, p.n - 1);
-        const f16x4 v = *reinterpret_cast<const f16x4*>(p.b + ((int64_t)a * p.n + at) * p.R + (k < p.R ? k : 0));
+      for (int c = 0; c < 4; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) b[c][e] = k + e < rank ? (float)v[e] : 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < NRT; ++i) {
-        if (!GATHER && !((members >> (i * 16)) & 0xFFFF)) continue;
+      for (int j = 0; j < NR; ++j) {
+        if (j * 16 >= rank) break;
+        const int k = j * 16 + lg * 4;
         const f32x4 t = *reinterpret_cast<const f32x4*>(&s_t[i * 16 + col][k]);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) d[i][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[c][e], t[e], d[i][c], 0, 0, 0);
+          for (int e = 0; e < 4; ++e)
+            d[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(k + e < rank ? (float)b[j][c][e] : 0.f, t[e], d[c], 0, 0, 0);
       }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) y[i][c] = mine[i] == a ? y[i][c] + d[c] : y[i][c];
     }
-#pragma unroll
-    for (int i = 0; i < NRT; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) add[i][c] = mine[i] == a ? d[i][c] : add[i][c];
   }
 #pragma unroll
-  for (int i = 0; i < NRT; ++i) {
-    if (i * 16 + col >= n_rows) continue;
-    const bool with = has_adapter(p, mine[i]);
-    if (!with && p.y == p.base) continue;
+  for (int i = 0; i < NX; ++i) {
+    if (i * 16 + col >= n_rows || (!has_adapter(p, mine[i]) && p.y == p.base)) continue;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int at = c0 + c * 16 + lg * 4;
       float* o = p.y + (int64_t)rows[i] * p.y_stride + at;
-      const f32x4 v = with ? y[i][c] + add[i][c] : y[i][c];
-      if (at + 4 <= p.n)
-        *reinterpret_cast<f32x4*>(o) = v;
-      else
+      if (whole) {
+        *reinterpret_cast<f32x4*>(o) = y[i][c];
+      } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (at + e < p.n) o[e] = v[e];
+          if (at + e < p.n) o[e] = y[i][c][e];
+      }
     }
   }
 }
@@ -304,10 +323,8 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
 
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
 int lora_splits(int m, int k) {
-  const int steps = (k + 31) / 32;
   const int tiles = m <= kGatherRows ? m : (m + kTileRows - 1) / kTileRows;
-  const int want = m <= kGatherRows ? 1024 / tiles : 512 / tiles;
-  const int most = m <= kGatherRows ? steps / 8 : steps / 8;
+  const int want = (m <= kGatherRows ? 1024 : 512) / tiles, most = (k + 31) / 32 / 8;
   const int ns = want < most ? want : most;
   return ns < 1 ? 1 : ns > 16 ? 16 : ns;
 }
