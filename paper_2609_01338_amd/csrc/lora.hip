@@ -4,10 +4,12 @@
 //
 // Two launches: the first forms t = x A^T, fp32, in K splits; the second adds
 // the splits in order, scales them and adds t B^T to the rows.  The products
-// of f16 x and A are exact and summed in fp32 (v_mfma_f32_16x16x32_f16); t
-// stays fp32 and multiplies B, widened to fp32, on v_mfma_f32_16x16x4_f32, so
-// no value on the way is rounded to f16 and y keeps the projection's
-// precision.
+// of f16 x and A are exact and summed in fp32 (v_mfma_f32_16x16x32_f16).  For
+// the second product t is written as hi + lo, two f16 values, after the row's
+// largest was brought to 2^14 by a power of two: together they hold 22 bits
+// of each t (and all of it down to 2^-38 of the row's largest), so no
+// precision of the projection's fp32 is lost, B is used as it is, and the
+// products run at an eighth of the time of the fp32 matrix instructions.
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
 //  - Few rows (up to kGatherRows, any order): a workgroup per (group of up to
@@ -77,7 +79,7 @@ __device__ __forceinline__ void shrink_steps(int k_all, const _Float16* const (&
                                              int s0, int s1, f32x4 (&acc)[NX][NR]) {
   const int lg = (threadIdx.x & 63) >> 4;
   const int full = min(s1, k_all / 32);
-  constexpr int U = NX + NT <= 4 ? 4 : 2;
+  constexpr int U = NX + NT <= 6 ? 4 : 2;
   int s = s0;
   for (; s + U <= full; s += U) {
     f16x8 xv[U][NX], av[U][NT];
@@ -191,9 +193,11 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // that a lane holds four neighbouring columns of one row.
 template <int NR, bool GATHER>
 __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
-  constexpr int RP = 16 * NR, PITCH = RP + 4, NX = GATHER ? 1 : kTileRows / 16, ROWS = 16 * NX;
+  constexpr int RP = 16 * NR, KS = (RP + 31) / 32, PITCH = KS * 32 + 8;
+  constexpr int NX = GATHER ? 1 : kTileRows / 16, ROWS = 16 * NX;
   __shared__ int s_rows[16];
-  __shared__ __attribute__((aligned(16))) float s_t[ROWS][PITCH];
+  __shared__ __attribute__((aligned(16))) _Float16 s_hi[ROWS][PITCH], s_lo[ROWS][PITCH];
+  __shared__ float s_unit[ROWS];         // what a row's d is multiplied by
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int c0 = blockIdx.y * kColsWg + w * 64;
@@ -235,9 +239,11 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
         for (int e = 0; e < 4; ++e) y[i][c][e] = at + e < p.n ? b[e] : 0.f;
       }
     }
-  // t of the rows: the splits added in order, times the row's scale
-  for (int idx = threadIdx.x; idx < n_rows * (RP / 4); idx += 256) {
-    const int i = idx / (RP / 4), j = (idx % (RP / 4)) * 4, r = row_of(i), a = p.adapter[r];
+  // t of the rows: the splits added in order, times the row's scale, then in two halves.  A row's lanes are
+  // neighbours, a power of two of them
+  constexpr int LPR = RP / 4;
+  for (int idx = threadIdx.x; idx < n_rows * LPR; idx += 256) {
+    const int i = idx / LPR, j = (idx % LPR) * 4, r = row_of(i), a = p.adapter[r];
     f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
     if (has_adapter(p, a)) {
       const float* t = p.t + (int64_t)r * RP + j;
@@ -245,7 +251,27 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
       for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * RP);
       if (p.scale) v *= p.scale[a];
     }
-    *reinterpret_cast<f32x4*>(&s_t[i][j]) = v;
+    float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    // 2^(14 - exponent of the largest); a row of zeros or with an infinity stays as it is, its finite values
+    // within f16
+    const int up = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+    f16x4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float u = ldexpf(v[e], up);
+      if (fabsf(u) < INFINITY) u = fminf(fmaxf(u, -65504.f), 65504.f);
+      hi[e] = (_Float16)u;
+      lo[e] = fabsf(u) < INFINITY ? (_Float16)(u - (float)hi[e]) : (_Float16)0.f;
+    }
+    *reinterpret_cast<f16x4*>(&s_hi[i][j]) = hi;
+    *reinterpret_cast<f16x4*>(&s_lo[i][j]) = lo;
+    if (RP < KS * 32) {
+      *reinterpret_cast<f16x4*>(&s_hi[i][RP + j]) = f16x4{0, 0, 0, 0};
+      *reinterpret_cast<f16x4*>(&s_lo[i][RP + j]) = f16x4{0, 0, 0, 0};
+    }
+    if (j == 0) s_unit[i] = ldexpf(1.f, -up);
   }
   __syncthreads();
   if (c0 >= p.n) return;
@@ -256,15 +282,23 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
     const uint64_t members = GATHER ? 1ull : __ballot(seen == a);
     todo &= ~members;
     const int rank = rank_of(p, a);
-    // B of columns c0 + 16 c + l % 16, ranks 16 j + 4 (l / 16) .. + 3; past the rank the last four that exist are
-    // read, and not used
-    f16x4 b[NR][4];
+    // B of columns c0 + 16 c + l % 16, ranks 32 j + 8 (l / 16) .. + 7; past the rank the last eight that exist
+    // are read, and zeroed
+    f16x8 b[KS][4];
 #pragma unroll
-    for (int j = 0; j < NR; ++j)
+    for (int j = 0; j < KS; ++j)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        b[j][c] = *reinterpret_cast<const f16x4*>(p.b + ((int64_t)a * p.n + min(c0 + c * 16 + col, p.n - 1)) * p.R +
-                                                  min(j * 16 + lg * 4, max(rank - 1, 0) & ~3));
+        b[j][c] = *reinterpret_cast<const f16x8*>(p.b + ((int64_t)a * p.n + min(c0 + c * 16 + col, p.n - 1)) * p.R +
+                                                  min(j * 32 + lg * 8, max(rank - 1, 0) & ~7));
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+      if (j * 32 + 32 > rank) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) b[j][c][e] = j * 32 + lg * 8 + e < rank ? b[j][c][e] : (_Float16)0.f;
+      }
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       if (!GATHER && !((members >> (i * 16)) & 0xFFFF)) continue;
@@ -272,18 +306,21 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < NR; ++j) {
-        if (j * 16 >= rank) break;
-        const int k = j * 16 + lg * 4;
-        const f32x4 t = *reinterpret_cast<const f32x4*>(&s_t[i * 16 + col][k]);
+      for (int j = 0; j < KS; ++j) {
+        if (j * 32 >= rank) break;
+        const f16x8 lo = *reinterpret_cast<const f16x8*>(&s_lo[i * 16 + col][j * 32 + lg * 8]);
+        const f16x8 hi = *reinterpret_cast<const f16x8*>(&s_hi[i * 16 + col][j * 32 + lg * 8]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            d[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(k + e < rank ? (float)b[j][c][e] : 0.f, t[e], d[c], 0, 0, 0);
+        for (int c = 0; c < 4; ++c) {
+          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo, d[c], 0, 0, 0);
+          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi, d[c], 0, 0, 0);
+        }
       }
+      const float unit = s_unit[min(i * 16 + col, n_rows - 1)];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) y[i][c] = mine[i] == a ? y[i][c] + d[c] : y[i][c];
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[i][c][e] = mine[i] == a ? __builtin_fmaf(d[c][e], unit, y[i][c][e]) : y[i][c][e];
     }
   }
 #pragma unroll
@@ -324,7 +361,7 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
 int lora_splits(int m, int k) {
   const int tiles = m <= kGatherRows ? m : (m + kTileRows - 1) / kTileRows;
-  const int want = (m <= kGatherRows ? 1024 : 512) / tiles, most = (k + 31) / 32 / 8;
+  const int want = (m <= kGatherRows ? 1024 : 640) / tiles, most = (k + 31) / 32 / 8;
   const int ns = want < most ? want : most;
   return ns < 1 ? 1 : ns > 16 ? 16 : ns;
 }
