@@ -200,12 +200,16 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
   __shared__ float s_unit[ROWS];         // what a row's d is multiplied by
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
-  const int c0 = blockIdx.y * kColsWg + w * 64;
+  // Workgroup b runs on XCD b % 8: it serves every eighth row block, whose column ranges follow each other, so
+  // that t is read into one L2 and the rows in flight cover whole lines of all memory channels
+  const int cols = (p.n + kColsWg - 1) / kColsWg, xb = blockIdx.x & 7, rest = blockIdx.x >> 3;
+  const int block = rest / cols * 8 + xb, c_wg = rest % cols * kColsWg, c0 = c_wg + w * 64;
+  if (block >= p.row_blocks) return;
   int n_rows, r0 = 0;
   if constexpr (GATHER) {
-    const int r = blockIdx.x, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
+    const int r = block, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
     if (!has_adapter(p, a)) {            // such a row is the base's
-      const int c = blockIdx.y * kColsWg + threadIdx.x;
+      const int c = c_wg + threadIdx.x;
       if (p.y != p.base && c < p.n) p.y[r * p.y_stride + c] = p.base[r * p.y_stride + c];
       return;
     }
@@ -213,7 +217,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
     if (n_rows == 0) return;
     __syncthreads();
   } else {
-    r0 = blockIdx.x * ROWS;
+    r0 = block * ROWS;
     n_rows = min(ROWS, p.m - r0);
   }
   auto row_of = [&](int i) { return GATHER ? s_rows[i] : r0 + i; };
@@ -346,22 +350,29 @@ int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
 template <int NR>
 void launch_lora_nr(const Lora& p, hipStream_t s) {
   const int cols = (p.n + kColsWg - 1) / kColsWg;
+  const dim3 grid((unsigned)((p.row_blocks + 7) / 8 * 8 * cols));
   if (p.m <= kGatherRows) {
     hipLaunchKernelGGL((lora_shrink_kernel<NR, true>), dim3(p.m, p.n_split), dim3(256), 0, s, p);
-    hipLaunchKernelGGL((lora_expand_kernel<NR, true>), dim3(p.m, cols), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((lora_expand_kernel<NR, true>), grid, dim3(256), 0, s, p);
   } else {
-    const int tiles = (p.m + kTileRows - 1) / kTileRows;
-    hipLaunchKernelGGL((lora_shrink_kernel<NR, false>), dim3(tiles, p.n_split), dim3(256), 0, s, p);
-    hipLaunchKernelGGL((lora_expand_kernel<NR, false>), dim3(tiles, cols), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((lora_shrink_kernel<NR, false>), dim3(p.row_blocks, p.n_split), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((lora_expand_kernel<NR, false>), grid, dim3(256), 0, s, p);
   }
 }
 
 }  // namespace
 
+// Groups of rows that workgroups are numbered by: every row where groups are
+// searched, else tiles.
+static int lora_row_blocks(int m) { return m <= kGatherRows ? m : (m - 1) / kTileRows + 1; }
+
+bool lora_fits(int m, int n) {
+  return ((int64_t)lora_row_blocks(m) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31);
+}
+
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
 int lora_splits(int m, int k) {
-  const int tiles = m <= kGatherRows ? m : (m + kTileRows - 1) / kTileRows;
-  const int want = (m <= kGatherRows ? 1024 : 640) / tiles, most = (k + 31) / 32 / 8;
+  const int want = (m <= kGatherRows ? 1024 : 640) / lora_row_blocks(m), most = (k + 31) / 32 / 8;
   const int ns = want < most ? want : most;
   return ns < 1 ? 1 : ns > 16 ? 16 : ns;
 }
@@ -371,6 +382,7 @@ int64_t lora_ws_bytes(int m, int k, int R) { return (int64_t)lora_splits(m, k) *
 void launch_lora(Lora p, void* ws, hipStream_t s) {
   p.t = reinterpret_cast<float*>(ws);
   p.n_split = lora_splits(p.m, p.k);
+  p.row_blocks = lora_row_blocks(p.m);
   switch (rank_tiles(p.R)) {
     case 1: launch_lora_nr<1>(p, s); break;
     case 2: launch_lora_nr<2>(p, s); break;

@@ -196,8 +196,8 @@ void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
 
 // y = base + scale (x A^T) B^T with each row's adapter (see mz.h,
 // mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8, y_stride of 4,
-// every pointer 16-byte aligned.  t and n_split are the launcher's own, in ws
-// (lora_ws_bytes bytes).
+// every pointer 16-byte aligned, lora_fits(m, n).  The last three lines are the
+// launcher's own, t in ws (lora_ws_bytes bytes).
 struct Lora {
   const _Float16 *x, *a, *b;
   const int32_t *adapter, *rank;
@@ -207,7 +207,9 @@ struct Lora {
   int m, k, n, R, n_adapters;
   float* t;          // [n_split][m][R rounded up] partials of x A^T
   int n_split;
+  int row_blocks;
 };
+bool lora_fits(int m, int n);
 int64_t lora_ws_bytes(int m, int k, int R);
 void launch_lora(Lora p, void* ws, hipStream_t s);
 

@@ -2287,9 +2287,9 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
     if (y_stride < n || y_stride % 4) fail(MZ_EINVAL, "y_stride must be a multiple of 4 and at least n");
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(base) || !aligned16(y) || !aligned16(workspace))
       fail(MZ_EINVAL, "x, a, b, base, y and workspace must lie on 16-byte boundaries");
-    if ((int64_t)n > 65535 * 256) fail(MZ_EINVAL, "n exceeds 65535 * 256");
     check_stream(stream);
     if (m == 0) return;
+    if (!mzk::lora_fits(m, n)) fail(MZ_EINVAL, "m rows of n columns are too many");
     if (workspace_bytes < mzk::lora_ws_bytes(m, k, max_rank)) fail(MZ_EINVAL, "workspace too small");
     mzk::Lora p{};
     p.x = reinterpret_cast<const _Float16*>(x);

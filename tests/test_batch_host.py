@@ -96,7 +96,7 @@ LORA = dict(x_ptr=P, m=3, k=64, adapter_ptr=P, n_adapters=2, a_ptr=P, b_ptr=P, m
     (dict(y_stride=96), "y_stride"), (dict(y_stride=102), "y_stride"), (dict(y_stride=-4), "y_stride"),
     (dict(x_ptr=P + 2), "16-byte"), (dict(a_ptr=P + 8), "16-byte"), (dict(b_ptr=P + 8), "16-byte"),
     (dict(base_ptr=P + 4), "16-byte"), (dict(y_ptr=P + 4), "16-byte"), (dict(ws_ptr=P + 4), "16-byte"),
-    (dict(n=1 << 30, y_stride=1 << 30), "65535"), (dict(ws_bytes=0), "workspace"), (dict(ws_bytes=-1), "workspace"),
+    (dict(m=1 << 30, n=1 << 30, y_stride=1 << 30), "too many"), (dict(ws_bytes=0), "workspace"), (dict(ws_bytes=-1), "workspace"),
 ])
 def test_lora_add_refusals(bad, match):
     refused(mz.mz_lora_add, **{**LORA, **bad}, match=match)
