@@ -2,7 +2,7 @@
 //   y_r = base_r + s_a (x_r A_a^T) B_a^T,  a = adapter[r],
 // with A_a [R][k] and B_a [n][R] f16 of which the first rank[a] ranks count.
 //
-// Two launches: the first forms t = x A^T, fp32, in K splits; the second adds
+// Two steps: the first forms t = x A^T, fp32, in K splits; the second adds
 // the splits in order, scales them and adds t B^T to the rows.  The products
 // of f16 x and A are exact and summed in fp32 (v_mfma_f32_16x16x32_f16).  For
 // the second product t is written as hi + lo, two f16 values, after the row's
@@ -17,8 +17,10 @@
 //    workgroup from the adapter list: row r begins a group when the rows
 //    before it with its adapter fill whole groups.  Each adapter is read once
 //    per 16 of its rows, however the rows are mixed.
-//  - Many rows: tiles of 32 neighbouring rows; a tile with several adapters
-//    runs once for each of them and keeps each row's own result.
+//  - Many rows: the first product in tiles of 64 neighbouring rows staged
+//    through LDS, a third launch that makes the halves of t once, the second
+//    product in tiles of 32; a tile with several adapters runs once for each
+//    of them and keeps each row's own result.
 // A row's results depend on no other row: a row is one column (or row) of an
 // MFMA operand, and what other adapters make of it is dropped, not masked by
 // zeros.
@@ -32,7 +34,8 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kGatherRows = 512;     // rows up to which the adapter list is searched
-constexpr int kTileRows = 32;
+constexpr int kTileRows = 32;       // rows of a tile of the second product
+constexpr int kStageRows = 64;      // and of the first, with 64 of k at a time
 constexpr int kColsWg = 256;         // columns of a workgroup of the second product: 64 a wave
 
 __device__ __forceinline__ bool has_adapter(const Lora& p, int a) { return (unsigned)a < (unsigned)p.n_adapters; }
@@ -70,122 +73,223 @@ __device__ __forceinline__ int gather_group(const Lora& p, int r, int a, int* ro
   return min(seen - before, 16);
 }
 
-// acc += x A^T over the 32-wide K steps s0 .. s1 - 1: NX tiles of 16 rows x
-// NT tiles of 16 ranks.  xr: this lane's x row of each tile, ar: its A row
-// (rank l % 16 of each tile).  No branch lies between the loads of a few
-// steps, so all of them are in flight together; the last step may pass k.
-template <int NX, int NT, int NR>
-__device__ __forceinline__ void shrink_steps(int k_all, const _Float16* const (&xr)[NX], const _Float16* const (&ar)[NR],
-                                             int s0, int s1, f32x4 (&acc)[NX][NR]) {
+// acc += x A^T over the 32-wide K steps s0 .. s1 - 1 of 16 rows and NT tiles
+// of 16 ranks.  xr: this lane's x row, ar: its A row (rank l % 16 of each
+// tile).  No branch lies between the loads of a few steps, so all of them are
+// in flight together; the last step may pass k.
+template <int NT, int NR>
+__device__ __forceinline__ void shrink_steps(int k_all, const _Float16* xr, const _Float16* const (&ar)[NR], int s0, int s1,
+                                             f32x4 (&acc)[NR]) {
   const int lg = (threadIdx.x & 63) >> 4;
   const int full = min(s1, k_all / 32);
-  constexpr int U = NX + NT <= 6 ? 4 : 2;
+  constexpr int U = 4;
   int s = s0;
   for (; s + U <= full; s += U) {
-    f16x8 xv[U][NX], av[U][NT];
+    f16x8 xv[U], av[U][NT];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = (s + u) * 32 + lg * 8;
-#pragma unroll
-      for (int i = 0; i < NX; ++i) xv[u][i] = *reinterpret_cast<const f16x8*>(xr[i] + k);
+      xv[u] = *reinterpret_cast<const f16x8*>(xr + k);
 #pragma unroll
       for (int j = 0; j < NT; ++j) av[u][j] = *reinterpret_cast<const f16x8*>(ar[j] + k);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < NX; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[u][i], av[u][j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[u], av[u][j], acc[j], 0, 0, 0);
   }
   for (; s < s1; ++s) {
     const int k = s * 32 + lg * 8;
     const bool in = k < k_all;             // k_all is a multiple of 8
-    f16x8 xv[NX], av[NT];
-#pragma unroll
-    for (int i = 0; i < NX; ++i) xv[i] = *reinterpret_cast<const f16x8*>(xr[i] + (in ? k : 0));
+    const f16x8 xv = *reinterpret_cast<const f16x8*>(xr + (in ? k : 0));
+    f16x8 av[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) av[j] = *reinterpret_cast<const f16x8*>(ar[j] + (in ? k : 0));
 #pragma unroll
-    for (int i = 0; i < NX; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(in ? xv[i] : f16x8{}, in ? av[j] : f16x8{}, acc[i][j], 0, 0, 0);
+    for (int j = 0; j < NT; ++j)
+      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(in ? xv : f16x8{}, in ? av[j] : f16x8{}, acc[j], 0, 0, 0);
   }
 }
 
-// The rows of a workgroup that share adapter a: bit i of members is row i of
-// its 16 NX; row_of(i) its index.  The four waves take a quarter of the
-// split's K range each and join through LDS.
-template <int NX, int NR, class RowOf>
-__device__ __forceinline__ void shrink_adapter(const Lora& p, float* t, int a, uint64_t members, int n_rows, RowOf row_of,
-                                               f32x4 (&s_acc)[4][NX][NR][64]) {
+// Few rows: t [split][m][16 NR] of the K range of split blockIdx.y for the
+// group that begins at row blockIdx.x.  The four waves take a quarter of the
+// range each and join through LDS.
+template <int NR>
+__global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
   constexpr int RP = 16 * NR;
+  __shared__ int s_rows[16];
+  __shared__ f32x4 s_acc[4][NR][64];
+  const int r = blockIdx.x, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
+  if (!has_adapter(p, a)) return;
+  const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
+  if (n == 0) return;
+  __syncthreads();
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int steps = (p.k + 31) / 32, ns = gridDim.y;
   const int s0 = (int)((int64_t)blockIdx.y * steps / ns), s1 = (int)((int64_t)(blockIdx.y + 1) * steps / ns);
   const int q0 = s0 + (s1 - s0) * w / 4, q1 = s0 + (s1 - s0) * (w + 1) / 4;
   const int rank = rank_of(p, a), n_rt = (rank + 15) / 16;
-  const _Float16 *ar[NR], *xr[NX];
-  f32x4 acc[NX][NR];
+  const _Float16 *ar[NR], *xr = p.x + (int64_t)s_rows[min(col, n - 1)] * p.k;
+  f32x4 acc[NR];
 #pragma unroll
-  for (int j = 0; j < NR; ++j) ar[j] = p.a + ((int64_t)a * p.R + max(min(j * 16 + col, rank - 1), 0)) * p.k;
-#pragma unroll
-  for (int i = 0; i < NX; ++i) {
-    xr[i] = p.x + (int64_t)row_of(min(i * 16 + col, n_rows - 1)) * p.k;
-#pragma unroll
-    for (int j = 0; j < NR; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < NR; ++j) {
+    ar[j] = p.a + ((int64_t)a * p.R + max(min(j * 16 + col, rank - 1), 0)) * p.k;
+    acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // rank tiles past the rank are left out, by powers of two
-  if (n_rt <= 1) shrink_steps<NX, 1>(p.k, xr, ar, q0, q1, acc);
-  else if (NR == 2 || (NR > 2 && n_rt <= 2)) shrink_steps<NX, NR >= 2 ? 2 : 1>(p.k, xr, ar, q0, q1, acc);
-  else if (NR == 4 || (NR > 4 && n_rt <= 4)) shrink_steps<NX, NR >= 4 ? 4 : 1>(p.k, xr, ar, q0, q1, acc);
-  else shrink_steps<NX, NR>(p.k, xr, ar, q0, q1, acc);
+  if (n_rt <= 1) shrink_steps<1>(p.k, xr, ar, q0, q1, acc);
+  else if (NR == 2 || (NR > 2 && n_rt <= 2)) shrink_steps<NR >= 2 ? 2 : 1>(p.k, xr, ar, q0, q1, acc);
+  else if (NR == 4 || (NR > 4 && n_rt <= 4)) shrink_steps<NR >= 4 ? 4 : 1>(p.k, xr, ar, q0, q1, acc);
+  else shrink_steps<NR>(p.k, xr, ar, q0, q1, acc);
 #pragma unroll
-  for (int i = 0; i < NX; ++i)
-#pragma unroll
-    for (int j = 0; j < NR; ++j) s_acc[w][i][j][lane] = acc[i][j];
+  for (int j = 0; j < NR; ++j) s_acc[w][j][lane] = acc[j];
   __syncthreads();
+  float* t = p.t + (int64_t)blockIdx.y * p.m * RP;
   // element e of lane l is row 4 (l / 16) + e, rank l % 16
-  for (int ij = w; ij < NX * NR; ij += 4) {
-    const int i = ij / NR, j = ij % NR;
-    const f32x4 v = s_acc[0][i][j][lane] + s_acc[1][i][j][lane] + s_acc[2][i][j][lane] + s_acc[3][i][j][lane];
+  for (int j = w; j < NR; j += 4) {
+    const f32x4 v = s_acc[0][j][lane] + s_acc[1][j][lane] + s_acc[2][j][lane] + s_acc[3][j][lane];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int at = i * 16 + lg * 4 + e;
-      if ((members >> at) & 1) t[(int64_t)row_of(at) * RP + j * 16 + col] = j * 16 + col < rank ? v[e] : 0.f;
-    }
+    for (int e = 0; e < 4; ++e)
+      if (lg * 4 + e < n) t[(int64_t)s_rows[lg * 4 + e] * RP + j * 16 + col] = j * 16 + col < rank ? v[e] : 0.f;
   }
 }
 
-// t [split][m][16 NR] of the K range of split blockIdx.y.
-template <int NR, bool GATHER>
-__global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
-  constexpr int RP = 16 * NR, NX = GATHER ? 1 : kTileRows / 16;
-  __shared__ int s_rows[16];
-  __shared__ f32x4 s_acc[4][NX][NR][64];
+// Many rows: the same for 64 neighbouring rows.  x and A go through LDS, 64 of
+// k at a time, as whole 128-byte lines that are read once per workgroup (with
+// fragments straight from memory, 16 rows of 64 bytes an instruction, and each
+// wave's own copy of A, the L2's answers bound it: 24.7 us for 4099 rows of
+// 4096 by 64 ranks); three tiles are in flight while one is multiplied.  Wave
+// w has rows 16 w .. 16 w + 15.
+template <int NR>
+__global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
+  constexpr int RP = 16 * NR, KT = 64, PITCH = KT + 8, DEPTH = 3;
+  constexpr int NXL = kStageRows * 8 / 256, NAL = (RP * 8 + 255) / 256;   // 16-byte pieces a thread
+  __shared__ __attribute__((aligned(16))) _Float16 s_x[2][kStageRows][PITCH];
+  __shared__ __attribute__((aligned(16))) _Float16 s_a[2][RP][PITCH];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, lg = lane >> 4;
+  const int r0 = blockIdx.x * kStageRows, n = min(kStageRows, p.m - r0);
+  const int tiles = (p.k + KT - 1) / KT, ns = gridDim.y;
+  const int t0 = (int)((int64_t)blockIdx.y * tiles / ns), nt = (int)((int64_t)(blockIdx.y + 1) * tiles / ns) - t0;
   float* t = p.t + (int64_t)blockIdx.y * p.m * RP;
-  if constexpr (GATHER) {
-    const int r = blockIdx.x, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
-    if (!has_adapter(p, a)) return;
-    const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
-    if (n == 0) return;
-    __syncthreads();
-    shrink_adapter<NX, NR>(p, t, a, (1ull << n) - 1, n, [&](int i) { return s_rows[i]; }, s_acc);
-  } else {
-    const int r0 = blockIdx.x * kTileRows, lane = threadIdx.x & 63, n = min(kTileRows, p.m - r0);
-    const int mine = lane < n ? p.adapter[r0 + lane] : -1;
-    uint64_t todo = __ballot(has_adapter(p, mine));
-    while (todo) {
-      const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
-      const uint64_t members = __ballot(mine == a);
-      todo &= ~members;
-      shrink_adapter<NX, NR>(p, t, a, members, n, [&](int i) { return r0 + i; }, s_acc);
-      if (todo) __syncthreads();
+  const int mine = lane < n ? p.adapter[r0 + lane] : -1;
+  uint64_t todo = __ballot(has_adapter(p, mine));
+  while (todo) {
+    const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+    const uint64_t members = __ballot(mine == a);
+    todo &= ~members;
+    const int rank = rank_of(p, a);
+    const int seg = (tid & 7) * 8;
+    const _Float16 *xp[NXL], *ap[NAL];
+#pragma unroll
+    for (int e = 0; e < NXL; ++e) xp[e] = p.x + (int64_t)(r0 + min((tid >> 3) + 32 * e, n - 1)) * p.k + seg;
+#pragma unroll
+    for (int e = 0; e < NAL; ++e)
+      ap[e] = p.a + ((int64_t)a * p.R + max(min((tid >> 3) + 32 * e, rank - 1), 0)) * p.k + seg;
+    f16x8 xr[DEPTH][NXL], ar[DEPTH][NAL];
+    auto load = [&](int i, int tile) {
+      const int k = (t0 + tile) * KT;
+      const bool in = k + seg < p.k;         // k is a multiple of 8
+#pragma unroll
+      for (int e = 0; e < NXL; ++e) {
+        xr[i][e] = *reinterpret_cast<const f16x8*>(xp[e] + (in ? k : -seg));
+        if (!in) xr[i][e] = f16x8{};
+      }
+#pragma unroll
+      for (int e = 0; e < NAL; ++e) {
+        ar[i][e] = *reinterpret_cast<const f16x8*>(ap[e] + (in ? k : -seg));
+        if (!in) ar[i][e] = f16x8{};
+      }
+    };
+    f32x4 acc[NR];
+#pragma unroll
+    for (int j = 0; j < NR; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) load(i, min(i, nt - 1));
+    for (int tb = 0; tb < nt; tb += DEPTH) {
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i) {
+        const int tile = tb + i, buf = tile & 1;
+        if (tile >= nt) break;
+#pragma unroll
+        for (int e = 0; e < NXL; ++e) *reinterpret_cast<f16x8*>(&s_x[buf][(tid >> 3) + 32 * e][seg]) = xr[i][e];
+#pragma unroll
+        for (int e = 0; e < NAL; ++e)
+          if ((tid >> 3) + 32 * e < RP) *reinterpret_cast<f16x8*>(&s_a[buf][(tid >> 3) + 32 * e][seg]) = ar[i][e];
+        load(i, min(tile + DEPTH, nt - 1));
+        __syncthreads();     // the buffer before last was read before the previous tile's barrier
+#pragma unroll
+        for (int ks = 0; ks < KT / 32; ++ks) {
+          const f16x8 xv = *reinterpret_cast<const f16x8*>(&s_x[buf][w * 16 + col][ks * 32 + lg * 8]);
+#pragma unroll
+          for (int j = 0; j < NR; ++j) {
+            if (j * 16 >= rank) break;
+            const f16x8 av = *reinterpret_cast<const f16x8*>(&s_a[buf][j * 16 + col][ks * 32 + lg * 8]);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av, acc[j], 0, 0, 0);
+          }
+        }
+      }
     }
+#pragma unroll
+    for (int j = 0; j < NR; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = w * 16 + lg * 4 + e;
+        if ((members >> at) & 1) t[(int64_t)(r0 + at) * RP + j * 16 + col] = j * 16 + col < rank ? acc[j][e] : 0.f;
+      }
+    __syncthreads();         // before the next adapter's first tile
   }
+}
+
+// Four ranks j .. j + 3 of row r: the splits of t added in order, times the
+// row's scale, in two f16 halves after the row's largest was brought to 2^14;
+// unit: what undoes that.  The LPR lanes of a row are neighbours, a power of
+// two of them, and run this together.
+template <int NR>
+__device__ __forceinline__ void t_halves(const Lora& p, int r, int j, f16x4& hi, f16x4& lo, float& unit) {
+  constexpr int RP = 16 * NR, LPR = RP / 4;
+  const int a = p.adapter[r];
+  f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (has_adapter(p, a)) {
+    const float* t = p.t + (int64_t)r * RP + j;
+#pragma unroll 8
+    for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * RP);
+    if (p.scale) v *= p.scale[a];
+  }
+  float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  // a row of zeros or with an infinity stays as it is, its finite values within f16
+  const int up = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float u = ldexpf(v[e], up);
+    if (fabsf(u) < INFINITY) u = fminf(fmaxf(u, -65504.f), 65504.f);
+    hi[e] = (_Float16)u;
+    lo[e] = fabsf(u) < INFINITY ? (_Float16)(u - (float)hi[e]) : (_Float16)0.f;
+  }
+  unit = ldexpf(1.f, -up);
+}
+
+// Many rows: the halves of t, [m][32 KS] each, and every row's unit.
+template <int NR>
+__global__ __launch_bounds__(256) void lora_halves_kernel(Lora p) {
+  constexpr int RP = 16 * NR, LPR = RP / 4, W = (RP + 31) / 32 * 32;
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int r = (int)(idx / LPR), j = (int)(idx % LPR) * 4;
+  if (r >= p.m) return;
+  f16x4 hi, lo;
+  float unit;
+  t_halves<NR>(p, r, j, hi, lo, unit);
+  _Float16 *h = p.hi + (int64_t)r * W + j, *l = p.lo + (int64_t)r * W + j;
+  *reinterpret_cast<f16x4*>(h) = hi;
+  *reinterpret_cast<f16x4*>(l) = lo;
+  if (RP < W) {
+    *reinterpret_cast<f16x4*>(h + RP) = f16x4{0, 0, 0, 0};
+    *reinterpret_cast<f16x4*>(l + RP) = f16x4{0, 0, 0, 0};
+  }
+  if (j == 0) p.unit[r] = unit;
 }
 
 // y of 16 NX rows x 256 columns: wave w has columns 64 w .. 64 w + 63 of the
@@ -196,8 +300,8 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
   constexpr int RP = 16 * NR, KS = (RP + 31) / 32, PITCH = KS * 32 + 8;
   constexpr int NX = GATHER ? 1 : kTileRows / 16, ROWS = 16 * NX;
   __shared__ int s_rows[16];
-  __shared__ __attribute__((aligned(16))) _Float16 s_hi[ROWS][PITCH], s_lo[ROWS][PITCH];
-  __shared__ float s_unit[ROWS];         // what a row's d is multiplied by
+  __shared__ __attribute__((aligned(16))) _Float16 s_hi[GATHER ? 16 : 1][PITCH], s_lo[GATHER ? 16 : 1][PITCH];
+  __shared__ float s_unit[16];           // what a row's d is multiplied by
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   // Workgroup b runs on XCD b % 8: it serves every eighth row block, whose column ranges follow each other, so
@@ -243,42 +347,37 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
         for (int e = 0; e < 4; ++e) y[i][c][e] = at + e < p.n ? b[e] : 0.f;
       }
     }
-  // t of the rows: the splits added in order, times the row's scale, then in two halves.  A row's lanes are
-  // neighbours, a power of two of them
   constexpr int LPR = RP / 4;
-  for (int idx = threadIdx.x; idx < n_rows * LPR; idx += 256) {
-    const int i = idx / LPR, j = (idx % LPR) * 4, r = row_of(i), a = p.adapter[r];
-    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (has_adapter(p, a)) {
-      const float* t = p.t + (int64_t)r * RP + j;
-#pragma unroll 8
-      for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * RP);
-      if (p.scale) v *= p.scale[a];
+  if constexpr (GATHER) {
+    for (int idx = threadIdx.x; idx < n_rows * LPR; idx += 256) {
+      const int i = idx / LPR, j = (idx % LPR) * 4;
+      f16x4 hi, lo;
+      float unit;
+      t_halves<NR>(p, s_rows[i], j, hi, lo, unit);
+      *reinterpret_cast<f16x4*>(&s_hi[i][j]) = hi;
+      *reinterpret_cast<f16x4*>(&s_lo[i][j]) = lo;
+      if (RP < KS * 32) {
+        *reinterpret_cast<f16x4*>(&s_hi[i][RP + j]) = f16x4{0, 0, 0, 0};
+        *reinterpret_cast<f16x4*>(&s_lo[i][RP + j]) = f16x4{0, 0, 0, 0};
+      }
+      if (j == 0) s_unit[i] = unit;
     }
-    float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    // 2^(14 - exponent of the largest); a row of zeros or with an infinity stays as it is, its finite values
-    // within f16
-    const int up = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-    f16x4 hi, lo;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float u = ldexpf(v[e], up);
-      if (fabsf(u) < INFINITY) u = fminf(fmaxf(u, -65504.f), 65504.f);
-      hi[e] = (_Float16)u;
-      lo[e] = fabsf(u) < INFINITY ? (_Float16)(u - (float)hi[e]) : (_Float16)0.f;
-    }
-    *reinterpret_cast<f16x4*>(&s_hi[i][j]) = hi;
-    *reinterpret_cast<f16x4*>(&s_lo[i][j]) = lo;
-    if (RP < KS * 32) {
-      *reinterpret_cast<f16x4*>(&s_hi[i][RP + j]) = f16x4{0, 0, 0, 0};
-      *reinterpret_cast<f16x4*>(&s_lo[i][RP + j]) = f16x4{0, 0, 0, 0};
-    }
-    if (j == 0) s_unit[i] = ldexpf(1.f, -up);
+    __syncthreads();
   }
-  __syncthreads();
   if (c0 >= p.n) return;
+  // this lane's halves, ranks 32 j + 8 (l / 16) .. + 7 of its rows
+  f16x8 hi[NX][KS], lo[NX][KS];
+  float unit[NX];
+#pragma unroll
+  for (int i = 0; i < NX; ++i) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      const int at = j * 32 + lg * 8;
+      hi[i][j] = *reinterpret_cast<const f16x8*>(GATHER ? &s_hi[col][at] : p.hi + (int64_t)rows[i] * (KS * 32) + at);
+      lo[i][j] = *reinterpret_cast<const f16x8*>(GATHER ? &s_lo[col][at] : p.lo + (int64_t)rows[i] * (KS * 32) + at);
+    }
+    unit[i] = GATHER ? s_unit[min(col, n_rows - 1)] : p.unit[rows[i]];
+  }
   const int seen = GATHER ? mine[0] : (lane < n_rows ? p.adapter[r0 + lane] : -1);
   uint64_t todo = GATHER ? 1ull : __ballot(has_adapter(p, seen));
   while (todo) {
@@ -312,19 +411,16 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
         if (j * 32 >= rank) break;
-        const f16x8 lo = *reinterpret_cast<const f16x8*>(&s_lo[i * 16 + col][j * 32 + lg * 8]);
-        const f16x8 hi = *reinterpret_cast<const f16x8*>(&s_hi[i * 16 + col][j * 32 + lg * 8]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo, d[c], 0, 0, 0);
-          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi, d[c], 0, 0, 0);
+          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo[i][j], d[c], 0, 0, 0);
+          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi[i][j], d[c], 0, 0, 0);
         }
       }
-      const float unit = s_unit[min(i * 16 + col, n_rows - 1)];
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][c][e] = mine[i] == a ? __builtin_fmaf(d[c][e], unit, y[i][c][e]) : y[i][c][e];
+        for (int e = 0; e < 4; ++e) y[i][c][e] = mine[i] == a ? __builtin_fmaf(d[c][e], unit[i], y[i][c][e]) : y[i][c][e];
     }
   }
 #pragma unroll
@@ -352,10 +448,12 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
   const int cols = (p.n + kColsWg - 1) / kColsWg;
   const dim3 grid((unsigned)((p.row_blocks + 7) / 8 * 8 * cols));
   if (p.m <= kGatherRows) {
-    hipLaunchKernelGGL((lora_shrink_kernel<NR, true>), dim3(p.m, p.n_split), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_shrink_kernel<NR>, dim3(p.m, p.n_split), dim3(256), 0, s, p);
     hipLaunchKernelGGL((lora_expand_kernel<NR, true>), grid, dim3(256), 0, s, p);
   } else {
-    hipLaunchKernelGGL((lora_shrink_kernel<NR, false>), dim3(p.row_blocks, p.n_split), dim3(256), 0, s, p);
+    const int stages = (p.m - 1) / kStageRows + 1;
+    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(stages, p.n_split), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((unsigned)(((int64_t)p.m * 4 * NR + 255) / 256)), dim3(256), 0, s, p);
     hipLaunchKernelGGL((lora_expand_kernel<NR, false>), grid, dim3(256), 0, s, p);
   }
 }
@@ -372,17 +470,27 @@ bool lora_fits(int m, int n) {
 
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
 int lora_splits(int m, int k) {
-  const int want = (m <= kGatherRows ? 1024 : 640) / lora_row_blocks(m), most = (k + 31) / 32 / 8;
+  const int groups = m <= kGatherRows ? m : (m - 1) / kStageRows + 1;
+  const int want = (m <= kGatherRows ? 1024 : 520) / groups, most = (k + 31) / 32 / 8;
   const int ns = want < most ? want : most;
   return ns < 1 ? 1 : ns > 16 ? 16 : ns;
 }
 
-int64_t lora_ws_bytes(int m, int k, int R) { return (int64_t)lora_splits(m, k) * m * rank_tiles(R) * 16 * 4; }
+static int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
+static int64_t t_bytes(int m, int k, int R) { return (int64_t)lora_splits(m, k) * m * rank_tiles(R) * 16 * 4; }
+static int64_t half_bytes(int m, int R) { return (int64_t)m * ((rank_tiles(R) * 16 + 31) / 32 * 32) * 2; }
+
+int64_t lora_ws_bytes(int m, int k, int R) {
+  return t_bytes(m, k, R) + (m > kGatherRows ? 2 * half_bytes(m, R) + up16((int64_t)m * 4) : 0);
+}
 
 void launch_lora(Lora p, void* ws, hipStream_t s) {
   p.t = reinterpret_cast<float*>(ws);
   p.n_split = lora_splits(p.m, p.k);
   p.row_blocks = lora_row_blocks(p.m);
+  p.hi = reinterpret_cast<_Float16*>(reinterpret_cast<uint8_t*>(ws) + t_bytes(p.m, p.k, p.R));
+  p.lo = p.hi + half_bytes(p.m, p.R) / 2;
+  p.unit = reinterpret_cast<float*>(p.lo + half_bytes(p.m, p.R) / 2);
   switch (rank_tiles(p.R)) {
     case 1: launch_lora_nr<1>(p, s); break;
     case 2: launch_lora_nr<2>(p, s); break;

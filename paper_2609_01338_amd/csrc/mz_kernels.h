@@ -196,8 +196,8 @@ void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
 
 // y = base + scale (x A^T) B^T with each row's adapter (see mz.h,
 // mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8, y_stride of 4,
-// every pointer 16-byte aligned, lora_fits(m, n).  The last three lines are the
-// launcher's own, t in ws (lora_ws_bytes bytes).
+// every pointer 16-byte aligned, lora_fits(m, n).  The fields from t on are the
+// launcher's own, in ws (lora_ws_bytes bytes).
 struct Lora {
   const _Float16 *x, *a, *b;
   const int32_t *adapter, *rank;
@@ -206,6 +206,8 @@ struct Lora {
   int64_t y_stride;
   int m, k, n, R, n_adapters;
   float* t;          // [n_split][m][R rounded up] partials of x A^T
+  _Float16 *hi, *lo; // many rows: t in two halves, and what each row of them
+  float* unit;       // is multiplied by
   int n_split;
   int row_blocks;
 };
