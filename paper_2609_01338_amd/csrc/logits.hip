@@ -12,7 +12,10 @@
 // list and keeps what falls into its slice in LDS, as counts (integer adds)
 // and as the highest entry index per token (integer max), so neither needs
 // vocabulary-sized memory, and the order in which lanes arrive changes
-// nothing.  The slices' largest values meet in a second, small kernel.
+// nothing.  What a workgroup waits for is short and of one kind, so loads go
+// out early (the first tokens of the history and the whole of a short bias
+// list with the logits), and slices are small enough for eight workgroups a
+// CU.  The slices' largest values meet in a second, small kernel.
 #include "mz_kernels.h"
 
 namespace mzk {
@@ -45,17 +48,23 @@ __device__ __forceinline__ float penalised(float x, float count, float rep, floa
   return y - pres;
 }
 
-template <int SLICE, int VEC>
-__global__ __launch_bounds__(256) void logits_rules_kernel(LogitsRules p) {
-  constexpr int GROUPS = SLICE / (256 * VEC);
+// History tokens and bias entries that the threads load ahead of the slice's
+// other work, all together; what stands for a token without a bias: -0 as a value, below
+// every index.
+constexpr int kAheadHistory = 2048, kAheadBias = 512, kNone = (int)0x80000000;
+
+template <int NT, int SLICE, int VEC>
+__global__ __launch_bounds__(NT) void logits_rules_kernel(LogitsRules p) {
+  constexpr int GROUPS = SLICE / (NT * VEC);
+  constexpr int AH = kAheadHistory / NT < 1 ? 1 : kAheadHistory / NT, AB = kAheadBias / NT < 1 ? 1 : kAheadBias / NT;
   __shared__ __attribute__((aligned(16))) int s_count[SLICE];
   __shared__ __attribute__((aligned(16))) int s_last[SLICE];
-  __shared__ float s_val[4];
-  __shared__ int s_idx[4];
+  __shared__ float s_val[NT / 64];
+  __shared__ int s_idx[NT / 64];
   const int row = blockIdx.x / p.slices, v0 = (blockIdx.x % p.slices) * SLICE, tid = threadIdx.x;
   const float* x = p.logits + (int64_t)row * p.stride;
   // value e of group i: token at(i) + e
-  auto at = [&](int i) { return v0 + (i * 256 + tid) * VEC; };
+  auto at = [&](int i) { return v0 + (i * NT + tid) * VEC; };
   float val[GROUPS][VEC];
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) {
@@ -80,33 +89,67 @@ __global__ __launch_bounds__(256) void logits_rules_kernel(LogitsRules p) {
   int64_t h0 = 0, h1 = p.n_history, b0 = 0, b1 = p.n_bias;
   if (p.history_off) h0 = p.history_off[row], h1 = p.history_off[row + 1];
   if (p.bias_off) b0 = p.bias_off[row], b1 = p.bias_off[row + 1];
-  const bool hist = h1 > h0, bias = b1 > b0;
-  if (hist || bias) {
-    for (int i = tid * 4; i < SLICE; i += 1024) {
+  const int nh = (int)(h1 - h0), nb = (int)(b1 - b0);
+  if (nh > 0 || nb > 0) {
+    const unsigned here = (unsigned)min(SLICE, p.vocab - v0);
+    const int32_t *history = p.history + h0, *bias_token = p.bias_token + b0;
+    const float* bias_value = p.bias_value + b0;
+    // tokens relative to the slice: inside it only below `here`
+    unsigned ht[AH], bt[AB];
+    float bval[AB];
+    const bool held = nb <= NT * AB;       // the list's values stay in registers
+#pragma unroll
+    for (int k = 0; k < AH; ++k) ht[k] = tid + NT * k < nh ? (unsigned)history[tid + NT * k] - (unsigned)v0 : ~0u;
+#pragma unroll
+    for (int k = 0; k < AB; ++k) {
+      const bool in = tid + NT * k < nb;
+      bt[k] = in ? (unsigned)bias_token[tid + NT * k] - (unsigned)v0 : ~0u;
+      bval[k] = in ? bias_value[tid + NT * k] : 0.f;
+    }
+    for (int i = tid * 4; i < SLICE; i += NT * 4) {
       *reinterpret_cast<int4*>(&s_count[i]) = make_int4(0, 0, 0, 0);
-      *reinterpret_cast<int4*>(&s_last[i]) = make_int4(0, 0, 0, 0);
+      *reinterpret_cast<int4*>(&s_last[i]) = make_int4(kNone, kNone, kNone, kNone);
     }
     __syncthreads();
-    const unsigned here = (unsigned)min(SLICE, p.vocab - v0);
+#pragma unroll
+    for (int k = 0; k < AH; ++k)
+      if (ht[k] < here) atomicAdd(&s_count[ht[k]], 1);
 #pragma unroll 4
-    for (int64_t i = h0 + tid; i < h1; i += 256) {
-      const unsigned t = (unsigned)p.history[i] - (unsigned)v0;
+    for (int i = NT * AH + tid; i < nh; i += NT) {
+      const unsigned t = (unsigned)history[i] - (unsigned)v0;
       if (t < here) atomicAdd(&s_count[t], 1);
     }
-    for (int64_t i = b0 + tid; i < b1; i += 256) {
-      const unsigned t = (unsigned)p.bias_token[i] - (unsigned)v0;
-      if (t < here) atomicMax(&s_last[t], (int)(i - b0) + 1);
+    // entry e of the list stands as e + 1
+#pragma unroll
+    for (int k = 0; k < AB; ++k)
+      if (bt[k] < here) atomicMax(&s_last[bt[k]], tid + NT * k + 1);
+    for (int i = NT * AB + tid; i < nb; i += NT) {
+      const unsigned t = (unsigned)bias_token[i] - (unsigned)v0;
+      if (t < here) atomicMax(&s_last[t], i + 1);
     }
     __syncthreads();
+    if (nb > 0 && held) {    // the last entry of a token puts its value in the place of its index
+      bool last[AB];
+#pragma unroll
+      for (int k = 0; k < AB; ++k) last[k] = bt[k] < here && s_last[bt[k]] == tid + NT * k + 1;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < AB; ++k)
+        if (last[k]) s_last[bt[k]] = __float_as_int(bval[k]);
+      __syncthreads();
+    }
     const float* pen = p.penalty + (int64_t)row * 3;
-    const float rep = hist ? pen[0] : 1.f, freq = hist ? pen[1] : 0.f, pres = hist ? pen[2] : 0.f;
+    const float rep = nh > 0 ? pen[0] : 1.f, freq = nh > 0 ? pen[1] : 0.f, pres = nh > 0 ? pen[2] : 0.f;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const int t = at(i) + e - v0, c = s_count[t], last = s_last[t];
         if (c > 0) val[i][e] = penalised(val[i][e], (float)c, rep, freq, pres);
-        if (last > 0) val[i][e] += p.bias_value[b0 + last - 1];
+        if (held)
+          val[i][e] += __int_as_float(last);         // -0 where there is no bias: it changes no value
+        else if (last != kNone)
+          val[i][e] += bias_value[last - 1];
       }
   }
   float bv = -INFINITY;
@@ -145,7 +188,7 @@ __global__ __launch_bounds__(256) void logits_rules_kernel(LogitsRules p) {
   __syncthreads();
   if (tid == 0) {
 #pragma unroll
-    for (int i = 1; i < 4; ++i) take(bv, bi, s_val[i], s_idx[i]);
+    for (int i = 1; i < NT / 64; ++i) take(bv, bi, s_val[i], s_idx[i]);
     p.part_val[blockIdx.x] = bv;
     p.part_idx[blockIdx.x] = bi;
   }
@@ -160,7 +203,7 @@ __global__ __launch_bounds__(64) void logits_token_kernel(LogitsRules p) {
   if (threadIdx.x == 0) p.token[blockIdx.x] = bi == 0x7fffffff ? -1 : bi;
 }
 
-constexpr int kSmallSlice = 1024, kSlice = 4096;
+constexpr int kSmallThreads = 256, kSmallSlice = 1024, kThreads = 512, kSlice = 4096;
 
 int logits_slice(int m, int vocab) { return (int64_t)m * ((vocab + kSlice - 1) / kSlice) >= 512 ? kSlice : kSmallSlice; }
 
@@ -177,17 +220,17 @@ void launch_logits_rules(LogitsRules p, int m, void* ws, hipStream_t s) {
   p.part_val = reinterpret_cast<float*>(ws);
   p.part_idx = reinterpret_cast<int32_t*>(p.part_val + (int64_t)m * p.slices);
   const bool vec = p.stride % 4 == 0 && ((uintptr_t)p.logits & 15) == 0 && ((uintptr_t)p.out & 15) == 0;
-  const dim3 grid(m * p.slices), block(256);
+  const dim3 grid(m * p.slices);
   if (slice == kSlice) {
     if (vec)
-      hipLaunchKernelGGL((logits_rules_kernel<kSlice, 4>), grid, block, 0, s, p);
+      hipLaunchKernelGGL((logits_rules_kernel<kThreads, kSlice, 4>), grid, dim3(kThreads), 0, s, p);
     else
-      hipLaunchKernelGGL((logits_rules_kernel<kSlice, 1>), grid, block, 0, s, p);
+      hipLaunchKernelGGL((logits_rules_kernel<kThreads, kSlice, 1>), grid, dim3(kThreads), 0, s, p);
   } else {
     if (vec)
-      hipLaunchKernelGGL((logits_rules_kernel<kSmallSlice, 4>), grid, block, 0, s, p);
+      hipLaunchKernelGGL((logits_rules_kernel<kSmallThreads, kSmallSlice, 4>), grid, dim3(kSmallThreads), 0, s, p);
     else
-      hipLaunchKernelGGL((logits_rules_kernel<kSmallSlice, 1>), grid, block, 0, s, p);
+      hipLaunchKernelGGL((logits_rules_kernel<kSmallThreads, kSmallSlice, 1>), grid, dim3(kSmallThreads), 0, s, p);
   }
   if (p.token) hipLaunchKernelGGL(logits_token_kernel, dim3(m), dim3(64), 0, s, p);
 }
