@@ -69,8 +69,18 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& sum) {
   return v + before;
 }
 
+// Slots of a lane's K rows and of its V^T run in the block at key j0.
+struct Slots {
+  int k, v;
+};
 // SMALL: chunks of fewer than 32 tokens, a slot per 8 keys of a lane instead
-// of one per block.
+// of one per block.  (Keys past the last one take its entry.)
+template <bool SMALL>
+__device__ __forceinline__ Slots slots_of(const int32_t* table, int cshift, int j0, int col, int lg, int last) {
+  if constexpr (SMALL) return {table[min(j0 + 8 * (col >> 2), last) >> cshift], table[min(j0 + 8 * lg, last) >> cshift]};
+  return {0, table[j0 >> cshift]};
+}
+
 template <int HD, bool SMALL>
 __global__ __launch_bounds__(64 * kWaves) void attn_batch_kernel(AttnBatch a) {
   constexpr int KS = HD / 32;          // 32-wide dimension steps of a score product
@@ -139,28 +149,26 @@ __global__ __launch_bounds__(64 * kWaves) void attn_batch_kernel(AttnBatch a) {
     for (int d = 0; d < DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_c = -INFINITY, l_c = 0.f;
 
-    // this wave's blocks: j0, j0 + 128, ... below the share's end and the sequence's
+    // This wave's blocks: j0, j0 + 128, ... below the share's end and the
+    // sequence's.  Table entries are read a block ahead, so that a block waits
+    // for one trip to memory, not two.
     const int j_end = min(t1 * kUnit, len), last = len - 1;
+    Slots next = slots_of<SMALL>(table, a.cshift, min(t0 * kUnit + w * kBlock, last), col, lg, last);
     for (int j0 = t0 * kUnit + w * kBlock; j0 < j_end; j0 += kUnit) {
-      // slots of this lane's K rows and of its V^T runs
-      int slot_k[1], slot_v;
-      bool ok;
+      Slots at = next;
+      next = slots_of<SMALL>(table, a.cshift, min(j0 + kUnit, last), col, lg, last);
+      const bool ok = (unsigned)at.v < (unsigned)a.n_slots;
       if constexpr (SMALL) {
-        slot_k[0] = table[min(j0 + 8 * (col >> 2), last) >> a.cshift];
-        slot_v = table[min(j0 + 8 * lg, last) >> a.cshift];
-        ok = (unsigned)slot_v < (unsigned)a.n_slots;
-        if ((unsigned)slot_k[0] >= (unsigned)a.n_slots) slot_k[0] = 0;
-        if (!ok) slot_v = 0;
+        if ((unsigned)at.k >= (unsigned)a.n_slots) at.k = 0;
+        if (!ok) at.v = 0;
       } else {
-        slot_k[0] = __builtin_amdgcn_readfirstlane(table[j0 >> a.cshift]);
-        ok = (unsigned)slot_k[0] < (unsigned)a.n_slots;
+        at.k = at.v = __builtin_amdgcn_readfirstlane(at.v);
         if (!ok) continue;
-        slot_v = slot_k[0];
       }
       f16x8 ka[2][KS], va[DB];
       const int kj = j0 + 8 * (col >> 2), vj = j0 + 8 * lg;
-      const uint8_t* kp = a.slab + (int64_t)slot_k[0] * a.slot_bytes;
-      const uint8_t* vp = a.slab + (int64_t)slot_v * a.slot_bytes;
+      const uint8_t* kp = a.slab + (int64_t)at.k * a.slot_bytes;
+      const uint8_t* vp = a.slab + (int64_t)at.v * a.slot_bytes;
       const unsigned k_at = (unsigned)((kj & (a.C - 1)) + (col & 3)) * (unsigned)dkv * 2u + (h * HD + lg * 8) * 2u;
       const unsigned v_at = (unsigned)a.C * dkv * 2u + ((unsigned)(h * HD + col) * a.C + (vj & (a.C - 1))) * 2u;
 #pragma unroll
