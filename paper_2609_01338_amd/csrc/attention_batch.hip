@@ -82,7 +82,7 @@ __device__ __forceinline__ Slots slots_of(const int32_t* table, int cshift, int 
 }
 
 template <int HD, bool SMALL>
-__global__ __launch_bounds__(64 * kWaves) void attn_batch_kernel(AttnBatch a) {
+__global__ __launch_bounds__(64 * kWaves, 3) void attn_batch_kernel(AttnBatch a) {
   constexpr int KS = HD / 32;          // 32-wide dimension steps of a score product
   constexpr int DB = HD / 16;          // 16-dimension blocks of the output
   __shared__ float s_o[kWaves][DB][4][64];
@@ -283,14 +283,14 @@ __global__ __launch_bounds__(64 * kWaves) void attn_batch_kernel(AttnBatch a) {
 }
 
 // Joins the partials of one (sequence, query head): those of workgroups g0 ..
-// g1, in that order.  Every thread takes four dimensions of each eighth
-// (sixteenth for 64 dimensions) partial, loads in flight together.
+// g1.  Group pg of LPP lanes takes partials pg, pg + NG, ... with their own
+// running max, four dimensions a lane, and the groups meet in LDS; a partial's
+// max, sum and values come in one trip to memory.
 template <int HD>
 __global__ __launch_bounds__(256) void attn_batch_join_kernel(AttnBatch a) {
-  constexpr int LPP = HD / 4, NG = 256 / LPP;     // lanes per partial, partials at once
-  __shared__ float s_w[kAttnBatchWgs];
-  __shared__ float s_red[8];
-  __shared__ float4 s_acc[NG][LPP];
+  constexpr int LPP = HD / 4, NG = 256 / LPP, AHEAD = 4;     // lanes per partial, partials at once
+  __shared__ float s_m[NG], s_l[NG];
+  __shared__ f32x4 s_acc[NG][LPP];
   const int b = blockIdx.x / a.nq, hq = blockIdx.x % a.nq, h = hq / a.group, c = hq % a.group;
   const int u0 = a.base[b], nu = a.base[b + 1] - u0, n_units = a.base[a.n_seq] * a.nkv;
   const int t = threadIdx.x, dl = t % LPP, pg = t / LPP;
@@ -304,54 +304,45 @@ __global__ __launch_bounds__(256) void attn_batch_join_kernel(AttnBatch a) {
   const int g0 = share_of(f0, nw, n_units), n = share_of(f0 + nu - 1, nw, n_units) - g0 + 1;
   if (n == 1) return;                              // written whole
   auto part = [&](int i) { return (int64_t)(2 * (g0 + i) + (i == 0)) * a.group + c; };
-  float mx = -INFINITY;
-  float2 ml[kAttnBatchWgs / 256];
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = pg; i0 < n; i0 += AHEAD * NG) {
+    float2 ml[AHEAD];
+    f32x4 v[AHEAD];
 #pragma unroll
-  for (int k = 0; k < kAttnBatchWgs / 256; ++k) {
-    ml[k] = make_float2(-INFINITY, 0.f);
-    if (t + 256 * k < n) ml[k] = a.ml[part(t + 256 * k)];
-    mx = fmaxf(mx, ml[k].x);
+    for (int k = 0; k < AHEAD; ++k) {
+      const int64_t at = part(min(i0 + k * NG, n - 1));
+      ml[k] = a.ml[at];
+      v[k] = *reinterpret_cast<const f32x4*>(a.part + at * HD + dl * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (i0 + k * NG >= n || ml[k].x == -INFINITY) continue;      // no key seen
+      const float top = fmaxf(m, ml[k].x), old = m == top ? 1.f : exp2_hw(m - top), wt = exp2_hw(ml[k].x - top);
+      m = top;
+      l = l * old + wt * ml[k].y;
+      acc = acc * old + v[k] * wt;
+    }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  if ((t & 63) == 0) s_red[t >> 6] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-  float den = 0.f;
-#pragma unroll
-  for (int k = 0; k < kAttnBatchWgs / 256; ++k) {
-    const float wt = ml[k].x == -INFINITY ? 0.f : exp2_hw(ml[k].x - mx);
-    if (t + 256 * k < n) s_w[t + 256 * k] = wt;
-    den += wt * ml[k].y;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
-  if ((t & 63) == 0) s_red[4 + (t >> 6)] = den;
-  __syncthreads();
-  den = s_red[4] + s_red[5] + s_red[6] + s_red[7];
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = pg; i < n; i += NG) {
-    const float4 v = *reinterpret_cast<const float4*>(a.part + part(i) * HD + dl * 4);
-    const float wt = s_w[i];
-    acc.x = __builtin_fmaf(wt, v.x, acc.x);
-    acc.y = __builtin_fmaf(wt, v.y, acc.y);
-    acc.z = __builtin_fmaf(wt, v.z, acc.z);
-    acc.w = __builtin_fmaf(wt, v.w, acc.w);
+  if (dl == 0) {
+    s_m[pg] = m;
+    s_l[pg] = l;
   }
   s_acc[pg][dl] = acc;
   __syncthreads();
   if (pg == 0) {
+    float top = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int i = 1; i < NG; ++i) {
-      const float4 v = s_acc[i][dl];
-      acc.x += v.x;
-      acc.y += v.y;
-      acc.z += v.z;
-      acc.w += v.w;
+    for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[i]);
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const float wt = s_m[i] == -INFINITY ? 0.f : exp2_hw(s_m[i] - top);
+      den += wt * s_l[i];
+      acc += s_acc[i][dl] * wt;
     }
-    const float inv = mx == -INFINITY ? 0.f : 1.0f / den;
-    *out = f16x4{(_Float16)(acc.x * inv), (_Float16)(acc.y * inv), (_Float16)(acc.z * inv), (_Float16)(acc.w * inv)};
+    const float inv = top == -INFINITY ? 0.f : 1.0f / den;
+    *out = f16x4{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv), (_Float16)(acc[3] * inv)};
   }
 }
 
