@@ -159,26 +159,29 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // k at a time, as whole 128-byte lines that are read once per workgroup (with
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
 // wave's own copy of A, the L2's answers bound it: 24.7 us for 4099 rows of
-// 4096 by 64 ranks); three tiles are in flight while one is multiplied.  Wave
-// w has rows 16 w .. 16 w + 15.
+// 4096 by 64 ranks); two tiles are in flight while one is multiplied.  Wave
+// w has rows 16 w .. 16 w + 15.  Of a tile's adapters blockIdx.z takes every
+// second one: the tiles where one request ends and the next begins would
+// otherwise take twice as long as the others, and the launch with them.
 template <int NR>
 __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
-  constexpr int RP = 16 * NR, KT = 64, PITCH = KT + 8, DEPTH = 3;
+  constexpr int RP = 16 * NR, KT = 64, PITCH = KT + 8, DEPTH = 2;
   constexpr int NXL = kStageRows * 8 / 256, NAL = (RP * 8 + 255) / 256;   // 16-byte pieces a thread
   __shared__ __attribute__((aligned(16))) _Float16 s_x[2][kStageRows][PITCH];
   __shared__ __attribute__((aligned(16))) _Float16 s_a[2][RP][PITCH];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, lg = lane >> 4;
-  const int r0 = blockIdx.x * kStageRows, n = min(kStageRows, p.m - r0);
-  const int tiles = (p.k + KT - 1) / KT, ns = gridDim.y;
-  const int t0 = (int)((int64_t)blockIdx.y * tiles / ns), nt = (int)((int64_t)(blockIdx.y + 1) * tiles / ns) - t0;
-  float* t = p.t + (int64_t)blockIdx.y * p.m * RP;
+  const int r0 = blockIdx.y * kStageRows, n = min(kStageRows, p.m - r0);
+  const int tiles = (p.k + KT - 1) / KT, ns = gridDim.x;
+  const int t0 = (int)((int64_t)blockIdx.x * tiles / ns), nt = (int)((int64_t)(blockIdx.x + 1) * tiles / ns) - t0;
+  float* t = p.t + (int64_t)blockIdx.x * p.m * RP;
   const int mine = lane < n ? p.adapter[r0 + lane] : -1;
   uint64_t todo = __ballot(has_adapter(p, mine));
-  while (todo) {
+  for (int nth = 0; todo; ++nth) {
     const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
     const uint64_t members = __ballot(mine == a);
     todo &= ~members;
+    if ((nth & 1) != (int)blockIdx.z) continue;
     const int rank = rank_of(p, a);
     const int seg = (tid & 7) * 8;
     const _Float16 *xp[NXL], *ap[NAL];
@@ -452,7 +455,7 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
     hipLaunchKernelGGL((lora_expand_kernel<NR, true>), grid, dim3(256), 0, s, p);
   } else {
     const int stages = (p.m - 1) / kStageRows + 1;
-    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(stages, p.n_split), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, stages, 2), dim3(256), 0, s, p);
     hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((unsigned)(((int64_t)p.m * 4 * NR + 255) / 256)), dim3(256), 0, s, p);
     hipLaunchKernelGGL((lora_expand_kernel<NR, false>), grid, dim3(256), 0, s, p);
   }
@@ -465,7 +468,8 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
 static int lora_row_blocks(int m) { return m <= kGatherRows ? m : (m - 1) / kTileRows + 1; }
 
 bool lora_fits(int m, int n) {
-  return ((int64_t)lora_row_blocks(m) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31);
+  return (m <= kGatherRows || (m - 1) / kStageRows < 65535) &&
+         ((int64_t)lora_row_blocks(m) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31);
 }
 
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
