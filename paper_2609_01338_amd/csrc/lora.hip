@@ -37,6 +37,7 @@ constexpr int kGatherRows = 512;     // rows up to which the adapter list is sea
 constexpr int kTileRows = 32;       // rows of a tile of the second product
 constexpr int kStageRows = 64;      // and of the first, with 64 of k at a time
 constexpr int kColsWg = 256;         // columns of a workgroup of the second product: 64 a wave
+constexpr int kColsFused = 128;      // the same where one launch does both: 32 a wave
 
 __device__ __forceinline__ bool has_adapter(const Lora& p, int a) { return (unsigned)a < (unsigned)p.n_adapters; }
 
@@ -111,25 +112,16 @@ __device__ __forceinline__ void shrink_steps(int k_all, const _Float16* xr, cons
   }
 }
 
-// Few rows: t [split][m][16 NR] of the K range of split blockIdx.y for the
-// group that begins at row blockIdx.x.  The four waves take a quarter of the
-// range each and join through LDS.
+// x A^T of the group's n rows over the steps s0 .. s1 - 1: a quarter of them
+// for each of the four waves, joined through LDS; wave w then has the rank
+// tiles w, w + 4, ... in v, element e of lane l being row 4 (l / 16) + e,
+// rank l % 16 of the tile.
 template <int NR>
-__global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
-  constexpr int RP = 16 * NR;
-  __shared__ int s_rows[16];
-  __shared__ f32x4 s_acc[4][NR][64];
-  const int r = blockIdx.x, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
-  if (!has_adapter(p, a)) return;
-  const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
-  if (n == 0) return;
-  __syncthreads();
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, lg = lane >> 4;
-  const int steps = (p.k + 31) / 32, ns = gridDim.y;
-  const int s0 = (int)((int64_t)blockIdx.y * steps / ns), s1 = (int)((int64_t)(blockIdx.y + 1) * steps / ns);
+__device__ __forceinline__ void shrink_group(const Lora& p, int a, int rank, int n, const int* s_rows, int s0, int s1,
+                                             f32x4 (&s_acc)[4][NR][64], f32x4 (&v)[(NR + 3) / 4]) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15;
   const int q0 = s0 + (s1 - s0) * w / 4, q1 = s0 + (s1 - s0) * (w + 1) / 4;
-  const int rank = rank_of(p, a), n_rt = (rank + 15) / 16;
+  const int n_rt = (rank + 15) / 16;
   const _Float16 *ar[NR], *xr = p.x + (int64_t)s_rows[min(col, n - 1)] * p.k;
   f32x4 acc[NR];
 #pragma unroll
@@ -145,13 +137,38 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 #pragma unroll
   for (int j = 0; j < NR; ++j) s_acc[w][j][lane] = acc[j];
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < (NR + 3) / 4; ++i) {
+    const int j = min(w + 4 * i, NR - 1);
+    v[i] = s_acc[0][j][lane] + s_acc[1][j][lane] + s_acc[2][j][lane] + s_acc[3][j][lane];
+  }
+}
+
+// Few rows: t [split][m][16 NR] of the K range of split blockIdx.y for the
+// group that begins at row blockIdx.x.
+template <int NR>
+__global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
+  constexpr int RP = 16 * NR;
+  __shared__ int s_rows[16];
+  __shared__ f32x4 s_acc[4][NR][64];
+  const int r = blockIdx.x, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
+  if (!has_adapter(p, a)) return;
+  const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
+  if (n == 0) return;
+  __syncthreads();
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, lg = lane >> 4, rank = rank_of(p, a);
+  const int steps = (p.k + 31) / 32, ns = gridDim.y;
+  const int s0 = (int)((int64_t)blockIdx.y * steps / ns), s1 = (int)((int64_t)(blockIdx.y + 1) * steps / ns);
+  f32x4 v[(NR + 3) / 4];
+  shrink_group<NR>(p, a, rank, n, s_rows, s0, s1, s_acc, v);
   float* t = p.t + (int64_t)blockIdx.y * p.m * RP;
-  // element e of lane l is row 4 (l / 16) + e, rank l % 16
-  for (int j = w; j < NR; j += 4) {
-    const f32x4 v = s_acc[0][j][lane] + s_acc[1][j][lane] + s_acc[2][j][lane] + s_acc[3][j][lane];
+#pragma unroll
+  for (int i = 0; i < (NR + 3) / 4; ++i) {
+    const int k = (w + 4 * i) * 16 + col;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (lg * 4 + e < n) t[(int64_t)s_rows[lg * 4 + e] * RP + j * 16 + col] = j * 16 + col < rank ? v[e] : 0.f;
+      if (k < RP && lg * 4 + e < n) t[(int64_t)s_rows[lg * 4 + e] * RP + k] = k < rank ? v[i][e] : 0.f;
   }
 }
 
@@ -245,21 +262,27 @@ __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
   }
 }
 
-// Four ranks j .. j + 3 of row r: the splits of t added in order, times the
-// row's scale, in two f16 halves after the row's largest was brought to 2^14;
-// unit: what undoes that.  The LPR lanes of a row are neighbours, a power of
-// two of them, and run this together.
+// Ranks j .. j + 3 of row r's t: the splits added in order, times the row's
+// scale.
 template <int NR>
-__device__ __forceinline__ void t_halves(const Lora& p, int r, int j, f16x4& hi, f16x4& lo, float& unit) {
-  constexpr int RP = 16 * NR, LPR = RP / 4;
+__device__ __forceinline__ f32x4 t_sum(const Lora& p, int r, int j) {
   const int a = p.adapter[r];
   f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
   if (has_adapter(p, a)) {
-    const float* t = p.t + (int64_t)r * RP + j;
+    const float* t = p.t + (int64_t)r * (16 * NR) + j;
 #pragma unroll 8
-    for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * RP);
+    for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * (16 * NR));
     if (p.scale) v *= p.scale[a];
   }
+  return v;
+}
+
+// Four ranks of a row in two f16 halves after the row's largest was brought to
+// 2^14; unit: what undoes that.  The 4 NR lanes of a row are neighbours, a
+// power of two of them, and run this together.
+template <int NR>
+__device__ __forceinline__ void t_halves(f32x4 v, f16x4& hi, f16x4& lo, float& unit) {
+  constexpr int LPR = 4 * NR;
   float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
@@ -284,7 +307,7 @@ __global__ __launch_bounds__(256) void lora_halves_kernel(Lora p) {
   if (r >= p.m) return;
   f16x4 hi, lo;
   float unit;
-  t_halves<NR>(p, r, j, hi, lo, unit);
+  t_halves<NR>(t_sum<NR>(p, r, j), hi, lo, unit);
   _Float16 *h = p.hi + (int64_t)r * W + j, *l = p.lo + (int64_t)r * W + j;
   *reinterpret_cast<f16x4*>(h) = hi;
   *reinterpret_cast<f16x4*>(l) = lo;
@@ -295,119 +318,237 @@ __global__ __launch_bounds__(256) void lora_halves_kernel(Lora p) {
   if (j == 0) p.unit[r] = unit;
 }
 
-// y of 16 NX rows x 256 columns: wave w has columns 64 w .. 64 w + 63 of the
-// range, as four tiles of 16.  The products run transposed, D[column][row], so
-// that a lane holds four neighbouring columns of one row.
-template <int NR, bool GATHER>
+// Few rows: the LDS copy of a group's halves, and its row of the output: CT
+// tiles of 16 columns from c0 for each wave.  The products run transposed,
+// D[column][row], so that a lane holds four neighbouring columns of one row.
+template <int NR>
+struct GroupHalves {
+  static constexpr int RP = 16 * NR, KS = (RP + 31) / 32, PITCH = KS * 32 + 8;
+  _Float16 hi[16][PITCH], lo[16][PITCH];
+  float unit[16];                          // what a row's d is multiplied by
+
+  // ranks j .. j + 3 of row i
+  __device__ __forceinline__ void put(int i, int j, f32x4 v) {
+    f16x4 h, l;
+    float u;
+    t_halves<NR>(v, h, l, u);
+    *reinterpret_cast<f16x4*>(&hi[i][j]) = h;
+    *reinterpret_cast<f16x4*>(&lo[i][j]) = l;
+    if (RP < KS * 32) {
+      *reinterpret_cast<f16x4*>(&hi[i][RP + j]) = f16x4{0, 0, 0, 0};
+      *reinterpret_cast<f16x4*>(&lo[i][RP + j]) = f16x4{0, 0, 0, 0};
+    }
+    if (j == 0) unit[i] = u;
+  }
+};
+
+// B of columns c0 + 16 c + l % 16, ranks 32 j + 8 (l / 16) .. + 7; ranks that
+// do not count are zero (the last eight that exist are read there).
+template <int KS, int CT>
+__device__ __forceinline__ void load_b(const Lora& p, int a, int rank, int c0, f16x8 (&b)[KS][CT]) {
+  const int lane = threadIdx.x & 63, col = lane & 15, lg = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < KS; ++j)
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      b[j][c] = *reinterpret_cast<const f16x8*>(p.b + ((int64_t)a * p.n + min(c0 + c * 16 + col, p.n - 1)) * p.R +
+                                                min(j * 32 + lg * 8, max(rank - 1, 0) & ~7));
+#pragma unroll
+  for (int j = 0; j < KS; ++j)
+    if (j * 32 + 32 > rank) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[j][c][e] = j * 32 + lg * 8 + e < rank ? b[j][c][e] : (_Float16)0.f;
+    }
+}
+
+// The base's values of one row at columns c0 + 16 c + 4 lg .. + 3, and y's.
+template <int CT>
+__device__ __forceinline__ void load_base(const Lora& p, int row, int c0, int lg, bool whole, f32x4 (&y)[CT]) {
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int at = c0 + c * 16 + lg * 4;
+    const float* b = p.base + (int64_t)row * p.y_stride + at;
+    if (whole) {
+      y[c] = *reinterpret_cast<const f32x4*>(b);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[c][e] = at + e < p.n ? b[e] : 0.f;
+    }
+  }
+}
+template <int CT>
+__device__ __forceinline__ void store_y(const Lora& p, int row, int c0, int lg, bool whole, const f32x4 (&y)[CT]) {
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int at = c0 + c * 16 + lg * 4;
+    float* o = p.y + (int64_t)row * p.y_stride + at;
+    if (whole) {
+      *reinterpret_cast<f32x4*>(o) = y[c];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (at + e < p.n) o[e] = y[c][e];
+    }
+  }
+}
+
+template <int NR, int CT>
+__device__ __forceinline__ void expand_group(const Lora& p, int a, int rank, int n, const int* s_rows,
+                                             const GroupHalves<NR>& t, int c0, f32x4 (&y)[CT]) {
+  constexpr int KS = GroupHalves<NR>::KS;
+  const int lane = threadIdx.x & 63, col = lane & 15, lg = lane >> 4;
+  f16x8 b[KS][CT];
+  load_b<KS, CT>(p, a, rank, c0, b);
+  f32x4 d[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < KS; ++j) {
+    if (j * 32 >= rank) break;
+    const f16x8 lo = *reinterpret_cast<const f16x8*>(&t.lo[col][j * 32 + lg * 8]);
+    const f16x8 hi = *reinterpret_cast<const f16x8*>(&t.hi[col][j * 32 + lg * 8]);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo, d[c], 0, 0, 0);
+      d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi, d[c], 0, 0, 0);
+    }
+  }
+  if (col >= n) return;
+  const float unit = t.unit[col];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[c][e] = __builtin_fmaf(d[c][e], unit, y[c][e]);
+  store_y<CT>(p, s_rows[col], c0, lg, c0 + 16 * CT <= p.n, y);
+}
+
+// A row without an adapter is the base's: columns c0 .. c0 + 256 - 1.
+__device__ __forceinline__ void copy_row(const Lora& p, int r, int c0, int cols) {
+  const int c = c0 + threadIdx.x;
+  if (p.y != p.base && (int)threadIdx.x < cols && c < p.n) p.y[r * p.y_stride + c] = p.base[r * p.y_stride + c];
+}
+
+// Few rows, second product: the group that begins at row `block`, 256 columns.
+// Workgroup b runs on XCD b % 8: it serves every eighth row block, whose
+// column ranges follow each other, so that t is read into one L2 and the rows
+// in flight cover whole lines of all memory channels.
+template <int NR>
 __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
-  constexpr int RP = 16 * NR, KS = (RP + 31) / 32, PITCH = KS * 32 + 8;
-  constexpr int NX = GATHER ? 1 : kTileRows / 16, ROWS = 16 * NX;
   __shared__ int s_rows[16];
-  __shared__ __attribute__((aligned(16))) _Float16 s_hi[GATHER ? 16 : 1][PITCH], s_lo[GATHER ? 16 : 1][PITCH];
-  __shared__ float s_unit[16];           // what a row's d is multiplied by
+  __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cols = (p.n + kColsWg - 1) / kColsWg, rest = blockIdx.x >> 3;
+  const int r = rest / cols * 8 + (blockIdx.x & 7), c_wg = rest % cols * kColsWg, c0 = c_wg + w * 64;
+  if (r >= p.m) return;
+  const int a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
+  if (!has_adapter(p, a)) {
+    copy_row(p, r, c_wg, kColsWg);
+    return;
+  }
+  const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
+  if (n == 0) return;
+  __syncthreads();
+  f32x4 y[4];                              // goes out first, needed last
+  load_base<4>(p, s_rows[min(lane & 15, n - 1)], c0, lane >> 4, c0 + 64 <= p.n, y);
+  for (int idx = threadIdx.x; idx < n * 4 * NR; idx += 256) {
+    const int i = idx / (4 * NR), j = idx % (4 * NR) * 4;
+    s_t.put(i, j, t_sum<NR>(p, s_rows[i], j));
+  }
+  __syncthreads();
+  if (c0 < p.n) expand_group<NR, 4>(p, a, rank_of(p, a), n, s_rows, s_t, c0, y);
+}
+
+// Very few rows: both products in one launch.  Every workgroup of a group's
+// column ranges forms t for itself, reading A again (from the L2): dearer
+// than a second launch where A is long or the ranges are many, so lora_fused
+// bounds both.
+template <int NR>
+__global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
+  constexpr int RP = 16 * NR, CT = kColsFused / 64;
+  __shared__ int s_rows[16];
+  __shared__ f32x4 s_acc[4][NR][64];
+  __shared__ float s_sum[16][RP + 4];
+  __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
-  // Workgroup b runs on XCD b % 8: it serves every eighth row block, whose column ranges follow each other, so
-  // that t is read into one L2 and the rows in flight cover whole lines of all memory channels
-  const int cols = (p.n + kColsWg - 1) / kColsWg, xb = blockIdx.x & 7, rest = blockIdx.x >> 3;
-  const int block = rest / cols * 8 + xb, c_wg = rest % cols * kColsWg, c0 = c_wg + w * 64;
-  if (block >= p.row_blocks) return;
-  int n_rows, r0 = 0;
-  if constexpr (GATHER) {
-    const int r = block, a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
-    if (!has_adapter(p, a)) {            // such a row is the base's
-      const int c = c_wg + threadIdx.x;
-      if (p.y != p.base && c < p.n) p.y[r * p.y_stride + c] = p.base[r * p.y_stride + c];
-      return;
-    }
-    n_rows = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
-    if (n_rows == 0) return;
-    __syncthreads();
-  } else {
-    r0 = block * ROWS;
-    n_rows = min(ROWS, p.m - r0);
+  const int r = blockIdx.y, c_wg = blockIdx.x * kColsFused, c0 = c_wg + w * 16 * CT;
+  const int a = __builtin_amdgcn_readfirstlane(p.adapter[r]);
+  if (!has_adapter(p, a)) {
+    copy_row(p, r, c_wg, kColsFused);
+    return;
   }
-  auto row_of = [&](int i) { return GATHER ? s_rows[i] : r0 + i; };
-  // the base's values go out first; they are needed last
-  f32x4 y[NX][4];
+  const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
+  if (n == 0) return;
+  __syncthreads();
+  f32x4 y[CT];
+  load_base<CT>(p, s_rows[min(col, n - 1)], c0, lg, c0 + 16 * CT <= p.n, y);
+  const int rank = rank_of(p, a);
+  const float scale = p.scale ? p.scale[a] : 1.f;
+  f32x4 v[(NR + 3) / 4];
+  shrink_group<NR>(p, a, rank, n, s_rows, 0, (p.k + 31) / 32, s_acc, v);
+#pragma unroll
+  for (int i = 0; i < (NR + 3) / 4; ++i) {
+    const int k = (w + 4 * i) * 16 + col;
+    if (k < RP) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s_sum[lg * 4 + e][k] = k < rank ? v[i][e] * scale : 0.f;
+    }
+  }
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < n * 4 * NR; idx += 256) {
+    const int i = idx / (4 * NR), j = idx % (4 * NR) * 4;
+    s_t.put(i, j, f32x4{s_sum[i][j], s_sum[i][j + 1], s_sum[i][j + 2], s_sum[i][j + 3]});
+  }
+  __syncthreads();
+  if (c0 < p.n) expand_group<NR, CT>(p, a, rank, n, s_rows, s_t, c0, y);
+}
+
+// Many rows, second product: 32 neighbouring rows x 256 columns, 64 a wave,
+// the halves straight from memory.  Workgroups are numbered as above.
+template <int NR>
+__global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
+  constexpr int KS = GroupHalves<NR>::KS, NX = kTileRows / 16;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, lg = lane >> 4;
+  const int cols = (p.n + kColsWg - 1) / kColsWg, rest = blockIdx.x >> 3;
+  const int r0 = (rest / cols * 8 + (blockIdx.x & 7)) * kTileRows, c0 = rest % cols * kColsWg + w * 64;
+  if (r0 >= p.m || c0 >= p.n) return;
+  const int n = min(kTileRows, p.m - r0);
+  const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
+  f32x4 y[NX][4];                          // goes out first, needed last
+  f16x8 hi[NX][KS], lo[NX][KS];
+  float unit[NX];
   int rows[NX], mine[NX];
 #pragma unroll
   for (int i = 0; i < NX; ++i) {
-    rows[i] = row_of(min(i * 16 + col, n_rows - 1));
+    rows[i] = r0 + min(i * 16 + col, n - 1);
     mine[i] = p.adapter[rows[i]];
+    load_base<4>(p, rows[i], c0, lg, whole, y[i]);
   }
-  const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
-#pragma unroll
-  for (int i = 0; i < NX; ++i)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int at = c0 + c * 16 + lg * 4;
-      const float* b = p.base + (int64_t)rows[i] * p.y_stride + at;
-      if (whole) {
-        y[i][c] = *reinterpret_cast<const f32x4*>(b);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][c][e] = at + e < p.n ? b[e] : 0.f;
-      }
-    }
-  constexpr int LPR = RP / 4;
-  if constexpr (GATHER) {
-    for (int idx = threadIdx.x; idx < n_rows * LPR; idx += 256) {
-      const int i = idx / LPR, j = (idx % LPR) * 4;
-      f16x4 hi, lo;
-      float unit;
-      t_halves<NR>(p, s_rows[i], j, hi, lo, unit);
-      *reinterpret_cast<f16x4*>(&s_hi[i][j]) = hi;
-      *reinterpret_cast<f16x4*>(&s_lo[i][j]) = lo;
-      if (RP < KS * 32) {
-        *reinterpret_cast<f16x4*>(&s_hi[i][RP + j]) = f16x4{0, 0, 0, 0};
-        *reinterpret_cast<f16x4*>(&s_lo[i][RP + j]) = f16x4{0, 0, 0, 0};
-      }
-      if (j == 0) s_unit[i] = unit;
-    }
-    __syncthreads();
-  }
-  if (c0 >= p.n) return;
-  // this lane's halves, ranks 32 j + 8 (l / 16) .. + 7 of its rows
-  f16x8 hi[NX][KS], lo[NX][KS];
-  float unit[NX];
 #pragma unroll
   for (int i = 0; i < NX; ++i) {
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
-      const int at = j * 32 + lg * 8;
-      hi[i][j] = *reinterpret_cast<const f16x8*>(GATHER ? &s_hi[col][at] : p.hi + (int64_t)rows[i] * (KS * 32) + at);
-      lo[i][j] = *reinterpret_cast<const f16x8*>(GATHER ? &s_lo[col][at] : p.lo + (int64_t)rows[i] * (KS * 32) + at);
+      const int64_t at = (int64_t)rows[i] * (KS * 32) + j * 32 + lg * 8;
+      hi[i][j] = *reinterpret_cast<const f16x8*>(p.hi + at);
+      lo[i][j] = *reinterpret_cast<const f16x8*>(p.lo + at);
     }
-    unit[i] = GATHER ? s_unit[min(col, n_rows - 1)] : p.unit[rows[i]];
+    unit[i] = p.unit[rows[i]];
   }
-  const int seen = GATHER ? mine[0] : (lane < n_rows ? p.adapter[r0 + lane] : -1);
-  uint64_t todo = GATHER ? 1ull : __ballot(has_adapter(p, seen));
+  const int seen = lane < n ? p.adapter[r0 + lane] : -1;
+  uint64_t todo = __ballot(has_adapter(p, seen));
   while (todo) {
     const int a = __builtin_amdgcn_readlane(seen, __builtin_ctzll(todo));
-    const uint64_t members = GATHER ? 1ull : __ballot(seen == a);
+    const uint64_t members = __ballot(seen == a);
     todo &= ~members;
     const int rank = rank_of(p, a);
-    // B of columns c0 + 16 c + l % 16, ranks 32 j + 8 (l / 16) .. + 7; past the rank the last eight that exist
-    // are read, and zeroed
     f16x8 b[KS][4];
-#pragma unroll
-    for (int j = 0; j < KS; ++j)
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        b[j][c] = *reinterpret_cast<const f16x8*>(p.b + ((int64_t)a * p.n + min(c0 + c * 16 + col, p.n - 1)) * p.R +
-                                                  min(j * 32 + lg * 8, max(rank - 1, 0) & ~7));
-#pragma unroll
-    for (int j = 0; j < KS; ++j)
-      if (j * 32 + 32 > rank) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) b[j][c][e] = j * 32 + lg * 8 + e < rank ? b[j][c][e] : (_Float16)0.f;
-      }
+    load_b<KS, 4>(p, a, rank, c0, b);
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
-      if (!GATHER && !((members >> (i * 16)) & 0xFFFF)) continue;
+      if (!((members >> (i * 16)) & 0xFFFF)) continue;
       f32x4 d[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -427,37 +568,33 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < NX; ++i) {
-    if (i * 16 + col >= n_rows || (!has_adapter(p, mine[i]) && p.y == p.base)) continue;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int at = c0 + c * 16 + lg * 4;
-      float* o = p.y + (int64_t)rows[i] * p.y_stride + at;
-      if (whole) {
-        *reinterpret_cast<f32x4*>(o) = y[i][c];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (at + e < p.n) o[e] = y[i][c][e];
-      }
-    }
-  }
+  for (int i = 0; i < NX; ++i)
+    if (i * 16 + col < n && (has_adapter(p, mine[i]) || p.y != p.base)) store_y<4>(p, rows[i], c0, lg, whole, y[i]);
 }
 
 int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
+
+// Both products in one launch: where every workgroup's A is at most 128 KB and
+// all that they read again at most 8 MB.
+bool lora_fused(const Lora& p) {
+  const int64_t a_bytes = (int64_t)p.R * p.k * 2, ranges = (p.n + kColsFused - 1) / kColsFused;
+  return p.m <= kGatherRows && a_bytes <= (128 << 10) && a_bytes * ranges * p.m <= (8 << 20);
+}
 
 template <int NR>
 void launch_lora_nr(const Lora& p, hipStream_t s) {
   const int cols = (p.n + kColsWg - 1) / kColsWg;
   const dim3 grid((unsigned)((p.row_blocks + 7) / 8 * 8 * cols));
-  if (p.m <= kGatherRows) {
+  if (lora_fused(p)) {
+    hipLaunchKernelGGL(lora_fused_kernel<NR>, dim3((p.n + kColsFused - 1) / kColsFused, p.m), dim3(256), 0, s, p);
+  } else if (p.m <= kGatherRows) {
     hipLaunchKernelGGL(lora_shrink_kernel<NR>, dim3(p.m, p.n_split), dim3(256), 0, s, p);
-    hipLaunchKernelGGL((lora_expand_kernel<NR, true>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_expand_kernel<NR>, grid, dim3(256), 0, s, p);
   } else {
     const int stages = (p.m - 1) / kStageRows + 1;
     hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, stages, 2), dim3(256), 0, s, p);
     hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((unsigned)(((int64_t)p.m * 4 * NR + 255) / 256)), dim3(256), 0, s, p);
-    hipLaunchKernelGGL((lora_expand_kernel<NR, false>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_expand_tile_kernel<NR>, grid, dim3(256), 0, s, p);
   }
 }
 
