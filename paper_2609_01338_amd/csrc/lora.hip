@@ -462,8 +462,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
 
 // Very few rows: both products in one launch.  Every workgroup of a group's
 // column ranges forms t for itself, reading A again (from the L2): dearer
-// than a second launch where A is long or the ranges are many, so lora_fused
-// bounds both.
+// than a second launch where A is long or the ranges are many (lora_fused).
 template <int NR>
 __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
   constexpr int RP = 16 * NR, CT = kColsFused / 64;
@@ -574,11 +573,15 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
 
 int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
 
-// Both products in one launch: where every workgroup's A is at most 128 KB and
-// all that they read again at most 8 MB.
+// Both products in one launch: where a workgroup's A is at most 64 KB and all
+// that the workgroups read of it at most 16 MB.  Measured in a graph, one
+// launch against two: 2048 x 2048, rank 16 (64 KB), 1 row 5.8 against 6.4 us,
+// 16 rows with an adapter each (16 MB) 6.1 against 6.7, 32 rows 9.2 against
+// 6.9; 4096 x 4096, rank 16 (128 KB), 1 row 7.9 against 6.7; 256 x 1024 (8 KB),
+// 32 rows 4.1 against 6.6.
 bool lora_fused(const Lora& p) {
   const int64_t a_bytes = (int64_t)p.R * p.k * 2, ranges = (p.n + kColsFused - 1) / kColsFused;
-  return p.m <= kGatherRows && a_bytes <= (128 << 10) && a_bytes * ranges * p.m <= (8 << 20);
+  return p.m <= kGatherRows && a_bytes <= (64 << 10) && a_bytes * ranges * p.m <= (16 << 20);
 }
 
 template <int NR>
