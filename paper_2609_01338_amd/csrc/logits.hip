@@ -140,17 +140,32 @@ __global__ __launch_bounds__(NT) void logits_rules_kernel(LogitsRules p) {
     }
     const float* pen = p.penalty + (int64_t)row * 3;
     const float rep = nh > 0 ? pen[0] : 1.f, freq = nh > 0 ? pen[1] : 0.f, pres = nh > 0 ? pen[2] : 0.f;
+    // most waves hold no token of a list: what there is to do for one is left out whole
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i)
+    for (int i = 0; i < GROUPS; ++i) {
+      int c[VEC], last[VEC], any = 0, some = 0;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const int t = at(i) + e - v0, c = s_count[t], last = s_last[t];
-        if (c > 0) val[i][e] = penalised(val[i][e], (float)c, rep, freq, pres);
-        if (held)
-          val[i][e] += __int_as_float(last);         // -0 where there is no bias: it changes no value
-        else if (last != kNone)
-          val[i][e] += bias_value[last - 1];
+        c[e] = s_count[at(i) + e - v0];
+        last[e] = s_last[at(i) + e - v0];
+        any |= c[e];
+        some |= last[e] != kNone;
       }
+      if (__any(any)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (c[e] > 0) val[i][e] = penalised(val[i][e], (float)c[e], rep, freq, pres);
+      }
+      if (__any(some)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          if (held)
+            val[i][e] += __int_as_float(last[e]);      // -0 where there is no bias: it changes no value
+          else if (last[e] != kNone)
+            val[i][e] += bias_value[last[e] - 1];
+        }
+      }
+    }
   }
   float bv = -INFINITY;
   int bi = 0x7fffffff;
