@@ -703,10 +703,10 @@ int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int
  * device int32 [m], in any order; a row whose entry is outside
  * 0..n_adapters-1 has none: its y is the base's (in place it is not
  * touched).  Rows do not affect each other.  Nothing is rounded to f16 on the
- * way: x A^T and its product with B are fp32.  k a multiple of 8, max_rank a
- * multiple of 8 in 8..128, y_stride a multiple of 4, m may be 0.  workspace:
- * device, caller-owned, at least mz_lora_workspace_bytes(m, k, max_rank)
- * bytes, any content, not shared by calls in flight together (two graphs that
+ * way: x A^T keeps 22 bits and sums are fp32.  k a multiple of 8, max_rank a
+ * multiple of 8 in 8..128, n_adapters at most 2047, y_stride a multiple of 4, m
+ * may be 0.  workspace: device, caller-owned, at least
+ * mz_lora_workspace_bytes(m, k, max_rank, n_adapters) bytes, any content, not shared by calls in flight together (two graphs that
  * may run at once need two).  Results do not change from run to run.  Errors:
  * EINVAL for the above, a NULL pointer, pointers off 16-byte boundaries, or a
  * short workspace. */
@@ -716,7 +716,7 @@ mz_status mz_lora_add(const void *x_f16, int32_t m, int32_t k, const int32_t *ad
                       int64_t y_stride, void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Workspace bytes of mz_lora_add (-1 for invalid arguments). */
-int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank);
+int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank, int32_t n_adapters);
 
 /* Rules on m rows of logits; a zeroed struct means none of them. */
 typedef struct {

@@ -12,15 +12,16 @@
 // products run at an eighth of the time of the fp32 matrix instructions.
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
-//  - Few rows (up to kGatherRows, any order): a workgroup per (group of up to
-//    16 rows of one adapter, K split or column range), found by each
-//    workgroup from the adapter list: row r begins a group when the rows
-//    before it with its adapter fill whole groups.  Each adapter is read once
-//    per 16 of its rows, however the rows are mixed.
-//  - Many rows: the first product in tiles of 64 neighbouring rows staged
-//    through LDS, a third launch that makes the halves of t once, the second
-//    product in tiles of 32; a tile with several adapters runs once for each
-//    of them and keeps each row's own result.
+//  - Few rows (up to kGatherRows): a workgroup per (group of up to 16 rows of
+//    one adapter, K split or column range), found by each workgroup from the
+//    adapter list: row r begins a group when the rows before it with its
+//    adapter fill whole groups.
+//  - Many rows: tiles of up to 64 rows of one adapter.  The workgroups of the
+//    first product count the adapter list and pick their tile's rows out of
+//    it, and leave the tiles to the second; between them a launch makes the
+//    halves of t once.  More than kPlanRows rows run as several such calls.
+//  Either way rows may be mixed as they like: an adapter is read once per 16
+//  (64) of its rows.
 // A row's results depend on no other row: a row is one column (or row) of an
 // MFMA operand, and what other adapters make of it is dropped, not masked by
 // zeros.
@@ -33,9 +34,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kGatherRows = 512;     // rows up to which the adapter list is searched
-constexpr int kTileRows = 32;       // rows of a tile of the second product
-constexpr int kStageRows = 64;      // and of the first, with 64 of k at a time
+constexpr int kGatherRows = 64;      // rows up to which groups are searched
+constexpr int kPlanRows = 8192;      // rows of a call whose tiles are counted: 32 entries a thread
+constexpr int kTile = 64;            // rows of a tile
 constexpr int kColsWg = 256;         // columns of a workgroup of the second product: 64 a wave
 constexpr int kColsFused = 128;      // the same where one launch does both: 32 a wave
 
@@ -72,6 +73,93 @@ __device__ __forceinline__ int gather_group(const Lora& p, int r, int a, int* ro
     seen += __popcll(mask);
   }
   return min(seen - before, 16);
+}
+
+// The rows of tile `tile`: sorted by adapter (rows without one last), each
+// adapter's rows in their order and in tiles of their own, the tiles follow
+// each other.  Gives the adapter (p.n_adapters: none), the rows (LDS, written
+// up to the count) and the count, 0 where there is no such tile.  hist: LDS,
+// p.n_adapters + 1 counts.  Every thread of 256 takes part.
+__device__ __forceinline__ int plan_tile(const Lora& p, int tile, int* hist, int* rows, int& adapter) {
+  constexpr int PER = kPlanRows / 256;
+  __shared__ int s_red[4], s_found[2];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int buckets = p.n_adapters + 1, per = (p.m + 255) / 256;     // entries a thread holds
+  const int r0 = w * per * 64;                                       // this wave's rows: r0 .. r0 + 64 per - 1
+  const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
+  int v[PER];
+#pragma unroll
+  for (int c = 0; c < PER; ++c) {
+    v[c] = -1;
+    if (c < per) {
+      const int r = r0 + c * 64 + lane, a = p.adapter[min(r, p.m - 1)];
+      v[c] = r < p.m ? (has_adapter(p, a) ? a : p.n_adapters) : -1;
+    }
+  }
+  for (int i = threadIdx.x; i < buckets; i += 256) hist[i] = 0;
+  if (threadIdx.x == 0) s_found[0] = -1;
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < PER; ++c) {
+    if (c >= per) break;
+    // one add for many lanes that agree, as in a prompt's rows; an add a lane where they are mixed
+    uint64_t todo = __ballot(v[c] >= 0);
+    while (todo) {
+      const int a = __builtin_amdgcn_readlane(v[c], __builtin_ctzll(todo));
+      const uint64_t same = __ballot(v[c] == a);
+      if (__popcll(same) < 8) {
+        if ((todo >> lane) & 1) atomicAdd(&hist[v[c]], 1);
+        break;
+      }
+      todo &= ~same;
+      if (lane == 0) atomicAdd(&hist[a], (int)__popcll(same));
+    }
+  }
+  __syncthreads();
+  int before = 0;
+  for (int b0 = 0; b0 < buckets; b0 += 256) {
+    const int b = b0 + threadIdx.x, mine = b < buckets ? (hist[b] + kTile - 1) / kTile : 0;
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(sum, o);
+      if (lane >= o) sum += u;
+    }
+    __syncthreads();
+    if (lane == 63) s_red[w] = sum;
+    __syncthreads();
+    int first = before + sum - mine;
+    for (int i = 0; i < w; ++i) first += s_red[i];
+    if (tile >= first && tile < first + mine) {
+      s_found[0] = b;
+      s_found[1] = (tile - first) * kTile;
+    }
+    before += s_red[0] + s_red[1] + s_red[2] + s_red[3];
+  }
+  __syncthreads();
+  adapter = __builtin_amdgcn_readfirstlane(s_found[0]);
+  if (adapter < 0) return 0;
+  const int begin = s_found[1];
+  int count = 0;                       // of the adapter's rows among this wave's
+#pragma unroll
+  for (int c = 0; c < PER; ++c)
+    if (c < per) count += __popcll(__ballot(v[c] == adapter));
+  __syncthreads();
+  if (lane == 0) s_red[w] = count;
+  __syncthreads();
+  int rank = 0;                        // rows of the adapter before this wave's
+  for (int i = 0; i < w; ++i) rank += s_red[i];
+#pragma unroll
+  for (int c = 0; c < PER; ++c) {
+    if (c >= per) break;
+    const uint64_t same = __ballot(v[c] == adapter);
+    const int at = rank + __popcll(same & below) - begin;
+    if (v[c] == adapter && at >= 0 && at < kTile) rows[at] = r0 + c * 64 + lane;
+    rank += __popcll(same);
+  }
+  const int n = min(s_red[0] + s_red[1] + s_red[2] + s_red[3] - begin, kTile);
+  __syncthreads();
+  return n;
 }
 
 // acc += x A^T over the 32-wide K steps s0 .. s1 - 1 of 16 rows and NT tiles
@@ -172,94 +260,92 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
   }
 }
 
-// Many rows: the same for 64 neighbouring rows.  x and A go through LDS, 64 of
-// k at a time, as whole 128-byte lines that are read once per workgroup (with
+// Many rows: the same for a tile's rows.  x and A go through LDS, 64 of k at a
+// time, as whole 128-byte lines that are read once per workgroup (with
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
-// wave's own copy of A, the L2's answers bound it: 24.7 us for 4099 rows of
-// 4096 by 64 ranks); two tiles are in flight while one is multiplied.  Wave
-// w has rows 16 w .. 16 w + 15.  Of a tile's adapters blockIdx.z takes every
-// second one: the tiles where one request ends and the next begins would
-// otherwise take twice as long as the others, and the launch with them.
+// wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4);
+// two tiles of k are in flight while one is multiplied.  Wave w has rows 16 w
+// .. 16 w + 15.  The workgroups of a K range meet on one XCD where there are
+// eight ranges, so that each L2 holds its share of A.
 template <int NR>
 __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
   constexpr int RP = 16 * NR, KT = 64, PITCH = KT + 8, DEPTH = 2;
-  constexpr int NXL = kStageRows * 8 / 256, NAL = (RP * 8 + 255) / 256;   // 16-byte pieces a thread
-  __shared__ __attribute__((aligned(16))) _Float16 s_x[2][kStageRows][PITCH];
+  constexpr int NXL = kTile * 8 / 256, NAL = (RP * 8 + 255) / 256;   // 16-byte pieces a thread
+  __shared__ __attribute__((aligned(16))) _Float16 s_x[2][kTile][PITCH];
   __shared__ __attribute__((aligned(16))) _Float16 s_a[2][RP][PITCH];
+  __shared__ int s_rows[kTile];
+  extern __shared__ int s_hist[];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, lg = lane >> 4;
-  const int r0 = blockIdx.y * kStageRows, n = min(kStageRows, p.m - r0);
+  int a;
+  const int n = plan_tile(p, blockIdx.y, s_hist, s_rows, a);
+  if (blockIdx.x == 0) {                 // the tile, for the second product
+    if (tid == 0) p.tile_adapter[blockIdx.y] = n ? a : -1;
+    if (tid < kTile) p.tile_rows[blockIdx.y * kTile + tid] = tid < n ? s_rows[tid] : -1;
+  }
+  if (n == 0 || a == p.n_adapters) return;
   const int tiles = (p.k + KT - 1) / KT, ns = gridDim.x;
   const int t0 = (int)((int64_t)blockIdx.x * tiles / ns), nt = (int)((int64_t)(blockIdx.x + 1) * tiles / ns) - t0;
   float* t = p.t + (int64_t)blockIdx.x * p.m * RP;
-  const int mine = lane < n ? p.adapter[r0 + lane] : -1;
-  uint64_t todo = __ballot(has_adapter(p, mine));
-  for (int nth = 0; todo; ++nth) {
-    const int a = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
-    const uint64_t members = __ballot(mine == a);
-    todo &= ~members;
-    if ((nth & 1) != (int)blockIdx.z) continue;
-    const int rank = rank_of(p, a);
-    const int seg = (tid & 7) * 8;
-    const _Float16 *xp[NXL], *ap[NAL];
+  const int rank = rank_of(p, a);
+  const int seg = (tid & 7) * 8;
+  const _Float16 *xp[NXL], *ap[NAL];
 #pragma unroll
-    for (int e = 0; e < NXL; ++e) xp[e] = p.x + (int64_t)(r0 + min((tid >> 3) + 32 * e, n - 1)) * p.k + seg;
+  for (int e = 0; e < NXL; ++e) xp[e] = p.x + (int64_t)s_rows[min((tid >> 3) + 32 * e, n - 1)] * p.k + seg;
 #pragma unroll
-    for (int e = 0; e < NAL; ++e)
-      ap[e] = p.a + ((int64_t)a * p.R + max(min((tid >> 3) + 32 * e, rank - 1), 0)) * p.k + seg;
-    f16x8 xr[DEPTH][NXL], ar[DEPTH][NAL];
-    auto load = [&](int i, int tile) {
-      const int k = (t0 + tile) * KT;
-      const bool in = k + seg < p.k;         // k is a multiple of 8
+  for (int e = 0; e < NAL; ++e)
+    ap[e] = p.a + ((int64_t)a * p.R + max(min((tid >> 3) + 32 * e, rank - 1), 0)) * p.k + seg;
+  f16x8 xr[DEPTH][NXL], ar[DEPTH][NAL];
+  auto load = [&](int i, int tile) {
+    const int k = (t0 + tile) * KT;
+    const bool in = k + seg < p.k;         // k is a multiple of 8
 #pragma unroll
-      for (int e = 0; e < NXL; ++e) {
-        xr[i][e] = *reinterpret_cast<const f16x8*>(xp[e] + (in ? k : -seg));
-        if (!in) xr[i][e] = f16x8{};
-      }
+    for (int e = 0; e < NXL; ++e) {
+      xr[i][e] = *reinterpret_cast<const f16x8*>(xp[e] + (in ? k : -seg));
+      if (!in) xr[i][e] = f16x8{};
+    }
 #pragma unroll
-      for (int e = 0; e < NAL; ++e) {
-        ar[i][e] = *reinterpret_cast<const f16x8*>(ap[e] + (in ? k : -seg));
-        if (!in) ar[i][e] = f16x8{};
-      }
-    };
-    f32x4 acc[NR];
+    for (int e = 0; e < NAL; ++e) {
+      ar[i][e] = *reinterpret_cast<const f16x8*>(ap[e] + (in ? k : -seg));
+      if (!in) ar[i][e] = f16x8{};
+    }
+  };
+  f32x4 acc[NR];
 #pragma unroll
-    for (int j = 0; j < NR; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < NR; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < DEPTH; ++i) load(i, min(i, nt - 1));
-    for (int tb = 0; tb < nt; tb += DEPTH) {
+  for (int i = 0; i < DEPTH; ++i) load(i, min(i, nt - 1));
+  for (int tb = 0; tb < nt; tb += DEPTH) {
 #pragma unroll
-      for (int i = 0; i < DEPTH; ++i) {
-        const int tile = tb + i, buf = tile & 1;
-        if (tile >= nt) break;
+    for (int i = 0; i < DEPTH; ++i) {
+      const int tile = tb + i, buf = tile & 1;
+      if (tile >= nt) break;
 #pragma unroll
-        for (int e = 0; e < NXL; ++e) *reinterpret_cast<f16x8*>(&s_x[buf][(tid >> 3) + 32 * e][seg]) = xr[i][e];
+      for (int e = 0; e < NXL; ++e) *reinterpret_cast<f16x8*>(&s_x[buf][(tid >> 3) + 32 * e][seg]) = xr[i][e];
 #pragma unroll
-        for (int e = 0; e < NAL; ++e)
-          if ((tid >> 3) + 32 * e < RP) *reinterpret_cast<f16x8*>(&s_a[buf][(tid >> 3) + 32 * e][seg]) = ar[i][e];
-        load(i, min(tile + DEPTH, nt - 1));
-        __syncthreads();     // the buffer before last was read before the previous tile's barrier
+      for (int e = 0; e < NAL; ++e)
+        if ((tid >> 3) + 32 * e < RP) *reinterpret_cast<f16x8*>(&s_a[buf][(tid >> 3) + 32 * e][seg]) = ar[i][e];
+      load(i, min(tile + DEPTH, nt - 1));
+      __syncthreads();     // the buffer before last was read before the previous tile's barrier
 #pragma unroll
-        for (int ks = 0; ks < KT / 32; ++ks) {
-          const f16x8 xv = *reinterpret_cast<const f16x8*>(&s_x[buf][w * 16 + col][ks * 32 + lg * 8]);
+      for (int ks = 0; ks < KT / 32; ++ks) {
+        const f16x8 xv = *reinterpret_cast<const f16x8*>(&s_x[buf][w * 16 + col][ks * 32 + lg * 8]);
 #pragma unroll
-          for (int j = 0; j < NR; ++j) {
-            if (j * 16 >= rank) break;
-            const f16x8 av = *reinterpret_cast<const f16x8*>(&s_a[buf][j * 16 + col][ks * 32 + lg * 8]);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av, acc[j], 0, 0, 0);
-          }
+        for (int j = 0; j < NR; ++j) {
+          if (j * 16 >= rank) break;
+          const f16x8 av = *reinterpret_cast<const f16x8*>(&s_a[buf][j * 16 + col][ks * 32 + lg * 8]);
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av, acc[j], 0, 0, 0);
         }
       }
     }
-#pragma unroll
-    for (int j = 0; j < NR; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int at = w * 16 + lg * 4 + e;
-        if ((members >> at) & 1) t[(int64_t)(r0 + at) * RP + j * 16 + col] = j * 16 + col < rank ? acc[j][e] : 0.f;
-      }
-    __syncthreads();         // before the next adapter's first tile
   }
+#pragma unroll
+  for (int j = 0; j < NR; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = w * 16 + lg * 4 + e;
+      if (at < n) t[(int64_t)s_rows[at] * RP + j * 16 + col] = j * 16 + col < rank ? acc[j][e] : 0.f;
+    }
 }
 
 // Ranks j .. j + 3 of row r's t: the splits added in order, times the row's
@@ -504,50 +590,50 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
   if (c0 < p.n) expand_group<NR, CT>(p, a, rank, n, s_rows, s_t, c0, y);
 }
 
-// Many rows, second product: 32 neighbouring rows x 256 columns, 64 a wave,
-// the halves straight from memory.  Workgroups are numbered as above.
+// Many rows, second product: half a tile's rows x 256 columns, 64 a wave, the
+// halves straight from memory.  Workgroups are numbered as above.
 template <int NR>
 __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
-  constexpr int KS = GroupHalves<NR>::KS, NX = kTileRows / 16;
+  constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int cols = (p.n + kColsWg - 1) / kColsWg, rest = blockIdx.x >> 3;
-  const int r0 = (rest / cols * 8 + (blockIdx.x & 7)) * kTileRows, c0 = rest % cols * kColsWg + w * 64;
-  if (r0 >= p.m || c0 >= p.n) return;
-  const int n = min(kTileRows, p.m - r0);
+  const int block = rest / cols * 8 + (blockIdx.x & 7), c0 = rest % cols * kColsWg + w * 64;
+  if (block >= 2 * p.tiles || c0 >= p.n) return;
+  const int a = __builtin_amdgcn_readfirstlane(p.tile_adapter[block / 2]);
+  const bool with = has_adapter(p, a);
+  if (a < 0 || (!with && p.y == p.base)) return;
+  int rows[NX];
+  bool in[NX];
+#pragma unroll
+  for (int i = 0; i < NX; ++i) rows[i] = p.tile_rows[block * ROWS + i * 16 + col];
+  if (__builtin_amdgcn_readfirstlane(rows[0]) < 0) return;       // a tile's rows fill it from the front
   const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
+  const int first = __builtin_amdgcn_readfirstlane(rows[0]);
   f32x4 y[NX][4];                          // goes out first, needed last
-  f16x8 hi[NX][KS], lo[NX][KS];
-  float unit[NX];
-  int rows[NX], mine[NX];
 #pragma unroll
   for (int i = 0; i < NX; ++i) {
-    rows[i] = r0 + min(i * 16 + col, n - 1);
-    mine[i] = p.adapter[rows[i]];
+    in[i] = rows[i] >= 0;
+    if (!in[i]) rows[i] = first;           // loads of a row that exists stand in
     load_base<4>(p, rows[i], c0, lg, whole, y[i]);
   }
+  if (with) {
+    f16x8 hi[NX][KS], lo[NX][KS], b[KS][4];
+    float unit[NX];
 #pragma unroll
-  for (int i = 0; i < NX; ++i) {
+    for (int i = 0; i < NX; ++i) {
 #pragma unroll
-    for (int j = 0; j < KS; ++j) {
-      const int64_t at = (int64_t)rows[i] * (KS * 32) + j * 32 + lg * 8;
-      hi[i][j] = *reinterpret_cast<const f16x8*>(p.hi + at);
-      lo[i][j] = *reinterpret_cast<const f16x8*>(p.lo + at);
+      for (int j = 0; j < KS; ++j) {
+        const int64_t at = (int64_t)rows[i] * (KS * 32) + j * 32 + lg * 8;
+        hi[i][j] = *reinterpret_cast<const f16x8*>(p.hi + at);
+        lo[i][j] = *reinterpret_cast<const f16x8*>(p.lo + at);
+      }
+      unit[i] = p.unit[rows[i]];
     }
-    unit[i] = p.unit[rows[i]];
-  }
-  const int seen = lane < n ? p.adapter[r0 + lane] : -1;
-  uint64_t todo = __ballot(has_adapter(p, seen));
-  while (todo) {
-    const int a = __builtin_amdgcn_readlane(seen, __builtin_ctzll(todo));
-    const uint64_t members = __ballot(seen == a);
-    todo &= ~members;
     const int rank = rank_of(p, a);
-    f16x8 b[KS][4];
     load_b<KS, 4>(p, a, rank, c0, b);
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
-      if (!((members >> (i * 16)) & 0xFFFF)) continue;
       f32x4 d[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -563,12 +649,12 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][c][e] = mine[i] == a ? __builtin_fmaf(d[c][e], unit[i], y[i][c][e]) : y[i][c][e];
+        for (int e = 0; e < 4; ++e) y[i][c][e] = __builtin_fmaf(d[c][e], unit[i], y[i][c][e]);
     }
   }
 #pragma unroll
   for (int i = 0; i < NX; ++i)
-    if (i * 16 + col < n && (has_adapter(p, mine[i]) || p.y != p.base)) store_y<4>(p, rows[i], c0, lg, whole, y[i]);
+    if (in[i]) store_y<4>(p, rows[i], c0, lg, whole, y[i]);
 }
 
 int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
@@ -587,59 +673,93 @@ bool lora_fused(const Lora& p) {
 template <int NR>
 void launch_lora_nr(const Lora& p, hipStream_t s) {
   const int cols = (p.n + kColsWg - 1) / kColsWg;
-  const dim3 grid((unsigned)((p.row_blocks + 7) / 8 * 8 * cols));
+  auto grid = [&](int blocks) { return dim3((unsigned)((blocks + 7) / 8 * 8 * cols)); };
   if (lora_fused(p)) {
     hipLaunchKernelGGL(lora_fused_kernel<NR>, dim3((p.n + kColsFused - 1) / kColsFused, p.m), dim3(256), 0, s, p);
   } else if (p.m <= kGatherRows) {
     hipLaunchKernelGGL(lora_shrink_kernel<NR>, dim3(p.m, p.n_split), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(lora_expand_kernel<NR>, grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_expand_kernel<NR>, grid(p.m), dim3(256), 0, s, p);
   } else {
-    const int stages = (p.m - 1) / kStageRows + 1;
-    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, stages, 2), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((unsigned)(((int64_t)p.m * 4 * NR + 255) / 256)), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(lora_expand_tile_kernel<NR>, grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, p.tiles), dim3(256), (p.n_adapters + 1) * 4, s, p);
+    hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((p.m * 4 * NR + 255) / 256), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_expand_tile_kernel<NR>, grid(2 * p.tiles), dim3(256), 0, s, p);
   }
 }
 
-}  // namespace
-
-// Groups of rows that workgroups are numbered by: every row where groups are
-// searched, else tiles.
-static int lora_row_blocks(int m) { return m <= kGatherRows ? m : (m - 1) / kTileRows + 1; }
-
-bool lora_fits(int m, int n) {
-  return (m <= kGatherRows || (m - 1) / kStageRows < 65535) &&
-         ((int64_t)lora_row_blocks(m) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31);
-}
+// Tiles that rows of at most so many adapters (and of none) can make.
+int most_tiles(int m, int n_adapters) { return m / kTile + (n_adapters + 1 < m ? n_adapters + 1 : m); }
 
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
 int lora_splits(int m, int k) {
-  const int groups = m <= kGatherRows ? m : (m - 1) / kStageRows + 1;
+  const int groups = m <= kGatherRows ? m : (m - 1) / kTile + 1;
   const int want = (m <= kGatherRows ? 1024 : 520) / groups, most = (k + 31) / 32 / 8;
   const int ns = want < most ? want : most;
   return ns < 1 ? 1 : ns > 16 ? 16 : ns;
 }
 
-static int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
-static int64_t t_bytes(int m, int k, int R) { return (int64_t)lora_splits(m, k) * m * rank_tiles(R) * 16 * 4; }
-static int64_t half_bytes(int m, int R) { return (int64_t)m * ((rank_tiles(R) * 16 + 31) / 32 * 32) * 2; }
+// The workspace of a call of m <= kPlanRows rows.
+struct LoraWs {
+  int64_t t, hi, lo, unit, tile_adapter, tile_rows, bytes;
+};
+LoraWs lora_ws(int m, int k, int R, int n_adapters) {
+  LoraWs w{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += (bytes + 15) / 16 * 16;
+    return here;
+  };
+  const int64_t rp = rank_tiles(R) * 16, wide = (rp + 31) / 32 * 32;
+  w.t = take((int64_t)lora_splits(m, k) * m * rp * 4);
+  if (m > kGatherRows) {
+    w.hi = take(m * wide * 2);
+    w.lo = take(m * wide * 2);
+    w.unit = take((int64_t)m * 4);
+    w.tile_adapter = take((int64_t)most_tiles(m, n_adapters) * 4);
+    w.tile_rows = take((int64_t)most_tiles(m, n_adapters) * kTile * 4);
+  }
+  w.bytes = at;
+  return w;
+}
 
-int64_t lora_ws_bytes(int m, int k, int R) {
-  return t_bytes(m, k, R) + (m > kGatherRows ? 2 * half_bytes(m, R) + up16((int64_t)m * 4) : 0);
+}  // namespace
+
+bool lora_fits(int m, int n) {
+  const int64_t most = m < kPlanRows ? m : kPlanRows;
+  return (2 * (most / kTile + most) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31) && n < (1 << 30);
+}
+
+int64_t lora_ws_bytes(int m, int k, int R, int n_adapters) {
+  if (m <= kPlanRows) return lora_ws(m, k, R, n_adapters).bytes;
+  const int64_t whole = lora_ws(kPlanRows, k, R, n_adapters).bytes, rest = m % kPlanRows ? lora_ws(m % kPlanRows, k, R, n_adapters).bytes : 0;
+  return whole > rest ? whole : rest;
 }
 
 void launch_lora(Lora p, void* ws, hipStream_t s) {
-  p.t = reinterpret_cast<float*>(ws);
-  p.n_split = lora_splits(p.m, p.k);
-  p.row_blocks = lora_row_blocks(p.m);
-  p.hi = reinterpret_cast<_Float16*>(reinterpret_cast<uint8_t*>(ws) + t_bytes(p.m, p.k, p.R));
-  p.lo = p.hi + half_bytes(p.m, p.R) / 2;
-  p.unit = reinterpret_cast<float*>(p.lo + half_bytes(p.m, p.R) / 2);
-  switch (rank_tiles(p.R)) {
-    case 1: launch_lora_nr<1>(p, s); break;
-    case 2: launch_lora_nr<2>(p, s); break;
-    case 4: launch_lora_nr<4>(p, s); break;
-    default: launch_lora_nr<8>(p, s); break;
+  const int rows = p.m;
+  for (int r = 0; r < rows; r += kPlanRows) {
+    Lora q = p;
+    q.m = rows - r < kPlanRows ? rows - r : kPlanRows;
+    q.x += (int64_t)r * q.k;
+    q.adapter += r;
+    q.base += r * q.y_stride;
+    q.y += r * q.y_stride;
+    const LoraWs w = lora_ws(q.m, q.k, q.R, q.n_adapters);
+    uint8_t* b = reinterpret_cast<uint8_t*>(ws);
+    q.t = reinterpret_cast<float*>(b + w.t);
+    q.hi = reinterpret_cast<_Float16*>(b + w.hi);
+    q.lo = reinterpret_cast<_Float16*>(b + w.lo);
+    q.unit = reinterpret_cast<float*>(b + w.unit);
+    q.tile_adapter = reinterpret_cast<int32_t*>(b + w.tile_adapter);
+    q.tile_rows = reinterpret_cast<int32_t*>(b + w.tile_rows);
+    q.tiles = most_tiles(q.m, q.n_adapters);
+    q.n_split = lora_splits(q.m, q.k);
+    switch (rank_tiles(q.R)) {
+      case 1: launch_lora_nr<1>(q, s); break;
+      case 2: launch_lora_nr<2>(q, s); break;
+      case 4: launch_lora_nr<4>(q, s); break;
+      default: launch_lora_nr<8>(q, s); break;
+    }
   }
 }
 

@@ -196,7 +196,7 @@ void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
 
 // y = base + scale (x A^T) B^T with each row's adapter (see mz.h,
 // mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8, y_stride of 4,
-// every pointer 16-byte aligned, lora_fits(m, n).  The fields from t on are the
+// at most kLoraAdapters, every pointer 16-byte aligned, lora_fits(m, n).  The fields from t on are the
 // launcher's own, in ws (lora_ws_bytes bytes).
 struct Lora {
   const _Float16 *x, *a, *b;
@@ -208,11 +208,12 @@ struct Lora {
   float* t;          // [n_split][m][R rounded up] partials of x A^T
   _Float16 *hi, *lo; // many rows: t in two halves, and what each row of them
   float* unit;       // is multiplied by
-  int n_split;
-  int row_blocks;
+  int32_t *tile_adapter, *tile_rows;   // [tiles] (-1: not there), [tiles][64]
+  int n_split, tiles;
 };
+constexpr int kLoraAdapters = 2047;    // adapters of a call: their counts lie in LDS
 bool lora_fits(int m, int n);
-int64_t lora_ws_bytes(int m, int k, int R);
+int64_t lora_ws_bytes(int m, int k, int R, int n_adapters);
 void launch_lora(Lora p, void* ws, hipStream_t s);
 
 // Penalties, biases and masks on m rows of logits and the token of each (see

@@ -2270,9 +2270,9 @@ mz_status mz_attention_batch(const void* q, const int32_t* lens, int32_t n_seq, 
   });
 }
 
-int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank) {
-  if (m < 1 || k < 8 || max_rank < 8 || max_rank > 128) return -1;
-  return mzk::lora_ws_bytes(m, k, max_rank);
+int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank, int32_t n_adapters) {
+  if (m < 1 || k < 8 || max_rank < 8 || max_rank > 128 || n_adapters < 1 || n_adapters > mzk::kLoraAdapters) return -1;
+  return mzk::lora_ws_bytes(m, k, max_rank, n_adapters);
 }
 
 mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapter, int32_t n_adapters, const void* a,
@@ -2281,7 +2281,8 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
                       void* stream) {
   return guarded(nullptr, [&] {
     if (!x || !adapter || !a || !b || !base || !y || !workspace) fail(MZ_EINVAL, "NULL pointer");
-    if (m < 0 || n < 1 || n_adapters < 1) fail(MZ_EINVAL, "n and n_adapters must be positive, m at least 0");
+    if (m < 0 || n < 1) fail(MZ_EINVAL, "n must be positive, m at least 0");
+    if (n_adapters < 1 || n_adapters > mzk::kLoraAdapters) fail(MZ_EINVAL, "n_adapters must be 1..%d", mzk::kLoraAdapters);
     if (k < 8 || k % 8) fail(MZ_EINVAL, "k must be a positive multiple of 8");
     if (max_rank < 8 || max_rank > 128 || max_rank % 8) fail(MZ_EINVAL, "max_rank must be a multiple of 8 in 8..128");
     if (y_stride < n || y_stride % 4) fail(MZ_EINVAL, "y_stride must be a multiple of 4 and at least n");
@@ -2290,7 +2291,7 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
     check_stream(stream);
     if (m == 0) return;
     if (!mzk::lora_fits(m, n)) fail(MZ_EINVAL, "m rows of n columns are too many");
-    if (workspace_bytes < mzk::lora_ws_bytes(m, k, max_rank)) fail(MZ_EINVAL, "workspace too small");
+    if (workspace_bytes < mzk::lora_ws_bytes(m, k, max_rank, n_adapters)) fail(MZ_EINVAL, "workspace too small");
     mzk::Lora p{};
     p.x = reinterpret_cast<const _Float16*>(x);
     p.a = reinterpret_cast<const _Float16*>(a);

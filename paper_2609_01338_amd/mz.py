@@ -144,7 +144,7 @@ def lib() -> ctypes.CDLL:
         "mz_attention_batch": ([vp, vp, i32, vp, i32, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp], i32),
         "mz_attention_batch_workspace_bytes": ([i32, i32, i32, i32], i64),
         "mz_lora_add": ([vp, i32, i32, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp, i64, vp], i32),
-        "mz_lora_workspace_bytes": ([i32, i32, i32], i64),
+        "mz_lora_workspace_bytes": ([i32, i32, i32, i32], i64),
         "mz_logits_rules": ([vp, i32, i32, i64, ctypes.POINTER(mz_logits_rules_args), vp, vp, vp, i64, vp], i32),
         "mz_logits_rules_workspace_bytes": ([i32, i32], i64),
         "mz_rmsnorm": ([vp, i32, i32, ctypes.c_float, vp, vp], i32),
@@ -514,8 +514,8 @@ def mz_lora_add(x_ptr: int, m: int, k: int, adapter_ptr: int, n_adapters: int, a
                              base_ptr, y_ptr, y_stride, ws_ptr, ws_bytes, stream), None)
 
 
-def mz_lora_workspace_bytes(m: int, k: int, max_rank: int) -> int:
-    return int(lib().mz_lora_workspace_bytes(m, k, max_rank))
+def mz_lora_workspace_bytes(m: int, k: int, max_rank: int, n_adapters: int) -> int:
+    return int(lib().mz_lora_workspace_bytes(m, k, max_rank, n_adapters))
 
 
 def mz_logits_rules(logits_ptr: int, m: int, vocab: int, stride: int, out_ptr: Optional[int], token_ptr: Optional[int],

@@ -90,24 +90,28 @@ LORA = dict(x_ptr=P, m=3, k=64, adapter_ptr=P, n_adapters=2, a_ptr=P, b_ptr=P, m
 @pytest.mark.parametrize("bad,match", [
     (dict(x_ptr=0), "NULL"), (dict(adapter_ptr=0), "NULL"), (dict(a_ptr=0), "NULL"), (dict(b_ptr=0), "NULL"),
     (dict(base_ptr=0), "NULL"), (dict(y_ptr=0), "NULL"), (dict(ws_ptr=0), "NULL"),
-    (dict(m=-1), "positive"), (dict(n=0), "positive"), (dict(n_adapters=0), "positive"),
+    (dict(m=-1), "positive"), (dict(n=0), "positive"), (dict(n_adapters=0), "n_adapters"), (dict(n_adapters=2048), "n_adapters"),
     (dict(k=0), "k must"), (dict(k=60), "k must"), (dict(k=-8), "k must"),
     (dict(max_rank=0), "max_rank"), (dict(max_rank=12), "max_rank"), (dict(max_rank=136), "max_rank"),
     (dict(y_stride=96), "y_stride"), (dict(y_stride=102), "y_stride"), (dict(y_stride=-4), "y_stride"),
     (dict(x_ptr=P + 2), "16-byte"), (dict(a_ptr=P + 8), "16-byte"), (dict(b_ptr=P + 8), "16-byte"),
     (dict(base_ptr=P + 4), "16-byte"), (dict(y_ptr=P + 4), "16-byte"), (dict(ws_ptr=P + 4), "16-byte"),
-    (dict(m=1 << 30, n=1 << 30, y_stride=1 << 30), "too many"), (dict(ws_bytes=0), "workspace"), (dict(ws_bytes=-1), "workspace"),
+    (dict(m=1 << 30, n=1 << 30, y_stride=1 << 30), "too many"), (dict(n=1 << 30, y_stride=1 << 30), "too many"), (dict(ws_bytes=0), "workspace"), (dict(ws_bytes=-1), "workspace"),
 ])
 def test_lora_add_refusals(bad, match):
     refused(mz.mz_lora_add, **{**LORA, **bad}, match=match)
 
 
 def test_lora_workspace_and_no_rows():
-    need = mz.mz_lora_workspace_bytes(3, 64, 16)
+    need = mz.mz_lora_workspace_bytes(3, 64, 16, 2)
     assert need > 0
     refused(mz.mz_lora_add, **{**LORA, "ws_bytes": need - 1}, match="workspace")
-    for bad in [(0, 64, 16), (3, 4, 16), (3, 64, 4), (3, 64, 129)]:
+    for bad in [(0, 64, 16, 2), (3, 4, 16, 2), (3, 64, 4, 2), (3, 64, 129, 2), (3, 64, 16, 0), (3, 64, 16, 2048)]:
         assert mz.mz_lora_workspace_bytes(*bad) == -1
+    # rows beyond those of one pass run as several in the same workspace
+    most = max(mz.mz_lora_workspace_bytes(m, 4096, 64, 9) for m in range(1, 8193))
+    for m in (8193, 9000, 1 << 20, (1 << 30) + 77):
+        assert mz.mz_lora_workspace_bytes(8192, 4096, 64, 9) <= mz.mz_lora_workspace_bytes(m, 4096, 64, 9) <= most
     mz.mz_lora_add(**{**LORA, "m": 0, "ws_bytes": 0})
 
 

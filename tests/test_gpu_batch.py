@@ -493,7 +493,7 @@ def lora_run(x, adapter, a, b, scale, rank, base, n, in_place=False, ws=None):
     torch = torch_cuda()
     m, k = x.shape
     na, R, _ = a.shape
-    need = mz.mz_lora_workspace_bytes(m, k, R)
+    need = mz.mz_lora_workspace_bytes(m, k, R, na)
     if ws is None:
         ws = torch.full((need // 4,), float("nan"), device="cuda")
     d = [None if v is None else dev(v) for v in (x, adapter, a, b, scale, rank, base)]
@@ -562,16 +562,25 @@ def test_lora_one_adapter_for_all():
 def test_lora_no_adapters_used():
     lora_case([-1] * 5, 64, 60, 16, 2, seed=24)
     lora_case([-1] * 700, 64, 60, 16, 2, seed=25)
+    lora_case([-1] * 130 + [1] + [2] * 70, 64, 60, 16, 2, seed=25)
     lora_case([7] * 5 + [-(1 << 31), (1 << 31) - 1], 64, 60, 16, 2, seed=26)
 
 
-@pytest.mark.parametrize("m", [511, 512, 513, 576, 1025, 2000])
+@pytest.mark.parametrize("m", [64, 65, 129, 511, 512, 513, 576, 1025, 2000, 8192, 8193, 8300, 16500])
 def test_lora_runs_of_rows(m):
     """Requests one after the other: a tile may hold the end of one and the beginning of the next."""
     rng = np.random.default_rng(m)
     cuts = np.sort(rng.integers(0, m, 6))
     lora_case(np.searchsorted(cuts, np.arange(m), side="right") - 1, 320, 300, 32, 7, seed=m, stride=512)
     lora_case(rng.integers(-1, 4, m), 320, 300, 16, 4, seed=m + 1)
+
+
+@pytest.mark.parametrize("m", [65, 300, 1000])
+def test_lora_many_adapters(m):
+    """More adapters than rows, one for each row, and the most a call takes."""
+    rng = np.random.default_rng(m)
+    lora_case(rng.permutation(2 * m)[:m], 40, 20, 8, 2 * m, seed=m)
+    lora_case(rng.integers(-3, 2050, m), 16, 12, 8, 2047, seed=m + 1)
 
 
 def test_lora_without_scales_and_ranks():
@@ -609,7 +618,7 @@ def test_lora_captured_on_another_stream():
     torch = torch_cuda()
     rng = np.random.default_rng(30)
     x, adapter, a, b, scale, rank, base, n = lora_inputs([0] * 30, 256, 200, 16, 3, seed=30, ranks=[16, 9, 4])
-    need = mz.mz_lora_workspace_bytes(30, 256, 16)
+    need = mz.mz_lora_workspace_bytes(30, 256, 16, 3)
     ws = torch.full((need // 4,), float("nan"), device="cuda")
     d = [dev(v) for v in (x, adapter, a, b, scale, rank, base)]
     y = torch.zeros(base.shape, device="cuda")
@@ -636,7 +645,7 @@ def test_lora_offsets_past_32_bits():
     b = torch.zeros(na, n, R, device="cuda", dtype=torch.float16)
     x, adapter, a1, b1, scale, rank, base, _ = lora_inputs([0, 0, -1], k, n, R, 1, seed=31, ranks=[R])
     a[-1], b[-1] = dev(a1[0]), dev(b1[0])
-    need = mz.mz_lora_workspace_bytes(3, k, R)
+    need = mz.mz_lora_workspace_bytes(3, k, R, na)
     ws, y = torch.full((need // 4,), float("nan"), device="cuda"), torch.zeros(base.shape, device="cuda")
     d = [dev(v) for v in (x, np.where(adapter < 0, -1, na - 1).astype(np.int32), base)]
     mz.mz_lora_add(d[0].data_ptr(), 3, k, d[1].data_ptr(), na, a.data_ptr(), b.data_ptr(), R, n, d[2].data_ptr(),
