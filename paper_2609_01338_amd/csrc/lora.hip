@@ -75,50 +75,96 @@ __device__ __forceinline__ int gather_group(const Lora& p, int r, int a, int* ro
   return min(seen - before, 16);
 }
 
-// The rows of tile `tile`: sorted by adapter (rows without one last), each
-// adapter's rows in their order and in tiles of their own, the tiles follow
-// each other.  Gives the adapter (p.n_adapters: none), the rows (LDS, written
-// up to the count) and the count, 0 where there is no such tile.  hist: LDS,
-// p.n_adapters + 1 counts.  Every thread of 256 takes part.
-__device__ __forceinline__ int plan_tile(const Lora& p, int tile, int* hist, int* rows, int& adapter) {
-  constexpr int PER = kPlanRows / 256;
+// LDS of plan_tile: the call's adapters, where in each window of 64 rows the
+// adapter changes, how many rows each adapter has.
+struct PlanLds {
+  uint16_t list[kPlanRows];
+  uint64_t change[kPlanRows / 64];
+  int hist[kLoraAdapters + 1];
+};
+
+// Runs of one adapter, each within a window of 64 rows, that make the tiles as
+// they stand; with more of them the rows are sorted.
+__host__ __device__ inline int most_runs(int m) {
+  const int windows = (m + 63) / 64;
+  return windows + windows / 4 + 8;
+}
+
+// The rows of tile `tile`, of one adapter (p.n_adapters: none): the adapter,
+// the rows (LDS, written up to the count) and the count, 0 where there is no
+// such tile.  Where rows of one adapter follow each other (prompts), the runs
+// within windows of 64 rows are the tiles.  Else the rows are taken as sorted
+// by adapter, each adapter's in their order and in tiles of their own: counted
+// in LDS, then the tile's picked by their rank.  Every thread of 256 takes
+// part, and every workgroup comes to the same tiles.  (Loops over the list are
+// kept short: unrolled, their code took longer to fetch than to run.)
+__device__ __forceinline__ int plan_tile(const Lora& p, int tile, PlanLds& s, int* rows, int& adapter) {
   __shared__ int s_red[4], s_found[2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int buckets = p.n_adapters + 1, per = (p.m + 255) / 256;     // entries a thread holds
-  const int r0 = w * per * 64;                                       // this wave's rows: r0 .. r0 + 64 per - 1
+  const int buckets = p.n_adapters + 1, chunks = (p.m + 255) / 256;  // 64-row chunks of a wave
+  const int r0 = w * chunks * 64, r1 = min(r0 + chunks * 64, p.m);   // this wave's rows
   const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-  int v[PER];
+  constexpr int AHEAD = 8;
+#pragma unroll 1
+  for (int base = 0; base < p.m; base += 256 * AHEAD) {
+    int v[AHEAD];
 #pragma unroll
-  for (int c = 0; c < PER; ++c) {
-    v[c] = -1;
-    if (c < per) {
-      const int r = r0 + c * 64 + lane, a = p.adapter[min(r, p.m - 1)];
-      v[c] = r < p.m ? (has_adapter(p, a) ? a : p.n_adapters) : -1;
+    for (int i = 0; i < AHEAD; ++i) v[i] = p.adapter[min(base + 256 * i + (int)threadIdx.x, p.m - 1)];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int r = base + 256 * i + threadIdx.x;
+      const bool in = r < p.m;
+      const int mine = has_adapter(p, v[i]) ? v[i] : p.n_adapters, prev = __shfl_up(mine, 1);
+      if (in) s.list[r] = (uint16_t)mine;
+      const uint64_t change = __ballot(in && (lane == 0 || mine != prev));
+      if (lane == 0 && in) s.change[r / 64] = change;
     }
   }
-  for (int i = threadIdx.x; i < buckets; i += 256) hist[i] = 0;
   if (threadIdx.x == 0) s_found[0] = -1;
   __syncthreads();
+  {  // lane l: windows 2 l and 2 l + 1
+    static_assert(kPlanRows / 64 == 128, "windows of a wave's lanes");
+    const int windows = (p.m + 63) / 64;
+    const int c0 = 2 * lane < windows ? __popcll(s.change[2 * lane]) : 0;
+    const int c1 = 2 * lane + 1 < windows ? __popcll(s.change[2 * lane + 1]) : 0;
+    int sum = c0 + c1;
 #pragma unroll
-  for (int c = 0; c < PER; ++c) {
-    if (c >= per) break;
-    // one add for many lanes that agree, as in a prompt's rows; an add a lane where they are mixed
-    uint64_t todo = __ballot(v[c] >= 0);
-    while (todo) {
-      const int a = __builtin_amdgcn_readlane(v[c], __builtin_ctzll(todo));
-      const uint64_t same = __ballot(v[c] == a);
-      if (__popcll(same) < 8) {
-        if ((todo >> lane) & 1) atomicAdd(&hist[v[c]], 1);
-        break;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(sum, o);
+      if (lane >= o) sum += u;
+    }
+    const int total = __builtin_amdgcn_readlane(sum, 63);
+    if (total <= most_runs(p.m)) {
+      if (tile >= total) return 0;
+      const int first = sum - c0 - c1;
+      const int l = __builtin_ctzll(__ballot(tile < sum));         // the first window pair that ends past the tile
+      int nth = tile - __builtin_amdgcn_readlane(first, l), window = 2 * l;
+      const int in_first = __builtin_amdgcn_readlane(c0, l);
+      if (nth >= in_first) {
+        nth -= in_first;
+        ++window;
       }
-      todo &= ~same;
-      if (lane == 0) atomicAdd(&hist[a], (int)__popcll(same));
+      uint64_t change = s.change[window];
+      for (; nth > 0; --nth) change &= change - 1;
+      const int start = __builtin_ctzll(change);
+      change &= change - 1;
+      const int r = window * 64 + start, end = min(window * 64 + (change ? (int)__builtin_ctzll(change) : 64), p.m);
+      adapter = __builtin_amdgcn_readfirstlane(s.list[r]);
+      if (threadIdx.x < 64 && r + lane < end) rows[lane] = r + lane;
+      __syncthreads();
+      return end - r;
     }
   }
+  for (int i = threadIdx.x; i < buckets; i += 256) s.hist[i] = 0;
+  __syncthreads();
+#pragma unroll 2
+  for (int r = r0; r < r1; r += 64)
+    if (r + lane < r1) atomicAdd(&s.hist[s.list[r + lane]], 1);
   __syncthreads();
   int before = 0;
+#pragma unroll 1
   for (int b0 = 0; b0 < buckets; b0 += 256) {
-    const int b = b0 + threadIdx.x, mine = b < buckets ? (hist[b] + kTile - 1) / kTile : 0;
+    const int b = b0 + threadIdx.x, mine = b < buckets ? (s.hist[b] + kTile - 1) / kTile : 0;
     int sum = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -135,29 +181,28 @@ __device__ __forceinline__ int plan_tile(const Lora& p, int tile, int* hist, int
       s_found[1] = (tile - first) * kTile;
     }
     before += s_red[0] + s_red[1] + s_red[2] + s_red[3];
+    if (tile < before) break;
   }
   __syncthreads();
   adapter = __builtin_amdgcn_readfirstlane(s_found[0]);
   if (adapter < 0) return 0;
-  const int begin = s_found[1];
+  const int begin = s_found[1], n = min(s.hist[adapter] - begin, kTile);
   int count = 0;                       // of the adapter's rows among this wave's
-#pragma unroll
-  for (int c = 0; c < PER; ++c)
-    if (c < per) count += __popcll(__ballot(v[c] == adapter));
+#pragma unroll 4
+  for (int r = r0; r < r1; r += 64) count += __popcll(__ballot(r + lane < r1 && s.list[r + lane] == adapter));
   __syncthreads();
   if (lane == 0) s_red[w] = count;
   __syncthreads();
   int rank = 0;                        // rows of the adapter before this wave's
   for (int i = 0; i < w; ++i) rank += s_red[i];
-#pragma unroll
-  for (int c = 0; c < PER; ++c) {
-    if (c >= per) break;
-    const uint64_t same = __ballot(v[c] == adapter);
+#pragma unroll 2
+  for (int r = r0; r < r1 && rank < begin + kTile; r += 64) {
+    const bool is = r + lane < r1 && s.list[r + lane] == adapter;
+    const uint64_t same = __ballot(is);
     const int at = rank + __popcll(same & below) - begin;
-    if (v[c] == adapter && at >= 0 && at < kTile) rows[at] = r0 + c * 64 + lane;
+    if (is && at >= 0 && at < kTile) rows[at] = r + lane;
     rank += __popcll(same);
   }
-  const int n = min(s_red[0] + s_red[1] + s_red[2] + s_red[3] - begin, kTile);
   __syncthreads();
   return n;
 }
@@ -271,14 +316,20 @@ template <int NR>
 __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
   constexpr int RP = 16 * NR, KT = 64, PITCH = KT + 8, DEPTH = 2;
   constexpr int NXL = kTile * 8 / 256, NAL = (RP * 8 + 255) / 256;   // 16-byte pieces a thread
-  __shared__ __attribute__((aligned(16))) _Float16 s_x[2][kTile][PITCH];
-  __shared__ __attribute__((aligned(16))) _Float16 s_a[2][RP][PITCH];
+  union Lds {
+    PlanLds plan;
+    struct {
+      _Float16 x[2][kTile][PITCH], a[2][RP][PITCH];
+    } stage;
+  };
+  __shared__ __attribute__((aligned(16))) Lds s_lds;
+  auto &s_x = s_lds.stage.x;
+  auto &s_a = s_lds.stage.a;
   __shared__ int s_rows[kTile];
-  extern __shared__ int s_hist[];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, lg = lane >> 4;
   int a;
-  const int n = plan_tile(p, blockIdx.y, s_hist, s_rows, a);
+  const int n = plan_tile(p, blockIdx.y, s_lds.plan, s_rows, a);
   if (blockIdx.x == 0) {                 // the tile, for the second product
     if (tid == 0) p.tile_adapter[blockIdx.y] = n ? a : -1;
     if (tid < kTile) p.tile_rows[blockIdx.y * kTile + tid] = tid < n ? s_rows[tid] : -1;
@@ -680,14 +731,17 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
     hipLaunchKernelGGL(lora_shrink_kernel<NR>, dim3(p.m, p.n_split), dim3(256), 0, s, p);
     hipLaunchKernelGGL(lora_expand_kernel<NR>, grid(p.m), dim3(256), 0, s, p);
   } else {
-    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, p.tiles), dim3(256), (p.n_adapters + 1) * 4, s, p);
+    hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, p.tiles), dim3(256), 0, s, p);
     hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((p.m * 4 * NR + 255) / 256), dim3(256), 0, s, p);
     hipLaunchKernelGGL(lora_expand_tile_kernel<NR>, grid(2 * p.tiles), dim3(256), 0, s, p);
   }
 }
 
 // Tiles that rows of at most so many adapters (and of none) can make.
-int most_tiles(int m, int n_adapters) { return m / kTile + (n_adapters + 1 < m ? n_adapters + 1 : m); }
+int most_tiles(int m, int n_adapters) {
+  const int sorted = m / kTile + (n_adapters + 1 < m ? n_adapters + 1 : m), runs = most_runs(m);
+  return sorted > runs ? sorted : runs;
+}
 
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave.
 int lora_splits(int m, int k) {
@@ -726,7 +780,7 @@ LoraWs lora_ws(int m, int k, int R, int n_adapters) {
 
 bool lora_fits(int m, int n) {
   const int64_t most = m < kPlanRows ? m : kPlanRows;
-  return (2 * (most / kTile + most) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31) && n < (1 << 30);
+  return (2 * (most / kTile + most + 8) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31) && n < (1 << 30);
 }
 
 int64_t lora_ws_bytes(int m, int k, int R, int n_adapters) {
