@@ -677,11 +677,12 @@ mz_status mz_kv_append(const mz_kv_append_args *args, int32_t m, void *stream);
  * rounded to f16 for the product with the values.  head_dim 64 or 128,
  * n_q_heads a multiple of n_kv_heads with a group of at most 16, chunk_tokens
  * a power of two >= 8, n_table * chunk_tokens at most 2^30, a slot below 2^31
- * bytes.  workspace: device,
- * caller-owned, at least mz_attention_batch_workspace_bytes(...) bytes, any
- * content, not shared by calls in flight together (two graphs that may run at
- * once need two).  Errors: EINVAL for the above, a NULL pointer, q, slab,
- * workspace or out off 16-byte boundaries, or a short workspace. */
+ * bytes, n_seq * n_q_heads below 2^24.  workspace: device, caller-owned, at
+ * least mz_attention_batch_workspace_bytes(...) bytes (one for the most
+ * sequences serves fewer), any content, not shared by calls in flight together
+ * (two graphs that may run at once need two).  Errors: EINVAL for the above, a
+ * NULL pointer, q, slab, workspace or out off 16-byte boundaries, or a short
+ * workspace. */
 mz_status mz_attention_batch(const void *q_f16, const int32_t *lens, int32_t n_seq, const void *slab,
                              int32_t n_slots, const int32_t *table, int32_t n_table,
                              int32_t chunk_tokens, int32_t n_q_heads, int32_t n_kv_heads,
@@ -696,20 +697,22 @@ int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int
  *   y[r] = base[r] + scale[a] * (x[r] A_a^T) B_a^T,  a = adapter[r],
  * for the first n columns of rows of y_stride floats.  x: device f16 [m][k],
  * the projection's input; base: its output (mz_q4_gemm epilogue 0 or 1), y
- * may be base itself.  a: device f16 [n_adapters][max_rank][k], b: device f16
+ * may be base itself, else the two share no value.  a: device f16 [n_adapters][max_rank][k], b: device f16
  * [n_adapters][n][max_rank]; of adapter a the first rank[a] ranks count
  * (device int32 [n_adapters], clamped to 0..max_rank; NULL: all), whatever
  * the others hold.  scale: device float [n_adapters] (NULL: 1).  adapter:
  * device int32 [m], in any order; a row whose entry is outside
  * 0..n_adapters-1 has none: its y is the base's (in place it is not
  * touched).  Rows do not affect each other.  Nothing is rounded to f16 on the
- * way: x A^T keeps 22 bits and sums are fp32.  k a multiple of 8, max_rank a
- * multiple of 8 in 8..128, n_adapters at most 2047, y_stride a multiple of 4, m
- * may be 0.  workspace: device, caller-owned, at least
- * mz_lora_workspace_bytes(m, k, max_rank, n_adapters) bytes, any content, not shared by calls in flight together (two graphs that
- * may run at once need two).  Results do not change from run to run.  Errors:
- * EINVAL for the above, a NULL pointer, pointers off 16-byte boundaries, or a
- * short workspace. */
+ * way: x A^T keeps 22 bits and sums are fp32.  k a multiple of 8 up to 2^30,
+ * max_rank a multiple of 8 in 8..128, n_adapters at most 2047, y_stride a
+ * multiple of 4, m may be 0.  workspace: device, caller-owned, at least
+ * mz_lora_workspace_bytes(m, k, max_rank, n_adapters) bytes (one for the most
+ * rows serves fewer), any content, not shared by calls in flight together (two
+ * graphs that may run at once need two).  Results do not change from run to
+ * run.  Errors: EINVAL for the above, a NULL pointer, columns beyond one launch
+ * (for 8192 rows and more of 2047 adapters 2^19), pointers off 16-byte
+ * boundaries, or a short workspace. */
 mz_status mz_lora_add(const void *x_f16, int32_t m, int32_t k, const int32_t *adapter,
                       int32_t n_adapters, const void *a_f16, const void *b_f16, const float *scale,
                       const int32_t *rank, int32_t max_rank, int32_t n, const float *base, float *y,
@@ -738,16 +741,19 @@ typedef struct {
  * repetition) - frequency * c - presence; then the bias of v is added, of
  * several entries for v the last; then x = -inf where the mask forbids v.
  * Each operation is rounded to fp32, in this order.  Tokens outside 0..vocab-1
- * in a history or a bias list are passed over.  out: device float, rows stride
- * floats apart, may be logits itself or NULL; columns past vocab are not
- * touched.  token: device int32 [m] or NULL: the lowest token of the largest
+ * in a history or a bias list are passed over, and so is what a row's list
+ * holds beyond 2^30 entries.  out: device float, rows stride floats apart, may
+ * be logits itself (else the two share no value) or NULL; columns past vocab
+ * are not touched.  token: device int32 [m] or NULL: the lowest token of the largest
  * value, NaN aside; -1 where no value is above -inf (a mask that allows
  * nothing).  rules NULL: none.  The caller sees that the offsets ascend and
  * stay inside their lists.  workspace: device, caller-owned, needed for token
- * only, at least mz_logits_rules_workspace_bytes(m, vocab) bytes, any content,
- * not shared by calls in flight together.  m may be 0, vocab is at most 2^30.
- * Errors: EINVAL for sizes out of range, a list without its offsets, values or penalties, a mask
- * of too few words, neither out nor token, or a short workspace. */
+ * only, at least mz_logits_rules_workspace_bytes(m, vocab) bytes (one for the
+ * most rows serves fewer), any content, not shared by calls in flight together.
+ * m may be 0, vocab is at most 2^30, and m ceil(vocab / 4096) is below 2^23.
+ * Errors: EINVAL for sizes out of range, a list without its offsets, values or
+ * penalties, a mask of too few words, neither out nor token, or a short
+ * workspace. */
 mz_status mz_logits_rules(const float *logits, int32_t m, int32_t vocab, int64_t stride,
                           const mz_logits_rules_args *rules, float *out, int32_t *token,
                           void *workspace, int64_t workspace_bytes, void *stream);

@@ -210,7 +210,8 @@ int append_items(int nq, int nkv, int hd) {
 bool kv_append_fits(int m, int nq, int nkv, int hd) {
   const int64_t groups = ((int64_t)m + kRotRows - 1) / kRotRows;
   const int64_t tiles = ((int64_t)m + kValRows - 1) / kValRows * ((nkv * hd + kValDims - 1) / kValDims);
-  return groups * append_items<float>(nq, nkv, hd) + 256 + tiles < (int64_t(1) << 31);
+  const int64_t threads = groups * append_items<float>(nq, nkv, hd);
+  return threads < (int64_t(1) << 31) && threads / 256 + 1 + tiles <= kMaxBlocks;
 }
 
 void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s) {

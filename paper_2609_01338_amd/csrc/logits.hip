@@ -16,6 +16,8 @@
 // out early (the first tokens of the history and the whole of a short bias
 // list with the logits), and slices are small enough for eight workgroups a
 // CU.  The slices' largest values meet in a second, small kernel.
+#include <algorithm>
+
 #include "mz_kernels.h"
 
 namespace mzk {
@@ -52,6 +54,7 @@ __device__ __forceinline__ float penalised(float x, float count, float rep, floa
 // other work, all together; what stands for a token without a bias: -0 as a value, below
 // every index.
 constexpr int kAheadHistory = 2048, kAheadBias = 512, kNone = (int)0x80000000;
+constexpr int64_t kMostList = 1 << 30;      // entries of a row's list that are read
 
 template <int NT, int SLICE, int VEC>
 __global__ __launch_bounds__(NT) void logits_rules_kernel(LogitsRules p) {
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(NT) void logits_rules_kernel(LogitsRules p) {
   int64_t h0 = 0, h1 = p.n_history, b0 = 0, b1 = p.n_bias;
   if (p.history_off) h0 = p.history_off[row], h1 = p.history_off[row + 1];
   if (p.bias_off) b0 = p.bias_off[row], b1 = p.bias_off[row + 1];
-  const int nh = (int)(h1 - h0), nb = (int)(b1 - b0);
+  const int nh = (int)min(h1 - h0, kMostList), nb = (int)min(b1 - b0, kMostList);
   if (nh > 0 || nb > 0) {
     const unsigned here = (unsigned)min(SLICE, p.vocab - v0);
     const int32_t *history = p.history + h0, *bias_token = p.bias_token + b0;
@@ -220,13 +223,24 @@ __global__ __launch_bounds__(64) void logits_token_kernel(LogitsRules p) {
 
 constexpr int kSmallThreads = 256, kSmallSlice = 1024, kThreads = 512, kSlice = 4096;
 
-int logits_slice(int m, int vocab) { return (int64_t)m * ((vocab + kSlice - 1) / kSlice) >= 512 ? kSlice : kSmallSlice; }
+constexpr int kLargeSlices = 512;     // large slices from so many of them on
+
+int logits_slice(int m, int vocab) {
+  return (int64_t)m * ((vocab + kSlice - 1) / kSlice) >= kLargeSlices ? kSlice : kSmallSlice;
+}
 
 }  // namespace
 
-int64_t logits_rules_blocks(int m, int vocab) {
-  const int slice = logits_slice(m, vocab);
-  return ((int64_t)vocab + slice - 1) / slice * m;
+// In 512-thread workgroups half of kMaxBlocks.
+bool logits_rules_fits(int m, int vocab) {
+  return ((int64_t)vocab + kSlice - 1) / kSlice * m <= kMaxBlocks / 2;
+}
+
+// The slices of m rows, or of the fewer rows that small slices serve.
+int64_t logits_rules_ws_bytes(int m, int vocab) {
+  const int64_t large = ((int64_t)vocab + kSlice - 1) / kSlice, small = ((int64_t)vocab + kSmallSlice - 1) / kSmallSlice;
+  const int64_t few = std::min<int64_t>(m, (kLargeSlices - 1) / large);
+  return std::max(large * m, small * few) * 8;
 }
 
 void launch_logits_rules(LogitsRules p, int m, void* ws, hipStream_t s) {

@@ -34,7 +34,12 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kGatherRows = 64;      // rows up to which groups are searched
+// Rows up to which groups are searched.  Groups against tiles, measured in a
+// graph, 4096 x 4096 of rank 16: 33 rows of one adapter 9.4 against 12.8 us,
+// with an adapter each 8.7 against 15.7; 64 rows 13.0 against 13.1, 10.8 against
+// 19.8; 128 rows 16.7 against 13.7, 12.1 against 20.5.  4096 x 14336, rank 32,
+// 128 rows: one adapter 33.6 against 19.2, 64 adapters 25.5 against 37.5.
+constexpr int kGatherRows = 64;
 constexpr int kPlanRows = 8192;      // rows of a call whose tiles are counted: 32 entries a thread
 constexpr int kTile = 64;            // rows of a tile
 constexpr int kColsWg = 256;         // columns of a workgroup of the second product: 64 a wave
@@ -49,30 +54,14 @@ __device__ __forceinline__ int rank_of(const Lora& p, int a) { return p.rank ? m
 // where r begins none.
 __device__ __forceinline__ int gather_group(const Lora& p, int r, int a, int* rows) {
   const int lane = threadIdx.x & 63;
-  int v[kGatherRows / 64];
-#pragma unroll
-  for (int c = 0; c < kGatherRows / 64; ++c) {
-    v[c] = -1;
-    if (c * 64 < p.m) v[c] = p.adapter[min(c * 64 + lane, p.m - 1)];
-  }
-  const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-  int seen = 0, before = -1;       // rows of the adapter so far; those before r
-#pragma unroll
-  for (int c = 0; c < kGatherRows / 64; ++c) {
-    if (c * 64 >= p.m) break;
-    const bool match = c * 64 + lane < p.m && v[c] == a;
-    const uint64_t mask = __ballot(match);
-    if (r >> 6 == c) {
-      before = seen + __popcll(mask & ((1ull << (r & 63)) - 1));
-      if (before % 16) return 0;
-    }
-    if (before >= 0) {
-      const int at = seen + __popcll(mask & below) - before;
-      if (match && at >= 0 && at < 16) rows[at] = c * 64 + lane;
-    }
-    seen += __popcll(mask);
-  }
-  return min(seen - before, 16);
+  static_assert(kGatherRows == 64, "a row a lane");
+  const bool match = lane < p.m && p.adapter[min(lane, p.m - 1)] == a;
+  const uint64_t mask = __ballot(match);
+  const int before = __popcll(mask & ((1ull << r) - 1));
+  if (before % 16) return 0;
+  const int at = __popcll(mask & ((1ull << lane) - 1)) - before;
+  if (match && at >= 0 && at < 16) rows[at] = lane;
+  return min(__popcll(mask) - before, 16);
 }
 
 // LDS of plan_tile: the call's adapters, where in each window of 64 rows the
@@ -84,7 +73,10 @@ struct PlanLds {
 };
 
 // Runs of one adapter, each within a window of 64 rows, that make the tiles as
-// they stand; with more of them the rows are sorted.
+// they stand; with more of them the rows are sorted.  As they stand against
+// sorted, 4096 rows of 4096 x 4096, rank 64: runs of 64 rows (as many as
+// windows) 62.7 against 76.4 us, of 100 (1.3 a window) 78 against 85, of 48
+// (1.5) 89 against 79, of 24 (3) 118 against 79.
 __host__ __device__ inline int most_runs(int m) {
   const int windows = (m + 63) / 64;
   return windows + windows / 4 + 8;
@@ -743,15 +735,25 @@ int most_tiles(int m, int n_adapters) {
   return sorted > runs ? sorted : runs;
 }
 
-// K splits: enough workgroups for the chip, at least two steps of 32 a wave.
-int lora_splits(int m, int k) {
-  const int groups = m <= kGatherRows ? m : (m - 1) / kTile + 1;
-  const int want = (m <= kGatherRows ? 1024 : 520) / groups, most = (k + 31) / 32 / 8;
-  const int ns = want < most ? want : most;
-  return ns < 1 ? 1 : ns > 16 ? 16 : ns;
+// K splits: enough workgroups for the chip, at least two steps of 32 a wave,
+// at most 16.  With at most 8, 1 row of 8960 x 1536, rank 64, takes 11.3 for 9.7
+// us, 512 rows of 14336 x 4096, rank 16, 24.7 for 20.2; with 32 18.8.  Half the
+// workgroups for many rows: 4096 of the latter 67.8 for 58.2; twice: 59.3.
+constexpr int kFewBlocks = 1024, kManyBlocks = 520;
+
+int most_splits(int k) {
+  const int most = (k + 31) / 32 / 8;
+  return most < 1 ? 1 : most > 16 ? 16 : most;
 }
 
-// The workspace of a call of m <= kPlanRows rows.
+int lora_splits(int m, int k) {
+  const int groups = m <= kGatherRows ? m : (m - 1) / kTile + 1;
+  const int want = (m <= kGatherRows ? kFewBlocks : kManyBlocks) / groups, most = most_splits(k);
+  return want < 1 ? 1 : want > most ? most : want;
+}
+
+// The workspace of a call of up to m <= kPlanRows rows: every part grows with
+// m, so that one for the largest call serves all.
 struct LoraWs {
   int64_t t, hi, lo, unit, tile_adapter, tile_rows, bytes;
 };
@@ -764,7 +766,9 @@ LoraWs lora_ws(int m, int k, int R, int n_adapters) {
     return here;
   };
   const int64_t rp = rank_tiles(R) * 16, wide = (rp + 31) / 32 * 32;
-  w.t = take((int64_t)lora_splits(m, k) * m * rp * 4);
+  // splits x rows of t: at most the workgroups wanted times a group's rows
+  const int64_t most = m <= kGatherRows ? kFewBlocks : kManyBlocks * kTile, all = (int64_t)most_splits(k) * m;
+  w.t = take((all < most ? all : most) * rp * 4);
   if (m > kGatherRows) {
     w.hi = take(m * wide * 2);
     w.lo = take(m * wide * 2);
@@ -778,23 +782,22 @@ LoraWs lora_ws(int m, int k, int R, int n_adapters) {
 
 }  // namespace
 
-bool lora_fits(int m, int n) {
-  const int64_t most = m < kPlanRows ? m : kPlanRows;
-  return (2 * (most / kTile + most + 8) + 7) * ((n - 1) / kColsWg + 1) < (int64_t(1) << 31) && n < (1 << 30);
+bool lora_fits(int m, int n, int n_adapters) {
+  const int rows = m < kPlanRows ? m : kPlanRows;
+  const int64_t blocks = rows <= kGatherRows ? rows : 2 * most_tiles(rows, n_adapters);
+  return (blocks + 7) / 8 * 8 * ((n - 1) / kColsWg + 1) <= kMaxBlocks;
 }
 
 int64_t lora_ws_bytes(int m, int k, int R, int n_adapters) {
-  if (m <= kPlanRows) return lora_ws(m, k, R, n_adapters).bytes;
-  const int64_t whole = lora_ws(kPlanRows, k, R, n_adapters).bytes, rest = m % kPlanRows ? lora_ws(m % kPlanRows, k, R, n_adapters).bytes : 0;
-  return whole > rest ? whole : rest;
+  return lora_ws(m < kPlanRows ? m : kPlanRows, k, R, n_adapters).bytes;
 }
 
 void launch_lora(Lora p, void* ws, hipStream_t s) {
   const int rows = p.m;
-  for (int r = 0; r < rows; r += kPlanRows) {
+  for (int64_t r = 0; r < rows; r += kPlanRows) {
     Lora q = p;
-    q.m = rows - r < kPlanRows ? rows - r : kPlanRows;
-    q.x += (int64_t)r * q.k;
+    q.m = rows - r < kPlanRows ? (int)(rows - r) : kPlanRows;
+    q.x += r * q.k;
     q.adapter += r;
     q.base += r * q.y_stride;
     q.y += r * q.y_stride;

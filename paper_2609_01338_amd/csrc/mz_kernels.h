@@ -153,6 +153,10 @@ void launch_rope_kv(const float* qkv, int qkv_stride, int m, const int32_t* pos,
                     const int64_t* kv_off, const float2* rope_cs, int nq, int nkv, int hd, int C,
                     void* q_out, void* slab, hipStream_t s);
 
+// Most workgroups of 256 threads in a launch: the runtime takes fewer than 2^32
+// threads.
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;
+
 // Keys and values of m rows of many sequences, rotated and written through
 // the sequences' chunk tables, and the rows' queries rotated (see mz.h,
 // mz_kv_append).  q, k, v: rows of fp32 or f16, strides in elements; C = 1 <<
@@ -174,8 +178,9 @@ void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s);
 
 // Attention of one token of every sequence over its chunks (see mz.h,
 // mz_attention_batch); hd 64 or 128, group = nq / nkv <= 16, C = 1 << cshift,
-// slot_bytes and attention_batch_units below 2^31.  The fields after slot_bytes'
-// line are the launcher's own, in ws (attention_batch_ws_bytes bytes).
+// slot_bytes and attention_batch_units below 2^31, n_seq nq at most
+// kMaxBlocks.  The fields after slot_bytes' line are the launcher's own, in ws
+// (attention_batch_ws_bytes bytes).
 struct AttnBatch {
   const _Float16* q;
   const int32_t *lens, *table;
@@ -195,9 +200,10 @@ int64_t attention_batch_ws_bytes(int n_seq, int group, int hd);
 void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
 
 // y = base + scale (x A^T) B^T with each row's adapter (see mz.h,
-// mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8, y_stride of 4,
-// at most kLoraAdapters, every pointer 16-byte aligned, lora_fits(m, n).  The fields from t on are the
-// launcher's own, in ws (lora_ws_bytes bytes).
+// mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8 up to 2^30,
+// y_stride of 4, at most kLoraAdapters, every pointer 16-byte aligned,
+// lora_fits(m, n, n_adapters).  The fields from t on are the launcher's own, in
+// ws: lora_ws_bytes bytes, which also do for fewer rows.
 struct Lora {
   const _Float16 *x, *a, *b;
   const int32_t *adapter, *rank;
@@ -212,7 +218,7 @@ struct Lora {
   int n_split, tiles;
 };
 constexpr int kLoraAdapters = 2047;    // adapters of a call: their counts lie in LDS
-bool lora_fits(int m, int n);
+bool lora_fits(int m, int n, int n_adapters);
 int64_t lora_ws_bytes(int m, int k, int R, int n_adapters);
 void launch_lora(Lora p, void* ws, hipStream_t s);
 
@@ -220,8 +226,8 @@ void launch_lora(Lora p, void* ws, hipStream_t s);
 // mz.h, mz_logits_rules); out and token may be null, and each of history,
 // bias_token and mask.  A single row may leave out the offsets (its lists are
 // n_history and n_bias long) and mask_row (mask 0).  The last line is the
-// launcher's own, in ws (8 bytes for each of logits_rules_blocks(m, vocab),
-// which is below 2^31).
+// launcher's own, in ws: logits_rules_ws_bytes bytes, which also do for fewer
+// rows.  Only for logits_rules_fits(m, vocab).
 struct LogitsRules {
   const float* logits;
   float* out;
@@ -239,7 +245,8 @@ struct LogitsRules {
   int32_t* token;
   int slices; float* part_val; int32_t* part_idx;
 };
-int64_t logits_rules_blocks(int m, int vocab);
+bool logits_rules_fits(int m, int vocab);
+int64_t logits_rules_ws_bytes(int m, int vocab);
 void launch_logits_rules(LogitsRules p, int m, void* ws, hipStream_t s);
 
 // h float [m][d] = dequant(E[tok[i]]) with E split into nibbles [V][d/2] and

@@ -1752,7 +1752,7 @@ mz_status mz_set_token_rules(mz_ctx* x, const mz_token_rules* rules) {
     }
     HIPCHK(hipStreamSynchronize(x->s_compute));
     // the kernel's workspace first, then penalties, bias tokens, bias values and mask
-    const int64_t b_ws = round_up(mzk::logits_rules_blocks(1, x->V) * 8, 256), b_bias = round_up((int64_t)x->V * 4, 256);
+    const int64_t b_ws = round_up(mzk::logits_rules_ws_bytes(1, x->V), 256), b_bias = round_up((int64_t)x->V * 4, 256);
     if (!x->d_logits) x->d_logits = (float*)dmalloc((size_t)x->V * 4);
     if (!x->d_hist) x->d_hist = (int32_t*)dmalloc((size_t)x->max_ctx * 4);
     if (!x->d_rules) x->d_rules = (uint8_t*)dmalloc((size_t)(b_ws + 256 + 2 * b_bias + words * 4));
@@ -2243,7 +2243,7 @@ mz_status mz_attention_batch(const void* q, const int32_t* lens, int32_t n_seq, 
     const int64_t slot_bytes = (int64_t)chunk_tokens * n_kv * head_dim * 4;
     if (slot_bytes > INT32_MAX) fail(MZ_EINVAL, "a chunk slot exceeds 2^31 - 1 bytes");
     if (mzk::attention_batch_units(n_seq, n_table, chunk_tokens, n_kv) > INT32_MAX ||
-        (int64_t)n_seq * n_q > INT32_MAX)
+        (int64_t)n_seq * n_q > mzk::kMaxBlocks)
       fail(MZ_EINVAL, "n_seq sequences of n_table chunks are too many");
     if (workspace_bytes < mzk::attention_batch_ws_bytes(n_seq, n_q / n_kv, head_dim))
       fail(MZ_EINVAL, "workspace too small");
@@ -2271,7 +2271,9 @@ mz_status mz_attention_batch(const void* q, const int32_t* lens, int32_t n_seq, 
 }
 
 int64_t mz_lora_workspace_bytes(int32_t m, int32_t k, int32_t max_rank, int32_t n_adapters) {
-  if (m < 1 || k < 8 || max_rank < 8 || max_rank > 128 || n_adapters < 1 || n_adapters > mzk::kLoraAdapters) return -1;
+  if (m < 1 || k < 8 || k % 8 || k > (1 << 30) || max_rank < 8 || max_rank > 128 || max_rank % 8 || n_adapters < 1 ||
+      n_adapters > mzk::kLoraAdapters)
+    return -1;
   return mzk::lora_ws_bytes(m, k, max_rank, n_adapters);
 }
 
@@ -2283,14 +2285,14 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
     if (!x || !adapter || !a || !b || !base || !y || !workspace) fail(MZ_EINVAL, "NULL pointer");
     if (m < 0 || n < 1) fail(MZ_EINVAL, "n must be positive, m at least 0");
     if (n_adapters < 1 || n_adapters > mzk::kLoraAdapters) fail(MZ_EINVAL, "n_adapters must be 1..%d", mzk::kLoraAdapters);
-    if (k < 8 || k % 8) fail(MZ_EINVAL, "k must be a positive multiple of 8");
+    if (k < 8 || k % 8 || k > (1 << 30)) fail(MZ_EINVAL, "k must be a multiple of 8 in 8..2^30");
     if (max_rank < 8 || max_rank > 128 || max_rank % 8) fail(MZ_EINVAL, "max_rank must be a multiple of 8 in 8..128");
     if (y_stride < n || y_stride % 4) fail(MZ_EINVAL, "y_stride must be a multiple of 4 and at least n");
     if (!aligned16(x) || !aligned16(a) || !aligned16(b) || !aligned16(base) || !aligned16(y) || !aligned16(workspace))
       fail(MZ_EINVAL, "x, a, b, base, y and workspace must lie on 16-byte boundaries");
     check_stream(stream);
     if (m == 0) return;
-    if (!mzk::lora_fits(m, n)) fail(MZ_EINVAL, "m rows of n columns are too many");
+    if (!mzk::lora_fits(m, n, n_adapters)) fail(MZ_EINVAL, "m rows of n columns are too many");
     if (workspace_bytes < mzk::lora_ws_bytes(m, k, max_rank, n_adapters)) fail(MZ_EINVAL, "workspace too small");
     mzk::Lora p{};
     p.x = reinterpret_cast<const _Float16*>(x);
@@ -2313,8 +2315,8 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
 }
 
 int64_t mz_logits_rules_workspace_bytes(int32_t m, int32_t vocab) {
-  if (m < 1 || vocab < 1) return -1;
-  return mzk::logits_rules_blocks(m, vocab) * 8;
+  if (m < 1 || vocab < 1 || vocab > (1 << 30)) return -1;
+  return mzk::logits_rules_ws_bytes(m, vocab);
 }
 
 mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t stride, const mz_logits_rules_args* rules,
@@ -2331,9 +2333,8 @@ mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t
       fail(MZ_EINVAL, "mask needs mask_row, n_masks, and mask_words that cover vocab");
     check_stream(stream);
     if (m == 0) return;
-    const int64_t blocks = mzk::logits_rules_blocks(m, vocab);
-    if (blocks > INT32_MAX) fail(MZ_EINVAL, "too many rows");
-    if (token && (!workspace || ((uintptr_t)workspace & 3) || workspace_bytes < blocks * 8))
+    if (!mzk::logits_rules_fits(m, vocab)) fail(MZ_EINVAL, "too many rows");
+    if (token && (!workspace || ((uintptr_t)workspace & 3) || workspace_bytes < mzk::logits_rules_ws_bytes(m, vocab)))
       fail(MZ_EINVAL, "workspace too small");
     mzk::LogitsRules p{};
     p.logits = logits;

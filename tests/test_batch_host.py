@@ -139,3 +139,37 @@ def test_logits_rules_workspace_and_no_rows():
     refused(mz.mz_logits_rules, **{**LOGITS, "ws_bytes": need - 1}, match="workspace")
     assert mz.mz_logits_rules_workspace_bytes(0, 1000) == -1 and mz.mz_logits_rules_workspace_bytes(3, 0) == -1
     mz.mz_logits_rules(**{**LOGITS, "m": 0, "ws_ptr": 0, "ws_bytes": 0})
+
+
+# ---- the largest calls and the workspaces of smaller ones: a launch holds fewer than 2^32 threads
+
+def test_calls_beyond_one_launch():
+    refused(mz.mz_attention_batch, **{**ATTENTION, "n_seq": 1 << 21, "ws_bytes": 1 << 40}, match="too many")      # 2^24 query rows
+    refused(mz.mz_logits_rules, **{**LOGITS, "m": 1 << 23, "ws_bytes": 1 << 40}, match="too many")
+    refused(mz.mz_logits_rules, **{**LOGITS, "m": 1 << 22, "vocab": 4097, "stride": 8192, "mask_words": 256, "ws_bytes": 1 << 40},
+            match="too many")
+    # a head of 32 alone: 4 items of 4 rows, 64-row tiles
+    refused(mz.mz_kv_append, **{**APPEND, "n_q": 0, "n_kv": 1, "head_dim": 32, "m": 900 << 20}, match="too many")
+    refused(mz.mz_lora_add, **{**LORA, "k": (1 << 30) + 8, "ws_bytes": 1 << 40}, match="k must")
+    # 8 rows: a range of 256 columns each
+    refused(mz.mz_lora_add, **{**LORA, "m": 8, "n": (1 << 29) + 1, "y_stride": (1 << 29) + 4, "ws_bytes": 1 << 40}, match="too many")
+    for bad in [(3, 60, 16, 2), (3, (1 << 30) + 8, 16, 2), (3, 64, 12, 2)]:
+        assert mz.mz_lora_workspace_bytes(*bad) == -1
+    assert mz.mz_logits_rules_workspace_bytes(3, (1 << 30) + 1) == -1
+
+
+@pytest.mark.parametrize("k,R,na", [(64, 8, 1), (2048, 16, 4), (4096, 64, 9), (8960, 128, 2047)])
+def test_lora_workspace_of_the_largest_call_serves_all(k, R, na):
+    need = [mz.mz_lora_workspace_bytes(m, k, R, na) for m in range(1, 8300)]
+    assert need == sorted(need)
+
+
+@pytest.mark.parametrize("vocab", [1, 1000, 4096, 4097, 128256, 151936, 1 << 21, 1 << 30])
+def test_logits_workspace_of_the_largest_call_serves_all(vocab):
+    need = [mz.mz_logits_rules_workspace_bytes(m, vocab) for m in range(1, 2000)]
+    assert need == sorted(need) and need[0] >= 8
+
+
+def test_attention_workspace_of_the_largest_call_serves_all():
+    need = [mz.mz_attention_batch_workspace_bytes(b, 32, 8, 128) for b in range(1, 2000)]
+    assert need == sorted(need)

@@ -430,6 +430,28 @@ def test_attention_offsets_past_32_bits():
     close(out, ref, bound, "out")
 
 
+def test_attention_as_many_queries_as_a_launch_holds():
+    """2^24 - 16 query rows; three sequences have keys, the first and the last among them."""
+    torch = torch_cuda()
+    nq, nkv, hd, C, n_seq = 16, 1, 64, 16, (1 << 20) - 1
+    q, lens, slab, table = attention_inputs([40, 1, 300], C, nq, nkv, hd, seed=17)
+    at = [0, 70000, n_seq - 1]
+    ref, bound = attention_oracle(q, lens, slab, table, C, nq, nkv, hd)
+    all_q = torch.zeros(n_seq, nq, hd, device="cuda", dtype=torch.float16)
+    all_lens = torch.zeros(n_seq, device="cuda", dtype=torch.int32)
+    all_table = torch.full((n_seq, table.shape[1]), -1, device="cuda", dtype=torch.int32)
+    all_q[at], all_lens[at], all_table[at] = dev(q).view(3, nq, hd), dev(lens), dev(table)
+    need = mz.mz_attention_batch_workspace_bytes(n_seq, nq, nkv, hd)
+    ws, d_slab = torch.empty(need, device="cuda", dtype=torch.uint8), dev(slab)
+    out = torch.full((n_seq, nq * hd), 7.0, device="cuda", dtype=torch.float16)
+    mz.mz_attention_batch(all_q.data_ptr(), all_lens.data_ptr(), n_seq, d_slab.data_ptr(), slab.shape[0], all_table.data_ptr(),
+                          table.shape[1], C, nq, nkv, hd, ws.data_ptr(), need, out.data_ptr(), stream())
+    torch.cuda.synchronize()
+    close(out[at].view(ref.shape), ref, bound, "out")
+    out[at] = 0
+    assert not out.any()
+
+
 def test_attention_captured_on_another_stream():
     """One graph over changing lengths; its workspace holds the last replay's partials."""
     torch = torch_cuda()
@@ -655,6 +677,27 @@ def test_lora_offsets_past_32_bits():
     close(y, ref, bound, "y")
 
 
+def test_lora_on_two_streams_at_once_and_a_larger_workspace():
+    """Many rows, sorted tiles; the first call's workspace is one for 8192 rows."""
+    torch = torch_cuda()
+    k, n, R, na, streams, calls = 512, 600, 24, 5, [torch.cuda.Stream() for _ in range(2)], []
+    for i, m in enumerate((700, 333)):
+        x, adapter, a, b, scale, rank, base, _ = lora_inputs([(3 * r + i) % na for r in range(m)], k, n, R, na, seed=33 + i)
+        need = mz.mz_lora_workspace_bytes(8192 if i == 0 else m, k, R, na)
+        calls.append(([dev(v) for v in (x, adapter, a, b, scale, rank, base)], m, need,
+                      torch.full((need // 4,), float("nan"), device="cuda"), torch.zeros(base.shape, device="cuda"),
+                      lora_oracle(x, adapter, a, b, scale, rank, base, n)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, (d, m, need, ws, y, _) in zip(streams, calls):
+            mz.mz_lora_add(d[0].data_ptr(), m, k, d[1].data_ptr(), na, d[2].data_ptr(), d[3].data_ptr(), R, n, d[6].data_ptr(),
+                           y.data_ptr(), y.shape[1], ws.data_ptr(), need, st.cuda_stream, scale_ptr=d[4].data_ptr(),
+                           rank_ptr=d[5].data_ptr())
+    torch.cuda.synchronize()
+    for _, _, _, _, y, (ref, bound) in calls:
+        close(y, ref, bound, "y")
+
+
 # ----------------------------------------------------------------------------- rules on logits
 
 def logits_oracle(x, penalty, histories, biases, mask, mask_row):
@@ -781,6 +824,24 @@ def test_logits_long_histories():
 def test_logits_many_rows():
     """The larger slices, and rows enough for many workgroups."""
     logits_case(logits_inputs(130, 20000, seed=32, n_hist=300))
+
+
+def test_logits_as_many_rows_as_a_launch_holds():
+    torch = torch_cuda()
+    m, v = (1 << 23) - 1, 5
+    x = torch.randint(-4, 5, (m, v), device="cuda", dtype=torch.int32).float()
+    need = mz.mz_logits_rules_workspace_bytes(m, v)
+    ws, token = torch.empty(need, device="cuda", dtype=torch.uint8), torch.full((m,), -7, device="cuda", dtype=torch.int32)
+    mask = dev(np.array([[0b11111], [0b01010], [0]], np.uint32).view(np.int32))
+    mask_row = torch.arange(m, device="cuda", dtype=torch.int32) % 4          # 3: none
+    mz.mz_logits_rules(x.data_ptr(), m, v, v, 0, token.data_ptr(), ws.data_ptr(), need, mask_ptr=mask.data_ptr(), n_masks=3,
+                       mask_words=1, mask_row_ptr=mask_row.data_ptr(), stream=stream())
+    torch.cuda.synchronize()
+    weight = x * 8 - torch.arange(v, device="cuda")              # of equal values the lowest index
+    want = weight.argmax(1)
+    want[1::4] = 1 + 2 * weight[1::4, 1::2].argmax(1)
+    want[2::4] = -1
+    assert torch.equal(token.long(), want)
 
 
 def test_logits_of_repeated_biases_the_last_counts():
