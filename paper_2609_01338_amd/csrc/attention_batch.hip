@@ -82,7 +82,7 @@ __device__ __forceinline__ Slots slots_of(const int32_t* table, int cshift, int 
 }
 
 template <int HD, bool SMALL>
-__global__ __launch_bounds__(64 * kWaves, 3) void attn_batch_kernel(AttnBatch a) {
+__global__ __launch_bounds__(64 * kWaves, 2) void attn_batch_kernel(AttnBatch a) {
   constexpr int KS = HD / 32;          // 32-wide dimension steps of a score product
   constexpr int DB = HD / 16;          // 16-dimension blocks of the output
   __shared__ float s_o[kWaves][DB][4][64];
@@ -346,6 +346,18 @@ __global__ __launch_bounds__(256) void attn_batch_join_kernel(AttnBatch a) {
   }
 }
 
+// Shares: one workgroup a CU where pairs are few (a share's keys are then
+// mostly one pair's, and fewer partials are joined), two where they are many
+// (what a pair costs beside its keys, its queries, its table and the waves'
+// join, hides behind the other workgroup).  256 against 512 (768) shares,
+// both kernels in a graph, 4 query heads a KV head, dimension 128: 8 pairs of
+// 12000 keys 16.2 against 18.2 (17.9) us, of 32768 27.2 against 28.3 (28.7);
+// 128 pairs of 260-4096 25.4 against 27.2 (29.0); 512 pairs of 50 11.5 against
+// 9.9 (9.9), of 300 22.4 against 20.1 (23.0), of 1000 46.2 against 46.0 (48.8);
+// dimension 64, 512 pairs of 130-2048 33.2 against 27.1 (26.0), of 1000 28.2
+// against 27.0 (30.6).
+constexpr int kFewPairs = 256;
+
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
@@ -366,7 +378,8 @@ void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s) {
   a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ml) + up256((int64_t)2 * kAttnBatchWgs * a.group * 8));
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)hd);
   const int64_t most = attention_batch_units(a.n_seq, a.n_table, a.C, a.nkv);
-  a.wgs = most < kAttnBatchWgs ? (int)most : kAttnBatchWgs;
+  a.wgs = (int64_t)a.n_seq * a.nkv <= kFewPairs ? kAttnBatchWgs / 2 : kAttnBatchWgs;
+  if (most < a.wgs) a.wgs = (int)most;
   const dim3 grid(a.wgs), block(64 * kWaves);
   if (hd == 128) {
     if (a.C < kBlock)

@@ -194,7 +194,7 @@ struct AttnBatch {
   int wgs;            // most workgroups that share the units
   float scale_log2;
 };
-constexpr int kAttnBatchWgs = 768;
+constexpr int kAttnBatchWgs = 512;
 int64_t attention_batch_units(int n_seq, int n_table, int chunk_tokens, int n_kv);
 int64_t attention_batch_ws_bytes(int n_seq, int group, int hd);
 void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
