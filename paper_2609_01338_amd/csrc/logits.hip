@@ -64,11 +64,25 @@ constexpr int kThreads = 512, kSlice = 4096;
 constexpr int kAheadHistory = 2048, kAheadBias = 512, kNone = (int)0x80000000;
 constexpr int64_t kMostList = 1 << 30;      // entries of a row's list that are read
 
+typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));      // lists begin anywhere
+
+// Tokens i .. i + 3 of a list, relative to v0; ~0 past its n entries.
+__device__ __forceinline__ void tokens4(const int32_t* list, int i, int n, int v0, unsigned (&t)[4]) {
+  if (i + 4 <= n) {
+    const i32x4 u = *reinterpret_cast<const i32x4*>(list + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = (unsigned)u[e] - (unsigned)v0;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = i + e < n ? (unsigned)list[i + e] - (unsigned)v0 : ~0u;
+  }
+}
+
 // VEC: logits a load, 4 where rows lie on 16-byte boundaries (22.3 us for 64
 // rows of 128256, one by one 22.9).
 template <int VEC>
 __global__ __launch_bounds__(kThreads) void logits_rules_kernel(LogitsRules p) {
-  constexpr int NT = kThreads, SLICE = kSlice, GROUPS = SLICE / (NT * VEC), AH = kAheadHistory / NT, AB = kAheadBias / NT;
+  constexpr int NT = kThreads, SLICE = kSlice, GROUPS = SLICE / (NT * VEC), AH = kAheadHistory / (4 * NT), AB = kAheadBias / NT;
   __shared__ __attribute__((aligned(16))) int s_count[SLICE];
   __shared__ __attribute__((aligned(16))) int s_last[SLICE];
   __shared__ float s_val[NT / 64];
@@ -107,11 +121,11 @@ __global__ __launch_bounds__(kThreads) void logits_rules_kernel(LogitsRules p) {
     const int32_t *history = p.history + h0, *bias_token = p.bias_token + b0;
     const float* bias_value = p.bias_value + b0;
     // tokens relative to the slice: inside it only below `here`
-    unsigned ht[AH], bt[AB];
+    unsigned ht[AH][4], bt[AB];
     float bval[AB];
     const bool held = nb <= NT * AB;       // the list's values stay in registers
 #pragma unroll
-    for (int k = 0; k < AH; ++k) ht[k] = tid + NT * k < nh ? (unsigned)history[tid + NT * k] - (unsigned)v0 : ~0u;
+    for (int k = 0; k < AH; ++k) tokens4(history, (tid + NT * k) * 4, nh, v0, ht[k]);
 #pragma unroll
     for (int k = 0; k < AB; ++k) {
       const bool in = tid + NT * k < nb;
@@ -125,11 +139,16 @@ __global__ __launch_bounds__(kThreads) void logits_rules_kernel(LogitsRules p) {
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < AH; ++k)
-      if (ht[k] < here) atomicAdd(&s_count[ht[k]], 1);
-#pragma unroll 4
-    for (int i = NT * AH + tid; i < nh; i += NT) {
-      const unsigned t = (unsigned)history[i] - (unsigned)v0;
-      if (t < here) atomicAdd(&s_count[t], 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (ht[k][e] < here) atomicAdd(&s_count[ht[k][e]], 1);
+#pragma unroll 2
+    for (int i = (NT * AH + tid) * 4; i < nh; i += NT * 4) {
+      unsigned t[4];
+      tokens4(history, i, nh, v0, t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (t[e] < here) atomicAdd(&s_count[t[e]], 1);
     }
     // entry e of the list stands as e + 1
 #pragma unroll
