@@ -24,6 +24,12 @@
 // that weights keep full precision down to 2^-28 of the largest (many small
 // ones add up in a long cache); the sums add the same rounded values, in
 // fp32.  Partials and their joins are fp32.
+//
+// Measured, both kernels: 64 sequences of 512-8192 keys, 8 KV heads of 128, 122
+// + 5 us: 640 MB at 5.2 TB/s, where reading them alone in this order takes
+// 5.3-5.8 TB/s; one of 32768 24 + 4; one of 2048, heads of 64, 5.3 + 4,
+// latency.  Two and more blocks in flight a wave gained nothing (137 us for the
+// former: the memory is busy, and what each share loads ahead in vain adds up).
 #include "mz_kernels.h"
 
 namespace mzk {

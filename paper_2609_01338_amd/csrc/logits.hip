@@ -18,9 +18,10 @@
 // kernel.
 //
 // Measured (kernels, with penalties, biases, masks and tokens): 1 row of
-// 128256, 2048 tokens held, 6.2 + 1.9 us, all latency; 64 rows of 151936, 4096
-// tokens held, 25 + 4 us: 78 MB at 3.1 TB/s, where the logits' way alone, the
-// lists left out, takes 16.
+// 128256, 2048 tokens held, 5.9 + 1.9 us, all latency; 64 rows of 151936, 4096
+// tokens held, 25.2 us in all: 79 MB at 3.1 TB/s.  In a graph the same without
+// lists 18.2, with one token held 21.1 (LDS is cleared and read), 2048 23.0,
+// 4096 25.0, and with 300 biases 26.4.
 #include "mz_kernels.h"
 
 namespace mzk {

@@ -12,6 +12,9 @@
 // products run at an eighth of the time of the fp32 matrix instructions.
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
+// Measured: 1 row of 2048 x 2048, rank 16, 5.6 us, latency; 33 rows over 24
+// adapters, 4096 x 4096, rank 32, 4.2 + 5.5; 4099 rows over 6, rank 64, 19.7 +
+// 4.9 + 41.5: 171 MB at 2.6 TB/s.
 //  - Few rows (up to kGatherRows): a workgroup per (group of up to 16 rows of
 //    one adapter, K split or column range), found by each workgroup from the
 //    adapter list: row r begins a group when the rows before it with its
@@ -300,8 +303,9 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // Many rows: the same for a tile's rows.  x and A go through LDS, 64 of k at a
 // time, as whole 128-byte lines that are read once per workgroup (with
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
-// wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4);
-// two tiles of k are in flight while one is multiplied.  Wave w has rows 16 w
+// wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4,
+// and 19.7 with plan_tile); two tiles of k are in flight while one is
+// multiplied.  Wave w has rows 16 w
 // .. 16 w + 15.  The workgroups of a K range meet on one XCD where there are
 // eight ranges, so that each L2 holds its share of A.
 template <int NR>
@@ -634,7 +638,10 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
 }
 
 // Many rows, second product: half a tile's rows x 256 columns, 64 a wave, the
-// halves straight from memory.  Workgroups are numbered as above.
+// halves straight from memory.  Workgroups are numbered as above.  4099 rows of
+// 4096 columns, rank 64: 41.5 us, 3.2 TB/s of base and y, where base to y alone
+// takes 29 in this order; the rest is B, from the L2 for every half tile.  A
+// whole tile a workgroup 42.6, a quarter 48.8; the base's loads before B's 43.
 template <int NR>
 __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
   constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16;
@@ -653,13 +660,12 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
   if (__builtin_amdgcn_readfirstlane(rows[0]) < 0) return;       // a tile's rows fill it from the front
   const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
   const int first = __builtin_amdgcn_readfirstlane(rows[0]);
-  f32x4 y[NX][4];                          // goes out first, needed last
 #pragma unroll
   for (int i = 0; i < NX; ++i) {
     in[i] = rows[i] >= 0;
     if (!in[i]) rows[i] = first;           // loads of a row that exists stand in
-    load_base<4>(p, rows[i], c0, lg, whole, y[i]);
   }
+  f32x4 y[NX][4];
   if (with) {
     f16x8 hi[NX][KS], lo[NX][KS], b[KS][4];
     float unit[NX];
@@ -675,6 +681,8 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
     }
     const int rank = rank_of(p, a);
     load_b<KS, 4>(p, a, rank, c0, b);
+#pragma unroll
+    for (int i = 0; i < NX; ++i) load_base<4>(p, rows[i], c0, lg, whole, y[i]);
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       f32x4 d[4];
@@ -694,6 +702,9 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[i][c][e] = __builtin_fmaf(d[c][e], unit[i], y[i][c][e]);
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) load_base<4>(p, rows[i], c0, lg, whole, y[i]);
   }
 #pragma unroll
   for (int i = 0; i < NX; ++i)
