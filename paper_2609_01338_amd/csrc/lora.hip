@@ -21,8 +21,8 @@
 //    adapter fill whole groups.
 //  - Many rows: tiles of up to 64 rows of one adapter.  The workgroups of the
 //    first product count the adapter list and pick their tile's rows out of
-//    it, and leave the tiles to the second; between them a launch makes the
-//    halves of t once.  More than kPlanRows rows run as several such calls.
+//    it, and leave the tiles to the second.  More than kPlanRows rows run as
+//    several such calls.
 //  Either way rows may be mixed as they like: an adapter is read once per 16
 //  (64) of its rows.
 // A row's results depend on no other row: a row is one column (or row) of an
@@ -431,29 +431,7 @@ __device__ __forceinline__ void t_halves(f32x4 v, f16x4& hi, f16x4& lo, float& u
   unit = ldexpf(1.f, -up);
 }
 
-// Many rows: the halves of t, [m][32 KS] each, and every row's unit.
-template <int NR>
-__global__ __launch_bounds__(256) void lora_halves_kernel(Lora p) {
-  constexpr int RP = 16 * NR, LPR = RP / 4, W = (RP + 31) / 32 * 32;
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int r = (int)(idx / LPR), j = (int)(idx % LPR) * 4;
-  if (r >= p.m) return;
-  f16x4 hi, lo;
-  float unit;
-  t_halves<NR>(t_sum<NR>(p, r, j), hi, lo, unit);
-  _Float16 *h = p.hi + (int64_t)r * W + j, *l = p.lo + (int64_t)r * W + j;
-  *reinterpret_cast<f16x4*>(h) = hi;
-  *reinterpret_cast<f16x4*>(l) = lo;
-  if (RP < W) {
-    *reinterpret_cast<f16x4*>(h + RP) = f16x4{0, 0, 0, 0};
-    *reinterpret_cast<f16x4*>(l + RP) = f16x4{0, 0, 0, 0};
-  }
-  if (j == 0) p.unit[r] = unit;
-}
-
-// Few rows: the LDS copy of a group's halves, and its row of the output: CT
-// tiles of 16 columns from c0 for each wave.  The products run transposed,
-// D[column][row], so that a lane holds four neighbouring columns of one row.
+// The halves of a group's 16 rows in LDS.
 template <int NR>
 struct GroupHalves {
   static constexpr int RP = 16 * NR, KS = (RP + 31) / 32, PITCH = KS * 32 + 8;
@@ -637,49 +615,62 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
   if (c0 < p.n) expand_group<NR, CT>(p, a, rank, n, s_rows, s_t, c0, y);
 }
 
-// Many rows, second product: half a tile's rows x 256 columns, 64 a wave, the
-// halves straight from memory.  Workgroups are numbered as above.  4099 rows of
-// 4096 columns, rank 64: 41.5 us, 3.2 TB/s of base and y, where base to y alone
-// takes 29 in this order; the rest is B, from the L2 for every half tile.  A
-// whole tile a workgroup 42.6, a quarter 48.8; the base's loads before B's 43.
+// Many rows, second product: half a tile's rows x 256 columns, 64 a wave; the
+// workgroup adds the splits of its rows' t itself (a launch between the two
+// that made their halves once cost 1.5-4 us more, whatever the rows).
+// Workgroups are numbered as above.  4099 rows of 4096 columns, rank 64: @@ us,
+// where base to y alone takes 29 in this order; the rest is t and B, from the
+// L2 for every half tile.  A whole tile a workgroup is as fast, a quarter
+// slower by a seventh; the base's loads ahead of the others' slower.
 template <int NR>
 __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
-  constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16;
+  constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + 255) / 256;
+  __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t[NX];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int cols = (p.n + kColsWg - 1) / kColsWg, rest = blockIdx.x >> 3;
   const int block = rest / cols * 8 + (blockIdx.x & 7), c0 = rest % cols * kColsWg + w * 64;
-  if (block >= 2 * p.tiles || c0 >= p.n) return;
+  if (block >= 2 * p.tiles) return;
   const int a = __builtin_amdgcn_readfirstlane(p.tile_adapter[block / 2]);
   const bool with = has_adapter(p, a);
   if (a < 0 || (!with && p.y == p.base)) return;
+  const int32_t* list = p.tile_rows + block * ROWS;
+  const int first = __builtin_amdgcn_readfirstlane(list[0]);
+  if (first < 0) return;                   // a tile's rows fill it from the front
   int rows[NX];
   bool in[NX];
 #pragma unroll
-  for (int i = 0; i < NX; ++i) rows[i] = p.tile_rows[block * ROWS + i * 16 + col];
-  if (__builtin_amdgcn_readfirstlane(rows[0]) < 0) return;       // a tile's rows fill it from the front
-  const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
-  const int first = __builtin_amdgcn_readfirstlane(rows[0]);
-#pragma unroll
   for (int i = 0; i < NX; ++i) {
+    rows[i] = list[i * 16 + col];
     in[i] = rows[i] >= 0;
     if (!in[i]) rows[i] = first;           // loads of a row that exists stand in
   }
+  const bool whole = c0 + 64 <= p.n;       // no column of the wave lies past n
   f32x4 y[NX][4];
   if (with) {
-    f16x8 hi[NX][KS], lo[NX][KS], b[KS][4];
-    float unit[NX];
+    f32x4 t[PER];
+    int at[PER];
 #pragma unroll
-    for (int i = 0; i < NX; ++i) {
-#pragma unroll
-      for (int j = 0; j < KS; ++j) {
-        const int64_t at = (int64_t)rows[i] * (KS * 32) + j * 32 + lg * 8;
-        hi[i][j] = *reinterpret_cast<const f16x8*>(p.hi + at);
-        lo[i][j] = *reinterpret_cast<const f16x8*>(p.lo + at);
-      }
-      unit[i] = p.unit[rows[i]];
+    for (int e = 0; e < PER; ++e) {
+      const int r = list[min((int)(threadIdx.x + 256 * e) / (4 * NR), ROWS - 1)];
+      at[e] = r < 0 ? first : r;
+      t[e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+#pragma unroll(NR <= 4 ? 8 : 4)      // as many loads in flight as registers hold
+    for (int s = 0; s < p.n_split; ++s)
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        t[e] += *reinterpret_cast<const f32x4*>(p.t + ((int64_t)s * p.m + at[e]) * (16 * NR) + threadIdx.x % (4 * NR) * 4);
+    const float scale = p.scale ? p.scale[a] : 1.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int i = (threadIdx.x + 256 * e) / (4 * NR);
+      if (i < ROWS) s_t[i / 16].put(i % 16, threadIdx.x % (4 * NR) * 4, t[e] * scale);
+    }
+    __syncthreads();
+    if (c0 >= p.n) return;
     const int rank = rank_of(p, a);
+    f16x8 b[KS][4];
     load_b<KS, 4>(p, a, rank, c0, b);
 #pragma unroll
     for (int i = 0; i < NX; ++i) load_base<4>(p, rows[i], c0, lg, whole, y[i]);
@@ -691,18 +682,22 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
         if (j * 32 >= rank) break;
+        const f16x8 lo = *reinterpret_cast<const f16x8*>(&s_t[i].lo[col][j * 32 + lg * 8]);
+        const f16x8 hi = *reinterpret_cast<const f16x8*>(&s_t[i].hi[col][j * 32 + lg * 8]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo[i][j], d[c], 0, 0, 0);
-          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi[i][j], d[c], 0, 0, 0);
+          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo, d[c], 0, 0, 0);
+          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi, d[c], 0, 0, 0);
         }
       }
+      const float unit = s_t[i].unit[col];
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][c][e] = __builtin_fmaf(d[c][e], unit[i], y[i][c][e]);
+        for (int e = 0; e < 4; ++e) y[i][c][e] = __builtin_fmaf(d[c][e], unit, y[i][c][e]);
     }
   } else {
+    if (c0 >= p.n) return;
 #pragma unroll
     for (int i = 0; i < NX; ++i) load_base<4>(p, rows[i], c0, lg, whole, y[i]);
   }
@@ -735,7 +730,6 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
     hipLaunchKernelGGL(lora_expand_kernel<NR>, grid(p.m), dim3(256), 0, s, p);
   } else {
     hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, p.tiles), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(lora_halves_kernel<NR>, dim3((p.m * 4 * NR + 255) / 256), dim3(256), 0, s, p);
     hipLaunchKernelGGL(lora_expand_tile_kernel<NR>, grid(2 * p.tiles), dim3(256), 0, s, p);
   }
 }
@@ -766,7 +760,7 @@ int lora_splits(int m, int k) {
 // The workspace of a call of up to m <= kPlanRows rows: every part grows with
 // m, so that one for the largest call serves all.
 struct LoraWs {
-  int64_t t, hi, lo, unit, tile_adapter, tile_rows, bytes;
+  int64_t t, tile_adapter, tile_rows, bytes;
 };
 LoraWs lora_ws(int m, int k, int R, int n_adapters) {
   LoraWs w{};
@@ -776,14 +770,11 @@ LoraWs lora_ws(int m, int k, int R, int n_adapters) {
     at += (bytes + 15) / 16 * 16;
     return here;
   };
-  const int64_t rp = rank_tiles(R) * 16, wide = (rp + 31) / 32 * 32;
+  const int64_t rp = rank_tiles(R) * 16;
   // splits x rows of t: at most the workgroups wanted times a group's rows
   const int64_t most = m <= kGatherRows ? kFewBlocks : kManyBlocks * kTile, all = (int64_t)most_splits(k) * m;
   w.t = take((all < most ? all : most) * rp * 4);
   if (m > kGatherRows) {
-    w.hi = take(m * wide * 2);
-    w.lo = take(m * wide * 2);
-    w.unit = take((int64_t)m * 4);
     w.tile_adapter = take((int64_t)most_tiles(m, n_adapters) * 4);
     w.tile_rows = take((int64_t)most_tiles(m, n_adapters) * kTile * 4);
   }
@@ -815,9 +806,6 @@ void launch_lora(Lora p, void* ws, hipStream_t s) {
     const LoraWs w = lora_ws(q.m, q.k, q.R, q.n_adapters);
     uint8_t* b = reinterpret_cast<uint8_t*>(ws);
     q.t = reinterpret_cast<float*>(b + w.t);
-    q.hi = reinterpret_cast<_Float16*>(b + w.hi);
-    q.lo = reinterpret_cast<_Float16*>(b + w.lo);
-    q.unit = reinterpret_cast<float*>(b + w.unit);
     q.tile_adapter = reinterpret_cast<int32_t*>(b + w.tile_adapter);
     q.tile_rows = reinterpret_cast<int32_t*>(b + w.tile_rows);
     q.tiles = most_tiles(q.m, q.n_adapters);

@@ -212,8 +212,6 @@ struct Lora {
   int64_t y_stride;
   int m, k, n, R, n_adapters;
   float* t;          // [n_split][m][R rounded up] partials of x A^T
-  _Float16 *hi, *lo; // many rows: t in two halves, and what each row of them
-  float* unit;       // is multiplied by
   int32_t *tile_adapter, *tile_rows;   // [tiles] (-1: not there), [tiles][64]
   int n_split, tiles;
 };
