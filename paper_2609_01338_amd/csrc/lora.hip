@@ -36,6 +36,8 @@ namespace {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));      // the adapter list begins anywhere
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
 // Rows up to which groups are searched.  Groups against tiles, measured in a
 // graph, 4096 x 4096 of rank 16: 33 rows of one adapter 9.4 against 12.8 us,
@@ -67,11 +69,11 @@ __device__ __forceinline__ int gather_group(const Lora& p, int r, int a, int* ro
   return min(__popcll(mask) - before, 16);
 }
 
-// LDS of plan_tile: the call's adapters, where in each window of 64 rows the
-// adapter changes, how many rows each adapter has.
+// LDS of plan_tile: the call's adapters, where the adapter changes (or a window
+// of 64 rows begins), how many rows each adapter has.
 struct PlanLds {
   uint16_t list[kPlanRows];
-  uint64_t change[kPlanRows / 64];
+  uint8_t change[kPlanRows / 4];         // bit e: row 4 i + e
   int hist[kLoraAdapters + 1];
 };
 
@@ -85,43 +87,69 @@ __host__ __device__ inline int most_runs(int m) {
   return windows + windows / 4 + 8;
 }
 
+// Four nibbles, one a byte, together.
+__device__ __forceinline__ uint64_t sixteen(uint32_t d) {
+  const uint32_t x = d | d >> 4;
+  return (x & 0xff) | (x >> 8 & 0xff00);
+}
+
 // The rows of tile `tile`, of one adapter (p.n_adapters: none): the adapter,
 // the rows (LDS, written up to the count) and the count, 0 where there is no
 // such tile.  Where rows of one adapter follow each other (prompts), the runs
 // within windows of 64 rows are the tiles.  Else the rows are taken as sorted
 // by adapter, each adapter's in their order and in tiles of their own: counted
 // in LDS, then the tile's picked by their rank.  Every thread of 256 takes
-// part, and every workgroup comes to the same tiles.  (Loops over the list are
-// kept short: unrolled, their code took longer to fetch than to run.)
+// part, and every workgroup comes to the same tiles.  (The sort's loops over
+// the list are kept short: unrolled, their code took longer to fetch than to
+// run.)
 __device__ __forceinline__ int plan_tile(const Lora& p, int tile, PlanLds& s, int* rows, int& adapter) {
   __shared__ int s_red[4], s_found[2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int buckets = p.n_adapters + 1, chunks = (p.m + 255) / 256;  // 64-row chunks of a wave
   const int r0 = w * chunks * 64, r1 = min(r0 + chunks * 64, p.m);   // this wave's rows
   const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-  constexpr int AHEAD = 8;
-#pragma unroll 1
-  for (int base = 0; base < p.m; base += 256 * AHEAD) {
-    int v[AHEAD];
+  constexpr int AHEAD = kPlanRows / 1024;    // 16 bytes of the list a thread each: all of it in one trip
+  i32x4 v[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) v[i] = p.adapter[min(base + 256 * i + (int)threadIdx.x, p.m - 1)];
+  for (int i = 0; i < AHEAD; ++i) {
+    const int r = 1024 * i + 4 * (int)threadIdx.x;
+    if (1024 * i >= p.m) break;
+    if (r + 4 <= p.m) {
+      v[i] = *reinterpret_cast<const i32x4*>(p.adapter + r);
+    } else {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int r = base + 256 * i + threadIdx.x;
-      const bool in = r < p.m;
-      const int mine = has_adapter(p, v[i]) ? v[i] : p.n_adapters, prev = __shfl_up(mine, 1);
-      if (in) s.list[r] = (uint16_t)mine;
-      const uint64_t change = __ballot(in && (lane == 0 || mine != prev));
-      if (lane == 0 && in) s.change[r / 64] = change;
+      for (int e = 0; e < 4; ++e) v[i][e] = r + e < p.m ? p.adapter[r + e] : -1;
     }
+  }
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int r = 1024 * i + 4 * (int)threadIdx.x;
+    if (1024 * i >= p.m) break;
+    u16x4 mine;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine[e] = (uint16_t)(has_adapter(p, v[i][e]) ? v[i][e] : p.n_adapters);
+    int prev = __shfl_up((int)mine[3], 1), change = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (r + e < p.m && ((r + e) % 64 == 0 || mine[e] != prev)) change |= 1 << e;
+      prev = mine[e];
+    }
+    *reinterpret_cast<u16x4*>(&s.list[r]) = mine;
+    s.change[r / 4] = (uint8_t)change;
   }
   if (threadIdx.x == 0) s_found[0] = -1;
   __syncthreads();
   {  // lane l: windows 2 l and 2 l + 1
     static_assert(kPlanRows / 64 == 128, "windows of a wave's lanes");
-    const int windows = (p.m + 63) / 64;
-    const int c0 = 2 * lane < windows ? __popcll(s.change[2 * lane]) : 0;
-    const int c1 = 2 * lane + 1 < windows ? __popcll(s.change[2 * lane + 1]) : 0;
+    uint64_t change[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      change[i] = 0;
+      if ((2 * lane + i) * 64 >= p.m) continue;
+      const uint4 d = *reinterpret_cast<const uint4*>(&s.change[(2 * lane + i) * 16]);
+      change[i] = sixteen(d.x) | sixteen(d.y) << 16 | sixteen(d.z) << 32 | sixteen(d.w) << 48;
+    }
+    const int c0 = __popcll(change[0]), c1 = __popcll(change[1]);
     int sum = c0 + c1;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -135,15 +163,18 @@ __device__ __forceinline__ int plan_tile(const Lora& p, int tile, PlanLds& s, in
       const int l = __builtin_ctzll(__ballot(tile < sum));         // the first window pair that ends past the tile
       int nth = tile - __builtin_amdgcn_readlane(first, l), window = 2 * l;
       const int in_first = __builtin_amdgcn_readlane(c0, l);
+      uint64_t starts = change[0];
       if (nth >= in_first) {
         nth -= in_first;
         ++window;
+        starts = change[1];
       }
-      uint64_t change = s.change[window];
-      for (; nth > 0; --nth) change &= change - 1;
-      const int start = __builtin_ctzll(change);
-      change &= change - 1;
-      const int r = window * 64 + start, end = min(window * 64 + (change ? (int)__builtin_ctzll(change) : 64), p.m);
+      starts = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(starts >> 32), l) << 32 |
+               (unsigned)__builtin_amdgcn_readlane((int)starts, l);
+      for (; nth > 0; --nth) starts &= starts - 1;
+      const int start = __builtin_ctzll(starts);
+      starts &= starts - 1;
+      const int r = window * 64 + start, end = min(window * 64 + (starts ? (int)__builtin_ctzll(starts) : 64), p.m);
       adapter = __builtin_amdgcn_readfirstlane(s.list[r]);
       if (threadIdx.x < 64 && r + lane < end) rows[lane] = r + lane;
       __syncthreads();
