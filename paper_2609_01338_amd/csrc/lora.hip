@@ -47,7 +47,7 @@ typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 constexpr int kGatherRows = 64;
 constexpr int kPlanRows = 8192;      // rows of a call whose tiles are counted: 32 entries a thread
 constexpr int kTile = 64;            // rows of a tile
-constexpr int kColsWg = 256;         // columns of a workgroup of the second product: 64 a wave
+constexpr int kColsWg = 256;         // columns of a workgroup of few rows' second product: 64 a wave
 constexpr int kColsFused = 128;      // the same where one launch does both: 32 a wave
 
 __device__ __forceinline__ bool has_adapter(const Lora& p, int a) { return (unsigned)a < (unsigned)p.n_adapters; }
@@ -646,21 +646,21 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
   if (c0 < p.n) expand_group<NR, CT>(p, a, rank, n, s_rows, s_t, c0, y);
 }
 
-// Many rows, second product: half a tile's rows x 256 columns, 64 a wave; the
+// Many rows, second product: half a tile's rows x COLS columns, 64 a wave; the
 // workgroup adds the splits of its rows' t itself (a launch between the two
 // that made their halves once cost 1.5-4 us more, whatever the rows).
-// Workgroups are numbered as above.  4099 rows of 4096 columns, rank 64: @@ us,
+// Workgroups are numbered as above.  4099 rows of 4096 columns, rank 64: 41 us,
 // where base to y alone takes 29 in this order; the rest is t and B, from the
 // L2 for every half tile.  A whole tile a workgroup is as fast, a quarter
 // slower by a seventh; the base's loads ahead of the others' slower.
-template <int NR>
-__global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
-  constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + 255) / 256;
+template <int NR, int COLS>
+__global__ __launch_bounds__(COLS) void lora_expand_tile_kernel(Lora p) {
+  constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + COLS - 1) / COLS;
   __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t[NX];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
-  const int cols = (p.n + kColsWg - 1) / kColsWg, rest = blockIdx.x >> 3;
-  const int block = rest / cols * 8 + (blockIdx.x & 7), c0 = rest % cols * kColsWg + w * 64;
+  const int cols = (p.n + COLS - 1) / COLS, rest = blockIdx.x >> 3;
+  const int block = rest / cols * 8 + (blockIdx.x & 7), c0 = rest % cols * COLS + w * 64;
   if (block >= 2 * p.tiles) return;
   const int a = __builtin_amdgcn_readfirstlane(p.tile_adapter[block / 2]);
   const bool with = has_adapter(p, a);
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
     int at[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const int r = list[min((int)(threadIdx.x + 256 * e) / (4 * NR), ROWS - 1)];
+      const int r = list[min((int)(threadIdx.x + COLS * e) / (4 * NR), ROWS - 1)];
       at[e] = r < 0 ? first : r;
       t[e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -695,7 +695,7 @@ __global__ __launch_bounds__(256) void lora_expand_tile_kernel(Lora p) {
     const float scale = p.scale ? p.scale[a] : 1.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const int i = (threadIdx.x + 256 * e) / (4 * NR);
+      const int i = (threadIdx.x + COLS * e) / (4 * NR);
       if (i < ROWS) s_t[i / 16].put(i % 16, threadIdx.x % (4 * NR) * 4, t[e] * scale);
     }
     __syncthreads();
@@ -750,18 +750,28 @@ bool lora_fused(const Lora& p) {
   return p.m <= kGatherRows && a_bytes <= (64 << 10) && a_bytes * ranges * p.m <= (16 << 20);
 }
 
+// The second product of many rows in ranges of 512 columns: halves what its
+// workgroups read of t, where ranks are many and the workgroups still fill the
+// chip.  512 against 256, both launches, 4096 x 4096, 4 adapters: rank 64, 4096
+// rows 50.4 against 53.9 us, 1024 (512 workgroups of 256) 22.5 against 23.7, 512
+// rows 19.6 against 18.9; rank 128, 4096 rows 71.2 against 76.4; rank 16 42.2
+// against 42.0.
+bool lora_wide(const Lora& p) { return (int64_t)(p.m + kTile / 2 - 1) / (kTile / 2) * ((p.n + 255) / 256) >= 512; }
+
 template <int NR>
 void launch_lora_nr(const Lora& p, hipStream_t s) {
-  const int cols = (p.n + kColsWg - 1) / kColsWg;
-  auto grid = [&](int blocks) { return dim3((unsigned)((blocks + 7) / 8 * 8 * cols)); };
+  auto grid = [&](int blocks, int cols) { return dim3((unsigned)((blocks + 7) / 8 * 8 * ((p.n + cols - 1) / cols))); };
   if (lora_fused(p)) {
     hipLaunchKernelGGL(lora_fused_kernel<NR>, dim3((p.n + kColsFused - 1) / kColsFused, p.m), dim3(256), 0, s, p);
   } else if (p.m <= kGatherRows) {
     hipLaunchKernelGGL(lora_shrink_kernel<NR>, dim3(p.m, p.n_split), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(lora_expand_kernel<NR>, grid(p.m), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(lora_expand_kernel<NR>, grid(p.m, kColsWg), dim3(256), 0, s, p);
   } else {
     hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, p.tiles), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(lora_expand_tile_kernel<NR>, grid(2 * p.tiles), dim3(256), 0, s, p);
+    if (NR >= 4 && lora_wide(p))
+      hipLaunchKernelGGL((lora_expand_tile_kernel<NR, 512>), grid(2 * p.tiles, 512), dim3(512), 0, s, p);
+    else
+      hipLaunchKernelGGL((lora_expand_tile_kernel<NR, 256>), grid(2 * p.tiles, 256), dim3(256), 0, s, p);
   }
 }
 
@@ -818,7 +828,7 @@ LoraWs lora_ws(int m, int k, int R, int n_adapters) {
 bool lora_fits(int m, int n, int n_adapters) {
   const int rows = m < kPlanRows ? m : kPlanRows;
   const int64_t blocks = rows <= kGatherRows ? rows : 2 * most_tiles(rows, n_adapters);
-  return (blocks + 7) / 8 * 8 * ((n - 1) / kColsWg + 1) <= kMaxBlocks;
+  return (blocks + 7) / 8 * 8 * ((n - 1) / 512 + 1) * 2 <= kMaxBlocks;      // in 256 threads
 }
 
 int64_t lora_ws_bytes(int m, int k, int R, int n_adapters) {

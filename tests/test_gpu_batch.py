@@ -605,6 +605,58 @@ def test_lora_many_adapters(m):
     lora_case(rng.integers(-3, 2050, m), 16, 12, 8, 2047, seed=m + 1)
 
 
+@pytest.mark.parametrize("m,n,R", [(1024, 4100, 64), (1030, 4097, 104), (2100, 2048, 128)])
+def test_lora_many_rows_and_columns(m, n, R):
+    """Wide ranges of the second product, the last of them short."""
+    rng = np.random.default_rng(m)
+    lora_case(rng.integers(-1, 3, m), 40, n, R, 3, seed=m, stride=(n + 7) // 4 * 4)
+    lora_case(np.arange(m) * 4 // m - 1, 24, n, R, 3, seed=m + 1)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_lora_list_off_16_bytes(shift):
+    torch = torch_cuda()
+    rng = np.random.default_rng(34)
+    for m in (66, 1027):
+        x, adapter, a, b, scale, rank, base, n = lora_inputs(rng.integers(-1, 3, m), 64, 32, 16, 3, seed=35)
+        need = mz.mz_lora_workspace_bytes(m, 64, 16, 3)
+        ws = torch.full((need // 4,), float("nan"), device="cuda")
+        ids = torch.full((shift + m,), 1, device="cuda", dtype=torch.int32)
+        ids[shift:] = dev(adapter)
+        d = [dev(v) for v in (x, a, b, scale, rank, base)]
+        y = torch.zeros(base.shape, device="cuda")
+        mz.mz_lora_add(d[0].data_ptr(), m, 64, ids[shift:].data_ptr(), 3, d[1].data_ptr(), d[2].data_ptr(), 16, n, d[5].data_ptr(),
+                       y.data_ptr(), base.shape[1], ws.data_ptr(), need, stream(), scale_ptr=d[3].data_ptr(),
+                       rank_ptr=d[4].data_ptr())
+        torch.cuda.synchronize()
+        close(y, *lora_oracle(x, adapter, a, b, scale, rank, base, n), f"{m} rows")
+
+
+def test_lora_many_rows_replayed_over_other_lists():
+    """One graph of 500 rows: lists in runs, mixed, of one adapter and of none."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(36)
+    m, k, na = 500, 128, 5
+    x, adapter, a, b, scale, rank, base, n = lora_inputs([0] * m, k, 300, 64, na, seed=36, ranks=[64, 9, 0, 33, 48])
+    need = mz.mz_lora_workspace_bytes(m, k, 64, na)
+    ws = torch.full((need // 4,), float("nan"), device="cuda")
+    d = [dev(v) for v in (x, adapter, a, b, scale, rank, base)]
+    y = torch.zeros(base.shape, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        mz.mz_lora_add(d[0].data_ptr(), m, k, d[1].data_ptr(), na, d[2].data_ptr(), d[3].data_ptr(), 64, n, d[6].data_ptr(),
+                       y.data_ptr(), base.shape[1], ws.data_ptr(), need, stream(), scale_ptr=d[4].data_ptr(),
+                       rank_ptr=d[5].data_ptr())
+    for ids in (np.arange(m) * na // m, rng.integers(-1, na, m), np.full(m, 3), np.full(m, -1), np.arange(m) // 7 % na):
+        ids = ids.astype(np.int32)
+        d[1].copy_(dev(ids))
+        y.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        ref, bound = lora_oracle(x, ids, a, b, scale, rank, base, n)
+        close(y[:, :n], ref[:, :n], bound[:, :n], "y")
+
+
 def test_lora_without_scales_and_ranks():
     x, adapter, a, b, scale, rank, base, n = lora_inputs([1, 0, -1, 1, 1], 96, 48, 16, 2, seed=27, ranks=[16, 16])
     ref, bound = lora_oracle(x, adapter, a, b, None, None, base, n)
