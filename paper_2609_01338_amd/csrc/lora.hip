@@ -13,8 +13,8 @@
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
 // Measured: 1 row of 2048 x 2048, rank 16, 5.6 us, latency; 33 rows over 24
-// adapters, 4096 x 4096, rank 32, 4.2 + 5.5; 4099 rows over 6, rank 64, 19.7 +
-// 4.9 + 41.5: 171 MB at 2.6 TB/s.
+// adapters, 4096 x 4096, rank 32, 4.2 + 5.5; 4099 rows over 6, rank 64, 18.9 +
+// 41.8: 171 MB at 2.9 TB/s.
 //  - Few rows (up to kGatherRows): a workgroup per (group of up to 16 rows of
 //    one adapter, K split or column range), found by each workgroup from the
 //    adapter list: row r begins a group when the rows before it with its
@@ -40,10 +40,11 @@ typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));      // the a
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
 // Rows up to which groups are searched.  Groups against tiles, measured in a
-// graph, 4096 x 4096 of rank 16: 33 rows of one adapter 9.4 against 12.8 us,
-// with an adapter each 8.7 against 15.7; 64 rows 13.0 against 13.1, 10.8 against
-// 19.8; 128 rows 16.7 against 13.7, 12.1 against 20.5.  4096 x 14336, rank 32,
-// 128 rows: one adapter 33.6 against 19.2, 64 adapters 25.5 against 37.5.
+// graph, 4096 x 4096 of rank 16: 33 rows of one adapter 9.6 against 11.2 us,
+// with an adapter each 8.6 against 15.9; 64 rows 13.0 against 11.6, over 8 mixed
+// adapters 8.7 against 11.5, with an adapter each 10.5 against 20.7.  4096 x
+// 14336, rank 32, 64 rows: 21.2 against 16.6, 10.7 against 16.5, 24.3 against
+// 45.8.  At 128 rows the first kind is nearly twice as slow.
 constexpr int kGatherRows = 64;
 constexpr int kPlanRows = 8192;      // rows of a call whose tiles are counted: 32 entries a thread
 constexpr int kTile = 64;            // rows of a tile
@@ -79,12 +80,13 @@ struct PlanLds {
 
 // Runs of one adapter, each within a window of 64 rows, that make the tiles as
 // they stand; with more of them the rows are sorted.  As they stand against
-// sorted, 4096 rows of 4096 x 4096, rank 64: runs of 64 rows (as many as
-// windows) 62.7 against 76.4 us, of 100 (1.3 a window) 78 against 85, of 48
-// (1.5) 89 against 79, of 24 (3) 118 against 79.
+// sorted, 4096 rows of 4096 x 4096, rank 64 (16): runs of 64 rows (as many as
+// windows) 56.6 (43.5) against 69.4 (57.6) us, of 100 (1.6 a window) 70.8
+// (52.5) against 81.3 (63.8), of 48 (2) 79.2 (59.5) against 73.9 (59.7), of 24
+// (3.3) 109 (77) against 72 (59).
 __host__ __device__ inline int most_runs(int m) {
   const int windows = (m + 63) / 64;
-  return windows + windows / 4 + 8;
+  return windows + windows * 3 / 4 + 8;
 }
 
 // Four nibbles, one a byte, together.
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // time, as whole 128-byte lines that are read once per workgroup (with
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
 // wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4,
-// and 19.7 with plan_tile); two tiles of k are in flight while one is
+// and 18.9 with plan_tile); two tiles of k are in flight while one is
 // multiplied.  Wave w has rows 16 w
 // .. 16 w + 15.  The workgroups of a K range meet on one XCD where there are
 // eight ranges, so that each L2 holds its share of A.
@@ -781,20 +783,21 @@ int most_tiles(int m, int n_adapters) {
   return sorted > runs ? sorted : runs;
 }
 
-// K splits: enough workgroups for the chip, at least two steps of 32 a wave,
-// at most 16.  With at most 8, 1 row of 8960 x 1536, rank 64, takes 11.3 for 9.7
-// us, 512 rows of 14336 x 4096, rank 16, 24.7 for 20.2; with 32 18.8.  Half the
-// workgroups for many rows: 4096 of the latter 67.8 for 58.2; twice: 59.3.
+// K splits: enough workgroups for the chip, at least two steps of 32 a wave, at
+// most 16 (few rows) or 32.  With at most 8, 1 row of 8960 x 1536, rank 64,
+// takes 11.2 for 9.8 us, 512 rows of 14336 x 4096, rank 16, 22.1, with 16 17.8,
+// with 32 16.2; 33 rows of the latter with 32 12.5 for 11.6.  Half the
+// workgroups for many rows: 4096 of the latter 64.2 for 53.7 us; twice: 55.2.
 constexpr int kFewBlocks = 1024, kManyBlocks = 520;
 
-int most_splits(int k) {
-  const int most = (k + 31) / 32 / 8;
-  return most < 1 ? 1 : most > 16 ? 16 : most;
+int most_splits(int m, int k) {
+  const int most = (k + 31) / 32 / 8, cap = m <= kGatherRows ? 16 : 32;
+  return most < 1 ? 1 : most > cap ? cap : most;
 }
 
 int lora_splits(int m, int k) {
   const int groups = m <= kGatherRows ? m : (m - 1) / kTile + 1;
-  const int want = (m <= kGatherRows ? kFewBlocks : kManyBlocks) / groups, most = most_splits(k);
+  const int want = (m <= kGatherRows ? kFewBlocks : kManyBlocks) / groups, most = most_splits(m, k);
   return want < 1 ? 1 : want > most ? most : want;
 }
 
@@ -813,7 +816,7 @@ LoraWs lora_ws(int m, int k, int R, int n_adapters) {
   };
   const int64_t rp = rank_tiles(R) * 16;
   // splits x rows of t: at most the workgroups wanted times a group's rows
-  const int64_t most = m <= kGatherRows ? kFewBlocks : kManyBlocks * kTile, all = (int64_t)most_splits(k) * m;
+  const int64_t most = m <= kGatherRows ? kFewBlocks : kManyBlocks * kTile, all = (int64_t)most_splits(m, k) * m;
   w.t = take((all < most ? all : most) * rp * 4);
   if (m > kGatherRows) {
     w.tile_adapter = take((int64_t)most_tiles(m, n_adapters) * 4);
