@@ -653,7 +653,8 @@ typedef struct {
  * come in any order, a whole prompt or one row per sequence.  A row whose seq
  * is outside 0..n_seq-1 (padding), or whose pos is outside 0..n_rope-1 or the
  * table, writes nothing, its row of q_out included; one whose chunk's entry is
- * outside 0..n_slots-1 writes its query only.  The caller sees that no two
+ * outside 0..n_slots-1 writes its query only.  q_out and the slab share nothing
+ * with the rows that are read.  The caller sees that no two
  * rows name the same position of a sequence and that no two sequences share
  * a chunk that is written.  m may be 0.  Errors: EINVAL for a NULL pointer,
  * sizes or heads out of range, a stride below the row, n_table * chunk_tokens
@@ -700,7 +701,7 @@ int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int
  * may be base itself, else the two share no value.  a: device f16 [n_adapters][max_rank][k], b: device f16
  * [n_adapters][n][max_rank]; of adapter a the first rank[a] ranks count
  * (device int32 [n_adapters], clamped to 0..max_rank; NULL: all), whatever
- * the others hold.  scale: device float [n_adapters] (NULL: 1).  adapter:
+ * the others hold.  scale: device float [n_adapters], finite (NULL: 1).  adapter:
  * device int32 [m], in any order; a row whose entry is outside
  * 0..n_adapters-1 has none: its y is the base's (in place it is not
  * touched).  Rows do not affect each other.  Nothing is rounded to f16 on the

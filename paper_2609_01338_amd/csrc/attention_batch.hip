@@ -133,12 +133,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_batch_kernel(AttnBatch a)
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(s_at[0]), first = __builtin_amdgcn_readfirstlane(s_at[1]) * a.nkv;
 
+  int len = seq_len(a, b);
   while (u < u_end) {
-    const int len = seq_len(a, b), nu = (len + kUnit - 1) / kUnit;
-    if (u >= first + nu * a.nkv) {       // past this sequence (or it is empty)
+    int nu = (len + kUnit - 1) / kUnit;
+    if (u >= first + nu * a.nkv) {       // past this sequence: on to the next that has keys, 64 in a look
       first += nu * a.nkv;
-      ++b;
-      continue;
+      uint64_t some = 0;
+      for (++b; !some; b += some ? __builtin_ctzll(some) : 64) {
+        len = b + lane < a.n_seq ? seq_len(a, b + lane) : 1;
+        some = __ballot(len > 0);
+      }
+      len = __builtin_amdgcn_readlane(len, __builtin_ctzll(some));
+      nu = (len + kUnit - 1) / kUnit;
     }
     const int h = (u - first) / nu, t0 = u - first - h * nu, t1 = min(nu, t0 + u_end - u);
     u += t1 - t0;

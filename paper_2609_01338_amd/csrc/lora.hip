@@ -338,9 +338,9 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
 // wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4,
 // and 18.9 with plan_tile); two tiles of k are in flight while one is
-// multiplied.  Wave w has rows 16 w
-// .. 16 w + 15.  The workgroups of a K range meet on one XCD where there are
-// eight ranges, so that each L2 holds its share of A.
+// multiplied.  Wave w has rows 16 w .. 16 w + 15.  The workgroups of a K range
+// meet on one XCD where there are a multiple of eight ranges, so that each L2
+// holds its share of A.
 template <int NR>
 __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
   constexpr int RP = 16 * NR, KT = 64, PITCH = KT + 8, DEPTH = 2;
@@ -770,10 +770,13 @@ void launch_lora_nr(const Lora& p, hipStream_t s) {
     hipLaunchKernelGGL(lora_expand_kernel<NR>, grid(p.m, kColsWg), dim3(256), 0, s, p);
   } else {
     hipLaunchKernelGGL(lora_shrink_tile_kernel<NR>, dim3(p.n_split, p.tiles), dim3(256), 0, s, p);
-    if (NR >= 4 && lora_wide(p))
-      hipLaunchKernelGGL((lora_expand_tile_kernel<NR, 512>), grid(2 * p.tiles, 512), dim3(512), 0, s, p);
-    else
-      hipLaunchKernelGGL((lora_expand_tile_kernel<NR, 256>), grid(2 * p.tiles, 256), dim3(256), 0, s, p);
+    if constexpr (NR >= 4) {
+      if (lora_wide(p)) {
+        hipLaunchKernelGGL((lora_expand_tile_kernel<NR, 512>), grid(2 * p.tiles, 512), dim3(512), 0, s, p);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((lora_expand_tile_kernel<NR, 256>), grid(2 * p.tiles, 256), dim3(256), 0, s, p);
   }
 }
 

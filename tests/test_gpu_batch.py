@@ -352,6 +352,16 @@ def test_attention_sharp_and_flat():
     attention_case([9000], 64, 4, 1, 64, seed=8, spread=0.01)
 
 
+@pytest.mark.parametrize("n_seq", [63, 64, 65, 257, 700])
+def test_attention_padded_batch(n_seq):
+    """Few sequences with keys, far apart, first and last or in the middle: shares span runs of empty ones."""
+    for at in ([0, n_seq - 1], [n_seq // 2], [1, 2, n_seq - 62, n_seq - 2] if n_seq > 64 else [5, 40]):
+        lens = [0] * n_seq
+        for i, b in enumerate(at):
+            lens[b] = 130 + 97 * i
+        attention_case(lens, 16, 4, 2, 64, seed=n_seq)
+
+
 def test_attention_lengths_outside_the_table():
     a = list(attention_inputs([64, 40, 16], 16, 4, 2, 64, seed=9, extra_table=-1))
     assert a[3].shape[1] == 4
