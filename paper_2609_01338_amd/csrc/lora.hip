@@ -13,8 +13,8 @@
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
 // Measured: 1 row of 2048 x 2048, rank 16, 5.6 us, latency; 33 rows over 24
-// adapters, 4096 x 4096, rank 32, 4.2 + 5.5; 4099 rows over 6, rank 64, 18.9 +
-// 41.8: 171 MB at 2.9 TB/s.
+// adapters, 4096 x 4096, rank 32, 4.2 + 5.5; 4099 rows over 6, rank 64, 18.1 +
+// 41.5: 171 MB at 2.9 TB/s.
 //  - Few rows (up to kGatherRows): a workgroup per (group of up to 16 rows of
 //    one adapter, K split or column range), found by each workgroup from the
 //    adapter list: row r begins a group when the rows before it with its
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // time, as whole 128-byte lines that are read once per workgroup (with
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
 // wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4,
-// and 18.9 with plan_tile); two tiles of k are in flight while one is
+// and 18.1 with plan_tile); two tiles of k are in flight while one is
 // multiplied.  Wave w has rows 16 w .. 16 w + 15.  The workgroups of a K range
 // meet on one XCD where there are a multiple of eight ranges, so that each L2
 // holds its share of A.
@@ -393,32 +393,37 @@ __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
   f32x4 acc[NR];
 #pragma unroll
   for (int j = 0; j < NR; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // one tile of k: its loads' registers take those of the tile DEPTH later
+  auto step = [&](int i, int tile, bool more) {
+    const int buf = tile & 1;
 #pragma unroll
-  for (int i = 0; i < DEPTH; ++i) load(i, min(i, nt - 1));
-  for (int tb = 0; tb < nt; tb += DEPTH) {
+    for (int e = 0; e < NXL; ++e) *reinterpret_cast<f16x8*>(&s_x[buf][(tid >> 3) + 32 * e][seg]) = xr[i][e];
 #pragma unroll
-    for (int i = 0; i < DEPTH; ++i) {
-      const int tile = tb + i, buf = tile & 1;
-      if (tile >= nt) break;
+    for (int e = 0; e < NAL; ++e)
+      if ((tid >> 3) + 32 * e < RP) *reinterpret_cast<f16x8*>(&s_a[buf][(tid >> 3) + 32 * e][seg]) = ar[i][e];
+    if (more) load(i, tile + DEPTH);
+    __syncthreads();     // the buffer before last was read before the previous tile's barrier
 #pragma unroll
-      for (int e = 0; e < NXL; ++e) *reinterpret_cast<f16x8*>(&s_x[buf][(tid >> 3) + 32 * e][seg]) = xr[i][e];
+    for (int ks = 0; ks < KT / 32; ++ks) {
+      const f16x8 xv = *reinterpret_cast<const f16x8*>(&s_x[buf][w * 16 + col][ks * 32 + lg * 8]);
 #pragma unroll
-      for (int e = 0; e < NAL; ++e)
-        if ((tid >> 3) + 32 * e < RP) *reinterpret_cast<f16x8*>(&s_a[buf][(tid >> 3) + 32 * e][seg]) = ar[i][e];
-      load(i, min(tile + DEPTH, nt - 1));
-      __syncthreads();     // the buffer before last was read before the previous tile's barrier
-#pragma unroll
-      for (int ks = 0; ks < KT / 32; ++ks) {
-        const f16x8 xv = *reinterpret_cast<const f16x8*>(&s_x[buf][w * 16 + col][ks * 32 + lg * 8]);
-#pragma unroll
-        for (int j = 0; j < NR; ++j) {
-          if (j * 16 >= rank) break;
-          const f16x8 av = *reinterpret_cast<const f16x8*>(&s_a[buf][j * 16 + col][ks * 32 + lg * 8]);
-          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av, acc[j], 0, 0, 0);
-        }
+      for (int j = 0; j < NR; ++j) {
+        if (j * 16 >= rank) break;
+        const f16x8 av = *reinterpret_cast<const f16x8*>(&s_a[buf][j * 16 + col][ks * 32 + lg * 8]);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, av, acc[j], 0, 0, 0);
       }
     }
+  };
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i) load(i, min(i, nt - 1));
+  int tb = 0;
+  for (; tb + 2 * DEPTH <= nt; tb += DEPTH) {
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) step(i, tb + i, true);
   }
+#pragma unroll
+  for (int i = 0; i < 2 * DEPTH - 1; ++i)
+    if (tb + i < nt) step(i % DEPTH, tb + i, tb + i + DEPTH < nt);
 #pragma unroll
   for (int j = 0; j < NR; ++j)
 #pragma unroll
