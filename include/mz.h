@@ -674,9 +674,9 @@ mz_status mz_kv_append(const mz_kv_append_args *args, int32_t m, void *stream);
  * counts as 0, one beyond the table as n_table * chunk_tokens; a chunk whose
  * entry is outside 0..n_slots-1 is left out, as if its keys were not there; a
  * token that sees no key gets zeros.  What slots hold past the last key is
- * never used.  Scores, sums and joins are fp32; the softmax weights are
- * rounded to f16 for the product with the values.  head_dim 64 or 128,
- * n_q_heads a multiple of n_kv_heads with a group of at most 16, chunk_tokens
+ * never used.  Scores, sums and joins are fp32, and the softmax weights keep 22
+ * bits for the product with the values.  head_dim 64 or 128, n_q_heads a
+ * multiple of n_kv_heads with a group of at most 16, chunk_tokens
  * a power of two >= 8, n_table * chunk_tokens at most 2^30, a slot below 2^31
  * bytes, n_seq * n_q_heads below 2^24.  workspace: device, caller-owned, at
  * least mz_attention_batch_workspace_bytes(...) bytes (one for the most

@@ -20,10 +20,11 @@
 // the eight scores of a lane are eight consecutive keys, and the P operand
 // of the output product meets one 16-byte run of a V^T row.
 //
-// P is rounded to f16 for the product, as 2^(14 + s - max): up to 2^14, so
-// that weights keep full precision down to 2^-28 of the largest (many small
-// ones add up in a long cache); the sums add the same rounded values, in
-// fp32.  Partials and their joins are fp32.
+// P goes into the product as two f16 values, hi + lo / 2^11, of 2^(14 + s - max),
+// whose products are summed apart: 22 bits of a weight (and what they hold down
+// to 2^-50 of the largest), so that nothing of an output's f16 is lost to the
+// weights; matrix instructions are not what bounds this.  Their sum, the partials
+// and the joins are fp32.
 //
 // Measured, both kernels: 64 sequences of 512-8192 keys, 8 KV heads of 128, 122
 // + 5 us: 640 MB at 5.2 TB/s, where reading them alone in this order takes
@@ -41,6 +42,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kUnit = 128;          // keys of a unit: a 32-key block for each wave
 constexpr int kWaves = 4, kBlock = 32, kCols = 16;
 constexpr float kBias = 14.f;
+constexpr float kLo = 2048.f;       // what a weight's lower half is multiplied by
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -156,9 +158,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_batch_kernel(AttnBatch a)
       if (col < a.group)
         bq[ks] = *reinterpret_cast<const f16x8*>(a.q + ((int64_t)b * a.nq + h * a.group + col) * HD + ks * 32 + lg * 8);
     }
-    f32x4 o[DB];
+    f32x4 o[DB], o_lo[DB];
 #pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DB; ++d) o[d] = o_lo[d] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_c = -INFINITY, l_c = 0.f;
 
     // This wave's blocks: j0, j0 + 128, ... below the share's end and the
@@ -221,17 +223,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_batch_kernel(AttnBatch a)
         m_c = m_new;
         l_c *= alpha;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] *= alpha;
+        for (int d = 0; d < DB; ++d) o[d] *= alpha, o_lo[d] *= alpha;
       }
       const float base = m_c == -INFINITY ? 0.f : m_c - kBias;
-      f16x8 pb;
+      f16x8 pb, pb_lo;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const _Float16 e = (_Float16)exp2_hw(sc[t][r] - base);
-          pb[t * 4 + r] = e;
-          l_c += (float)e;
+          const float e = exp2_hw(sc[t][r] - base);
+          const _Float16 hi = (_Float16)e;
+          pb[t * 4 + r] = hi;
+          pb_lo[t * 4 + r] = (_Float16)((e - (float)hi) * kLo);
+          l_c += e;
         }
       // values of keys that do not count are not data: zero them
       if (__any(n_ok < 8)) {
@@ -241,7 +245,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_batch_kernel(AttnBatch a)
           for (int e = 0; e < 8; ++e) va[d][e] = e < n_ok ? va[d][e] : (_Float16)0.f;
       }
 #pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pb, o[d], 0, 0, 0);
+      for (int d = 0; d < DB; ++d) {
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pb, o[d], 0, 0, 0);
+        o_lo[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pb_lo, o_lo[d], 0, 0, 0);
+      }
     }
     l_c += __shfl_xor(l_c, 16);
     l_c += __shfl_xor(l_c, 32);
@@ -253,7 +260,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attn_batch_kernel(AttnBatch a)
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s_o[w][d][r][lane] = o[d][r];
+      for (int r = 0; r < 4; ++r)      // a sum with infinite or NaN values is what the upper halves make of it
+        s_o[w][d][r][lane] = fabsf(o[d][r]) < INFINITY ? __builtin_fmaf(o_lo[d][r], 1.f / kLo, o[d][r]) : o[d][r];
     __syncthreads();
     // thread t: head t % 16 of the group, output dimensions (t / 16) * DPT .. + DPT
     constexpr int DPT = HD / 16;

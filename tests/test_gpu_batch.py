@@ -410,6 +410,57 @@ def test_attention_not_numbers(C):
     close(out, ref, bound, "out")
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("C", [8, 32, 256])
+def test_attention_weights_keep_their_bits(C, hd):
+    """Values that cancel: what weights lose shows beside an output near 0, as weights of 11 bits (2^-12 of each) would."""
+    nq, nkv, lens = 8, 2, [2, 4, 10, 32, 64, 130, 300]
+    q, lens, slab, table = attention_inputs(lens, C, nq, nkv, hd, seed=20)
+    rng = np.random.default_rng(21)
+    q = np.zeros_like(q).reshape(len(lens), nq, hd)      # a score is one product: q[0] k[0], q[0] at most 4
+    q[:, :, 0] = rng.uniform(1, 4, q.shape[:2])
+    ref, bound = np.zeros((len(lens), nq, hd)), np.zeros((len(lens), nq, hd))
+    for b, n in enumerate(lens):
+        k0 = (rng.uniform(0, 0.25, (n, nkv))).astype(np.float16)
+        v = ((-1.0) ** np.arange(n)[:, None, None] * rng.uniform(1, 2, (1, nkv, hd))).astype(np.float16)
+        for j in range(n):
+            slot = slab[table[b, j // C]].reshape(2, -1)
+            slot[0].reshape(C, nkv, hd)[j % C] = 0
+            slot[0].reshape(C, nkv, hd)[j % C, :, 0] = k0[j]
+            slot[1].reshape(nkv, hd, C)[:, :, j % C] = v[j]
+        for h in range(nq):
+            g = h // (nq // nkv)
+            s = k0[:, g].astype(np.float64) * float(q[b, h, 0]) / np.sqrt(hd)
+            w = np.exp(s - s.max())
+            p = w / w.sum()
+            size = p @ np.abs(v[:, g].astype(np.float64))
+            ref[b, h] = p @ v[:, g].astype(np.float64)
+            # exponents of at most 15 + 1.5 |s| <= 16: the scale, its product, the bias's sum and the difference are
+            # rounded, 4 * 16 U32 in all, times ln 2; the exponential itself 2 U32; the weight's halves 2^-22; fp32
+            # sums of n terms.  All that in numerator and denominator, then the output's own f16.
+            e = 64 * 0.7 * U32 + 2 * U32 + 2.0 ** -22 + (n + 8) * U32
+            bound[b, h] = 2.1 * e * size + U16 * np.abs(ref[b, h]) + TINY16
+    out = attention_run(q.reshape(len(lens), -1), lens, slab, table, C, nq, nkv, hd)
+    for b, n in enumerate(lens):
+        close(out[b].view(nq, hd), ref[b], bound[b], f"{n} keys")
+
+
+@pytest.mark.parametrize("C", [16, 64])
+def test_attention_infinite_values(C):
+    """Infinite values under weights that one f16 holds exactly (the largest is 1 beside itself) and under others."""
+    nq, nkv, hd, n = 4, 1, 64, 70
+    q, lens, slab, table = attention_inputs([1, n, n, n], C, nq, nkv, hd, seed=22)
+    v = lambda b, j: slab[table[b, j // C], C * hd:].reshape(hd, C)[:, j % C]    # noqa: E731
+    v(0, 0)[2], v(0, 0)[3] = np.inf, -np.inf
+    q[1] = 0                                     # every weight the same
+    v(1, 7)[4], v(1, 8)[5] = -np.inf, np.inf
+    for j in range(n):
+        v(2, j)[6] = np.inf
+    v(3, 69)[7] = np.inf
+    out = attention_run(q, lens, slab, table, C, nq, nkv, hd)
+    close(out, *attention_oracle(q, lens, slab, table, C, nq, nkv, hd), "out")
+
+
 def test_attention_against_the_single_sequence_call():
     torch = torch_cuda()
     nq, nkv, hd, C, n = 8, 2, 128, 64, 3000
