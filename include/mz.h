@@ -704,8 +704,9 @@ int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int
  * the others hold.  scale: device float [n_adapters], finite (NULL: 1).  adapter:
  * device int32 [m], in any order; a row whose entry is outside
  * 0..n_adapters-1 has none: its y is the base's (in place it is not
- * touched).  Rows do not affect each other.  Nothing is rounded to f16 on the
- * way: x A^T keeps 22 bits and sums are fp32.  k a multiple of 8 up to 2^30,
+ * touched).  Rows do not affect each other.  Nothing is rounded to fewer bits
+ * than fp32's on the way: x A^T and its product with B are fp32 sums of exact
+ * products, whatever the sizes of their values.  k a multiple of 8 up to 2^30,
  * max_rank a multiple of 8 in 8..128, n_adapters at most 2047, y_stride a
  * multiple of 4, m may be 0.  workspace: device, caller-owned, at least
  * mz_lora_workspace_bytes(m, k, max_rank, n_adapters) bytes (one for the most

@@ -3,13 +3,13 @@
 // with A_a [R][k] and B_a [n][R] f16 of which the first rank[a] ranks count.
 //
 // Two steps: the first forms t = x A^T, fp32, in K splits; the second adds
-// the splits in order, scales them and adds t B^T to the rows.  The products
-// of f16 x and A are exact and summed in fp32 (v_mfma_f32_16x16x32_f16).  For
-// the second product t is written as hi + lo, two f16 values, after the row's
-// largest was brought to 2^14 by a power of two: together they hold 22 bits
-// of each t (and all of it down to 2^-38 of the row's largest), so no
-// precision of the projection's fp32 is lost, B is used as it is, and the
-// products run at an eighth of the time of the fp32 matrix instructions.
+// the splits in order and adds s (t B^T) to the rows.  The products of f16 x and
+// A are exact and summed in fp32 (v_mfma_f32_16x16x32_f16).  For the second
+// product t is cut into three bf16 values of 8 bits each and B into two (8 and 3
+// bits), both exactly and whatever their size: the six products of the parts are
+// exact too (v_mfma_f32_16x16x32_bf16), so nothing of t or B is lost, also where
+// a small t meets a large B, in 3/8 of the time of the fp32 matrix instructions.
+// The scale comes last, in one rounding with the base.
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
 // Measured: 1 row of 2048 x 2048, rank 16, 5.6 us, latency; 33 rows over 24
@@ -34,7 +34,7 @@ namespace mzk {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));      // the adapter list begins anywhere
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
@@ -433,63 +433,111 @@ __global__ __launch_bounds__(256) void lora_shrink_tile_kernel(Lora p) {
     }
 }
 
-// Ranks j .. j + 3 of row r's t: the splits added in order, times the row's
-// scale.
+// Ranks j .. j + 3 of row r's t: the splits added in order.
 template <int NR>
 __device__ __forceinline__ f32x4 t_sum(const Lora& p, int r, int j) {
-  const int a = p.adapter[r];
+  const float* t = p.t + (int64_t)r * (16 * NR) + j;
   f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (has_adapter(p, a)) {
-    const float* t = p.t + (int64_t)r * (16 * NR) + j;
 #pragma unroll 8
-    for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * (16 * NR));
-    if (p.scale) v *= p.scale[a];
-  }
+  for (int s = 0; s < p.n_split; ++s) v += *reinterpret_cast<const f32x4*>(t + (int64_t)s * p.m * (16 * NR));
   return v;
 }
 
-// Four ranks of a row in two f16 halves after the row's largest was brought to
-// 2^14; unit: what undoes that.  The 4 NR lanes of a row are neighbours, a
-// power of two of them, and run this together.
-template <int NR>
-__device__ __forceinline__ void t_halves(f32x4 v, f16x4& hi, f16x4& lo, float& unit) {
-  constexpr int LPR = 4 * NR;
-  float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-#pragma unroll
-  for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  // a row of zeros or with an infinity stays as it is, its finite values within f16
-  const int up = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float u = ldexpf(v[e], up);
-    if (fabsf(u) < INFINITY) u = fminf(fmaxf(u, -65504.f), 65504.f);
-    hi[e] = (_Float16)u;
-    lo[e] = fabsf(u) < INFINITY ? (_Float16)(u - (float)hi[e]) : (_Float16)0.f;
-  }
-  unit = ldexpf(1.f, -up);
-}
+__device__ __forceinline__ float scale_of(const Lora& p, int a) { return p.scale ? p.scale[a] : 1.f; }
 
-// The halves of a group's 16 rows in LDS.
+// The upper 16 bits of two fp32 values as two bf16, and what is left of a value
+// without them.
+__device__ __forceinline__ uint32_t tops(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+}
+__device__ __forceinline__ float rest(float v) { return v - __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+
+// t of a group's 16 rows in LDS, in three bf16 parts that add up to it.  Only
+// the first part of an infinite or NaN value means something.
 template <int NR>
-struct GroupHalves {
+struct GroupParts {
   static constexpr int RP = 16 * NR, KS = (RP + 31) / 32, PITCH = KS * 32 + 8;
-  _Float16 hi[16][PITCH], lo[16][PITCH];
-  float unit[16];                          // what a row's d is multiplied by
+  uint16_t part[3][16][PITCH];
 
   // ranks j .. j + 3 of row i
   __device__ __forceinline__ void put(int i, int j, f32x4 v) {
-    f16x4 h, l;
-    float u;
-    t_halves<NR>(v, h, l, u);
-    *reinterpret_cast<f16x4*>(&hi[i][j]) = h;
-    *reinterpret_cast<f16x4*>(&lo[i][j]) = l;
-    if (RP < KS * 32) {
-      *reinterpret_cast<f16x4*>(&hi[i][RP + j]) = f16x4{0, 0, 0, 0};
-      *reinterpret_cast<f16x4*>(&lo[i][RP + j]) = f16x4{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+      *reinterpret_cast<uint2*>(&part[c][i][j]) = make_uint2(tops(v[0], v[1]), tops(v[2], v[3]));
+      if (RP < KS * 32) *reinterpret_cast<uint2*>(&part[c][i][RP + j]) = make_uint2(0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = rest(v[e]);
     }
-    if (j == 0) unit[i] = u;
+  }
+  // row col's ranks of K step j
+  __device__ __forceinline__ bf16x8 get(int c, int col, int j) const {
+    return *reinterpret_cast<const bf16x8*>(&part[c][col][j * 32 + ((threadIdx.x & 63) >> 4) * 8]);
   }
 };
+
+// Eight f16 values of B in two bf16 parts that add up to them (of an infinite or
+// NaN one the first alone).
+__device__ __forceinline__ void split_b(f16x8 b, bf16x8& hi, bf16x8& lo) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 h, l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = (float)b[2 * e], y = (float)b[2 * e + 1];
+    h[e] = tops(x, y);
+    l[e] = tops(rest(x), rest(y));
+  }
+  hi = __builtin_bit_cast(bf16x8, h);
+  lo = __builtin_bit_cast(bf16x8, l);
+}
+
+// y += scale t B^T for NX groups of 16 rows and 16 CT columns.  The first parts'
+// product is summed apart from the others': where t or B are infinite or NaN it
+// is what the sum is, and the others mean nothing.  Columns of two groups come
+// one after the other, which leaves registers to a fourth wave a SIMD (4099 rows
+// of rank 64: 54.8 us, two columns at a time 57.8); those of one all together.
+template <int NR, int NX, int CT>
+__device__ __forceinline__ void expand_columns(const GroupParts<NR> (&t)[NX], int rank, float scale,
+                                               const f16x8 (&b)[GroupParts<NR>::KS][CT], f32x4 (&y)[NX][CT]) {
+  constexpr int CG = NX == 1 ? CT : 1;
+  const int col = threadIdx.x & 15;
+#pragma unroll
+  for (int c0 = 0; c0 < CT; c0 += CG) {
+    f32x4 d[CG][NX], d_lo[CG][NX];
+#pragma unroll
+    for (int c = 0; c < CG; ++c)
+#pragma unroll
+      for (int i = 0; i < NX; ++i) d[c][i] = d_lo[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < GroupParts<NR>::KS; ++j) {
+      if (j * 32 >= rank) break;
+      bf16x8 hi[CG], lo[CG];
+#pragma unroll
+      for (int c = 0; c < CG; ++c) split_b(b[j][c0 + c], hi[c], lo[c]);
+#pragma unroll
+      for (int part = 2; part >= 0; --part) {
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+          const bf16x8 tp = t[i].get(part, col, j);
+#pragma unroll
+          for (int c = 0; c < CG; ++c) {
+            d_lo[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo[c], tp, d_lo[c][i], 0, 0, 0);
+            f32x4& sum = part ? d_lo[c][i] : d[c][i];
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi[c], tp, sum, 0, 0, 0);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CG; ++c)
+#pragma unroll
+      for (int i = 0; i < NX; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = d[c][i][e];
+          y[i][c0 + c][e] = __builtin_fmaf(fabsf(v) < INFINITY ? v + d_lo[c][i][e] : v, scale, y[i][c0 + c][e]);
+        }
+  }
+}
 
 // B of columns c0 + 16 c + l % 16, ranks 32 j + 8 (l / 16) .. + 7; ranks that
 // do not count are zero (the last eight that exist are read there).
@@ -545,32 +593,15 @@ __device__ __forceinline__ void store_y(const Lora& p, int row, int c0, int lg, 
 
 template <int NR, int CT>
 __device__ __forceinline__ void expand_group(const Lora& p, int a, int rank, int n, const int* s_rows,
-                                             const GroupHalves<NR>& t, int c0, f32x4 (&y)[CT]) {
-  constexpr int KS = GroupHalves<NR>::KS;
+                                             const GroupParts<NR> (&t)[1], int c0, f32x4 (&y)[1][CT]) {
+  constexpr int KS = GroupParts<NR>::KS;
   const int lane = threadIdx.x & 63, col = lane & 15, lg = lane >> 4;
+  const float scale = scale_of(p, a);
   f16x8 b[KS][CT];
   load_b<KS, CT>(p, a, rank, c0, b);
-  f32x4 d[CT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < KS; ++j) {
-    if (j * 32 >= rank) break;
-    const f16x8 lo = *reinterpret_cast<const f16x8*>(&t.lo[col][j * 32 + lg * 8]);
-    const f16x8 hi = *reinterpret_cast<const f16x8*>(&t.hi[col][j * 32 + lg * 8]);
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo, d[c], 0, 0, 0);
-      d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi, d[c], 0, 0, 0);
-    }
-  }
+  expand_columns<NR, 1, CT>(t, rank, scale, b, y);
   if (col >= n) return;
-  const float unit = t.unit[col];
-#pragma unroll
-  for (int c = 0; c < CT; ++c)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[c][e] = __builtin_fmaf(d[c][e], unit, y[c][e]);
-  store_y<CT>(p, s_rows[col], c0, lg, c0 + 16 * CT <= p.n, y);
+  store_y<CT>(p, s_rows[col], c0, lg, c0 + 16 * CT <= p.n, y[0]);
 }
 
 // A row without an adapter is the base's: columns c0 .. c0 + 256 - 1.
@@ -586,7 +617,7 @@ __device__ __forceinline__ void copy_row(const Lora& p, int r, int c0, int cols)
 template <int NR>
 __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
   __shared__ int s_rows[16];
-  __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t;
+  __shared__ __attribute__((aligned(16))) GroupParts<NR> s_t[1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cols = (p.n + kColsWg - 1) / kColsWg, rest = blockIdx.x >> 3;
   const int r = rest / cols * 8 + (blockIdx.x & 7), c_wg = rest % cols * kColsWg, c0 = c_wg + w * 64;
@@ -599,11 +630,11 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(Lora p) {
   const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
   if (n == 0) return;
   __syncthreads();
-  f32x4 y[4];                              // goes out first, needed last
-  load_base<4>(p, s_rows[min(lane & 15, n - 1)], c0, lane >> 4, c0 + 64 <= p.n, y);
+  f32x4 y[1][4];                           // goes out first, needed last
+  load_base<4>(p, s_rows[min(lane & 15, n - 1)], c0, lane >> 4, c0 + 64 <= p.n, y[0]);
   for (int idx = threadIdx.x; idx < n * 4 * NR; idx += 256) {
     const int i = idx / (4 * NR), j = idx % (4 * NR) * 4;
-    s_t.put(i, j, t_sum<NR>(p, s_rows[i], j));
+    s_t[0].put(i, j, t_sum<NR>(p, s_rows[i], j));
   }
   __syncthreads();
   if (c0 < p.n) expand_group<NR, 4>(p, a, rank_of(p, a), n, s_rows, s_t, c0, y);
@@ -618,7 +649,7 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
   __shared__ int s_rows[16];
   __shared__ f32x4 s_acc[4][NR][64];
   __shared__ float s_sum[16][RP + 4];
-  __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t;
+  __shared__ __attribute__((aligned(16))) GroupParts<NR> s_t[1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int r = blockIdx.y, c_wg = blockIdx.x * kColsFused, c0 = c_wg + w * 16 * CT;
@@ -630,10 +661,9 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
   const int n = __builtin_amdgcn_readfirstlane(gather_group(p, r, a, s_rows));
   if (n == 0) return;
   __syncthreads();
-  f32x4 y[CT];
-  load_base<CT>(p, s_rows[min(col, n - 1)], c0, lg, c0 + 16 * CT <= p.n, y);
+  f32x4 y[1][CT];
+  load_base<CT>(p, s_rows[min(col, n - 1)], c0, lg, c0 + 16 * CT <= p.n, y[0]);
   const int rank = rank_of(p, a);
-  const float scale = p.scale ? p.scale[a] : 1.f;
   f32x4 v[(NR + 3) / 4];
   shrink_group<NR>(p, a, rank, n, s_rows, 0, (p.k + 31) / 32, s_acc, v);
 #pragma unroll
@@ -641,13 +671,13 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
     const int k = (w + 4 * i) * 16 + col;
     if (k < RP) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s_sum[lg * 4 + e][k] = k < rank ? v[i][e] * scale : 0.f;
+      for (int e = 0; e < 4; ++e) s_sum[lg * 4 + e][k] = k < rank ? v[i][e] : 0.f;
     }
   }
   __syncthreads();
   for (int idx = threadIdx.x; idx < n * 4 * NR; idx += 256) {
     const int i = idx / (4 * NR), j = idx % (4 * NR) * 4;
-    s_t.put(i, j, f32x4{s_sum[i][j], s_sum[i][j + 1], s_sum[i][j + 2], s_sum[i][j + 3]});
+    s_t[0].put(i, j, f32x4{s_sum[i][j], s_sum[i][j + 1], s_sum[i][j + 2], s_sum[i][j + 3]});
   }
   __syncthreads();
   if (c0 < p.n) expand_group<NR, CT>(p, a, rank, n, s_rows, s_t, c0, y);
@@ -659,11 +689,14 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
 // Workgroups are numbered as above.  4099 rows of 4096 columns, rank 64: 41 us,
 // where base to y alone takes 29 in this order; the rest is t and B, from the
 // L2 for every half tile.  A whole tile a workgroup is as fast, a quarter
-// slower by a seventh; the base's loads ahead of the others' slower.
+// slower by a seventh; the base's loads ahead of the others' slower.  Four waves
+// a SIMD against three: rank 64 54.8 and 58.3 us for both launches, though 16
+// bytes a thread then lie in scratch, rank 16 40.6 and 42.2; with 512 rows, where
+// ranges of 256 columns do not fill the chip, 20.2 and 19.3.
 template <int NR, int COLS>
-__global__ __launch_bounds__(COLS) void lora_expand_tile_kernel(Lora p) {
-  constexpr int KS = GroupHalves<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + COLS - 1) / COLS;
-  __shared__ __attribute__((aligned(16))) GroupHalves<NR> s_t[NX];
+__global__ __launch_bounds__(COLS, NR <= 2 || (NR == 4 && COLS == 512) ? 4 : 1) void lora_expand_tile_kernel(Lora p) {
+  constexpr int KS = GroupParts<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + COLS - 1) / COLS;
+  __shared__ __attribute__((aligned(16))) GroupParts<NR> s_t[NX];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4;
   const int cols = (p.n + COLS - 1) / COLS, rest = blockIdx.x >> 3;
@@ -699,11 +732,11 @@ __global__ __launch_bounds__(COLS) void lora_expand_tile_kernel(Lora p) {
 #pragma unroll
       for (int e = 0; e < PER; ++e)
         t[e] += *reinterpret_cast<const f32x4*>(p.t + ((int64_t)s * p.m + at[e]) * (16 * NR) + threadIdx.x % (4 * NR) * 4);
-    const float scale = p.scale ? p.scale[a] : 1.f;
+    const float scale = scale_of(p, a);
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int i = (threadIdx.x + COLS * e) / (4 * NR);
-      if (i < ROWS) s_t[i / 16].put(i % 16, threadIdx.x % (4 * NR) * 4, t[e] * scale);
+      if (i < ROWS) s_t[i / 16].put(i % 16, threadIdx.x % (4 * NR) * 4, t[e]);
     }
     __syncthreads();
     if (c0 >= p.n) return;
@@ -712,28 +745,7 @@ __global__ __launch_bounds__(COLS) void lora_expand_tile_kernel(Lora p) {
     load_b<KS, 4>(p, a, rank, c0, b);
 #pragma unroll
     for (int i = 0; i < NX; ++i) load_base<4>(p, rows[i], c0, lg, whole, y[i]);
-#pragma unroll
-    for (int i = 0; i < NX; ++i) {
-      f32x4 d[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) d[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < KS; ++j) {
-        if (j * 32 >= rank) break;
-        const f16x8 lo = *reinterpret_cast<const f16x8*>(&s_t[i].lo[col][j * 32 + lg * 8]);
-        const f16x8 hi = *reinterpret_cast<const f16x8*>(&s_t[i].hi[col][j * 32 + lg * 8]);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], lo, d[c], 0, 0, 0);
-          d[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j][c], hi, d[c], 0, 0, 0);
-        }
-      }
-      const float unit = s_t[i].unit[col];
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][c][e] = __builtin_fmaf(d[c][e], unit, y[i][c][e]);
-    }
+    expand_columns<NR, NX, 4>(s_t, rank, scale, b, y);
   } else {
     if (c0 >= p.n) return;
 #pragma unroll

@@ -749,6 +749,57 @@ def test_lora_large_and_small_values():
     close(lora_run(x, adapter, a, b, scale, rank, base, n), ref, bound, "y")
 
 
+@pytest.mark.parametrize("m,k,n,R", [(1, 64, 256, 16), (20, 64, 100, 32), (20, 4096, 130, 32), (64, 2048, 300, 128),
+                                     (200, 64, 300, 16), (500, 328, 300, 40), (600, 64, 8200, 64), (530, 64, 8300, 128)])
+def test_lora_small_ranks_meet_large_columns(m, k, n, R):
+    """Ranks of t far below others of their row, with columns of B that make up for it.  In every third column the
+    smallest rank, 2^-35 of the largest, counts alone, so that it needs bits of its own.  Fused, few-row and tile
+    forms."""
+    rng = np.random.default_rng(m + R)
+    x, adapter, a, b, scale, rank, base, n = lora_inputs(rng.integers(-1, 3, m), k, n, R, 3, seed=37, ranks=[R, R - 3, 7])
+    down = rng.integers(0, 20, (3, R))                       # t of rank r falls by 2^down, B rises by as much
+    down[:, :2] = [[0, 22]] * 3
+    a = (a.astype(np.float64) * 2.0 ** np.minimum(8 - down, 8)[:, :, None]).astype(np.float16)
+    x[:, :k // 2] *= np.float16(2.0 ** 5)
+    a[:, 1, :k // 2] = 0                                     # one rank that sees the small half of x only
+    x[:, k // 2:] *= np.float16(2.0 ** -8)
+    b = (b.astype(np.float64) * 2.0 ** (down - 12)[:, None, :]).astype(np.float16)
+    for i, r in enumerate(rank):
+        a[i, r:], b[i, :, r:] = np.nan, np.inf
+        b[i, ::3, [j for j in range(R) if j != 1]] = 0
+        b[i, 1::3, 0] = 2.0 ** -24
+    base[: m // 2] = 0
+    ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+    y = lora_run(x, adapter, a, b, scale, rank, base, n)
+    close(y[:, :n], ref[:, :n], bound[:, :n], "y")
+
+
+@pytest.mark.parametrize("m", [3, 40, 130])
+def test_lora_infinite_adapters(m):
+    """Infinite values in B, in A and in x beside ranks that one part of them holds exactly."""
+    x, adapter, a, b, scale, rank, base, n = lora_inputs([r % 2 for r in range(m)], 64, 48, 16, 2, seed=38, ranks=[16, 16])
+    b[0, 5, 3], b[0, 6, 4], b[1, 7, 2] = np.inf, -np.inf, np.inf
+    b[1, 8, :] = 0
+    b[1, 9, 2] = 1
+    a[:] = 0
+    a[:, :, 0] = 1                              # t = x[0] for every rank: 1, a power of two, in the first rows
+    x[:2, 0] = 1
+    x[2, 0] = np.inf
+    ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+    close(lora_run(x, adapter, a, b, scale, rank, base, n), ref, bound, "y")
+
+
+@pytest.mark.parametrize("m", [2, 40, 130])
+def test_lora_scales_of_any_size(m):
+    """Scales near the ends of fp32's range with B, or x, that brings the result back."""
+    x, adapter, a, b, scale, rank, base, n = lora_inputs([r % 2 for r in range(m)], 64, 48, 16, 2, seed=39, ranks=[16, 11])
+    scale[:] = [2.0 ** 122, 2.0 ** -120]
+    x, base[:] = np.where(adapter[:, None] == 0, x * np.float16(2.0 ** 3), x * np.float16(2.0 ** 8)).astype(np.float16), 0
+    b[0, :, :16] = (b[0, :, :16].astype(np.float64) * 2.0 ** -12).astype(np.float16)
+    ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+    close(lora_run(x, adapter, a, b, scale, rank, base, n), ref, bound, "y")
+
+
 def test_lora_captured_on_another_stream():
     torch = torch_cuda()
     rng = np.random.default_rng(30)
