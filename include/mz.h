@@ -690,7 +690,8 @@ mz_status mz_attention_batch(const void *q_f16, const int32_t *lens, int32_t n_s
                              int32_t head_dim, void *workspace, int64_t workspace_bytes,
                              void *out_f16, void *stream);
 
-/* Workspace bytes of mz_attention_batch (-1 for invalid arguments). */
+/* Workspace bytes of mz_attention_batch (-1 for invalid arguments, n_seq
+ * n_q_heads of 2^24 and more among them). */
 int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
                                            int32_t head_dim);
 

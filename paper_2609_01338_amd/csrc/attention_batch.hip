@@ -387,14 +387,14 @@ int64_t attention_batch_units(int n_seq, int n_table, int chunk_tokens, int n_kv
 }
 
 int64_t attention_batch_ws_bytes(int n_seq, int group, int hd) {
-  return up256((int64_t)(n_seq + 1) * 4) + up256((int64_t)2 * kAttnBatchWgs * group * 8) +
+  return up256(((int64_t)n_seq + 1) * 4) + up256((int64_t)2 * kAttnBatchWgs * group * 8) +
          (int64_t)2 * kAttnBatchWgs * group * hd * 4;
 }
 
 void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s) {
   uint8_t* p = reinterpret_cast<uint8_t*>(ws);
   a.base = reinterpret_cast<int32_t*>(p);
-  a.ml = reinterpret_cast<float2*>(p + up256((int64_t)(a.n_seq + 1) * 4));
+  a.ml = reinterpret_cast<float2*>(p + up256(((int64_t)a.n_seq + 1) * 4));
   a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.ml) + up256((int64_t)2 * kAttnBatchWgs * a.group * 8));
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)hd);
   const int64_t most = attention_batch_units(a.n_seq, a.n_table, a.C, a.nkv);

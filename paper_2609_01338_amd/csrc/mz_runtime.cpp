@@ -2227,7 +2227,8 @@ mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
 }
 
 int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t head_dim) {
-  if (n_seq < 1 || n_kv < 1 || n_q < n_kv || n_q % n_kv || n_q / n_kv > 16 || (head_dim != 64 && head_dim != 128))
+  if (n_seq < 1 || n_kv < 1 || n_q < n_kv || n_q % n_kv || n_q / n_kv > 16 || (head_dim != 64 && head_dim != 128) ||
+      (int64_t)n_seq * n_q > mzk::kMaxBlocks)
     return -1;
   return mzk::attention_batch_ws_bytes(n_seq, n_q / n_kv, head_dim);
 }
@@ -2240,10 +2241,11 @@ mz_status mz_attention_batch(const void* q, const int32_t* lens, int32_t n_seq, 
     check_chunks(n_seq, n_slots, n_table, chunk_tokens);
     if (head_dim != 64 && head_dim != 128) fail(MZ_EINVAL, "head_dim must be 64 or 128");
     if (n_kv < 1 || n_q < n_kv || n_q % n_kv || n_q / n_kv > 16) fail(MZ_EINVAL, "bad head counts");
+    // what is counted below stays within 64 bits for that many query heads
+    if ((int64_t)n_seq * n_q > mzk::kMaxBlocks) fail(MZ_EINVAL, "n_seq sequences of n_q_heads are too many");
     const int64_t slot_bytes = (int64_t)chunk_tokens * n_kv * head_dim * 4;
     if (slot_bytes > INT32_MAX) fail(MZ_EINVAL, "a chunk slot exceeds 2^31 - 1 bytes");
-    if (mzk::attention_batch_units(n_seq, n_table, chunk_tokens, n_kv) > INT32_MAX ||
-        (int64_t)n_seq * n_q > mzk::kMaxBlocks)
+    if (mzk::attention_batch_units(n_seq, n_table, chunk_tokens, n_kv) > INT32_MAX)
       fail(MZ_EINVAL, "n_seq sequences of n_table chunks are too many");
     if (workspace_bytes < mzk::attention_batch_ws_bytes(n_seq, n_q / n_kv, head_dim))
       fail(MZ_EINVAL, "workspace too small");

@@ -83,6 +83,14 @@ def test_attention_batch_workspace():
         assert mz.mz_attention_batch_workspace_bytes(*bad) == -1
 
 
+@pytest.mark.parametrize("n_seq", [(1 << 31) - 1, 1 << 30, 1 << 24, 1 << 21])
+def test_attention_batch_workspace_of_a_refused_batch(n_seq):
+    assert mz.mz_attention_batch_workspace_bytes(n_seq, 8, 2, 64) == -1
+    assert mz.mz_attention_batch_workspace_bytes(n_seq, (1 << 31) - 16, (1 << 31) - 16, 64) == -1
+    refused(mz.mz_attention_batch, **{**ATTENTION, "n_seq": n_seq, "ws_bytes": 1 << 40}, match="too many")
+    assert mz.mz_attention_batch_workspace_bytes((1 << 21) - 1, 8, 2, 64) > (1 << 21) * 4
+
+
 LORA = dict(x_ptr=P, m=3, k=64, adapter_ptr=P, n_adapters=2, a_ptr=P, b_ptr=P, max_rank=16, n=100, base_ptr=P, y_ptr=P,
             y_stride=256, ws_ptr=P, ws_bytes=1 << 30)
 
