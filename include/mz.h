@@ -174,7 +174,8 @@ typedef struct {
  * holds the logits after them, and mz_generate takes its steps one by one.
  * Where they leave no token above -inf (finite biases and a mask that allows
  * something do, unless logits are not numbers), mz_first_token gives -1 and
- * MZ_ESTATE, and mz_generate ends there.  Synchronizes; allocates device
+ * MZ_ESTATE, and mz_generate ends there; mz_first_token may then be called again,
+ * under other rules, without another prefill.  Synchronizes; allocates device
  * memory the first time.  Errors: EINVAL for a repetition that is not
  * positive, penalties that are not finite, n_bias out of range, a bias token
  * outside the vocabulary, a NaN bias or a mask without a token; ENOMEM. */

@@ -1714,7 +1714,7 @@ mz_status mz_first_token(mz_ctx* x, int32_t* token_out, float* logits_out) {
     HIPCHK(hipStreamSynchronize(cs));
     if (logits_out) memcpy(logits_out, x->h_logits, (size_t)x->V * 4);
     *token_out = *x->h_token;
-    x->have_last = false;
+    x->have_last = x->rules_on && *token_out < 0;      // other rules may still choose from the same logits
     if (x->swap_timed) {
       HIPCHK(hipEventSynchronize(x->ev_swap_end));
       float ms = 0;

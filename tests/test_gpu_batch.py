@@ -1161,6 +1161,41 @@ def test_token_rules_that_leave_no_token():
         assert 0 <= mz.mz_first_token(e) < m.vocab
 
 
+def test_token_rules_that_left_no_token_may_be_relaxed():
+    """The prefill is not used up: other rules, or none, choose from the same logits, after a step of mz_generate too."""
+    m, ctx, eng = tiny_engine()
+    with eng:
+        e = eng.ctx
+        mz.mz_prefill_context(e, ctx)
+        plain, raw = mz.mz_first_token(e, m.vocab)
+        none = dict(mask=words_of([9], m.vocab), bias=[(9, float("-inf"))])
+        for after in ("prefill", "generate"):
+            mz.mz_set_token_rules(e, **none)
+            if after == "prefill":
+                mz.mz_prefill_context(e, ctx)
+                call = lambda: mz.mz_first_token(e)                     # noqa: E731
+            else:
+                mz.mz_truncate_context(e, ctx.size - 1)
+                call = lambda: mz.mz_generate(e, int(ctx[-1]), 3)       # noqa: E731
+            with pytest.raises(mz.MzError) as err:
+                call()
+            assert err.value.status == mz.MZ_ESTATE and "rules" in str(err.value)
+            with pytest.raises(mz.MzError) as err:                  # and once more under the same
+                mz.mz_first_token(e)
+            assert err.value.status == mz.MZ_ESTATE and "rules" in str(err.value)
+            if after == "prefill":
+                mz.mz_clear_token_rules(e)
+                tok, logits = mz.mz_first_token(e, m.vocab)
+                assert tok == plain and logits.tobytes() == raw.tobytes()
+            else:
+                mz.mz_set_token_rules(e, mask=words_of([9, 11], m.vocab))
+                tok = mz.mz_first_token(e)
+                assert tok in (9, 11)
+            with pytest.raises(mz.MzError) as err:                  # a chosen token uses it up
+                mz.mz_first_token(e)
+            assert err.value.status == mz.MZ_ESTATE and "no prefill" in str(err.value)
+
+
 def test_token_rules_refusals_keep_the_rules():
     m, ctx, eng = tiny_engine()
     nan, inf = float("nan"), float("inf")
