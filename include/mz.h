@@ -648,16 +648,22 @@ typedef struct {
 } mz_kv_append_args;
 
 /* Rotate the keys of m rows of any sequences to their positions (rotate-half
- * pairs i, i + head_dim/2, as the rotary epilogues of mz_q4_gemm_ex, the same
- * bits) and write them with the values into the chunks (paper Sec. 4.2) that
- * the sequences' tables name; rotate the rows' queries into q_out.  Rows may
- * come in any order, a whole prompt or one row per sequence.  A row whose seq
- * is outside 0..n_seq-1 (padding), or whose pos is outside 0..n_rope-1 or the
- * table, writes nothing, its row of q_out included; one whose chunk's entry is
- * outside 0..n_slots-1 writes its query only.  q_out and the slab share nothing
- * with the rows that are read.  The caller sees that no two
- * rows name the same position of a sequence and that no two sequences share
- * a chunk that is written.  m may be 0.  Errors: EINVAL for a NULL pointer,
+ * pairs i, i + head_dim/2) and write them with the values into the chunks (paper
+ * Sec. 4.2) that the sequences' tables name; rotate the rows' queries into
+ * q_out.  Given the fp32 products of mz_q4_gemm_ex's epilogue 0, the bits are
+ * those that its epilogues 4 and 5 leave (all without a workspace; with one, rows
+ * that run split over K differ in the order of their sums), so either may write
+ * a chunk: the epilogues where nothing comes between the product and the
+ * rotation and the host knows the rows' places, this call where an adapter
+ * (mz_lora_add), a bias or a norm comes in between, where sequences, positions
+ * and tables are on the device, as in a captured graph, or where rows are f16.
+ * Rows may come in any order, a whole prompt or one row per sequence.  A row
+ * whose seq is outside 0..n_seq-1 (padding), or whose pos is outside 0..n_rope-1
+ * or the table, writes nothing, its row of q_out included; one whose chunk's
+ * entry is outside 0..n_slots-1 writes its query only.  q_out and the slab share
+ * nothing with the rows that are read.  The caller sees that no two rows name
+ * the same position of a sequence and that no two sequences share a chunk that
+ * is written.  m may be 0.  Errors: EINVAL for a NULL pointer,
  * sizes or heads out of range, a stride below the row, n_table * chunk_tokens
  * above 2^30, or rows (pointers, strides), rope_cs, slab or q_out off
  * 16-byte boundaries. */

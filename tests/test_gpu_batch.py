@@ -202,6 +202,47 @@ def test_append_offsets_past_32_bits():
     assert int(slab[:-2].count_nonzero()) == 0
 
 
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("m", [1, 17, 130, 1100])
+def test_append_leaves_the_bits_of_the_projections_epilogues(m, hd):
+    """Rows of a projection's fp32 output, appended, leave the slab and the queries that the rotary epilogues of the
+    same products leave, bit for bit: chunks may be written by either."""
+    torch = torch_cuda()
+    K, C, dq, dkv, n_rope = 512, 16, 512, 256, 1500
+    gen = torch.Generator(device="cuda").manual_seed(m + hd)
+    x = torch.randn(m, K, device="cuda", generator=gen).half()
+
+    def weights(n):
+        w = torch.randint(0, 256, (n // 256, K // 64, 9216), device="cuda", dtype=torch.uint8, generator=gen)
+        sc = (torch.rand(n // 256, K // 64, 512, device="cuda", generator=gen) * 0.01 + 0.01).half()
+        w[..., 8192:] = sc.view(torch.uint8).view(n // 256, K // 64, 1024)
+        return w
+
+    wq, wkv, cs = weights(dq), weights(2 * dkv), dev(rope_table(n_rope, hd))
+    pos = torch.arange(7, 7 + m, device="cuda", dtype=torch.int32)
+    n_table = (7 + m + C - 1) // C
+    table = torch.randperm(n_table + 3, device="cuda", generator=gen)[:n_table].int()
+    slot_halves = 2 * C * dkv
+    off = table[pos.long() // C].long() * slot_halves * 2 + (pos.long() % C) * dkv * 2
+    slabs = [torch.full((n_table + 3, slot_halves), 7.0, device="cuda", dtype=torch.float16) for _ in range(2)]
+    qs = [torch.zeros(m, dq, device="cuda", dtype=torch.float16) for _ in range(2)]
+    rotary = dict(pos=pos.data_ptr(), rope_cs=cs.data_ptr(), head_dim=hd)
+    mz.mz_q4_gemm_ex(x.data_ptr(), m, dq, K, wq.data_ptr(), 4, qs[0].data_ptr(), stream(), n_valid=dq, **rotary)
+    mz.mz_q4_gemm_ex(x.data_ptr(), m, 2 * dkv, K, wkv.data_ptr(), 5, 0, stream(), n_valid=2 * dkv, kv_off=off.data_ptr(),
+                     slab=slabs[0].data_ptr(), chunk_tokens=C, **rotary)
+    q, kv = torch.zeros(m, dq, device="cuda"), torch.zeros(m, 2 * dkv, device="cuda")
+    mz.mz_q4_gemm_ex(x.data_ptr(), m, dq, K, wq.data_ptr(), 0, q.data_ptr(), stream())
+    mz.mz_q4_gemm_ex(x.data_ptr(), m, 2 * dkv, K, wkv.data_ptr(), 0, kv.data_ptr(), stream())
+    seq = torch.zeros(m, device="cuda", dtype=torch.int32)
+    mz.mz_kv_append(m, kv.data_ptr(), kv.data_ptr() + dkv * 4, seq.data_ptr(), pos.data_ptr(), cs.data_ptr(), n_rope,
+                    slabs[1].data_ptr(), n_table + 3, table.data_ptr(), 1, n_table, C, dkv // hd, hd, stream(),
+                    q_ptr=q.data_ptr(), n_q=dq // hd, q_out_ptr=qs[1].data_ptr(), k_stride=2 * dkv, v_stride=2 * dkv)
+    torch.cuda.synchronize()
+    for what, (a, b) in (("queries", qs), ("slab", slabs)):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)), what
+    assert int((slabs[1] != 7).sum()) > m * 2 * dkv * 0.99
+
+
 def test_append_captured_on_another_stream():
     """One graph serves every step: sequences, positions and rows change between its replays."""
     torch = torch_cuda()
