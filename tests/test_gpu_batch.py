@@ -882,6 +882,78 @@ def test_lora_offsets_past_32_bits():
     close(y, ref, bound, "y")
 
 
+@pytest.mark.parametrize("m,in_place", [(3, True), (3, False), (64, True), (70, True), (70, False), (600, True)])
+def test_lora_rows_past_32_bits(m, in_place):
+    """Rows of base and y whose last ones lie beyond 2^32 bytes, and beyond 2^31 elements, from the first."""
+    torch = torch_cuda()
+    k, n, R, na = 64, 300, 16, 4
+    rng = np.random.default_rng(m)
+    x, adapter, a, b, scale, rank, base, n = lora_inputs(rng.integers(-1, 4, m), k, n, R, na, seed=40)
+    stride = ((1 << 31) // (m - 1) + 5) // 4 * 4 + 4
+    assert (m - 1) * stride > 1 << 31
+    far = torch.empty((m - 1) * stride + n, device="cuda")
+    rows = far.as_strided((m, n), (stride, 1))
+    rows.copy_(dev(base)[:, :n])
+    out = far if in_place else torch.empty_like(far)
+    need = mz.mz_lora_workspace_bytes(m, k, R, na)
+    ws = torch.full((need // 4,), float("nan"), device="cuda")
+    d = [dev(v) for v in (x, adapter, a, b, scale, rank)]
+    mz.mz_lora_add(d[0].data_ptr(), m, k, d[1].data_ptr(), na, d[2].data_ptr(), d[3].data_ptr(), R, n, far.data_ptr(),
+                   out.data_ptr(), stride, ws.data_ptr(), need, stream(), scale_ptr=d[4].data_ptr(), rank_ptr=d[5].data_ptr())
+    torch.cuda.synchronize()
+    ref, bound = lora_oracle(x, adapter, a, b, scale, rank, base, n)
+    close(out.as_strided((m, n), (stride, 1)), ref[:, :n], bound[:, :n], "y")
+
+
+@pytest.mark.parametrize("m", [3, 130])
+def test_lora_adapters_past_32_bits(m):
+    """A and B of the last adapter beyond 2^32 bytes from the first one's, in the forms of few and of many rows."""
+    torch = torch_cuda()
+    k, n, R, na = 16384, 16384, 128, 1100
+    a = torch.zeros(na, R, k, device="cuda", dtype=torch.float16)       # 4 MiB each, as each of b
+    b = torch.zeros(na, n, R, device="cuda", dtype=torch.float16)
+    x, adapter, a1, b1, scale, rank, base, _ = lora_inputs([r % 3 - 1 for r in range(m)], k, n, R, 2, seed=41, ranks=[R, R])
+    a[na - 2:], b[na - 2:] = dev(a1), dev(b1)
+    need = mz.mz_lora_workspace_bytes(m, k, R, na)
+    ws, y = torch.full((need // 4,), float("nan"), device="cuda"), torch.zeros(base.shape, device="cuda")
+    d = [dev(v) for v in (x, np.where(adapter < 0, -1, na - 2 + adapter).astype(np.int32), base)]
+    mz.mz_lora_add(d[0].data_ptr(), m, k, d[1].data_ptr(), na, a.data_ptr(), b.data_ptr(), R, n, d[2].data_ptr(),
+                   y.data_ptr(), base.shape[1], ws.data_ptr(), need, stream())
+    torch.cuda.synchronize()
+    ref, bound = lora_oracle(x, adapter, a1, b1, None, None, base, n)
+    close(y, ref, bound, "y")
+
+
+def test_lora_rows_of_the_second_piece_past_32_bits():
+    """More rows than one pass takes, x beyond 2^32 bytes."""
+    torch = torch_cuda()
+    m, k, n, R, na = 8192 + 70, 1 << 18, 12, 8, 2
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    x = torch.randn(m, k, device="cuda", dtype=torch.float16, generator=gen)      # 4 GiB and more
+    a = (torch.randn(na, R, k, device="cuda", generator=gen) / 512).half()
+    b = torch.randn(na, n, R, device="cuda", generator=gen).half()
+    adapter = torch.randint(-1, na, (m,), device="cuda", generator=gen).int()
+    base = torch.randn(m, n, device="cuda", generator=gen)
+    need = mz.mz_lora_workspace_bytes(m, k, R, na)
+    ws, y = torch.full((need // 4,), float("nan"), device="cuda"), torch.zeros(m, n, device="cuda")
+    mz.mz_lora_add(x.data_ptr(), m, k, adapter.data_ptr(), na, a.data_ptr(), b.data_ptr(), R, n, base.data_ptr(), y.data_ptr(),
+                   n, ws.data_ptr(), need, stream())
+    torch.cuda.synchronize()
+    at = np.concatenate([np.arange(0, 70), np.arange(8100, m)])       # of both pieces, the last rows among them
+    some = lambda t: t[dev(at)].cpu().numpy()                         # noqa: E731
+    ref, bound = lora_oracle(some(x), some(adapter), a.cpu().numpy(), b.cpu().numpy(), None, None, some(base), n)
+    close(some(y), ref, bound, "y")
+
+
+@pytest.mark.parametrize("m,k,R", [(65, 14336, 16), (130, 8200, 32), (130, 14336, 64), (700, 8192, 24), (130, 2816, 16),
+                                   (1300, 14336, 16)])
+def test_lora_many_rows_in_many_splits(m, k, R):
+    """K splits of the tiles' first product up to 32, odd counts and counts that do not divide the steps among them."""
+    rng = np.random.default_rng(m + k)
+    lora_case(rng.integers(-1, 3, m), k, 70, R, 3, seed=43)
+    lora_case(np.arange(m) * 4 // m - 1, k, 70, R, 3, seed=44)
+
+
 def test_lora_on_two_streams_at_once_and_a_larger_workspace():
     """Many rows, sorted tiles; the first call's workspace is one for 8192 rows."""
     torch = torch_cuda()
