@@ -625,7 +625,9 @@ int32_t mz_attention_auto_splits_keys(int32_t m, int32_t max_pos, int64_t keys, 
  * mz_attention_batch reads them, and mz_logits_rules picks the tokens.
  * Lengths, positions and tables are read on the device, so one captured
  * graph serves steps of any lengths.  Each call allocates nothing and
- * enqueues on stream, which must belong to the current device (EINVAL). */
+ * enqueues on stream, which must belong to the current device (EINVAL).
+ * Where m may be 0, nothing is enqueued then, and what is one row after the
+ * other, or a workspace, may be NULL. */
 
 typedef struct {
   const void *q, *k, *v;     /* device: rows of query, key and value heads before rotation, [m][n_q_heads *

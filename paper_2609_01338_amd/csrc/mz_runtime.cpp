@@ -2181,11 +2181,11 @@ mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
     if (!args) fail(MZ_EINVAL, "args is NULL");
     const mz_kv_append_args& a = *args;
     if (m < 0) fail(MZ_EINVAL, "m is negative");
-    if (!a.k || !a.v || !a.seq || !a.pos || !a.rope_cs || !a.slab || !a.table) fail(MZ_EINVAL, "NULL pointer");
+    if (!a.rope_cs || !a.slab || !a.table || (m > 0 && (!a.k || !a.v || !a.seq || !a.pos))) fail(MZ_EINVAL, "NULL pointer");
     if (a.head_dim != 32 && a.head_dim != 64 && a.head_dim != 128) fail(MZ_EINVAL, "head_dim must be 32, 64 or 128");
     if (a.n_kv_heads < 1 || a.n_kv_heads > 1024 || a.n_q_heads < 0 || a.n_q_heads > 1024)
       fail(MZ_EINVAL, "bad head counts");
-    if (a.n_q_heads > 0 && (!a.q || !a.q_out)) fail(MZ_EINVAL, "n_q_heads without q or q_out");
+    if (m > 0 && a.n_q_heads > 0 && (!a.q || !a.q_out)) fail(MZ_EINVAL, "n_q_heads without q or q_out");
     if (a.f32 != 0 && a.f32 != 1) fail(MZ_EINVAL, "f32 must be 0 or 1");
     if (a.n_rope < 1) fail(MZ_EINVAL, "n_rope must be positive");
     check_chunks(a.n_seq, a.n_slots, a.n_table, a.chunk_tokens);
@@ -2284,7 +2284,7 @@ mz_status mz_lora_add(const void* x, int32_t m, int32_t k, const int32_t* adapte
                       const float* base, float* y, int64_t y_stride, void* workspace, int64_t workspace_bytes,
                       void* stream) {
   return guarded(nullptr, [&] {
-    if (!x || !adapter || !a || !b || !base || !y || !workspace) fail(MZ_EINVAL, "NULL pointer");
+    if (!a || !b || (m > 0 && (!x || !adapter || !base || !y || !workspace))) fail(MZ_EINVAL, "NULL pointer");
     if (m < 0 || n < 1) fail(MZ_EINVAL, "n must be positive, m at least 0");
     if (n_adapters < 1 || n_adapters > mzk::kLoraAdapters) fail(MZ_EINVAL, "n_adapters must be 1..%d", mzk::kLoraAdapters);
     if (k < 8 || k % 8 || k > (1 << 30)) fail(MZ_EINVAL, "k must be a multiple of 8 in 8..2^30");
@@ -2325,7 +2325,7 @@ mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t
                           float* out, int32_t* token, void* workspace, int64_t workspace_bytes, void* stream) {
   return guarded(nullptr, [&] {
     const mz_logits_rules_args r = rules ? *rules : mz_logits_rules_args{};
-    if (!logits || (!out && !token)) fail(MZ_EINVAL, "NULL pointer");
+    if (m > 0 && (!logits || (!out && !token))) fail(MZ_EINVAL, "NULL pointer");
     if (m < 0 || vocab < 1 || vocab > (1 << 30) || stride < vocab)
       fail(MZ_EINVAL, "m must be at least 0, vocab in 1..2^30, stride at least vocab");
     if (((uintptr_t)logits & 3) || ((uintptr_t)out & 3)) fail(MZ_EINVAL, "logits and out must lie on 4-byte boundaries");
