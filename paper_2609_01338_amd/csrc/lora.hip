@@ -216,14 +216,14 @@ __device__ __forceinline__ int plan_tile(const Lora& p, int tile, PlanLds& s, in
   if (adapter < 0) return 0;
   const int begin = s_found[1], n = min(s.hist[adapter] - begin, kTile);
   int count = 0;                       // of the adapter's rows among this wave's
-#pragma unroll 4
+#pragma unroll 1
   for (int r = r0; r < r1; r += 64) count += __popcll(__ballot(r + lane < r1 && s.list[r + lane] == adapter));
   __syncthreads();
   if (lane == 0) s_red[w] = count;
   __syncthreads();
   int rank = 0;                        // rows of the adapter before this wave's
   for (int i = 0; i < w; ++i) rank += s_red[i];
-#pragma unroll 2
+#pragma unroll 1
   for (int r = r0; r < r1 && rank < begin + kTile; r += 64) {
     const bool is = r + lane < r1 && s.list[r + lane] == adapter;
     const uint64_t same = __ballot(is);
@@ -604,7 +604,7 @@ __device__ __forceinline__ void expand_group(const Lora& p, int a, int rank, int
   store_y<CT>(p, s_rows[col], c0, lg, c0 + 16 * CT <= p.n, y[0]);
 }
 
-// A row without an adapter is the base's: columns c0 .. c0 + 256 - 1.
+// A row without an adapter is the base's: columns c0 .. c0 + cols - 1.
 __device__ __forceinline__ void copy_row(const Lora& p, int r, int c0, int cols) {
   const int c = c0 + threadIdx.x;
   if (p.y != p.base && (int)threadIdx.x < cols && c < p.n) p.y[r * p.y_stride + c] = p.base[r * p.y_stride + c];
@@ -727,7 +727,8 @@ __global__ __launch_bounds__(COLS, NR <= 2 || (NR == 4 && COLS == 512) ? 4 : 1) 
       at[e] = r < 0 ? first : r;
       t[e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-#pragma unroll(NR <= 4 ? 8 : 4)      // as many loads in flight as registers hold
+    constexpr int FLIGHT = NR <= 4 ? 8 : 4;      // as many loads in flight as registers hold
+#pragma unroll FLIGHT
     for (int s = 0; s < p.n_split; ++s)
 #pragma unroll
       for (int e = 0; e < PER; ++e)
