@@ -104,6 +104,7 @@ ORDERS = {"backward-out": 0, "forward-out": 1, "random-out": 2, "token-aligned":
 PLACEMENTS = {"balanced": 0, "all-swap": 1, "all-drop": 2, "interleave-2-1": 3}
 
 _lib = None
+_vocab = {}          # of the contexts that are loaded, by handle: the length of what is passed without one
 
 
 def lib() -> ctypes.CDLL:
@@ -202,10 +203,12 @@ def mz_load_model(cfg: mz_model_cfg, blob: np.ndarray, device: int = 0) -> ctype
     out = ctypes.c_void_p()
     _check(lib().mz_load_model(ctypes.byref(cfg), blob.ctypes.data, blob.nbytes, device,
                                ctypes.byref(out)), None)
+    _vocab[out.value] = cfg.vocab
     return out
 
 
 def mz_free(ctx) -> None:
+    _vocab.pop(getattr(ctx, "value", ctx), None)
     lib().mz_free(ctx)
 
 
@@ -284,6 +287,8 @@ def mz_set_token_rules(ctx, repetition: float = 1.0, frequency: float = 0.0, pre
     tok = np.array([t for t, _ in bias or []], np.int32)
     val = np.array([v for _, v in bias or []], np.float32)
     words = None if mask is None else np.ascontiguousarray(mask, dtype=np.uint32)
+    if words is not None and words.size < (_vocab.get(getattr(ctx, "value", ctx), 0) + 31) // 32:
+        raise MzError(MZ_EINVAL, f"a mask of {words.size} words does not cover the vocabulary")
     r = mz_token_rules(repetition, frequency, presence, tok.ctypes.data, val.ctypes.data, tok.size, _ptr(words))
     _check(lib().mz_set_token_rules(ctx, ctypes.byref(r)), ctx)
 

@@ -1326,6 +1326,20 @@ def test_token_rules_refusals_keep_the_rules():
         assert mz.mz_first_token(e) in (9, 10)
 
 
+def test_token_rules_of_a_short_mask():
+    """The binding refuses a mask that ends before the vocabulary; the rules stay."""
+    m, ctx, eng = tiny_engine()
+    with eng:
+        e = eng.ctx
+        mz.mz_set_token_rules(e, mask=words_of([9, 10], m.vocab))
+        for words in (0, 1, (m.vocab + 31) // 32 - 1):
+            with pytest.raises(mz.MzError) as err:
+                mz.mz_set_token_rules(e, mask=np.ones(words, np.uint32))
+            assert err.value.status == mz.MZ_EINVAL and "vocabulary" in str(err.value)
+        mz.mz_prefill_context(e, ctx)
+        assert mz.mz_first_token(e) in (9, 10)
+
+
 # ----------------------------------------------------------------------------- the calls together
 
 def test_decode_steps_of_a_batch_in_one_graph():
