@@ -159,7 +159,10 @@ mz_status mz_generate(mz_ctx *ctx, int32_t token, int32_t n, int32_t *tokens_out
 
 /* Rules on the tokens that mz_first_token and mz_generate choose (see
  * mz_logits_rules for what they do to the logits).  The history of the
- * penalties is the cached context, prompt included.  Arrays are host memory. */
+ * penalties is the cached context from position history_from on: with 0 all of
+ * it, the prompt included; with its length before the first token only what is
+ * chosen from then on, as frequency and presence penalties over the answer ask
+ * for.  All three penalties have the one history.  Arrays are host memory. */
 typedef struct {
   float repetition, frequency, presence;   /* 1, 0, 0: no penalties */
   const int32_t *bias_token;   /* [n_bias] tokens and what is added to their logits; of several entries */
@@ -167,6 +170,7 @@ typedef struct {
   int32_t n_bias;              /* 0..vocab */
   const uint32_t *mask;        /* [ceil(vocab / 32)], bit v % 32 of word v / 32 is 1 where token v is
                                   allowed, or NULL: all are */
+  int32_t history_from;        /* 0 and up */
 } mz_token_rules;
 
 /* Set the rules for the tokens chosen from now on (NULL: none, the default);
@@ -178,7 +182,8 @@ typedef struct {
  * under other rules, without another prefill.  Synchronizes; allocates device
  * memory the first time.  Errors: EINVAL for a repetition that is not
  * positive, penalties that are not finite, n_bias out of range, a bias token
- * outside the vocabulary, a NaN bias or a mask without a token; ENOMEM. */
+ * outside the vocabulary, a NaN bias, a mask without a token or a negative
+ * history_from; ENOMEM. */
 mz_status mz_set_token_rules(mz_ctx *ctx, const mz_token_rules *rules);
 
 /* Engine options: "overlap" (1: swap-in overlapped with compute, default;

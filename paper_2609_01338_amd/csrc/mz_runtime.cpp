@@ -469,6 +469,7 @@ struct mz_ctx {
   // from the first rules on
   bool rules_on = false;
   mzk::LogitsRules rules;
+  int rules_from = 0;                // first position of the penalties' history
   float* d_logits = nullptr;         // [V]
   uint8_t* d_rules = nullptr;        // penalties, bias tokens and values, mask, the kernel's workspace
   int32_t* d_hist = nullptr;         // [max_ctx] the context's tokens, the first hist_n of them up to date
@@ -1704,10 +1705,12 @@ mz_status mz_first_token(mz_ctx* x, int32_t* token_out, float* logits_out) {
                               hipMemcpyHostToDevice, cs));
         x->hist_n = n;
       }
-      x->timed(kKLogitsRules, 6.0 * x->V, x->V * (logits_out ? 8.0 : 4.0) + n * 4.0, cs, [&] {
+      const int from = std::min(x->rules_from, n), held = x->rules.history ? n - from : 0;
+      x->timed(kKLogitsRules, 6.0 * x->V, x->V * (logits_out ? 8.0 : 4.0) + held * 4.0, cs, [&] {
         mzk::LogitsRules r = x->rules;
         r.out = logits_out ? x->h_logits : nullptr;
-        r.n_history = r.history ? n : 0;
+        if (r.history) r.history += from;
+        r.n_history = held;
         mzk::launch_logits_rules(r, 1, x->d_rules, cs);
       });
     }
@@ -1750,6 +1753,7 @@ mz_status mz_set_token_rules(mz_ctx* x, const mz_token_rules* rules) {
         any |= (i + 1 < words || x->V % 32 == 0 ? t.mask[i] : t.mask[i] & ((1u << (x->V % 32)) - 1)) != 0;
       if (!any) fail(MZ_EINVAL, "the mask allows no token");
     }
+    if (t.history_from < 0) fail(MZ_EINVAL, "history_from is negative");
     HIPCHK(hipStreamSynchronize(x->s_compute));
     // the kernel's workspace first, then penalties, bias tokens, bias values and mask
     const int64_t b_ws = round_up(mzk::logits_rules_ws_bytes(1, x->V), 256), b_bias = round_up((int64_t)x->V * 4, 256);
@@ -1784,6 +1788,7 @@ mz_status mz_set_token_rules(mz_ctx* x, const mz_token_rules* rules) {
       r.mask_words = words;
     }
     x->rules = r;
+    x->rules_from = t.history_from;
     x->rules_on = true;
   });
 }

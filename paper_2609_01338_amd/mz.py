@@ -76,7 +76,7 @@ class mz_kv_append_args(ctypes.Structure):
 class mz_token_rules(ctypes.Structure):
     _fields_ = [("repetition", ctypes.c_float), ("frequency", ctypes.c_float), ("presence", ctypes.c_float),
                 ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
-                ("mask", ctypes.c_void_p)]
+                ("mask", ctypes.c_void_p), ("history_from", ctypes.c_int32)]
 
 
 class mz_logits_rules_args(ctypes.Structure):
@@ -281,15 +281,17 @@ def mz_generate(ctx, token: int, n: int) -> np.ndarray:
 
 
 def mz_set_token_rules(ctx, repetition: float = 1.0, frequency: float = 0.0, presence: float = 0.0,
-                       bias: Optional[list] = None, mask: Optional[np.ndarray] = None) -> None:
+                       bias: Optional[list] = None, mask: Optional[np.ndarray] = None, history_from: int = 0) -> None:
     """bias: (token, value) pairs; mask: uint32 words, bit v % 32 of word v / 32 set where token v is
-    allowed (one word per 32 tokens of the vocabulary)."""
+    allowed (one word per 32 tokens of the vocabulary); history_from: the position of the context from
+    which on tokens count for the penalties."""
     tok = np.array([t for t, _ in bias or []], np.int32)
     val = np.array([v for _, v in bias or []], np.float32)
     words = None if mask is None else np.ascontiguousarray(mask, dtype=np.uint32)
     if words is not None and words.size < (_vocab.get(getattr(ctx, "value", ctx), 0) + 31) // 32:
         raise MzError(MZ_EINVAL, f"a mask of {words.size} words does not cover the vocabulary")
-    r = mz_token_rules(repetition, frequency, presence, tok.ctypes.data, val.ctypes.data, tok.size, _ptr(words))
+    r = mz_token_rules(repetition, frequency, presence, tok.ctypes.data, val.ctypes.data, tok.size, _ptr(words),
+                       history_from)
     _check(lib().mz_set_token_rules(ctx, ctypes.byref(r)), ctx)
 
 

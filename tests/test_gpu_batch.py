@@ -1326,6 +1326,37 @@ def test_token_rules_refusals_keep_the_rules():
         assert mz.mz_first_token(e) in (9, 10)
 
 
+def test_token_rules_over_what_was_chosen():
+    """history_from leaves the prompt out, whatever its length; past the end of the context nothing counts yet."""
+    m, ctx, eng = tiny_engine()
+    with eng:
+        e = eng.ctx
+        mz.mz_prefill_context(e, ctx)
+        plain, raw = mz.mz_first_token(e, m.vocab)
+        pen = np.array([[1.5, 40.0, 3.0]], np.float32)
+        for at in (0, 1, 5, ctx.size - 1, ctx.size, ctx.size + 1, (1 << 31) - 1):
+            mz.mz_set_token_rules(e, 1.5, 40.0, 3.0, history_from=at)
+            mz.mz_prefill_context(e, ctx)
+            tok, logits = mz.mz_first_token(e, m.vocab)
+            ref, bound = logits_oracle(raw[None], pen, [ctx[at:].tolist()], [[]], None, [0])
+            close(logits[None], ref, bound, f"from {at}")
+            assert tok == picked(logits[None])[0]
+        # the answer's tokens count as they come, also by mz_generate and after a cut that leaves fewer than at
+        mz.mz_set_token_rules(e, presence=1000.0, history_from=ctx.size)
+        mz.mz_prefill_context(e, ctx)
+        first = mz.mz_first_token(e, m.vocab)[0]
+        assert first == plain
+        toks = [first] + mz.mz_generate(e, first, 8).tolist()
+        assert len(set(toks)) == 9
+        mz.mz_truncate_context(e, ctx.size - 1)
+        mz.mz_restore_and_prefill(e, ctx[-1:])
+        tok, logits = mz.mz_first_token(e, m.vocab)
+        assert not (logits < -500).any()
+        with pytest.raises(mz.MzError) as err:
+            mz.mz_set_token_rules(e, history_from=-1)
+        assert err.value.status == mz.MZ_EINVAL
+
+
 def test_token_rules_of_a_short_mask():
     """The binding refuses a mask that ends before the vocabulary; the rules stay."""
     m, ctx, eng = tiny_engine()
