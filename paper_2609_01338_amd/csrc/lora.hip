@@ -561,18 +561,23 @@ __device__ __forceinline__ void load_b(const Lora& p, int a, int rank, int c0, f
 }
 
 // The base's values of one row at columns c0 + 16 c + 4 lg .. + 3, and y's.
+// Columns past n take the last one's: with a zero for each under a condition, the
+// wide second product of rank 64 kept 16 bytes a thread in scratch (4099 rows 62.9
+// for 60.1 us).
 template <int CT>
 __device__ __forceinline__ void load_base(const Lora& p, int row, int c0, int lg, bool whole, f32x4 (&y)[CT]) {
+  const float* b = p.base + (int64_t)row * p.y_stride;
+  if (whole) {
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int at = c0 + c * 16 + lg * 4;
-    const float* b = p.base + (int64_t)row * p.y_stride + at;
-    if (whole) {
-      y[c] = *reinterpret_cast<const f32x4*>(b);
-    } else {
+    for (int c = 0; c < CT; ++c) y[c] = *reinterpret_cast<const f32x4*>(b + c0 + c * 16 + lg * 4);
+  } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[c][e] = at + e < p.n ? b[e] : 0.f;
-    }
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = c0 + c * 16 + lg * 4 + e;
+        y[c][e] = b[min(at, p.n - 1)];
+      }
   }
 }
 template <int CT>
@@ -689,12 +694,12 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
 // Workgroups are numbered as above.  4099 rows of 4096 columns, rank 64: 41 us,
 // where base to y alone takes 29 in this order; the rest is t and B, from the
 // L2 for every half tile.  A whole tile a workgroup is as fast, a quarter
-// slower by a seventh; the base's loads ahead of the others' slower.  Four waves
-// a SIMD against three: rank 64 54.8 and 58.3 us for both launches, though 16
-// bytes a thread then lie in scratch, rank 16 40.6 and 42.2; with 512 rows, where
-// ranges of 256 columns do not fill the chip, 20.2 and 19.3.
+// slower by a seventh; the base's loads ahead of the others' slower.  Wide ranges
+// of rank 64 at four waves a SIMD against three: 60.3 and 63.8 us for both
+// launches; with 512 rows, which do not fill the chip, four were slower (20.2 for
+// 19.3) in ranges of 256.
 template <int NR, int COLS>
-__global__ __launch_bounds__(COLS, NR <= 2 || (NR == 4 && COLS == 512) ? 4 : 1) void lora_expand_tile_kernel(Lora p) {
+__global__ __launch_bounds__(COLS, NR == 4 && COLS == 512 ? 4 : 1) void lora_expand_tile_kernel(Lora p) {
   constexpr int KS = GroupParts<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + COLS - 1) / COLS;
   __shared__ __attribute__((aligned(16))) GroupParts<NR> s_t[NX];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
