@@ -728,7 +728,7 @@ int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int
  * rows serves fewer), any content, not shared by calls in flight together (two
  * graphs that may run at once need two).  Results do not change from run to
  * run.  Errors: EINVAL for the above, a NULL pointer, columns beyond one launch
- * (for 8192 rows and more of 2047 adapters 2^19), pointers off 16-byte
+ * (for 8192 rows and more of 2047 adapters above 986624), pointers off 16-byte
  * boundaries, or a short workspace. */
 mz_status mz_lora_add(const void *x_f16, int32_t m, int32_t k, const int32_t *adapter,
                       int32_t n_adapters, const void *a_f16, const void *b_f16, const float *scale,

@@ -3,14 +3,14 @@
 //   out = sum_j w_j v_j / sum_j w_j,  w_j = 2^(s_j - max s),
 //   s_j = log2(e) / sqrt(hd) q . k_j,  j < len.
 //
-// Memory-bound: every key and value of the batch is read once (4 flops per
-// query head and value; a group of 4 heads is 8 flops per byte).  So the work
-// is cut by bytes, not by sequences: the units of 128 keys of all (sequence,
-// KV head) pairs lie in one line, and each workgroup takes an even share of
-// it, whatever the lengths, which are read here on the device.  A share that
-// covers a pair whole writes its output; a pair that several shares meet
-// leaves partials, at most two a workgroup (its first pair, begun by others,
-// and its last, ended by others), and a second kernel joins them.
+// Memory-bound: every key and value of the batch is read once (4 flops per query
+// head for the 4 bytes of a key's and a value's dimension; a group of 4 heads is 4
+// flops per byte).  So the work is cut by bytes, not by sequences: the units of
+// 128 keys of all (sequence, KV head) pairs lie in one line, and each workgroup
+// takes an even share of it, whatever the lengths, which are read here on the
+// device.  A share that covers a pair whole writes its output; a pair that several
+// shares meet leaves partials, at most two a workgroup (its first pair, begun by
+// others, and its last, ended by others), and a second kernel joins them.
 //
 // A workgroup's four waves take the 32-key blocks of its share in turn.  The
 // G query heads of the KV head are the 16-wide side of v_mfma_f32_16x16x32:
@@ -26,11 +26,13 @@
 // weights; matrix instructions are not what bounds this.  Their sum, the partials
 // and the joins are fp32.
 //
-// Measured, both kernels: 64 sequences of 512-8192 keys, 8 KV heads of 128, 122
-// + 5 us: 640 MB at 5.2 TB/s, where reading them alone in this order takes
-// 5.3-5.8 TB/s; one of 32768 24 + 4; one of 2048, heads of 64, 5.3 + 4,
-// latency.  Two and more blocks in flight a wave gained nothing (137 us for the
-// former: the memory is busy, and what each share loads ahead in vain adds up).
+// Measured, both kernels, three inputs in turn: 64 sequences of 512-8192 keys, 8 KV
+// heads of 128, 122 + 5 us: 640 MB at 5.2 TB/s, where only reading them in this
+// order takes 117 us; one of 32768 28 + 5 (reading 31 with a workgroup a CU, as
+// here, 29 with two); one of 2048, heads of 64, 5.4 + 4, latency.  With weights of
+// one f16 the products took 0.2-0.8 us less.  Two and more blocks in flight a wave
+// made the 64 sequences slower (137 us: the memory is busy, and what each share
+// loads ahead in vain adds up); they were not tried with one workgroup a CU.
 #include "mz_kernels.h"
 
 namespace mzk {
@@ -371,11 +373,14 @@ __global__ __launch_bounds__(256) void attn_batch_join_kernel(AttnBatch a) {
 // (what a pair costs beside its keys, its queries, its table and the waves'
 // join, hides behind the other workgroup).  256 against 512 (768) shares,
 // both kernels in a graph, 4 query heads a KV head, dimension 128: 8 pairs of
-// 12000 keys 16.2 against 18.2 (17.9) us, of 32768 27.2 against 28.3 (28.7);
-// 128 pairs of 260-4096 25.4 against 27.2 (29.0); 512 pairs of 50 11.5 against
-// 9.9 (9.9), of 300 22.4 against 20.1 (23.0), of 1000 46.2 against 46.0 (48.8);
-// dimension 64, 512 pairs of 130-2048 33.2 against 27.1 (26.0), of 1000 28.2
-// against 27.0 (30.6).
+// 12000 keys 16.5 against 18.5 (17.9) us, of 32768 28.2 against 28.9 (29.4);
+// 128 pairs of 260-4096 26.7 against 28.1 (26.1), 200 of 1000 25.8 against 27.2
+// (26.5); 256 pairs of 1000 26.2 against 28.1 (28.2), of 260-4096 40.8 against
+// 37.3 (37.4), so the border lies where lengths decide; 320 pairs of 1000 33.1
+// against 33.4 (34.0), of 260-4096 51.1 against 45.5 (45.3); 512 pairs of 50
+// 11.8 against 10.3 (10.2), of 300 22.5 against 20.6 (23.7), of 1000 47.0 against
+// 46.6 (49.8); dimension 64, 512 pairs of 130-2048 31.6 against 25.2 (24.4), of
+// 1000 28.6 against 27.2 (30.7).
 constexpr int kFewPairs = 256;
 
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }

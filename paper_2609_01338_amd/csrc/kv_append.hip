@@ -18,9 +18,10 @@
 // has no neighbour in its chunk: each of its values is a line of its own,
 // which the slot layout asks for.
 //
-// Measured: 4099 f16 rows of 32 + 8 + 8 heads of 128 in 18.6 us, 103 MB at 5.5
-// TB/s (a large copy: 4.6); 64 fp32 rows one a sequence 5.9, 1 row 3.1 us, both
-// latency.
+// Measured: 4099 f16 rows of 32 + 8 + 8 heads of 128 in 23.0 us, 103 MB at 4.5
+// TB/s (a large copy: 4.6), with three inputs in turn; 18.6 with two, which the
+// last-level cache partly holds.  64 fp32 rows one a sequence 6.0, 1 row 3.2 us,
+// both latency.
 #include "mz_kernels.h"
 #include "rope.h"
 

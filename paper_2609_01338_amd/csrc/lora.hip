@@ -13,8 +13,9 @@
 //
 // Memory-bound: a decode step reads each adapter once, a prefill its rows.
 // Measured: 1 row of 2048 x 2048, rank 16, 5.6 us, latency; 33 rows over 24
-// adapters, 4096 x 4096, rank 32, 4.2 + 5.5; 4099 rows over 6, rank 64, 18.1 +
-// 41.5: 171 MB at 2.9 TB/s.
+// adapters, 4096 x 4096, rank 32, 4.5 + 5.9, two chains of dependent loads (list,
+// rows, x and A; then list, t, B, base); 4099 rows over 6, rank 64, 18.5 + 43.7:
+// 171 MB at 2.7 TB/s.
 //  - Few rows (up to kGatherRows): a workgroup per (group of up to 16 rows of
 //    one adapter, K split or column range), found by each workgroup from the
 //    adapter list: row r begins a group when the rows before it with its
@@ -40,11 +41,11 @@ typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));      // the a
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 
 // Rows up to which groups are searched.  Groups against tiles, measured in a
-// graph, 4096 x 4096 of rank 16: 33 rows of one adapter 9.6 against 11.2 us,
-// with an adapter each 8.6 against 15.9; 64 rows 13.0 against 11.6, over 8 mixed
-// adapters 8.7 against 11.5, with an adapter each 10.5 against 20.7.  4096 x
-// 14336, rank 32, 64 rows: 21.2 against 16.6, 10.7 against 16.5, 24.3 against
-// 45.8.  At 128 rows the first kind is nearly twice as slow.
+// graph, 4096 x 4096 of rank 16: 33 rows of one adapter 9.9 against 11.7 us,
+// with an adapter each 9.6 against 17.8; 64 rows 12.4 against 12.3, over 8 mixed
+// adapters 9.0 against 12.2, with an adapter each 11.7 against 25.6.  4096 x
+// 14336, rank 32, 64 rows: 21.5 against 16.1, 10.5 against 18.5, 25.8 against
+// 58.4.  At 128 rows the first kind is nearly twice as slow.
 constexpr int kGatherRows = 64;
 constexpr int kPlanRows = 8192;      // rows of a call whose tiles are counted: 32 entries a thread
 constexpr int kTile = 64;            // rows of a tile
@@ -81,9 +82,13 @@ struct PlanLds {
 // Runs of one adapter, each within a window of 64 rows, that make the tiles as
 // they stand; with more of them the rows are sorted.  As they stand against
 // sorted, 4096 rows of 4096 x 4096, rank 64 (16): runs of 64 rows (as many as
-// windows) 56.6 (43.5) against 69.4 (57.6) us, of 100 (1.6 a window) 70.8
-// (52.5) against 81.3 (63.8), of 48 (2) 79.2 (59.5) against 73.9 (59.7), of 24
-// (3.3) 109 (77) against 72 (59).
+// windows) 50.9 (38.9) against 64.0 (51.8) us, of 100 (1.6 a window) 64.9
+// (49.1) against 75.9 (58.2), of 48 (2) 70.8 (54.4) against 68.0 (52.2), of 24
+// (3.3) 104 (78) against 67 (51).  The eight more are for few rows, whose tiles do
+// not fill the chip either way: 128 rows in 8 runs 15.6 (11.7) against 17.0 (13.3),
+// 256 in 8 17.0 (12.6) against 17.5 (13.7); near the rule's end ranks decide: 256
+// rows in 13 runs 19.7 (13.7) against 18.0 (13.9), 512 in 19 23.5 (17.3) against
+// 22.4 (15.8).
 __host__ __device__ inline int most_runs(int m) {
   const int windows = (m + 63) / 64;
   return windows + windows * 3 / 4 + 8;
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lora p) {
 // time, as whole 128-byte lines that are read once per workgroup (with
 // fragments straight from memory, 16 rows of 64 bytes an instruction, and each
 // wave's own copy of A, 4099 rows of 4096 by 64 ranks took 24.7 us, so 15.4,
-// and 18.1 with plan_tile); two tiles of k are in flight while one is
+// and 18.5 with plan_tile); two tiles of k are in flight while one is
 // multiplied.  Wave w has rows 16 w .. 16 w + 15.  The workgroups of a K range
 // meet on one XCD where there are a multiple of eight ranges, so that each L2
 // holds its share of A.
@@ -690,10 +695,12 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
 
 // Many rows, second product: half a tile's rows x COLS columns, 64 a wave; the
 // workgroup adds the splits of its rows' t itself (a launch between the two
-// that made their halves once cost 1.5-4 us more, whatever the rows).
-// Workgroups are numbered as above.  4099 rows of 4096 columns, rank 64: 41 us,
-// where base to y alone takes 29 in this order; the rest is t and B, from the
-// L2 for every half tile.  A whole tile a workgroup is as fast, a quarter
+// that prepared t once cost 1.5-4 us more, whatever the rows).  Workgroups are
+// numbered as above.  4099 rows of 4096 columns, rank 64: 43.7 us, where rows
+// without an adapter (base to y alone, in this order) take 29.2; the rest is t
+// and B, which every half tile reads from the L2.  100 MB come from memory, where
+// base, t and B once each are 79: B enters each of the eight L2s.  A whole tile a
+// workgroup is as fast, a quarter
 // slower by a seventh; the base's loads ahead of the others' slower.  Wide ranges
 // of rank 64 at four waves a SIMD against three: 60.3 and 63.8 us for both
 // launches; with 512 rows, which do not fill the chip, four were slower (20.2 for
@@ -766,10 +773,10 @@ int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
 
 // Both products in one launch: where a workgroup's A is at most 64 KB and all
 // that the workgroups read of it at most 16 MB.  Measured in a graph, one
-// launch against two: 2048 x 2048, rank 16 (64 KB), 1 row 5.8 against 6.4 us,
-// 16 rows with an adapter each (16 MB) 6.1 against 6.7, 32 rows 9.2 against
-// 6.9; 4096 x 4096, rank 16 (128 KB), 1 row 7.9 against 6.7; 256 x 1024 (8 KB),
-// 32 rows 4.1 against 6.6.
+// launch against two: 2048 x 2048, rank 16 (64 KB), 1 row 6.1 against 7.2 us,
+// 16 rows with an adapter each (16 MB) 6.3 against 7.4, 32 rows 8.6 against
+// 7.3; 4096 x 4096, rank 16 (128 KB), 1 row 8.2 against 7.2; 256 x 1024 (8 KB),
+// 32 rows 4.3 against 7.2.
 bool lora_fused(const Lora& p) {
   const int64_t a_bytes = (int64_t)p.R * p.k * 2, ranges = (p.n + kColsFused - 1) / kColsFused;
   return p.m <= kGatherRows && a_bytes <= (64 << 10) && a_bytes * ranges * p.m <= (16 << 20);
@@ -778,9 +785,9 @@ bool lora_fused(const Lora& p) {
 // The second product of many rows in ranges of 512 columns: halves what its
 // workgroups read of t, where ranks are many and the workgroups still fill the
 // chip.  512 against 256, both launches, 4096 x 4096, 4 adapters: rank 64, 4096
-// rows 50.4 against 53.9 us, 1024 (512 workgroups of 256) 22.5 against 23.7, 512
-// rows 19.6 against 18.9; rank 128, 4096 rows 71.2 against 76.4; rank 16 42.2
-// against 42.0.
+// rows 45.5 against 48.4 us, 1024 (512 workgroups of 256) 22.5 against 24.0, 512
+// rows 18.9 against 17.5; rank 128, 4096 rows 68.6 against 75.3, 512 26.0 against
+// 24.4; rank 16, 4096 rows, with f16 halves of t 42.2 against 42.0.
 bool lora_wide(const Lora& p) { return (int64_t)(p.m + kTile / 2 - 1) / (kTile / 2) * ((p.n + 255) / 256) >= 512; }
 
 template <int NR>
@@ -811,9 +818,9 @@ int most_tiles(int m, int n_adapters) {
 
 // K splits: enough workgroups for the chip, at least two steps of 32 a wave, at
 // most 16 (few rows) or 32.  With at most 8, 1 row of 8960 x 1536, rank 64,
-// takes 11.2 for 9.8 us, 512 rows of 14336 x 4096, rank 16, 22.1, with 16 17.8,
-// with 32 16.2; 33 rows of the latter with 32 12.5 for 11.6.  Half the
-// workgroups for many rows: 4096 of the latter 64.2 for 53.7 us; twice: 55.2.
+// takes 11.5 for 9.8 us, 512 rows of 14336 x 4096, rank 16, 21.1, with 16 17.3,
+// with 32 16.2; 33 rows of the latter with 32 12.9 for 11.6.  Half the
+// workgroups for many rows: 4096 of the latter 55.2 for 49.0 us; twice: 50.6.
 constexpr int kFewBlocks = 1024, kManyBlocks = 520;
 
 int most_splits(int m, int k) {
