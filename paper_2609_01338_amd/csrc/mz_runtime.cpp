@@ -2334,9 +2334,9 @@ mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t
     if (m < 0 || vocab < 1 || vocab > (1 << 30) || stride < vocab)
       fail(MZ_EINVAL, "m must be at least 0, vocab in 1..2^30, stride at least vocab");
     if (((uintptr_t)logits & 3) || ((uintptr_t)out & 3)) fail(MZ_EINVAL, "logits and out must lie on 4-byte boundaries");
-    if (r.history && (!r.history_off || !r.penalty)) fail(MZ_EINVAL, "history needs history_off and penalty");
+    if (r.history && (!r.history_off || (m > 0 && !r.penalty))) fail(MZ_EINVAL, "history needs history_off and penalty");
     if (r.bias_token && (!r.bias_value || !r.bias_off)) fail(MZ_EINVAL, "bias_token needs bias_value and bias_off");
-    if (r.mask && (!r.mask_row || r.n_masks < 1 || r.mask_words < ((int64_t)vocab + 31) / 32))
+    if (r.mask && ((m > 0 && !r.mask_row) || r.n_masks < 1 || r.mask_words < ((int64_t)vocab + 31) / 32))
       fail(MZ_EINVAL, "mask needs mask_row, n_masks, and mask_words that cover vocab");
     check_stream(stream);
     if (m == 0) return;

@@ -154,7 +154,10 @@ def test_no_rows_of_empty_tensors():
     mz.mz_kv_append(**{**APPEND, "m": 0, "k_ptr": 0, "v_ptr": 0, "q_ptr": 0, "q_out_ptr": 0, "seq_ptr": 0, "pos_ptr": 0})
     mz.mz_lora_add(**{**LORA, "m": 0, "x_ptr": 0, "adapter_ptr": 0, "base_ptr": 0, "y_ptr": 0, "ws_ptr": 0, "ws_bytes": 0})
     mz.mz_logits_rules(**{**LOGITS, "m": 0, "logits_ptr": 0, "out_ptr": 0, "token_ptr": 0, "ws_ptr": 0, "ws_bytes": 0})
+    mz.mz_logits_rules(**{**LOGITS, "m": 0, "logits_ptr": 0, "out_ptr": 0, "penalty_ptr": 0, "mask_row_ptr": 0})
     # what is not rows is looked at all the same
+    refused(mz.mz_logits_rules, **{**LOGITS, "m": 0, "history_off_ptr": 0}, match="history_off")
+    refused(mz.mz_logits_rules, **{**LOGITS, "m": 0, "n_masks": 0}, match="mask")
     refused(mz.mz_kv_append, **{**APPEND, "m": 0, "slab_ptr": 0}, match="NULL")
     refused(mz.mz_lora_add, **{**LORA, "m": 0, "a_ptr": 0}, match="NULL")
     refused(mz.mz_lora_add, **{**LORA, "m": 0, "max_rank": 12}, match="max_rank")
