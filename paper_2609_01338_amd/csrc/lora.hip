@@ -700,11 +700,10 @@ __global__ __launch_bounds__(256) void lora_fused_kernel(Lora p) {
 // without an adapter (base to y alone, in this order) take 29.2; the rest is t
 // and B, which every half tile reads from the L2.  100 MB come from memory, where
 // base, t and B once each are 79: B enters each of the eight L2s.  A whole tile a
-// workgroup is as fast, a quarter
-// slower by a seventh; the base's loads ahead of the others' slower.  Wide ranges
-// of rank 64 at four waves a SIMD against three: 60.3 and 63.8 us for both
-// launches; with 512 rows, which do not fill the chip, four were slower (20.2 for
-// 19.3) in ranges of 256.
+// workgroup is as fast, a quarter slower by a seventh; the base's loads ahead of
+// the others' slower.  Wide ranges of rank 64 at four waves a SIMD against three:
+// 60.3 and 63.8 us for both launches; with 512 rows, which do not fill the chip,
+// four were slower (20.2 for 19.3) in ranges of 256.
 template <int NR, int COLS>
 __global__ __launch_bounds__(COLS, NR == 4 && COLS == 512 ? 4 : 1) void lora_expand_tile_kernel(Lora p) {
   constexpr int KS = GroupParts<NR>::KS, ROWS = kTile / 2, NX = ROWS / 16, PER = (ROWS * 4 * NR + COLS - 1) / COLS;
