@@ -1,0 +1,710 @@
+"""The operators of a decode step that checks drafted trees: what they compute, in plain form, and what is timed.
+
+A drafter proposes a tree of tokens for every sequence; one step of the large model scores all of its nodes at once
+and keeps the branch that the model itself would have taken.  Beside the projections, that step is made of these calls,
+over the same chunked KV slab as the step of one token a sequence:
+
+* ``pages``: which slots the sequences hold from now on (keys that stay, forks, room for the step, slots given up
+  where the slab shrinks), and the copies that this asks for (``mz_kv_pages``, ``mz_kv_copy``);
+* ``plan``: the rows of the trees: sequences, places, rotary positions and what every node sees (``mz_tree_plan``);
+* ``append``: keys and values into the cache at their places, rotated to positions of one or several axes
+  (``mz_kv_append_axes``);
+* ``attention``: every node against its sequence's cache and its own ancestors (``mz_attention_tree``);
+* ``accept``: the branch that the chosen tokens take, its keys and values moved together (``mz_tree_accept``).
+
+Slots are laid out as for ``mz_attention``: keys [chunk][n_kv * head_dim], then values [n_kv * head_dim][chunk], in
+halves.  Shapes are those of the framework's model classes.
+"""
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEVICE = "cuda"
+
+# query heads, key/value heads, head dimension, layers, rotary base
+MODELS = {"tiny": (4, 2, 64, 4, 1e4), "1b": (32, 8, 64, 16, 5e5), "1p5b": (12, 2, 128, 28, 5e5), "8b": (32, 8, 128, 32, 5e5)}
+VOCAB = 128256
+
+
+# ----------------------------------------------------------------------------- the cases
+
+def listed():
+    return [
+        # one chat on the 1B class, a small tree: all latency
+        dict(name="tree_attn_1b_1x7", kind="attention", model="1b", seqs=1, nodes=7, even=True, ctx=2048, chain=False, chunk=256, mix=1),
+        # eight requests of uneven lengths and trees, small pages, a query group that is no power of two
+        dict(name="tree_attn_1p5b_8_ragged", kind="attention", model="1p5b", seqs=8, nodes=27, even=False, ctx=16384, chain=False,
+             chunk=16, mix=2),
+        # a batch of uneven lengths, trees of a drafter of a few branches
+        dict(name="tree_attn_8b_32_ragged", kind="attention", model="8b", seqs=32, nodes=16, even=False, ctx=8192, chain=False,
+             chunk=256, mix=3),
+        # four long documents and wide trees: as much arithmetic as memory
+        dict(name="tree_attn_8b_4x64", kind="attention", model="8b", seqs=4, nodes=64, even=True, ctx=24576, chain=False, chunk=256, mix=4),
+        # the drafted rows of one chat: positions by depth, places in a row
+        dict(name="axes_1b_7rows", kind="append", model="1b", rows=7, seqs=1, past=2048, axes=1, chunk=256, f32=True, mix=5),
+        # prompts of pictures and text, positions of time, height and width
+        dict(name="axes_1p5b_prompts", kind="append", model="1p5b", rows=4099, seqs=5, past=3000, axes=3, chunk=256, f32=False, mix=6),
+        # one small tree
+        dict(name="plan_1x7", kind="plan", seqs=1, nodes=7, even=True, ctx=2048, mix=7),
+        # a full batch of wide trees
+        dict(name="plan_64x61", kind="plan", seqs=64, nodes=61, even=False, ctx=16384, mix=8),
+        # one chat's step ends
+        dict(name="accept_1b_1x7", kind="accept", model="1b", seqs=1, nodes=7, even=True, ctx=2048, layers=16, chunk=256, mix=3),
+        # a full batch's step ends, all layers of the 8B class
+        dict(name="accept_8b_64x61", kind="accept", model="8b", seqs=64, nodes=61, even=False, ctx=8192, layers=32, chunk=256, mix=10),
+        # a step begins for 64 requests in small pages: room for their trees, a few leave and a few come
+        dict(name="pages_1p5b_step", kind="pages", model="1p5b", seqs=64, ctx=4096, room=16, forks=0, leave=4, shrink=0, layers=2,
+             chunk=16, mix=11),
+        # another program needs memory: the slab gives up a part of its slots while requests fork
+        dict(name="pages_8b_shrink", kind="pages", model="8b", seqs=32, ctx=2048, room=64, forks=12, leave=10, shrink=24, layers=16,
+             chunk=256, mix=12),
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    kind = rng.choice(["attention", "attention", "attention", "append", "plan", "accept", "pages"])
+    model = rng.choice(["tiny", "1b", "1p5b", "8b"])
+    mix = rng.randrange(100, 1 << 30)
+    if kind == "attention":
+        seqs = _log(rng, 1, 64)
+        nodes = _log(rng, 1, 256)
+        ctx = _log(rng, 1, min(32768, 8192 * 32 // seqs, max(1, 4 * 64 * 24576 // (seqs * nodes) - nodes)))
+        return dict(kind=kind, model=model, seqs=seqs, nodes=nodes, even=seqs * ctx <= 64 * 1024 and rng.random() < 0.5, ctx=ctx,
+                    chain=rng.random() < 0.3, chunk=rng.choice([8, 16, 64, 256]), mix=mix)
+    if kind == "append":
+        rows = _log(rng, 1, 4096)
+        return dict(kind=kind, model=model, rows=rows, seqs=rng.randint(1, min(rows, 8)), past=_log(rng, 1, 16384),
+                    axes=rng.choice([1, 2, 3, 4]), chunk=rng.choice([16, 64, 256]), f32=rng.random() < 0.5, mix=mix)
+    seqs = _log(rng, 1, 64)
+    if kind == "plan":
+        return dict(kind=kind, seqs=seqs, nodes=_log(rng, 1, 256), even=rng.random() < 0.5, ctx=_log(rng, 1, 32768), mix=mix)
+    layers = rng.choice([1, 4, 16])
+    if kind == "accept":
+        return dict(kind=kind, model=model, seqs=seqs, nodes=_log(rng, 1, 256), even=rng.random() < 0.5, ctx=_log(rng, 1, 32768),
+                    layers=layers, chunk=rng.choice([8, 16, 64, 256]), mix=mix)
+    seqs = min(seqs, 32)
+    return dict(kind=kind, model=model, seqs=seqs, ctx=_log(rng, 1, 2048), room=_log(rng, 1, 64), forks=rng.randint(0, seqs // 2),
+                leave=rng.randint(0, seqs // 4), shrink=rng.choice([0, 0, 12, 24]), layers=layers, chunk=rng.choice([8, 16, 64, 256]),
+                mix=mix)
+
+
+def _counts(case):
+    """Nodes of every tree: all of them `nodes`, or spread over its lower fourth part and up."""
+    r, n = random.Random(case["mix"]), case["nodes"]
+    return [n if case["even"] or i == 0 else _log(r, max(1, n // 4), n) for i in range(case["seqs"])]
+
+
+def _lens(case):
+    """Cached tokens of every sequence before its tree."""
+    r, ctx = random.Random(case["mix"] + 1), case["ctx"]
+    return [ctx if case["even"] or i == 0 else _log(r, max(1, ctx // 16), ctx) for i in range(case["seqs"])]
+
+
+def _trees(case):
+    """The parents of every tree's nodes, level by level (so they ascend), -1 for the root."""
+    r, trees = random.Random(case["mix"] + 2), []
+    for n in _counts(case):
+        p = [-1] + [0] * (n - 1)
+        for i in range(2, n):
+            p[i] = min(i - 1, p[i - 1] + r.choice([0, 0, 0, 1, 1]))
+        trees.append(p)
+    return trees
+
+
+def _branch(parents, r):
+    """A branch from the root, as the model may take it: its nodes lie where they will stay or behind all of it."""
+    at, way = len(parents) - 1 - r.randrange((len(parents) + 1) // 2), []
+    while at >= 0:
+        way.append(at)
+        at = parents[at]
+    way.reverse()
+    way = way[:r.randint(1, len(way))]
+    while not all(node == i or node >= len(way) for i, node in enumerate(way)):
+        way.pop()
+    return way
+
+
+def _branches(case):
+    r = random.Random(case["mix"] + 3)
+    return [_branch(p, r) for p in _trees(case)]
+
+
+def _spans(case):
+    """(first place, rows) of every sequence of an append."""
+    r, n, rows = random.Random(case["mix"]), case["seqs"], case["rows"]
+    cuts = [0] + sorted(r.sample(range(1, rows), n - 1)) + [rows]
+    return [(r.randint(0, case["past"]), b - a) for a, b in zip(cuts, cuts[1:])]
+
+
+def _page_plan(case):
+    """Held keys of every row of the table, and what becomes of it: (held, source, keys that stay, room)."""
+    r, n, ctx = random.Random(case["mix"]), case["seqs"], case["ctx"]
+    held = [_log(r, max(1, ctx // 8), ctx) for _ in range(n)]
+    rows = list(range(n))
+    r.shuffle(rows)
+    gone, forked = rows[:case["leave"]], rows[case["leave"]:case["leave"] + case["forks"]]
+    stay = rows[case["leave"] + case["forks"]:]
+    src, keep = list(range(n)), list(held)
+    for b in forked:
+        src[b] = r.choice(stay or [b])
+        keep[b] = held[src[b]]
+    for b in gone:      # a request leaves, in half of the rows another one comes
+        src[b], keep[b] = -1, 0
+    room = [case["room"] if b not in gone else r.choice([0, case["room"] * 4]) for b in range(n)]
+    return held, src, keep, room
+
+
+# ----------------------------------------------------------------------------- inputs
+
+def _gen(seed, salt):
+    return torch.Generator(device=DEVICE).manual_seed((int(seed) * 1000003 + salt) % (1 << 62))
+
+
+def _ints(v, dtype=torch.int32):
+    return torch.tensor(v, dtype=dtype, device=DEVICE)
+
+
+def _offsets(counts):
+    off = [0]
+    for n in counts:
+        off.append(off[-1] + n)
+    return off
+
+
+def _normal(shape, g):
+    return torch.empty(shape, device=DEVICE, dtype=torch.float16).normal_(generator=g)
+
+
+def _bits(parents, words):
+    """What every node of a tree sees of it, itself and its ancestors, as words of 32 bits."""
+    seen = []
+    for i, p in enumerate(parents):
+        seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+    return [[(s >> 32 * w & 0xFFFFFFFF) - (s >> 32 * w + 31 & 1) * (1 << 32) for w in range(words)] for s in seen]
+
+
+def _prepare_attention(case, seed):
+    nq, nkv, hd, _, _ = MODELS[case["model"]]
+    g, c, lens, counts = _gen(seed, 1), case["chunk"], _lens(case), _counts(case)
+    chunks = [(n + t + c - 1) // c for n, t in zip(lens, counts)]
+    table = torch.full((len(lens), max(chunks)), -1, dtype=torch.int32, device=DEVICE)
+    held = torch.arange(max(chunks), device=DEVICE)[None, :] < _ints(chunks)[:, None]
+    table[held] = torch.randperm(sum(chunks), device=DEVICE, generator=g).int()
+    m, words = sum(counts), (max(counts) + 31) // 32
+    mask = None if case["chain"] else _ints([row for p in _trees(case) for row in _bits(p, words)])
+    q = torch.randn(m, nq * hd, device=DEVICE, generator=g).half()
+    return dict(kind="attention", nq=nq, nkv=nkv, hd=hd, c=c, m=m, n_seq=len(lens), most=max(counts), q=q, mask=mask,
+                slab=_normal((sum(chunks), 2 * c * nkv * hd), g), n_slots=sum(chunks), table=table, lens=_ints(lens),
+                row_off=_ints(_offsets(counts)), out=torch.zeros_like(q), ws=None)
+
+
+def _prepare_append(case, seed):
+    nq, nkv, hd, _, theta = MODELS[case["model"]]
+    g, c, m, na = _gen(seed, 2), case["chunk"], case["rows"], case["axes"]
+    r = random.Random(case["mix"] + 1)
+    spans = _spans(case)
+    place = [p + i for p, n in spans for i in range(n)]
+    seq = [s for s, (_, n) in enumerate(spans) for _ in range(n)]
+    if na == 1:      # drafted rows: a depth below the tree's first
+        axes = [[p + (0 if i == 0 else r.randint(1, min(i, 8))) for p, n in spans for i in range(n)]]
+    else:            # rows of pictures: a time that goes on slowly, places on a grid that is `wide` wide
+        wide = max(2, math.isqrt(m))
+        axes = [[p + (i // (wide * wide) if a == 0 else i // wide % wide if a == 1 else i % wide if a == 2 else i // 7)
+                 for p, n in spans for i in range(n)] for a in range(na)]
+    half = hd // 2   # pairs of a head by their axis: a part of them each, one after the other
+    first = half // (na + 1) if na > 1 else half
+    pair_axis = [0] * first + [1 + i * (na - 1) // (half - first) for i in range(half - first)]
+    # chunks of the sequences' whole pasts are in the table; those that the step does not touch share slot 0
+    table = torch.zeros(len(spans), max(p + n - 1 for p, n in spans) // c + 1, dtype=torch.int32, device=DEVICE)
+    touched = sorted({(s, p // c) for s, p in zip(seq, place)})
+    at = _ints(touched, torch.int64)
+    table[at[:, 0], at[:, 1]] = 1 + torch.randperm(len(touched), device=DEVICE, generator=g).int()
+    n_slots, n_rope = len(touched) + 1, max(map(max, axes)) + 1
+    inv = theta ** (-2.0 * torch.arange(half, device=DEVICE, dtype=torch.float64) / hd)
+    ang = torch.arange(n_rope, device=DEVICE, dtype=torch.float64)[:, None] * inv[None, :]
+    qkv = torch.randn(m, (nq + 2 * nkv) * hd, device=DEVICE, generator=g)
+    return dict(kind="append", nq=nq, nkv=nkv, hd=hd, c=c, m=m, f32=case["f32"], qkv=qkv if case["f32"] else qkv.half(),
+                seq=_ints(seq), place=_ints(place), rope_pos=_ints(axes), n_axes=na, pair_axis=pair_axis, n_seq=len(spans),
+                table=table, n_slots=n_slots, n_rope=n_rope, rope=torch.stack([ang.cos(), ang.sin()], 2).float().contiguous(),
+                slab=_normal((n_slots, 2 * c * nkv * hd), g), q_out=torch.zeros(m, nq * hd, device=DEVICE, dtype=torch.float16))
+
+
+def _prepare_plan(case, seed):
+    counts, trees = _counts(case), _trees(case)
+    m, words = sum(counts), (max(counts) + 31) // 32
+    r = random.Random(int(seed))
+    depth = 1
+    for p in trees:
+        d = []
+        for i in p:
+            d.append(1 + (d[i] if i >= 0 else 0))
+        depth = max(depth, max(d))
+    new = lambda *shape: torch.zeros(shape, device=DEVICE, dtype=torch.int32)  # noqa: E731
+    return dict(kind="plan", m=m, n_seq=len(counts), words=words, most=max(counts), deep=depth, row_off=_ints(_offsets(counts)),
+                parent=_ints([i for p in trees for i in p]), lens=_ints([max(0, n - r.randint(0, 64)) for n in _lens(case)]),
+                seq=new(m), place=new(m), rope_pos=new(m), mask=new(m, words))
+
+
+def _prepare_accept(case, seed):
+    _, nkv, hd, _, _ = MODELS[case["model"]]
+    g, c, layers, lens, counts = _gen(seed, 4), case["chunk"], case["layers"], _lens(case), _counts(case)
+    r = random.Random(int(seed))
+    trees, ways = _trees(case), _branches(case)
+    token, choice = [], []
+    for p, way in zip(trees, ways):
+        t, taken = [], set()
+        for i, q in enumerate(p):     # siblings hold tokens of their own
+            v = r.randrange(VOCAB)
+            while (q, v) in taken:
+                v = r.randrange(VOCAB)
+            taken.add((q, v))
+            t.append(v)
+        ch = [r.randrange(VOCAB) for _ in p]
+        for a, b in zip(way, way[1:]):
+            ch[a] = t[b]
+        while (way[-1], ch[way[-1]]) in taken:
+            ch[way[-1]] = r.randrange(VOCAB)
+        token += t
+        choice += ch
+    # chunks that the trees do not touch share slot 0
+    wide = max((n + t - 1) // c for n, t in zip(lens, counts)) + 1
+    table = torch.zeros(len(lens), wide, dtype=torch.int32, device=DEVICE)
+    touched = [(b, k) for b, (n, t) in enumerate(zip(lens, counts)) for k in range(n // c, (n + t - 1) // c + 1)]
+    at = _ints(touched, torch.int64)
+    table[at[:, 0], at[:, 1]] = 1 + torch.randperm(len(touched), device=DEVICE, generator=g).int()
+    n_slots, m = len(touched) + 1, sum(counts)
+    new = lambda n: torch.zeros(n, device=DEVICE, dtype=torch.int32)  # noqa: E731
+    return dict(kind="accept", nkv=nkv, hd=hd, c=c, layers=layers, m=m, n_seq=len(lens), most=max(counts), row_off=_ints(_offsets(counts)),
+                deep=max(map(len, ways)), parent=_ints([i for p in trees for i in p]), token=_ints(token), choice=_ints(choice),
+                lens=_ints(lens), table=table, n_slots=n_slots, slab=_normal((layers, n_slots, 2 * c * nkv * hd), g),
+                accepted=new(len(lens)), path=new(m), next=new(len(lens)), len_out=new(len(lens)))
+
+
+def _prepare_pages(case, seed):
+    _, nkv, hd, _, _ = MODELS[case["model"]]
+    g, c, layers = _gen(seed, 5), case["chunk"], case["layers"]
+    held, src, keep, room = _page_plan(case)
+    chunks = [(n + c - 1) // c for n in held]
+    # the whole room of all rows and a few slots more; where the slab shrinks, it gives up that many of a hundred
+    after = sum((k + w + c - 1) // c + 1 for k, w in zip(keep, room))
+    n_slots = (max(sum(chunks), after) + 4) * 100 // (100 - case["shrink"]) + 1
+    wide = max((k + w + c - 1) // c for k, w in zip(held + keep, room + room)) + 1
+    table = torch.full((len(held), wide), -1, dtype=torch.int32, device=DEVICE)
+    here = torch.arange(wide, device=DEVICE)[None, :] < _ints(chunks)[:, None]
+    table[here] = torch.randperm(n_slots, device=DEVICE, generator=g)[:sum(chunks)].int()
+    limit = n_slots - n_slots * case["shrink"] // 100
+    new = lambda *shape: torch.zeros(shape, device=DEVICE, dtype=torch.int32)  # noqa: E731
+    return dict(kind="pages", nkv=nkv, hd=hd, c=c, layers=layers, n_seq=len(held), n_slots=n_slots, limit=limit, table=table,
+                table_out=torch.zeros_like(table), src=_ints(src), keep=_ints(keep), room=_ints(room), info=new(4),
+                copies=new(len(held) + n_slots - limit, 4), slab=_normal((layers, n_slots, 2 * c * nkv * hd), g), ws=None)
+
+
+def prepare(case, seed):
+    s = {"attention": _prepare_attention, "append": _prepare_append, "plan": _prepare_plan, "accept": _prepare_accept,
+         "pages": _prepare_pages}[case["kind"]](case, seed)
+    if own and "ws" in s:
+        from paper_2609_01338_amd import mz
+        need = (mz.mz_attention_tree_workspace_bytes(s["m"], s["n_seq"], s["nq"], s["nkv"], s["hd"]) if s["kind"] == "attention" else
+                mz.mz_kv_pages_workspace_bytes(s["n_seq"], s["table"].shape[1], s["n_slots"]))
+        s["ws"] = torch.empty(need, device=DEVICE, dtype=torch.uint8)
+    return s
+
+
+# ----------------------------------------------------------------------------- the calls of the framework
+
+def _own_attention(s):
+    from paper_2609_01338_amd import mz
+    mask = {} if s["mask"] is None else dict(mask_ptr=s["mask"].data_ptr(), mask_words=s["mask"].shape[1])
+    mz.mz_attention_tree(s["q"].data_ptr(), s["m"], s["row_off"].data_ptr(), s["lens"].data_ptr(), s["n_seq"], s["slab"].data_ptr(),
+                         s["n_slots"], s["table"].data_ptr(), s["table"].shape[1], s["c"], s["nq"], s["nkv"], s["hd"],
+                         s["ws"].data_ptr(), s["ws"].numel(), s["out"].data_ptr(), torch.cuda.current_stream().cuda_stream, **mask)
+    return s["out"]
+
+
+def _own_append(s):
+    from paper_2609_01338_amd import mz
+    q, size = s["qkv"].data_ptr(), 4 if s["f32"] else 2
+    wide, dq, dkv = s["qkv"].shape[1], s["nq"] * s["hd"], s["nkv"] * s["hd"]
+    mz.mz_kv_append_axes(s["m"], q + dq * size, q + (dq + dkv) * size, s["seq"].data_ptr(), s["place"].data_ptr(),
+                         s["rope_pos"].data_ptr(), s["n_axes"], s["pair_axis"], s["rope"].data_ptr(), s["n_rope"],
+                         s["slab"].data_ptr(), s["n_slots"], s["table"].data_ptr(), s["n_seq"], s["table"].shape[1], s["c"],
+                         s["nkv"], s["hd"], torch.cuda.current_stream().cuda_stream, q_ptr=q, n_q=s["nq"],
+                         q_out_ptr=s["q_out"].data_ptr(), k_stride=wide, v_stride=wide, q_stride=wide, f32=s["f32"])
+    return {"slab": s["slab"], "q": s["q_out"]}
+
+
+def _own_plan(s):
+    from paper_2609_01338_amd import mz
+    mz.mz_tree_plan(s["row_off"].data_ptr(), s["lens"].data_ptr(), s["n_seq"], s["m"], torch.cuda.current_stream().cuda_stream,
+                    parent_ptr=s["parent"].data_ptr(), seq_ptr=s["seq"].data_ptr(), place_ptr=s["place"].data_ptr(),
+                    rope_pos_ptr=s["rope_pos"].data_ptr(), mask_ptr=s["mask"].data_ptr(), mask_words=s["words"])
+    return {k: s[k] for k in ("seq", "place", "rope_pos", "mask")}
+
+
+def _own_accept(s):
+    from paper_2609_01338_amd import mz
+    mz.mz_tree_accept(s["row_off"].data_ptr(), s["token"].data_ptr(), s["choice"].data_ptr(), s["lens"].data_ptr(), s["n_seq"], s["m"],
+                      s["accepted"].data_ptr(), s["path"].data_ptr(), s["next"].data_ptr(), s["len_out"].data_ptr(),
+                      torch.cuda.current_stream().cuda_stream, parent_ptr=s["parent"].data_ptr(), slab_ptr=s["slab"].data_ptr(),
+                      n_slots=s["n_slots"], n_layers=s["layers"], layer_bytes=s["slab"].stride(0) * 2, table_ptr=s["table"].data_ptr(),
+                      n_table=s["table"].shape[1], chunk_tokens=s["c"], n_kv=s["nkv"], head_dim=s["hd"])
+    return {k: s[k] for k in ("accepted", "path", "next", "len_out", "slab")}
+
+
+def _own_pages(s):
+    from paper_2609_01338_amd import mz
+    stream = torch.cuda.current_stream().cuda_stream
+    mz.mz_kv_pages(s["table"].data_ptr(), s["table_out"].data_ptr(), s["n_seq"], s["table"].shape[1], s["n_slots"], s["c"],
+                   s["keep"].data_ptr(), s["copies"].data_ptr(), s["info"].data_ptr(), s["ws"].data_ptr(), s["ws"].numel(), stream,
+                   src_ptr=s["src"].data_ptr(), room_ptr=s["room"].data_ptr(), slot_limit=s["limit"])
+    mz.mz_kv_copy(s["copies"].data_ptr(), s["info"].data_ptr() + 8, s["copies"].shape[0], s["slab"].data_ptr(), s["n_slots"],
+                  s["layers"], s["slab"].stride(0) * 2, s["c"], s["nkv"], s["hd"], stream)
+    return {k: s[k] for k in ("table_out", "info", "slab")}
+
+
+# ----------------------------------------------------------------------------- the plain forms
+
+def _plain_attention(s):
+    b, nq, nkv, hd, c, most, m = s["n_seq"], s["nq"], s["nkv"], s["hd"], s["c"], s["most"], s["m"]
+    half = s["slab"].view(s["n_slots"], 2, -1)
+    slot = s["table"].long().clamp(min=0)
+    top = slot.shape[1] * c
+    # trees padded to the largest
+    node = torch.arange(most, device=DEVICE)
+    first, count = s["row_off"][:-1].long(), (s["row_off"][1:] - s["row_off"][:-1]).long()
+    row = (first[:, None] + node[None, :]).clamp(max=m - 1)
+    real = node[None, :] < count[:, None]
+    q = s["q"][row].float().view(b, most, nkv, nq // nkv, hd).permute(0, 2, 3, 1, 4).reshape(b, nkv, -1, hd)
+    # what a node sees: the keys before the tree, and of the tree what its mask says
+    at = torch.arange(top, device=DEVICE)[None, :] - s["lens"][:, None].long()
+    inside = (at >= 0) & (at < count[:, None])
+    if s["mask"] is None:
+        seen = node[None, :, None] >= at[:, None, :]
+    else:
+        words = s["mask"][row]
+        at = at.clamp(0, most - 1)
+        word = torch.gather(words, 2, (at // 32)[:, None, :].expand(b, most, top))
+        seen = (word >> (at % 32).int()[:, None, :]) & 1 == 1
+    seen = ((seen & inside[:, None, :]) | (torch.arange(top, device=DEVICE)[None, :] < s["lens"][:, None])[:, None, :])[:, None, None]
+    k = half[:, 0].unflatten(1, (c, nkv, hd))[slot].float().view(b, top, nkv, hd).permute(0, 2, 3, 1).contiguous()
+    score = (torch.matmul(q, k) / math.sqrt(hd)).view(b, nkv, nq // nkv, most, top)
+    del k
+    score = torch.where(seen, score, -math.inf)
+    high = score.amax(4, keepdim=True)
+    weight = torch.exp(score - torch.where(high == -math.inf, 0.0, high))
+    del score
+    v = half[:, 1].unflatten(1, (nkv, hd, c))[slot].float().permute(0, 2, 1, 4, 3).reshape(b, nkv, top, hd)
+    total = weight.sum(4)
+    out = torch.matmul(weight.view(b, nkv, -1, top), v).view(b, nkv, nq // nkv, most, hd)
+    out = torch.where(total[..., None] > 0, out / total[..., None], 0.0).permute(0, 3, 1, 2, 4).reshape(b, most, nq * hd)
+    s["out"][row[real]] = out[real].half()
+    return s["out"]
+
+
+def _plain_append(s):
+    m, nq, nkv, hd, c = s["m"], s["nq"], s["nkv"], s["hd"], s["c"]
+    heads = s["qkv"].float().view(m, nq + 2 * nkv, hd)
+    axis = _ints(s["pair_axis"], torch.int64)
+    rope = s["rope"][s["rope_pos"][axis].long().T, torch.arange(hd // 2, device=DEVICE)[None, :]][:, None]
+    a, b = heads[:, :nq + nkv].chunk(2, 2)
+    turned = torch.cat([a * rope[..., 0] - b * rope[..., 1], b * rope[..., 0] + a * rope[..., 1]], 2).half()
+    place, seq = s["place"].long(), s["seq"].long()
+    slot, at = s["table"][seq, place // c].long(), place % c
+    half = s["slab"].view(s["n_slots"], 2, -1)
+    half[:, 0].unflatten(1, (c, nkv, hd))[slot, at] = turned[:, nq:]
+    half[:, 1].unflatten(1, (nkv, hd, c))[slot, :, :, at] = heads[:, nq + nkv:].half()
+    s["q_out"].copy_(turned[:, :nq].reshape(m, -1))
+    return {"slab": s["slab"], "q": s["q_out"]}
+
+
+def _plain_plan(s):
+    m, words = s["m"], s["words"]
+    row = torch.arange(m, device=DEVICE)
+    seq = torch.searchsorted(s["row_off"][1:].long(), row, right=True)
+    first = s["row_off"].long()[seq]
+    parent, node = s["parent"].long(), row - first
+    at, depth = node, torch.zeros_like(node)
+    mask = torch.zeros(m, words, device=DEVICE, dtype=torch.int32)
+    word = torch.arange(words, device=DEVICE)[None, :]
+    for _ in range(s["deep"]):
+        bit = torch.ones_like(at).int() << (at.clamp(min=0) % 32).int()
+        mask |= torch.where((at[:, None] >= 0) & (at[:, None] // 32 == word), bit[:, None], 0)
+        at = torch.where(at >= 0, parent[(first + at.clamp(min=0))], -1)
+        depth += at >= 0
+    lens = s["lens"].long()[seq]
+    for k, v in (("seq", seq), ("place", lens + node), ("rope_pos", lens + depth), ("mask", mask)):
+        s[k].copy_(v)
+    return {k: s[k] for k in ("seq", "place", "rope_pos", "mask")}
+
+
+def _plain_accept(s):
+    b, m, c, deep, layers, dkv = s["n_seq"], s["m"], s["c"], s["deep"], s["layers"], s["nkv"] * s["hd"]
+    first, most = s["row_off"][:-1].long(), s["most"]
+    node = torch.arange(most, device=DEVICE)[None, :]
+    row = (first[:, None] + node).clamp(max=m - 1)
+    real = node < (s["row_off"][1:] - s["row_off"][:-1])[:, None]
+    parent, token, choice = s["parent"][row].long(), s["token"][row], s["choice"][row]
+    at, going = torch.zeros(b, 1, device=DEVICE, dtype=torch.int64), real[:, :1]
+    way, nxt = [], torch.full((b, 1), -1, device=DEVICE, dtype=torch.int32)
+    for _ in range(deep + 1):
+        way.append(torch.where(going, at, -1))
+        picked = torch.gather(choice, 1, at)
+        nxt = torch.where(going, picked, nxt)
+        fits = real & (parent == at) & (token == picked) & (node > 0) & going
+        child = torch.where(fits, node, most).amin(1, keepdim=True)
+        going = child < most
+        at = child.clamp(max=most - 1)
+    way = torch.cat(way, 1)
+    count = (way >= 0).sum(1)
+    s["accepted"].copy_(count)
+    s["next"].copy_(nxt[:, 0])
+    s["len_out"].copy_(s["lens"] + count)
+    path = torch.full((b, max(most, way.shape[1])), -1, device=DEVICE, dtype=torch.int64)
+    path[:, :way.shape[1]] = way
+    s["path"][row[real]] = path[:, :most][real].int()
+    seq, i = torch.nonzero(way >= 0, as_tuple=True)
+    start = s["lens"].long()[seq]
+    old, new = start + way[seq, i], start + i
+    from_slot, to_slot = s["table"][seq, old // c].long(), s["table"][seq, new // c].long()
+    half = s["slab"].view(layers, s["n_slots"], 2, -1)
+    k, v = half[:, :, 0].unflatten(2, (c, dkv)), half[:, :, 1].unflatten(2, (dkv, c))
+    moved_k, moved_v = k[:, from_slot, old % c], v[:, from_slot, :, old % c]
+    k[:, to_slot, new % c] = moved_k
+    v[:, to_slot, :, new % c] = moved_v
+    return {k: s[k] for k in ("accepted", "path", "next", "len_out", "slab")}
+
+
+def _plain_pages(s):
+    b, wide, n_slots, c = s["n_seq"], s["table"].shape[1], s["n_slots"], s["c"]
+    table, src = s["table"].long(), s["src"].long()
+    here = (src >= 0) & (src < b)
+    keep = torch.where(here, s["keep"].long().clamp(0, wide * c), 0)
+    end = (keep + s["room"].long().clamp(min=0)).clamp(max=wide * c)
+    chunk, row = torch.arange(wide, device=DEVICE)[None, :], torch.arange(b, device=DEVICE)
+    kept = torch.where(chunk < ((keep + c - 1) // c)[:, None], table[src.clamp(0, b - 1)], -1)
+    kept = torch.where((kept >= 0) & (kept < n_slots), kept, -1)
+    # holders of every slot (one place more for entries without one), and writers into chunks that are kept in part
+    to = lambda e: torch.where(e >= 0, e, n_slots)  # noqa: E731
+    count = torch.zeros(n_slots + 1, device=DEVICE, dtype=torch.int64)
+    count.index_add_(0, to(kept).reshape(-1), torch.ones(b * wide, device=DEVICE, dtype=torch.int64))
+    edge = kept.gather(1, (keep // c).clamp(max=wide - 1)[:, None])[:, 0]
+    edge = torch.where((end > keep) & (keep % c > 0), edge, -1)
+    writers = torch.zeros_like(count).index_add_(0, to(edge), torch.ones(b, device=DEVICE, dtype=torch.int64))
+    order = row + torch.where(src == row, 0, b)      # a slot stays with the row whose keys it holds, then with the lowest
+    lowest = torch.full_like(count, 2 * b).scatter_reduce_(0, to(edge), order, "amin")
+    at = to(edge)
+    stays = (count[at] == 1) | ((writers[at] == count[at]) & (lowest[at] == order))
+    forked = (edge >= 0) & ~stays
+    left = count.index_add(0, at, -forked.long())[:n_slots]
+    slots = torch.arange(n_slots, device=DEVICE)
+    moved = (left > 0) & (slots >= s["limit"])
+    # wanted: a slot for every one that moves, then row by row for the fork and for the chunks without one
+    fork_here = forked[:, None] & (chunk == (keep // c)[:, None])
+    fresh = (chunk >= (keep // c)[:, None]) & (chunk * c < end[:, None]) & ((kept < 0) | (chunk * c >= keep[:, None])) & (end > keep)[:, None]
+    wants = torch.cat([moved, (fork_here | fresh).reshape(-1)])
+    rank = torch.cumsum(wants.long(), 0) - 1
+    free = (count[:n_slots] == 0) & (slots < s["limit"])
+    given = torch.full((n_slots + b * wide + 1,), -1, device=DEVICE, dtype=torch.int64)
+    given[torch.where(free, torch.cumsum(free.long(), 0) - 1, n_slots + b * wide)] = torch.where(free, slots, -1)
+    got = torch.where(wants, given[rank.clamp(min=0)], -1)
+    missing = (wants.sum() - free.sum()).clamp(min=0)
+    moved_to = torch.cat([torch.where(moved, got[:n_slots], slots), _ints([-1], torch.int64)])
+    mine = got[n_slots:].view(b, wide)
+    after = torch.where(mine >= 0, mine, moved_to[to(kept)])
+    s["table_out"].copy_(torch.where(missing > 0, table, after))
+    n_copies = torch.where(missing > 0, 0, moved.sum() + forked.sum())
+    held = torch.zeros(n_slots + 1, device=DEVICE, dtype=torch.int64)
+    final = s["table_out"].long()
+    held[torch.where((final >= 0) & (final < n_slots), final, n_slots).reshape(-1)] = 1
+    s["info"].copy_(torch.stack([missing, held[:n_slots].sum(), n_copies, torch.zeros_like(missing)]))
+    if not int(n_copies):
+        return {k: s[k] for k in ("table_out", "info", "slab")}
+    old = torch.cat([slots[moved], edge[forked]])
+    new = torch.cat([got[:n_slots][moved], mine[fork_here]])
+    part = torch.cat([torch.full_like(slots[moved], c), (keep % c)[forked]])
+    sure = torch.arange(c, device=DEVICE)[None, :] < part[:, None]
+    dkv = s["nkv"] * s["hd"]
+    for layer in range(s["layers"]):
+        half = s["slab"][layer].view(n_slots, 2, -1)
+        k, v = half[:, 0].unflatten(1, (c, dkv)), half[:, 1].unflatten(1, (dkv, c))
+        k[new] = torch.where(sure[:, :, None], k[old], k[new])
+        v[new] = torch.where(sure[:, None, :], v[old], v[new])
+    return {k: s[k] for k in ("table_out", "info", "slab")}
+
+
+def run(state):
+    if own:
+        return {"attention": _own_attention, "append": _own_append, "plan": _own_plan, "accept": _own_accept,
+                "pages": _own_pages}[state["kind"]](state)
+    return {"attention": _plain_attention, "append": _plain_append, "plan": _plain_plan, "accept": _plain_accept,
+            "pages": _plain_pages}[state["kind"]](state)
+
+
+# ----------------------------------------------------------------------------- what a pass cannot do without
+
+def work(case):
+    if case["kind"] == "plan":
+        counts = _counts(case)
+        m, words = sum(counts), (max(counts) + 31) // 32
+        return {"bytes": 4 * (4 * m + m * words + 2 * len(counts) + 1), "flops": 0}
+    nq, nkv, hd, _, _ = MODELS[case["model"]]
+    if case["kind"] == "attention":
+        lens, counts = _lens(case), _counts(case)
+        words = 0 if case["chain"] else (max(counts) + 31) // 32
+        pairs = sum(t * n + (t * (t + 1) // 2 if case["chain"] else 0) for n, t in zip(lens, counts))
+        if not case["chain"]:
+            pairs += sum(bin(w & 0xFFFFFFFF).count("1") for p in _trees(case) for row in _bits(p, words) for w in row)
+        return {"bytes": sum(n + t for n, t in zip(lens, counts)) * nkv * hd * 4 + sum(counts) * (nq * hd * 4 + 4 * words),
+                "flops": 4.0 * pairs * nq * hd}
+    if case["kind"] == "append":
+        m, wide = case["rows"], (nq + 2 * nkv) * hd
+        return {"bytes": m * (wide * ((4 if case["f32"] else 2) + 2) + 4 * hd + 4 + 4 * (1 + case["axes"])), "flops": 3.0 * m * (nq + nkv) * hd}
+    if case["kind"] == "accept":
+        moves = sum(node != i for way in _branches(case) for i, node in enumerate(way))
+        return {"bytes": moves * case["layers"] * nkv * hd * 8 + sum(_counts(case)) * 16, "flops": 0}
+    held, src, keep, room = _page_plan(case)
+    c, b = case["chunk"], case["seqs"]
+    wide = max((k + w + c - 1) // c for k, w in zip(held + keep, room + room)) + 1
+    # every fork of a chunk that its source writes too, and the share of the slots that lies where the slab ends
+    forks = sum(k % c for i, k in enumerate(keep) if 0 <= src[i] != i)
+    moves = sum((held[i] + c - 1) // c for i in range(b) if i in src) * case["shrink"] / 100 * c
+    return {"bytes": 8 * b * wide + 12 * b + (forks + moves) * case["layers"] * nkv * hd * 8, "flops": 0}
+
+
+# ----------------------------------------------------------------------------- in 64 bits
+
+def _exact_attention(case, seed):
+    s = _prepare_attention(case, seed)
+    nq, nkv, hd, c = s["nq"], s["nkv"], s["hd"], s["c"]
+    out, trees, at = torch.zeros(s["m"], nq * hd, device=DEVICE, dtype=torch.float64), _trees(case), 0
+    for b, n in enumerate(s["lens"].tolist()):
+        parents = trees[b]
+        t = len(parents)
+        slots = s["slab"][s["table"][b, :(n + t + c - 1) // c].long()].double()
+        keys = slots[:, :c * nkv * hd].reshape(-1, nkv * hd)[:n + t]
+        values = slots[:, c * nkv * hd:].reshape(-1, nkv * hd, c).transpose(1, 2).reshape(-1, nkv * hd)[:n + t].contiguous()
+        hidden = torch.ones(t, n + t, dtype=torch.bool)
+        hidden[:, :n] = False
+        for i in range(t):
+            j = i
+            while j >= 0:
+                hidden[i, n + j] = False
+                j = j - 1 if case["chain"] else parents[j]
+        hidden = hidden.to(DEVICE)
+        for h in range(nq):
+            kv = slice(h // (nq // nkv) * hd, (h // (nq // nkv) + 1) * hd)
+            score = s["q"][at:at + t, h * hd:(h + 1) * hd].double() @ keys[:, kv].T.contiguous() / math.sqrt(hd)
+            out[at:at + t, h * hd:(h + 1) * hd] = torch.softmax(score.masked_fill_(hidden, -math.inf), 1) @ values[:, kv].contiguous()
+        at += t
+    return out
+
+
+def _exact_append(case, seed):
+    s = _prepare_append(case, seed)
+    nq, nkv, hd, c = s["nq"], s["nkv"], s["hd"], s["c"]
+    dq, dkv, h2 = nq * hd, nkv * hd, hd // 2
+    x, flat = s["qkv"].double(), s["slab"].double().view(-1)
+    place, seq, table = s["place"].tolist(), s["seq"].tolist(), s["table"].tolist()
+    start = torch.tensor([table[b][p // c] * 2 * c * dkv for b, p in zip(seq, place)], device=DEVICE)
+    at = torch.tensor([p % c for p in place], device=DEVICE)
+    cos, sin = (torch.stack([s["rope"][s["rope_pos"][a].long(), i, e].double() for i, a in enumerate(s["pair_axis"])], 1) for e in (0, 1))
+    q = torch.empty(s["m"], dq, device=DEVICE, dtype=torch.float64)
+    for head in range(nq + nkv):
+        u, w = x[:, head * hd:head * hd + h2], x[:, head * hd + h2:(head + 1) * hd]
+        turned = torch.cat([u * cos - w * sin, w * cos + u * sin], 1)
+        if head < nq:
+            q[:, head * hd:(head + 1) * hd] = turned
+        else:
+            flat[(start + at * dkv + (head - nq) * hd)[:, None] + torch.arange(hd, device=DEVICE)[None, :]] = turned
+    flat[(start + c * dkv + at)[:, None] + c * torch.arange(dkv, device=DEVICE)[None, :]] = x[:, dq + dkv:]
+    return {"slab": flat.view_as(s["slab"]), "q": q}
+
+
+def _exact_plan(case, seed):
+    s = _prepare_plan(case, seed)
+    out = {k: [] for k in ("seq", "place", "rope_pos", "mask")}
+    for b, (parents, n) in enumerate(zip(_trees(case), s["lens"].tolist())):
+        for i in range(len(parents)):
+            way = [i]
+            while parents[way[-1]] >= 0:
+                way.append(parents[way[-1]])
+            words = [0] * s["words"]
+            for j in way:
+                words[j // 32] += 1 << j % 32 if j % 32 < 31 else -(1 << 31)
+            for k, v in zip(out, (b, n + i, n + len(way) - 1, words)):
+                out[k].append(v)
+    return {k: _ints(v) for k, v in out.items()}
+
+
+def _exact_accept(case, seed):
+    s = _prepare_accept(case, seed)
+    c, dkv, table = s["c"], s["nkv"] * s["hd"], s["table"].tolist()
+    path = []
+    for b, (way, t, n) in enumerate(zip(_branches(case), _counts(case), s["lens"].tolist())):
+        path += way + [-1] * (t - len(way))
+        for i, node in enumerate(way):
+            (a, p), (z, r) = ((table[b][(n + j) // c], (n + j) % c) for j in (node, i))
+            s["slab"][:, z, r * dkv:(r + 1) * dkv] = s["slab"][:, a, p * dkv:(p + 1) * dkv].clone()
+            s["slab"][:, z, c * dkv + r::c] = s["slab"][:, a, c * dkv + p::c].clone()
+    choice, off, ways = s["choice"].tolist(), s["row_off"].tolist(), _branches(case)
+    taken = _ints([len(w) for w in ways])
+    return {"accepted": taken, "path": _ints(path), "next": _ints([choice[o + w[-1]] for o, w in zip(off, ways)]),
+            "len_out": s["lens"] + taken, "slab": s["slab"]}
+
+
+def _exact_pages(case, seed):
+    s = _prepare_pages(case, seed)
+    c, b, n_slots, limit, table = s["c"], s["n_seq"], s["n_slots"], s["limit"], s["table"].tolist()
+    _, src, keep, room = _page_plan(case)
+    wide, dkv = len(table[0]), s["nkv"] * s["hd"]
+    new, holders = [], {}
+    for i in range(b):
+        whole = -(-keep[i] // c) if src[i] >= 0 else 0
+        new.append([table[src[i]][k] if k < whole else -1 for k in range(wide)])
+        for k, e in enumerate(new[i]):
+            if e >= 0:
+                holders.setdefault(e, []).append((i, k))
+    writes = lambda i, k: room[i] > 0 and keep[i] % c > 0 and k == keep[i] // c  # noqa: E731
+    leaves = {}                                      # (row, chunk) that copies the slot it shares
+    for e, who in holders.items():
+        if len(who) > 1:
+            writing = [w for w in who if writes(*w)]
+            stays = min(who, key=lambda w: (src[w[0]] != w[0], w[0])) if len(writing) == len(who) else None
+            leaves.update({w: e for w in writing if w != stays})
+    free = (e for e in range(limit) if e not in holders)
+    copies, moved = [], {}
+    for e in sorted(holders):
+        if e >= limit and any(w not in leaves for w in holders[e]):
+            moved[e] = next(free)
+            copies.append((e, moved[e], c))
+    for i in range(b):
+        first, last = keep[i] // c, -(-(keep[i] + room[i]) // c)
+        for k in range(wide):
+            e = new[i][k]
+            if (i, k) in leaves:
+                new[i][k] = next(free)
+                copies.append((e, new[i][k], keep[i] % c))
+            elif e >= 0:
+                new[i][k] = moved.get(e, e)
+            elif room[i] > 0 and first <= k < last:
+                new[i][k] = next(free)
+    for a, z, n in copies:
+        k, v = (s["slab"][:, x, :c * dkv].unflatten(1, (c, dkv)) for x in (z, a))
+        k[:, :n] = v[:, :n]
+        k, v = (s["slab"][:, x, c * dkv:].unflatten(1, (dkv, c)) for x in (z, a))
+        k[..., :n] = v[..., :n]
+    held = len({e for row in new for e in row if e >= 0})
+    return {"table_out": _ints(new), "info": _ints([0, held, len(copies), 0]), "slab": s["slab"]}
+
+
+def exact(case, seed):
+    return {"attention": _exact_attention, "append": _exact_append, "plan": _exact_plan, "accept": _exact_accept,
+            "pages": _exact_pages}[case["kind"]](case, seed)
