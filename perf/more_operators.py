@@ -521,10 +521,9 @@ def _plain_pages(s):
     after = torch.where(mine >= 0, mine, moved_to[to(kept)])
     s["table_out"].copy_(torch.where(missing > 0, table, after))
     n_copies = torch.where(missing > 0, 0, moved.sum() + forked.sum())
-    held = torch.zeros(n_slots + 1, device=DEVICE, dtype=torch.int64)
-    final = s["table_out"].long()
-    held[torch.where((final >= 0) & (final < n_slots), final, n_slots).reshape(-1)] = 1
-    s["info"].copy_(torch.stack([missing, held[:n_slots].sum(), n_copies, torch.zeros_like(missing)]))
+    # slots that are held then (or would be, where some are missing)
+    held = (count[:n_slots] > 0).sum() + wants.sum() - moved.sum()
+    s["info"].copy_(torch.stack([missing, held, n_copies, torch.zeros_like(missing)]))
     if not int(n_copies):
         return {k: s[k] for k in ("table_out", "info", "slab")}
     old = torch.cat([slots[moved], edge[forked]])
