@@ -778,6 +778,206 @@ mz_status mz_logits_rules(const float *logits, int32_t m, int32_t vocab, int64_t
 /* Workspace bytes of mz_logits_rules (-1 for invalid arguments). */
 int64_t mz_logits_rules_workspace_bytes(int32_t m, int32_t vocab);
 
+/* ---- a decode step that checks drafted trees --------------------------- */
+/* A drafter proposes a tree of tokens for every sequence; one step scores all
+ * of its nodes and keeps the branch that the model itself takes.  In order:
+ * mz_kv_pages (and mz_kv_copy) sees to the chunks that the step writes,
+ * mz_tree_plan lays the trees' nodes out as rows, mz_kv_append_axes writes
+ * their keys and values, mz_attention_tree attends, mz_tree_accept takes the
+ * branch from the tokens of mz_logits_rules and moves its keys together.
+ * The nodes of sequence b's tree are the rows row_off[b] .. row_off[b + 1] - 1
+ * of m (device int32 [n_seq + 1]; the caller sees that they ascend within 0..m;
+ * what lies outside is cut off, and nothing out of range is read or written).
+ * Node i lies behind its parent (parent < i; any other entry makes it a root,
+ * which sees nothing of the tree but itself) and, until a branch is taken, in
+ * the cache at position lens[b] + i, whatever its depth.  A tree has at most
+ * 1024 nodes where its parents or a mask are given, and at most 32 mask_words
+ * with a mask; the rows of further nodes count as rows of no tree.  Without
+ * parents and mask the nodes are a chain, of any length: drafts without
+ * branches, or the next piece of every prompt.  Offsets, parents, lengths and
+ * tables are read on the device, as for the calls above, and what is said there
+ * about graphs, streams and allocation holds here too. */
+
+/* The rows of the trees, from parent (device int32 [m]; NULL: chains) and lens
+ * (device int32 [n_seq], tokens in the cache before the tree; below 0 counts as
+ * 0, above 2^30 as 2^30).  Any of the outputs may be NULL, all are device
+ * int32: seq [m], the sequence; place [m], lens + node; rope_pos [m], lens +
+ * depth; mask [m][mask_words], bit j % 32 of word j / 32 is 1 where the row's
+ * node is j or lies behind it.  Rows of no tree get -1, and a mask of 0.
+ * mask_words 0..32, 0 where mask is NULL; m at most 2^30, may be 0; n_seq at
+ * most 2^20.  Errors: EINVAL for the above, a NULL row_off or lens, no output,
+ * outputs that are one another or an input. */
+mz_status mz_tree_plan(const int32_t *row_off, const int32_t *parent, const int32_t *lens, int32_t n_seq,
+                       int32_t m, int32_t *seq, int32_t *place, int32_t *rope_pos, uint32_t *mask,
+                       int32_t mask_words, void *stream);
+
+typedef struct {
+  const int32_t *rope_pos;   /* device int32 [n_axes][m]: positions of the rows on every axis */
+  int32_t n_axes;            /* 1..4 */
+  const uint8_t *pair_axis;  /* host [head_dim / 2]: the axis that turns pair (i, i + head_dim / 2) of every
+                                head, or 255: the pair is not turned */
+} mz_rope_axes;
+
+/* mz_kv_append with the place of a row apart from the positions that it is
+ * turned by: args->pos is the position in the cache only, and pair i turns by
+ * rope_cs[rope_pos[pair_axis[i]][row]][i].  One axis is a drafted tree (places
+ * follow each other, positions go by depth); several are the time, height and
+ * width of pictures and video, their pairs in sections, alternating or as else
+ * the model has them; 255 leaves a part of each head as it is, only rounded to
+ * f16.  With one axis for all pairs and rope_pos = pos the bits are
+ * mz_kv_append's.  A row whose position on an axis that a pair turns by is
+ * outside 0..n_rope-1 writes nothing; pos need not lie below n_rope.  All else
+ * as mz_kv_append.  Errors: those, and EINVAL for axes NULL, n_axes outside
+ * 1..4, a NULL pair_axis or one that names another axis, a NULL rope_pos with m
+ * above 0. */
+mz_status mz_kv_append_axes(const mz_kv_append_args *args, const mz_rope_axes *axes, int32_t m, void *stream);
+
+typedef struct {
+  const void *q;             /* device f16 [m][n_q_heads][head_dim], rotated */
+  int32_t m, n_seq;
+  const int32_t *row_off;    /* device int32 [n_seq + 1] */
+  const int32_t *lens;       /* device int32 [n_seq]: keys before the tree */
+  const uint32_t *mask;      /* device uint32 [m][mask_words]: the nodes of its tree that a row's node sees;
+                                NULL: a chain, it sees those before it and itself */
+  int32_t mask_words;        /* 1..32; 0 without a mask */
+  int32_t n_slots;           /* chunk slots in slab */
+  const void *slab;          /* device: slots laid out as in mz_attention */
+  const int32_t *table;      /* device int32 [n_seq][n_table]: slots of the sequences' chunks */
+  int32_t n_table, chunk_tokens, n_q_heads, n_kv_heads, head_dim;
+  void *out;                 /* device f16 [m][n_q_heads * head_dim] */
+} mz_attention_tree_args;
+
+/* Attention of several new tokens of each of n_seq sequences, trees or chains,
+ * over their cached chunks (paper Sec. 2.1 and 4.2): row_off[b] + i attends to
+ * the keys 0..lens[b]-1 of its sequence and to the nodes j of its tree that
+ * its mask names (any set of them, of which mz_tree_plan's is one), whose keys
+ * lie at lens[b] + j.  Lengths and trees may differ freely, and as in
+ * mz_attention_batch the work is shared evenly and joined in a fixed order,
+ * so results do not change from run to run.  A length below 0
+ * counts as 0, keys beyond the table are not there, a chunk whose entry is
+ * outside 0..n_slots-1 is left out, a row that sees no key gets zeros, and rows
+ * of no tree are not written.  What slots hold at keys that no row sees is
+ * never used, and what a row does not see does not enter its output, be it NaN
+ * or infinite.  Scores, sums and joins are fp32, and the softmax weights keep 22
+ * bits for the product with the values.  head_dim 64 or 128, n_q_heads a
+ * multiple of n_kv_heads with a group of at most 16, chunk_tokens a power of
+ * two >= 8, n_table * chunk_tokens at most 2^30, a slot below 2^31 bytes, m *
+ * n_q_heads below 2^24, n_seq at most 2^20; m may be 0.  out shares nothing
+ * with what is read.  workspace: device,
+ * caller-owned, at least mz_attention_tree_workspace_bytes(...) bytes (one for
+ * the most rows and sequences serves fewer), any content, not shared by calls
+ * in flight together (two graphs that may run at once need two).  Errors:
+ * EINVAL for the above, a NULL pointer, more work than 2^31 blocks of 128 keys,
+ * q, slab, workspace or out off 16-byte boundaries, or a short workspace. */
+mz_status mz_attention_tree(const mz_attention_tree_args *args, void *workspace, int64_t workspace_bytes,
+                            void *stream);
+
+/* Workspace bytes of mz_attention_tree (-1 for invalid arguments). */
+int64_t mz_attention_tree_workspace_bytes(int32_t m, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
+                                          int32_t head_dim);
+
+typedef struct {
+  int32_t n_seq, m;
+  const int32_t *row_off;    /* device int32 [n_seq + 1] */
+  const int32_t *parent;     /* device int32 [m]; NULL: chains */
+  const int32_t *token;      /* device int32 [m]: the nodes' drafted tokens */
+  const int32_t *choice;     /* device int32 [m]: the token that the model takes after the node */
+  const int32_t *lens;       /* device int32 [n_seq]: tokens in the cache before the tree */
+  int32_t *accepted;         /* device int32 [n_seq]: nodes of the branch that is taken */
+  int32_t *path;             /* device int32 [m]: those nodes, from the tree's first row on, then -1 */
+  int32_t *next;             /* device int32 [n_seq]: the token after the branch, -1 for a tree of no nodes */
+  int32_t *len_out;          /* device int32 [n_seq]: lens + accepted */
+  /* the cache, whose keys and values are moved together; n_layers 0: nothing is moved */
+  int32_t n_layers, n_slots;
+  void *slab;                /* device: layer l's slots, laid out as in mz_attention, at slab + l * layer_bytes */
+  int64_t layer_bytes;       /* a multiple of 16; may be 0 for one layer */
+  const int32_t *table;      /* device int32 [n_seq][n_table], for all layers */
+  int32_t n_table, chunk_tokens, n_kv_heads, head_dim;
+} mz_tree_accept_args;
+
+/* Take the branch of every tree that the model's own tokens follow: node 0 (the
+ * token that was taken before the step), then, as long as there is one, the
+ * lowest child whose token is its parent's choice.  With the choice of a greedy
+ * or of a sampled token (mz_logits_rules) at every node, the tokens that are
+ * kept are what the model would have produced one at a time.  Then position
+ * lens[b] + path[i] of the cache moves to lens[b] + i, keys and values, in each
+ * layer, so that the sequence goes on at len_out.  All other positions stay as
+ * they are; a move from or to a chunk without a slot (an entry outside
+ * 0..n_slots-1, or beyond the table) is left out.  The caller sees that no
+ * other sequence holds the chunks that are written.  Layers held in other
+ * allocations take a call each.  Lengths below 0 count as 0, above 2^30 as
+ * 2^30; head_dim 32, 64 or 128; m at most 2^30, may be 0; n_seq at most 2^20;
+ * chunks as for mz_kv_append.  Errors: EINVAL for the above, a NULL pointer,
+ * outputs that are one another or an input, slab or layer_bytes off 16-byte
+ * boundaries, layers that overlap, too many layers and sequences for a launch. */
+mz_status mz_tree_accept(const mz_tree_accept_args *args, void *stream);
+
+typedef struct {
+  int32_t n_seq, n_table, n_slots, chunk_tokens;
+  int32_t slot_limit;        /* slots 0..slot_limit-1 may be held from now on; 0: all */
+  const int32_t *table;      /* device int32 [n_seq][n_table]: slots of the rows' chunks so far */
+  int32_t *table_out;        /* device int32 [n_seq][n_table]: from now on; may be table itself */
+  const int32_t *src;        /* device int32 [n_seq]: the row whose first keys the row holds from now on;
+                                outside 0..n_seq-1: none; NULL: its own */
+  const int32_t *keep;       /* device int32 [n_seq]: how many of those keys */
+  const int32_t *room;       /* device int32 [n_seq]: positions behind them that are about to be written; NULL: 0 */
+  int32_t *copies;           /* device int32 [n_seq + n_slots - slot_limit][4], 16-byte aligned: slots to copy (from,
+                                to, positions, 0); n_seq entries do without a slot_limit */
+  int32_t *info;             /* device int32 [4]: slots that are missing, slots held, copies, 0 */
+} mz_kv_pages_args;
+
+/* What the sequences hold of the slab from now on, for all rows at once: row b
+ * of table_out names the chunks of the first keep[b] keys of row src[b] of
+ * table, then fresh slots for the chunks up to position keep + room that have
+ * none.  So src = b continues or cuts a sequence, another row forks one (as
+ * beams or several answers do; rows may exchange places), keep 0 frees or
+ * begins one.  Rows share the slots of common chunks; a slot that no row names
+ * is free, there is no other count, and what outlives its request is kept by a
+ * row of its own.  Fresh slots are the lowest free ones below the limit, and what a row
+ * held past its keep is free again in the same call (so what is there is not
+ * kept for the row that held it).
+ * A chunk that is kept in part and written from now on (keep % chunk_tokens
+ * and room above 0) must not be shared: where other rows hold its slot too, the
+ * row gets a fresh one and an entry in copies; if all of them write it, the
+ * lowest row with src = b keeps the slot (the lowest of all where none has).
+ * With slot_limit, each slot above it that is still held moves below it, in
+ * all rows that name it.  Copies first name the slots that move, ascending, with
+ * chunk_tokens positions, then the rows' forks, row by row; slots are taken
+ * in the order of the copies that move, then row by row and chunk by chunk.  No
+ * slot is both copied from and to, so mz_kv_copy takes the entries in any order.
+ * Where the free slots do not suffice, nothing changes: table_out is table, no
+ * copies, and info[0] is how many are missing; else info[0] is 0.  info[1]
+ * counts the slots held afterwards (or that would be), info[2] the copies.
+ * keep and room below 0 count as 0, keep + room beyond the table as n_table *
+ * chunk_tokens; kept entries outside 0..n_slots-1 become -1, as do all behind
+ * the last chunk.  n_table * chunk_tokens at most 2^30, n_seq * n_table and n_slots
+ * at most 2^28, n_seq at most 2^20; table and table_out are the same or apart.
+ * workspace: device, caller-owned, at
+ * least mz_kv_pages_workspace_bytes(...) bytes (one for the largest sizes
+ * serves smaller ones), any content, not shared by calls in flight together.
+ * Errors: EINVAL for the above, slot_limit outside 0..n_slots, a NULL pointer,
+ * outputs that are one another or an input other than table, copies or
+ * workspace off 16-byte boundaries, or a short workspace. */
+mz_status mz_kv_pages(const mz_kv_pages_args *args, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Workspace bytes of mz_kv_pages (-1 for invalid arguments). */
+int64_t mz_kv_pages_workspace_bytes(int32_t n_seq, int32_t n_table, int32_t n_slots);
+
+/* Copy positions of slots in n_layers layers (layer l's slots at slab + l *
+ * layer_bytes, laid out as in mz_attention): for each of the first *n_copies
+ * (device int32, such as info + 2; at most max_copies) entries (from, to,
+ * positions, 0) of copies, keys and values of the first positions of slot from
+ * go to slot to, whose further positions stay as they are.  Entries with a slot
+ * outside 0..n_slots-1, or from = to, are left out, positions above chunk_tokens count as
+ * chunk_tokens.  No slot that is copied to is in another entry.  Layers in
+ * other allocations take a call each.  max_copies may be 0.  head_dim 32, 64 or
+ * 128, chunk_tokens a power of two >= 8, a slot below 2^31 bytes.  Errors:
+ * EINVAL for the above, n_layers below 1, a NULL pointer, copies, slab or
+ * layer_bytes off 16-byte boundaries, layers that overlap. */
+mz_status mz_kv_copy(const int32_t *copies, const int32_t *n_copies, int32_t max_copies, void *slab,
+                     int32_t n_slots, int32_t n_layers, int64_t layer_bytes, int32_t chunk_tokens,
+                     int32_t n_kv_heads, int32_t head_dim, void *stream);
+
 /* x = h / sqrt(mean(h^2) + eps) per row: h float [m][d] -> x f16 [m][d]. */
 mz_status mz_rmsnorm(const void *h_f32, int32_t m, int32_t d, float eps, void *x_f16,
                      void *stream);

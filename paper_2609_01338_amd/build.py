@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libmz.so")
 SOURCES = ["gemm_q4.hip", "gemm_rows.hip", "attention.hip", "elementwise.hip", "probe.hip", "codec.hip", "noalloc.hip", "kv_append.hip",
-           "attention_batch.hip", "lora.hip", "logits.hip",
+           "attention_batch.hip", "lora.hip", "logits.hip", "attention_tree.hip", "tree.hip", "kv_pages.hip",
            "mz_runtime.cpp", "planner.cpp"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -18,6 +18,11 @@
 // has no neighbour in its chunk: each of its values is a line of its own,
 // which the slot layout asks for.
 //
+// With axes, a row's place is apart from the positions it turns by, one for
+// each axis, and every pair has an axis: a run of pairs of one axis loads its
+// (cos, sin) as a row of the table, another pair by pair; a row counts if its
+// positions on all axes in use lie in the table.
+//
 // Measured: 4099 f16 rows of 32 + 8 + 8 heads of 128 in 23.0 us, 103 MB at 4.5
 // TB/s (a large copy: 4.6), with three inputs in turn; 18.6 with two, which the
 // last-level cache partly holds.  64 fp32 rows one a sequence 6.0, 1 row 3.2 us,
@@ -66,7 +71,19 @@ __device__ __forceinline__ bool row_ok(const KvAppend& a, int s, int p) {
   return (unsigned)s < (unsigned)a.n_seq && (unsigned)p < (unsigned)a.n_rope && (p >> a.cshift) < a.n_table;
 }
 
-template <typename T>
+// The same of row r of m with axes; t: its positions on them (0 on those not in use).
+__device__ __forceinline__ void axis_positions(const KvAppend& a, int r, int m, int (&t)[kAxes]) {
+#pragma unroll
+  for (int x = 0; x < kAxes; ++x) t[x] = (a.axes_used >> x) & 1 ? a.rope_pos[(int64_t)x * m + r] : 0;
+}
+__device__ __forceinline__ bool row_ok_axes(const KvAppend& a, int s, int p, const int (&t)[kAxes]) {
+  bool ok = (unsigned)s < (unsigned)a.n_seq && p >= 0 && (p >> a.cshift) < a.n_table;
+#pragma unroll
+  for (int x = 0; x < kAxes; ++x) ok &= !((a.axes_used >> x) & 1) || (unsigned)t[x] < (unsigned)a.n_rope;
+  return ok;
+}
+
+template <typename T, bool AXES>
 __device__ __forceinline__ void rotate_rows(const KvAppend& a, int m, int t, int items) {
   constexpr int N = Vec<T>::N;
   typedef typename Vec<T>::raw raw;
@@ -89,14 +106,48 @@ __device__ __forceinline__ void rotate_rows(const KvAppend& a, int m, int t, int
   }
   int slot[kRotRows];
   float4 cs[kRotRows][N / 2];
+  unsigned codes = 0;          // axes of the run's pairs, four bits each
+  if constexpr (AXES) {
+    const uint64_t w = i < 32 ? (i < 16 ? a.axis[0] : a.axis[1]) : i < 48 ? a.axis[2] : a.axis[3];
+    codes = (unsigned)(w >> (4 * (i & 15)));
+    if (N < 8) codes &= 0xFFFF;
+  }
 #pragma unroll
   for (int j = 0; j < kRotRows; ++j) {
-    const bool ok = row_ok(a, s[j], p[j]);
+    bool ok;
+    if constexpr (AXES) {
+      int t[kAxes];
+      axis_positions(a, min(rg * kRotRows + j, m - 1), m, t);
+      ok = row_ok_axes(a, s[j], p[j], t);
+      const unsigned c0 = codes & 15;
+      if (codes == c0 * (N < 8 ? 0x1111u : 0x11111111u)) {
+        const int at = !ok || c0 == kAxisNone ? 0 : c0 == 0 ? t[0] : c0 == 1 ? t[1] : c0 == 2 ? t[2] : t[3];
+        const float4* c = reinterpret_cast<const float4*>(a.rope_cs + (int64_t)at * halfd + i);
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) cs[j][e] = c[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const unsigned c = (codes >> (4 * e)) & 15;
+          const int at = !ok || c == kAxisNone ? 0 : c == 0 ? t[0] : c == 1 ? t[1] : c == 2 ? t[2] : t[3];
+          const float2 v = a.rope_cs[(int64_t)at * halfd + i + e];
+          if (e & 1) {
+            cs[j][e / 2].z = v.x;
+            cs[j][e / 2].w = v.y;
+          } else {
+            cs[j][e / 2].x = v.x;
+            cs[j][e / 2].y = v.y;
+          }
+        }
+      }
+    } else {
+      ok = row_ok(a, s[j], p[j]);
+      const float4* c = reinterpret_cast<const float4*>(a.rope_cs + (int64_t)(ok ? p[j] : 0) * halfd + i);
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e) cs[j][e] = c[e];
+    }
     slot[j] = ok ? 0 : -1;
     if (!is_q && ok) slot[j] = a.table[(int64_t)s[j] * a.n_table + (p[j] >> a.cshift)];
-    const float4* c = reinterpret_cast<const float4*>(a.rope_cs + (int64_t)(ok ? p[j] : 0) * halfd + i);
-#pragma unroll
-    for (int e = 0; e < N / 2; ++e) cs[j][e] = c[e];
   }
 #pragma unroll
   for (int j = 0; j < kRotRows; ++j) {
@@ -109,7 +160,9 @@ __device__ __forceinline__ void rotate_rows(const KvAppend& a, int m, int t, int
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       const float4 c = cs[j][e / 2];
-      const float2 y = rope_rotate(u[e], w[e], e & 1 ? c.z : c.x, e & 1 ? c.w : c.y);
+      float2 y = rope_rotate(u[e], w[e], e & 1 ? c.z : c.x, e & 1 ? c.w : c.y);
+      if constexpr (AXES)
+        if (((codes >> (4 * e)) & 15) == kAxisNone) y = make_float2(u[e], w[e]);
       y1[e] = (_Float16)y.x;
       y2[e] = (_Float16)y.y;
     }
@@ -129,7 +182,7 @@ __device__ __forceinline__ void rotate_rows(const KvAppend& a, int m, int t, int
 // sequence (so one chunk: chunks hold a multiple of eight), wherever in the
 // tile it begins; the rows outside runs leave value by value, lanes over
 // rows, so that neighbours still meet in one line.
-template <typename T>
+template <typename T, bool AXES>
 __device__ __forceinline__ void value_tile(const KvAppend& a, int m, int r0, int d0, _Float16* tile, int64_t* s_at,
                                            int* s_run, int* s_one, int* s_n) {
   constexpr int N = Vec<T>::N, PITCH = kValDims + 2;
@@ -147,7 +200,15 @@ __device__ __forceinline__ void value_tile(const KvAppend& a, int m, int r0, int
     const int lane = threadIdx.x, r = r0 + min(lane, rows - 1);
     const int s = a.seq[r], p = a.pos[r];
     int slot = -1;
-    if (lane < rows && row_ok(a, s, p)) slot = a.table[(int64_t)s * a.n_table + (p >> a.cshift)];
+    bool in = lane < rows;
+    if constexpr (AXES) {
+      int t[kAxes];
+      axis_positions(a, r, m, t);
+      in &= row_ok_axes(a, s, p, t);
+    } else {
+      in &= row_ok(a, s, p);
+    }
+    if (in) slot = a.table[(int64_t)s * a.n_table + (p >> a.cshift)];
     const bool ok = (unsigned)slot < (unsigned)a.n_slots;
     if (ok)
       s_at[lane] = (int64_t)slot * a.slot_bytes + (int64_t)a.C * dkv * 2 + (p & (a.C - 1)) * 2;
@@ -190,7 +251,7 @@ __device__ __forceinline__ void value_tile(const KvAppend& a, int m, int r0, int
   }
 }
 
-template <typename T>
+template <typename T, bool AXES>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppend a, int m, int items, int rot_blocks) {
   __shared__ _Float16 tile[kValRows * (kValDims + 2)];
   __shared__ int64_t s_at[kValRows];
@@ -198,11 +259,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppend a, int m, int i
   const int b = blockIdx.x;
   if (b < rot_blocks) {
     const int t = b * 256 + threadIdx.x;
-    if (t < (m + kRotRows - 1) / kRotRows * items) rotate_rows<T>(a, m, t, items);
+    if (t < (m + kRotRows - 1) / kRotRows * items) rotate_rows<T, AXES>(a, m, t, items);
     return;
   }
   const int col_tiles = (a.nkv * a.hd + kValDims - 1) / kValDims, vb = b - rot_blocks;
-  value_tile<T>(a, m, vb / col_tiles * kValRows, vb % col_tiles * kValDims, tile, s_at, s_run, s_one, s_n);
+  value_tile<T, AXES>(a, m, vb / col_tiles * kValRows, vb % col_tiles * kValDims, tile, s_at, s_run, s_one, s_n);
 }
 
 template <typename T>
@@ -223,10 +284,15 @@ void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s) {
   const int items = f32 ? append_items<float>(a.nq, a.nkv, a.hd) : append_items<_Float16>(a.nq, a.nkv, a.hd);
   const int rot = ((m + kRotRows - 1) / kRotRows * items + 255) / 256;
   const int tiles = (m + kValRows - 1) / kValRows * ((a.nkv * a.hd + kValDims - 1) / kValDims);
-  if (f32)
-    hipLaunchKernelGGL(kv_append_kernel<float>, dim3(rot + tiles), dim3(256), 0, s, a, m, items, rot);
+  const dim3 grid(rot + tiles), block(256);
+  if (f32 && a.rope_pos)
+    hipLaunchKernelGGL((kv_append_kernel<float, true>), grid, block, 0, s, a, m, items, rot);
+  else if (f32)
+    hipLaunchKernelGGL((kv_append_kernel<float, false>), grid, block, 0, s, a, m, items, rot);
+  else if (a.rope_pos)
+    hipLaunchKernelGGL((kv_append_kernel<_Float16, true>), grid, block, 0, s, a, m, items, rot);
   else
-    hipLaunchKernelGGL(kv_append_kernel<_Float16>, dim3(rot + tiles), dim3(256), 0, s, a, m, items, rot);
+    hipLaunchKernelGGL((kv_append_kernel<_Float16, false>), grid, block, 0, s, a, m, items, rot);
 }
 
 }  // namespace mzk

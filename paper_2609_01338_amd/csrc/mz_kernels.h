@@ -161,7 +161,10 @@ constexpr int64_t kMaxBlocks = (1 << 24) - 1;
 // the sequences' chunk tables, and the rows' queries rotated (see mz.h,
 // mz_kv_append).  q, k, v: rows of fp32 or f16, strides in elements; C = 1 <<
 // cshift; hd 32, 64 or 128; nq 0 leaves the queries out.  Every pointer and
-// row 16-byte aligned.  Only for kv_append_fits(m, ...).
+// row 16-byte aligned.  Only for kv_append_fits(m, ...).  With rope_pos
+// ([n_axes][m], mz_kv_append_axes) pair i turns by the position on the axis in
+// bits 4 (i % 16) .. + 3 of axis[i / 16] (15: it is not turned), and pos is the
+// place alone; axes_used has a bit for each axis that a pair names.
 struct KvAppend {
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride;
@@ -172,7 +175,11 @@ struct KvAppend {
   const int32_t* table;
   _Float16* q_out;
   int n_rope, n_slots, n_seq, n_table, C, cshift, nq, nkv, hd;
+  const int32_t* rope_pos;
+  uint64_t axis[4];
+  unsigned axes_used;
 };
+constexpr int kAxes = 4, kAxisNone = 15;
 bool kv_append_fits(int m, int nq, int nkv, int hd);
 void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s);
 
@@ -198,6 +205,83 @@ constexpr int kAttnBatchWgs = 512;
 int64_t attention_batch_units(int n_seq, int n_table, int chunk_tokens, int n_kv);
 int64_t attention_batch_ws_bytes(int n_seq, int group, int hd);
 void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
+
+// Most nodes of a tree whose parents or mask are given, and most sequences of
+// the calls on trees and pages.
+constexpr int kTreeNodes = 1024;
+constexpr int kTreeSeqs = 1 << 20;
+
+// Rows of the trees of n_seq sequences (see mz.h, mz_tree_plan); any output may be null.
+struct TreePlan {
+  const int32_t *row_off, *parent, *lens;
+  int32_t *seq, *place, *rope_pos;
+  uint32_t* mask;
+  int n_seq, m, mask_words;
+};
+void launch_tree_plan(const TreePlan& a, hipStream_t s);
+
+// The branches that the model's tokens take, and the moves of their keys and
+// values (see mz.h, mz_tree_accept); n_layers 0: none.  dkv a multiple of 8.
+// Only for tree_accept_fits(n_seq, n_layers, dkv).
+struct TreeAccept {
+  const int32_t *row_off, *parent, *token, *choice, *lens;
+  int32_t *accepted, *path, *next, *len_out;
+  uint8_t* slab;
+  const int32_t* table;
+  int64_t layer_bytes, slot_bytes;
+  int n_seq, m, n_layers, n_slots, n_table, C, cshift, dkv;
+};
+bool tree_accept_fits(int n_seq, int n_layers, int dkv);
+void launch_tree_accept(const TreeAccept& a, hipStream_t s);
+
+// Which slots the rows of a chunk table hold from now on (see mz.h,
+// mz_kv_pages).  The fields after info's line are the launcher's own, in ws
+// (kv_pages_ws_bytes bytes, which also do for smaller sizes).
+struct KvPages {
+  const int32_t *table, *src, *keep, *room;
+  int32_t* table_out;
+  int n_seq, n_table, n_slots, limit, C, cshift;
+  int4* copies;
+  int32_t* info;
+  int32_t *kept, *count, *writers, *lowest;      // [n_seq][n_table], [n_slots] three times
+  int32_t *free_at, *moved_to, *need, *forks;    // [n_slots] twice, [n_seq] twice
+  int32_t* sums;                                 // [8]
+};
+int64_t kv_pages_ws_bytes(int n_seq, int n_table, int n_slots);
+void launch_kv_pages(KvPages a, void* ws, hipStream_t s);
+
+// Copies of the first positions of slots in n_layers layers (see mz.h, mz_kv_copy).
+struct KvCopy {
+  const int4* copies;
+  const int32_t* n_copies;
+  uint8_t* slab;
+  int64_t layer_bytes, slot_bytes;
+  int max_copies, n_slots, n_layers, C, dkv;
+};
+void launch_kv_copy(const KvCopy& a, hipStream_t s);
+
+// Attention of several rows of every sequence over its chunks (see mz.h,
+// mz_attention_tree); hd 64 or 128, group = nq / nkv <= 16, C = 1 << cshift,
+// slot_bytes below 2^31, attention_tree_units below 2^31, m nq at most
+// kMaxBlocks.  The fields after slot_bytes' line are the launcher's own, in ws
+// (attention_tree_ws_bytes bytes).
+struct AttnTree {
+  const _Float16* q;
+  const int32_t *row_off, *lens, *table;
+  const uint32_t* mask;
+  const uint8_t* slab;
+  _Float16* out;
+  int n_seq, m, mask_words, n_slots, n_table, C, cshift, nq, nkv, group;
+  int64_t slot_bytes;
+  int32_t *base, *row_seq;   // [n_seq + 1] units of 128 keys a KV head of the sequences before, [m]
+  float2* ml;                // [2 wgs][columns of a tile] running max and sum of a partial
+  float* part;               // [2 wgs][columns of a tile][hd]
+  int wgs;                   // most workgroups that share the units
+  float scale_log2;
+};
+int64_t attention_tree_units(int m, int n_seq, int n_table, int chunk_tokens, int nq, int nkv);
+int64_t attention_tree_ws_bytes(int m, int n_seq, int nq, int nkv, int hd);
+void launch_attention_tree(AttnTree a, int hd, void* ws, hipStream_t s);
 
 // y = base + scale (x A^T) B^T with each row's adapter (see mz.h,
 // mz_lora_add); R a multiple of 8 up to 128, k a multiple of 8 up to 2^30,

@@ -2181,7 +2181,7 @@ static void check_chunks(int32_t n_seq, int32_t n_slots, int32_t n_table, int32_
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
+static mz_status append_entry(const mz_kv_append_args* args, const mz_rope_axes* axes, bool with_axes, int32_t m, void* stream) {
   return guarded(nullptr, [&] {
     if (!args) fail(MZ_EINVAL, "args is NULL");
     const mz_kv_append_args& a = *args;
@@ -2196,6 +2196,18 @@ mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
     check_chunks(a.n_seq, a.n_slots, a.n_table, a.chunk_tokens);
     const int64_t dkv = (int64_t)a.n_kv_heads * a.head_dim, dq = (int64_t)a.n_q_heads * a.head_dim;
     mzk::KvAppend k{};
+    if (with_axes) {
+      if (!axes) fail(MZ_EINVAL, "axes is NULL");
+      if (axes->n_axes < 1 || axes->n_axes > mzk::kAxes) fail(MZ_EINVAL, "n_axes must be 1..%d", mzk::kAxes);
+      if (!axes->pair_axis || (m > 0 && !axes->rope_pos)) fail(MZ_EINVAL, "NULL pointer");
+      for (int i = 0; i < a.head_dim / 2; ++i) {
+        const int x = axes->pair_axis[i];
+        if (x != 255 && x >= axes->n_axes) fail(MZ_EINVAL, "pair_axis names axis %d of %d", x, axes->n_axes);
+        k.axis[i / 16] |= (uint64_t)(x == 255 ? mzk::kAxisNone : x) << (i % 16 * 4);
+        if (x != 255) k.axes_used |= 1u << x;
+      }
+      k.rope_pos = axes->rope_pos;
+    }
     k.k_stride = a.k_stride ? a.k_stride : dkv;
     k.v_stride = a.v_stride ? a.v_stride : dkv;
     k.q_stride = a.q_stride ? a.q_stride : dq;
@@ -2229,6 +2241,14 @@ mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
     mzk::launch_kv_append(k, m, a.f32 != 0, (hipStream_t)stream);
     HIPCHK(hipGetLastError());
   });
+}
+
+mz_status mz_kv_append(const mz_kv_append_args* args, int32_t m, void* stream) {
+  return append_entry(args, nullptr, false, m, stream);
+}
+
+mz_status mz_kv_append_axes(const mz_kv_append_args* args, const mz_rope_axes* axes, int32_t m, void* stream) {
+  return append_entry(args, axes, true, m, stream);
 }
 
 int64_t mz_attention_batch_workspace_bytes(int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t head_dim) {
@@ -2360,6 +2380,231 @@ mz_status mz_logits_rules(const float* logits, int32_t m, int32_t vocab, int64_t
     p.mask_words = r.mask_words;
     p.token = token;
     mzk::launch_logits_rules(p, m, workspace, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
+// ---- a decode step that checks drafted trees
+
+// Device arrays of a call, for the refusal of outputs that lie in other arrays.
+namespace {
+struct Span {
+  const void* p;
+  int64_t bytes;
+};
+}  // namespace
+static void check_apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+  auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
+  };
+  for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+    for (auto p = o + 1; p != outputs.end(); ++p)
+      if (meet(*o, *p)) fail(MZ_EINVAL, "two outputs overlap");
+    for (const Span& i : inputs)
+      if (meet(*o, i)) fail(MZ_EINVAL, "an output overlaps an input");
+  }
+}
+
+static void check_trees(int32_t n_seq, int32_t m) {
+  if (n_seq < 1 || n_seq > mzk::kTreeSeqs) fail(MZ_EINVAL, "n_seq must be 1..%d", mzk::kTreeSeqs);
+  if (m < 0 || m > (1 << 30)) fail(MZ_EINVAL, "m must be 0..2^30");
+}
+
+// Layers of slots, layer_bytes apart: returns a slot's bytes.
+static int64_t check_layers(const void* slab, int32_t n_layers, int64_t layer_bytes, int32_t n_slots, int32_t chunk_tokens,
+                            int32_t n_kv, int32_t head_dim) {
+  if (head_dim != 32 && head_dim != 64 && head_dim != 128) fail(MZ_EINVAL, "head_dim must be 32, 64 or 128");
+  if (n_kv < 1 || n_kv > 1024) fail(MZ_EINVAL, "bad head counts");
+  const int64_t slot_bytes = (int64_t)chunk_tokens * n_kv * head_dim * 4;
+  if (slot_bytes > INT32_MAX) fail(MZ_EINVAL, "a chunk slot exceeds 2^31 - 1 bytes");
+  if (!aligned16(slab) || layer_bytes % 16) fail(MZ_EINVAL, "slab and layer_bytes must lie on 16-byte boundaries");
+  if (n_layers > 1 && layer_bytes < n_slots * slot_bytes) fail(MZ_EINVAL, "the layers overlap");
+  return slot_bytes;
+}
+
+mz_status mz_tree_plan(const int32_t* row_off, const int32_t* parent, const int32_t* lens, int32_t n_seq, int32_t m,
+                       int32_t* seq, int32_t* place, int32_t* rope_pos, uint32_t* mask, int32_t mask_words, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!row_off || !lens) fail(MZ_EINVAL, "NULL pointer");
+    check_trees(n_seq, m);
+    if (m > 0 && !seq && !place && !rope_pos && !mask) fail(MZ_EINVAL, "no output");
+    if (mask_words < 0 || mask_words > mzk::kTreeNodes / 32 || (mask && mask_words == 0))
+      fail(MZ_EINVAL, "mask_words must be 1..%d, 0 without a mask", mzk::kTreeNodes / 32);
+    if (m > 0 && !mask && mask_words) fail(MZ_EINVAL, "mask_words without a mask");
+    const int64_t row = (int64_t)m * 4;
+    check_apart({{seq, row}, {place, row}, {rope_pos, row}, {mask, row * mask_words}},
+                {{row_off, ((int64_t)n_seq + 1) * 4}, {parent, row}, {lens, (int64_t)n_seq * 4}});
+    check_stream(stream);
+    if (m == 0) return;
+    mzk::launch_tree_plan({row_off, parent, lens, seq, place, rope_pos, mask, n_seq, m, mask_words}, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
+int64_t mz_attention_tree_workspace_bytes(int32_t m, int32_t n_seq, int32_t n_q, int32_t n_kv, int32_t head_dim) {
+  if (m < 1 || n_seq < 1 || n_seq > mzk::kTreeSeqs || n_kv < 1 || n_q < n_kv || n_q % n_kv || n_q / n_kv > 16 ||
+      (head_dim != 64 && head_dim != 128) || (int64_t)m * n_q > mzk::kMaxBlocks)
+    return -1;
+  return mzk::attention_tree_ws_bytes(m, n_seq, n_q, n_kv, head_dim);
+}
+
+mz_status mz_attention_tree(const mz_attention_tree_args* args, void* workspace, int64_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!args) fail(MZ_EINVAL, "args is NULL");
+    const mz_attention_tree_args& a = *args;
+    if (a.m < 0) fail(MZ_EINVAL, "m is negative");
+    if (!a.row_off || !a.lens || !a.slab || !a.table || (a.m > 0 && (!a.q || !a.out || !workspace))) fail(MZ_EINVAL, "NULL pointer");
+    check_chunks(a.n_seq, a.n_slots, a.n_table, a.chunk_tokens);
+    check_trees(a.n_seq, a.m);
+    if (a.mask_words < 0 || a.mask_words > mzk::kTreeNodes / 32 || (a.mask && a.mask_words == 0))
+      fail(MZ_EINVAL, "mask_words must be 1..%d, 0 without a mask", mzk::kTreeNodes / 32);
+    if (a.m > 0 && !a.mask && a.mask_words) fail(MZ_EINVAL, "mask_words without a mask");
+    if (a.head_dim != 64 && a.head_dim != 128) fail(MZ_EINVAL, "head_dim must be 64 or 128");
+    const int32_t nq = a.n_q_heads, nkv = a.n_kv_heads;
+    if (nkv < 1 || nq < nkv || nq % nkv || nq / nkv > 16) fail(MZ_EINVAL, "bad head counts");
+    // what is counted below stays within 64 bits for that many rows and heads
+    if ((int64_t)a.m * nq > mzk::kMaxBlocks || nq > mzk::kMaxBlocks) fail(MZ_EINVAL, "m rows of n_q_heads are too many");
+    const int64_t slot_bytes = (int64_t)a.chunk_tokens * nkv * a.head_dim * 4;
+    if (slot_bytes > INT32_MAX) fail(MZ_EINVAL, "a chunk slot exceeds 2^31 - 1 bytes");
+    if (!aligned16(a.q) || !aligned16(a.slab) || !aligned16(a.out) || !aligned16(workspace))
+      fail(MZ_EINVAL, "q, slab, workspace and out must lie on 16-byte boundaries");
+    if (mzk::attention_tree_units(a.m, a.n_seq, a.n_table, a.chunk_tokens, nq, nkv) > INT32_MAX)
+      fail(MZ_EINVAL, "m rows of n_seq sequences of n_table chunks are too many");
+    check_stream(stream);
+    if (a.m == 0) return;
+    if (workspace_bytes < mzk::attention_tree_ws_bytes(a.m, a.n_seq, nq, nkv, a.head_dim)) fail(MZ_EINVAL, "workspace too small");
+    mzk::AttnTree t{};
+    t.q = reinterpret_cast<const _Float16*>(a.q);
+    t.row_off = a.row_off;
+    t.lens = a.lens;
+    t.table = a.table;
+    t.mask = a.mask;
+    t.slab = reinterpret_cast<const uint8_t*>(a.slab);
+    t.out = reinterpret_cast<_Float16*>(a.out);
+    t.n_seq = a.n_seq;
+    t.m = a.m;
+    t.mask_words = a.mask_words;
+    t.n_slots = a.n_slots;
+    t.n_table = a.n_table;
+    t.C = a.chunk_tokens;
+    t.cshift = __builtin_ctz((unsigned)a.chunk_tokens);
+    t.nq = nq;
+    t.nkv = nkv;
+    t.group = nq / nkv;
+    t.slot_bytes = slot_bytes;
+    mzk::launch_attention_tree(t, a.head_dim, workspace, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
+mz_status mz_tree_accept(const mz_tree_accept_args* args, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!args) fail(MZ_EINVAL, "args is NULL");
+    const mz_tree_accept_args& a = *args;
+    check_trees(a.n_seq, a.m);
+    if (!a.row_off || !a.lens || !a.accepted || !a.next || !a.len_out || (a.m > 0 && (!a.token || !a.choice || !a.path)))
+      fail(MZ_EINVAL, "NULL pointer");
+    if (a.n_layers < 0) fail(MZ_EINVAL, "n_layers is negative");
+    mzk::TreeAccept t{};
+    const int64_t row = (int64_t)a.m * 4, one = (int64_t)a.n_seq * 4;
+    Span slab{nullptr, 0}, table{nullptr, 0};
+    if (a.n_layers > 0) {
+      if (!a.slab || !a.table) fail(MZ_EINVAL, "NULL pointer");
+      check_chunks(a.n_seq, a.n_slots, a.n_table, a.chunk_tokens);
+      t.slot_bytes = check_layers(a.slab, a.n_layers, a.layer_bytes, a.n_slots, a.chunk_tokens, a.n_kv_heads, a.head_dim);
+      t.dkv = a.n_kv_heads * a.head_dim;
+      t.cshift = __builtin_ctz((unsigned)a.chunk_tokens);
+      slab = {a.slab, (a.n_layers - 1) * a.layer_bytes + a.n_slots * t.slot_bytes};
+      table = {a.table, (int64_t)a.n_seq * a.n_table * 4};
+    }
+    if (!mzk::tree_accept_fits(a.n_seq, a.n_layers, t.dkv)) fail(MZ_EINVAL, "n_seq sequences of these heads are too many");
+    check_apart({{a.accepted, one}, {a.path, row}, {a.next, one}, {a.len_out, one}, slab},
+                {{a.row_off, one + 4}, {a.parent, row}, {a.token, row}, {a.choice, row}, {a.lens, one}, table});
+    check_stream(stream);
+    t.row_off = a.row_off;
+    t.parent = a.parent;
+    t.token = a.token;
+    t.choice = a.choice;
+    t.lens = a.lens;
+    t.accepted = a.accepted;
+    t.path = a.path;
+    t.next = a.next;
+    t.len_out = a.len_out;
+    t.slab = reinterpret_cast<uint8_t*>(a.slab);
+    t.table = a.table;
+    t.layer_bytes = a.layer_bytes;
+    t.n_seq = a.n_seq;
+    t.m = a.m;
+    t.n_layers = a.n_layers;
+    t.n_slots = a.n_slots;
+    t.n_table = a.n_table;
+    t.C = a.chunk_tokens;
+    mzk::launch_tree_accept(t, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
+// Sizes of mz_kv_pages that its indexes hold.
+static bool pages_fit(int32_t n_seq, int32_t n_table, int32_t n_slots) {
+  return n_seq >= 1 && n_table >= 1 && n_slots >= 1 && n_seq <= mzk::kTreeSeqs && n_slots <= (1 << 28) &&
+         (int64_t)n_seq * n_table <= (1 << 28);
+}
+
+int64_t mz_kv_pages_workspace_bytes(int32_t n_seq, int32_t n_table, int32_t n_slots) {
+  return pages_fit(n_seq, n_table, n_slots) ? mzk::kv_pages_ws_bytes(n_seq, n_table, n_slots) : -1;
+}
+
+mz_status mz_kv_pages(const mz_kv_pages_args* args, void* workspace, int64_t workspace_bytes, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!args) fail(MZ_EINVAL, "args is NULL");
+    const mz_kv_pages_args& a = *args;
+    if (!a.table || !a.table_out || !a.keep || !a.copies || !a.info || !workspace) fail(MZ_EINVAL, "NULL pointer");
+    check_chunks(a.n_seq, a.n_slots, a.n_table, a.chunk_tokens);
+    if (!pages_fit(a.n_seq, a.n_table, a.n_slots)) fail(MZ_EINVAL, "n_seq rows of n_table chunks, or n_slots, are too many");
+    if (a.slot_limit < 0 || a.slot_limit > a.n_slots) fail(MZ_EINVAL, "slot_limit must be 0..n_slots");
+    if (!aligned16(a.copies) || !aligned16(workspace)) fail(MZ_EINVAL, "copies and workspace must lie on 16-byte boundaries");
+    const int64_t need = mzk::kv_pages_ws_bytes(a.n_seq, a.n_table, a.n_slots);
+    if (workspace_bytes < need) fail(MZ_EINVAL, "workspace too small");
+    const int32_t limit = a.slot_limit ? a.slot_limit : a.n_slots;
+    const int64_t one = (int64_t)a.n_seq * 4, entries = one * a.n_table;
+    const Span out{a.table_out, entries}, copies{a.copies, ((int64_t)a.n_seq + a.n_slots - limit) * 16}, info{a.info, 16}, ws{workspace, need};
+    check_apart({out, copies, info, ws}, {{a.src, one}, {a.keep, one}, {a.room, one}});
+    if (a.table != a.table_out) check_apart({out}, {{a.table, entries}});
+    check_apart({copies, info, ws}, {{a.table, entries}});
+    check_stream(stream);
+    mzk::KvPages p{};
+    p.table = a.table;
+    p.src = a.src;
+    p.keep = a.keep;
+    p.room = a.room;
+    p.table_out = a.table_out;
+    p.n_seq = a.n_seq;
+    p.n_table = a.n_table;
+    p.n_slots = a.n_slots;
+    p.limit = limit;
+    p.C = a.chunk_tokens;
+    p.cshift = __builtin_ctz((unsigned)a.chunk_tokens);
+    p.copies = reinterpret_cast<int4*>(a.copies);
+    p.info = a.info;
+    mzk::launch_kv_pages(p, workspace, (hipStream_t)stream);
+    HIPCHK(hipGetLastError());
+  });
+}
+
+mz_status mz_kv_copy(const int32_t* copies, const int32_t* n_copies, int32_t max_copies, void* slab, int32_t n_slots,
+                     int32_t n_layers, int64_t layer_bytes, int32_t chunk_tokens, int32_t n_kv, int32_t head_dim, void* stream) {
+  return guarded(nullptr, [&] {
+    if (!slab || (max_copies > 0 && (!copies || !n_copies))) fail(MZ_EINVAL, "NULL pointer");
+    if (max_copies < 0 || n_layers < 1) fail(MZ_EINVAL, "n_layers must be positive, max_copies at least 0");
+    check_chunks(1, n_slots, 1, chunk_tokens);
+    if (!aligned16(copies)) fail(MZ_EINVAL, "copies must lie on a 16-byte boundary");
+    const int64_t slot_bytes = check_layers(slab, n_layers, layer_bytes, n_slots, chunk_tokens, n_kv, head_dim);
+    check_stream(stream);
+    if (max_copies == 0) return;
+    mzk::launch_kv_copy({reinterpret_cast<const int4*>(copies), n_copies, reinterpret_cast<uint8_t*>(slab), layer_bytes, slot_bytes,
+                         max_copies, n_slots, n_layers, chunk_tokens, n_kv * head_dim},
+                        (hipStream_t)stream);
     HIPCHK(hipGetLastError());
   });
 }

@@ -73,6 +73,35 @@ class mz_kv_append_args(ctypes.Structure):
                 ("n_table", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32), ("q_out", ctypes.c_void_p)]
 
 
+class mz_rope_axes(ctypes.Structure):
+    _fields_ = [("rope_pos", ctypes.c_void_p), ("n_axes", ctypes.c_int32), ("pair_axis", ctypes.c_char_p)]
+
+
+class mz_attention_tree_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("m", ctypes.c_int32), ("n_seq", ctypes.c_int32), ("row_off", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int32),
+                ("n_slots", ctypes.c_int32), ("slab", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("n_table", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("out", ctypes.c_void_p)]
+
+
+class mz_tree_accept_args(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("m", ctypes.c_int32), ("row_off", ctypes.c_void_p), ("parent", ctypes.c_void_p),
+                ("token", ctypes.c_void_p), ("choice", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("accepted", ctypes.c_void_p), ("path", ctypes.c_void_p), ("next", ctypes.c_void_p),
+                ("len_out", ctypes.c_void_p), ("n_layers", ctypes.c_int32), ("n_slots", ctypes.c_int32),
+                ("slab", ctypes.c_void_p), ("layer_bytes", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("n_table", ctypes.c_int32), ("chunk_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class mz_kv_pages_args(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_table", ctypes.c_int32), ("n_slots", ctypes.c_int32),
+                ("chunk_tokens", ctypes.c_int32), ("slot_limit", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("table_out", ctypes.c_void_p), ("src", ctypes.c_void_p), ("keep", ctypes.c_void_p),
+                ("room", ctypes.c_void_p), ("copies", ctypes.c_void_p), ("info", ctypes.c_void_p)]
+
+
 class mz_token_rules(ctypes.Structure):
     _fields_ = [("repetition", ctypes.c_float), ("frequency", ctypes.c_float), ("presence", ctypes.c_float),
                 ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
@@ -148,6 +177,14 @@ def lib() -> ctypes.CDLL:
         "mz_lora_workspace_bytes": ([i32, i32, i32, i32], i64),
         "mz_logits_rules": ([vp, i32, i32, i64, ctypes.POINTER(mz_logits_rules_args), vp, vp, vp, i64, vp], i32),
         "mz_logits_rules_workspace_bytes": ([i32, i32], i64),
+        "mz_tree_plan": ([vp, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp], i32),
+        "mz_kv_append_axes": ([ctypes.POINTER(mz_kv_append_args), ctypes.POINTER(mz_rope_axes), i32, vp], i32),
+        "mz_attention_tree": ([ctypes.POINTER(mz_attention_tree_args), vp, i64, vp], i32),
+        "mz_attention_tree_workspace_bytes": ([i32, i32, i32, i32, i32], i64),
+        "mz_tree_accept": ([ctypes.POINTER(mz_tree_accept_args), vp], i32),
+        "mz_kv_pages": ([ctypes.POINTER(mz_kv_pages_args), vp, i64, vp], i32),
+        "mz_kv_pages_workspace_bytes": ([i32, i32, i32], i64),
+        "mz_kv_copy": ([vp, vp, i32, vp, i32, i32, i64, i32, i32, i32, vp], i32),
         "mz_rmsnorm": ([vp, i32, i32, ctypes.c_float, vp, vp], i32),
         "mz_probe_ceilings": ([i32, ctypes.c_char_p, sz], i32),
         "mz_plan_evict": ([ctypes.POINTER(mz_model_cfg), ctypes.POINTER(mz_evict_request), vp, vp, vp], i32),
@@ -539,6 +576,67 @@ def mz_logits_rules(logits_ptr: int, m: int, vocab: int, stride: int, out_ptr: O
 
 def mz_logits_rules_workspace_bytes(m: int, vocab: int) -> int:
     return int(lib().mz_logits_rules_workspace_bytes(m, vocab))
+
+
+def mz_tree_plan(row_off_ptr: int, lens_ptr: int, n_seq: int, m: int, stream: Optional[int] = None, parent_ptr: int = 0,
+                 seq_ptr: int = 0, place_ptr: int = 0, rope_pos_ptr: int = 0, mask_ptr: int = 0, mask_words: int = 0) -> None:
+    """Device pointers as integers (0: absent)."""
+    _check(lib().mz_tree_plan(row_off_ptr, parent_ptr or None, lens_ptr, n_seq, m, seq_ptr or None, place_ptr or None,
+                              rope_pos_ptr or None, mask_ptr or None, mask_words, stream), None)
+
+
+def mz_kv_append_axes(m: int, k_ptr: int, v_ptr: int, seq_ptr: int, pos_ptr: int, rope_pos_ptr: int, n_axes: int, pair_axis,
+                      rope_cs_ptr: int, n_rope: int, slab_ptr: int, n_slots: int, table_ptr: int, n_seq: int, n_table: int,
+                      chunk_tokens: int, n_kv: int, head_dim: int, stream: Optional[int] = None, q_ptr: int = 0, n_q: int = 0,
+                      q_out_ptr: int = 0, k_stride: int = 0, v_stride: int = 0, q_stride: int = 0, f32: bool = True) -> None:
+    """mz_kv_append by axes; pair_axis: the axis of each of the head_dim / 2 pairs (255: not turned)."""
+    pair_axis = None if pair_axis is None else bytes(pair_axis)
+    if pair_axis is not None and len(pair_axis) != head_dim // 2:
+        raise MzError(MZ_EINVAL, "pair_axis must name an axis for each of the head_dim / 2 pairs")
+    a = mz_kv_append_args(q_ptr, k_ptr, v_ptr, q_stride, k_stride, v_stride, f32, head_dim, n_q, n_kv, seq_ptr, pos_ptr,
+                          rope_cs_ptr, n_rope, n_slots, slab_ptr, table_ptr, n_seq, n_table, chunk_tokens, q_out_ptr)
+    x = mz_rope_axes(rope_pos_ptr, n_axes, pair_axis)
+    _check(lib().mz_kv_append_axes(ctypes.byref(a), ctypes.byref(x), m, stream), None)
+
+
+def mz_attention_tree(q_ptr: int, m: int, row_off_ptr: int, lens_ptr: int, n_seq: int, slab_ptr: int, n_slots: int, table_ptr: int,
+                      n_table: int, chunk_tokens: int, n_q: int, n_kv: int, head_dim: int, ws_ptr: int, ws_bytes: int,
+                      out_ptr: int, stream: Optional[int] = None, mask_ptr: int = 0, mask_words: int = 0) -> None:
+    a = mz_attention_tree_args(q_ptr, m, n_seq, row_off_ptr, lens_ptr, mask_ptr, mask_words, n_slots, slab_ptr, table_ptr, n_table,
+                               chunk_tokens, n_q, n_kv, head_dim, out_ptr)
+    _check(lib().mz_attention_tree(ctypes.byref(a), ws_ptr, ws_bytes, stream), None)
+
+
+def mz_attention_tree_workspace_bytes(m: int, n_seq: int, n_q: int, n_kv: int, head_dim: int) -> int:
+    return int(lib().mz_attention_tree_workspace_bytes(m, n_seq, n_q, n_kv, head_dim))
+
+
+def mz_tree_accept(row_off_ptr: int, token_ptr: int, choice_ptr: int, lens_ptr: int, n_seq: int, m: int, accepted_ptr: int,
+                   path_ptr: int, next_ptr: int, len_out_ptr: int, stream: Optional[int] = None, parent_ptr: int = 0,
+                   slab_ptr: int = 0, n_slots: int = 0, n_layers: int = 0, layer_bytes: int = 0, table_ptr: int = 0,
+                   n_table: int = 0, chunk_tokens: int = 0, n_kv: int = 0, head_dim: int = 0) -> None:
+    """Without layers (n_layers 0) the branches are taken and nothing is moved."""
+    a = mz_tree_accept_args(n_seq, m, row_off_ptr, parent_ptr, token_ptr, choice_ptr, lens_ptr, accepted_ptr, path_ptr, next_ptr,
+                            len_out_ptr, n_layers, n_slots, slab_ptr, layer_bytes, table_ptr, n_table, chunk_tokens, n_kv, head_dim)
+    _check(lib().mz_tree_accept(ctypes.byref(a), stream), None)
+
+
+def mz_kv_pages(table_ptr: int, table_out_ptr: int, n_seq: int, n_table: int, n_slots: int, chunk_tokens: int, keep_ptr: int,
+                copies_ptr: int, info_ptr: int, ws_ptr: int, ws_bytes: int, stream: Optional[int] = None, src_ptr: int = 0,
+                room_ptr: int = 0, slot_limit: int = 0) -> None:
+    a = mz_kv_pages_args(n_seq, n_table, n_slots, chunk_tokens, slot_limit, table_ptr, table_out_ptr, src_ptr, keep_ptr, room_ptr,
+                         copies_ptr, info_ptr)
+    _check(lib().mz_kv_pages(ctypes.byref(a), ws_ptr, ws_bytes, stream), None)
+
+
+def mz_kv_pages_workspace_bytes(n_seq: int, n_table: int, n_slots: int) -> int:
+    return int(lib().mz_kv_pages_workspace_bytes(n_seq, n_table, n_slots))
+
+
+def mz_kv_copy(copies_ptr: int, n_copies_ptr: int, max_copies: int, slab_ptr: int, n_slots: int, n_layers: int, layer_bytes: int,
+               chunk_tokens: int, n_kv: int, head_dim: int, stream: Optional[int] = None) -> None:
+    _check(lib().mz_kv_copy(copies_ptr, n_copies_ptr, max_copies, slab_ptr, n_slots, n_layers, layer_bytes, chunk_tokens, n_kv,
+                            head_dim, stream), None)
 
 
 def mz_rmsnorm(h_ptr: int, m: int, d: int, eps: float, x_ptr: int, stream: Optional[int] = None) -> None:
