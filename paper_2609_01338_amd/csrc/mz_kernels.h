@@ -274,7 +274,8 @@ struct AttnTree {
   int n_seq, m, mask_words, n_slots, n_table, C, cshift, nq, nkv, group;
   int64_t slot_bytes;
   int32_t *base, *row_seq;   // [n_seq + 1] units of 128 keys a KV head of the sequences before, [m]
-  float2* ml;                // [2 wgs][columns of a tile] running max and sum of a partial
+  uint8_t* again;            // [m][nq] whether what was written whole had sums that are not finite
+  float2* ml;                // [2 wgs][columns of a tile] running max (NaN: sums that are not finite) and sum of a partial
   float* part;               // [2 wgs][columns of a tile][hd]
   int wgs;                   // most workgroups that share the units
   float scale_log2;
