@@ -867,7 +867,7 @@ typedef struct {
  * caller-owned, at least mz_attention_tree_workspace_bytes(...) bytes (one for
  * the most rows and sequences serves fewer), any content, not shared by calls
  * in flight together (two graphs that may run at once need two).  Errors:
- * EINVAL for the above, a NULL pointer, more work than 2^31 blocks of 128 keys,
+ * EINVAL for the above, a NULL pointer, more work than 2^31 blocks of 32 keys,
  * q, slab, workspace or out off 16-byte boundaries, or a short workspace. */
 mz_status mz_attention_tree(const mz_attention_tree_args *args, void *workspace, int64_t workspace_bytes,
                             void *stream);

@@ -15,9 +15,9 @@
 // bits of a weight (and what it holds down to 2^-34 of the largest), so that an
 // output's only rounding to fewer bits is its own.  Both enter the same fp32
 // sums.  A weight of 0 removes what a node does not see, unless the value is
-// infinite or NaN: then sums that are not finite show it, and the second
-// kernel takes the columns that they belong to again, a (row, head) at a time, with
-// fp32 products of what the row sees alone.
+// infinite or NaN: then sums that are not finite show it, and the columns that
+// they belong to are taken again, a (row, head) at a time, with fp32 products of
+// what the row sees alone.
 #include <algorithm>
 
 #include "mz_kernels.h"
@@ -26,6 +26,7 @@ namespace mzk {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -52,7 +53,8 @@ __device__ __forceinline__ Seq seq_of(const AttnTree& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ int shares(const AttnTree& a, int total) { return min(a.wgs, total); }
+// Shares of `total` units: as many as there are workgroups, but of a.least units at least.
+__device__ __forceinline__ int shares(const AttnTree& a, int total) { return max(1, min(a.wgs, total / a.least)); }
 
 // The workgroup whose share [g total / nw, (g + 1) total / nw) holds unit u.
 __device__ __forceinline__ int share_of(int u, int nw, int total) {
@@ -83,7 +85,7 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& sum) {
 
 // A workgroup's share [u, end) of the units, and the sequence that it begins
 // in, whose units begin at `first`.  The second kernel's tables on the way: the
-// units before every sequence, and the sequence of every row.
+// units a KV head before every sequence, and the sequence of every row.
 struct Share {
   int u, end, b, first;
 };
@@ -96,8 +98,8 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_red, int* 
       const int end = min(max(a.row_off[b + 1], s.first), a.m);
       for (int r = s.first + threadIdx.x; r < end; r += NT) a.row_seq[r] = r - s.first < s.nodes ? b : -1;
     } else {
-      const int before = min(max(a.row_off[0], 0), a.m), last = min(max(a.row_off[a.n_seq], before), a.m);
-      for (int i = threadIdx.x; i < before + a.m - last; i += NT) a.row_seq[i < before ? i : last + i - before] = -1;
+      const int before = min(max(a.row_off[0], 0), a.m), behind = min(max(a.row_off[a.n_seq], before), a.m);
+      for (int i = threadIdx.x; i < before + a.m - behind; i += NT) a.row_seq[i < before ? i : behind + i - before] = -1;
     }
   }
   int total = 0, u_mine = 0, u_before = 0;
@@ -111,11 +113,11 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_red, int* 
     u_mine = units(b);
     int sum;
     u_before = total + block_scan<NW>(u_mine, s_red, sum) - u_mine;
-    if (blockIdx.x == 0 && b < a.n_seq) a.base[b] = u_before;
     total += sum;
+    if (blockIdx.x == 0 && b < a.n_seq) a.base[b] = u_before;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.base[a.n_seq] = total;
   const int n_units = total * a.nkv, nw = shares(a, n_units), g = blockIdx.x;
+  if (g == 0 && threadIdx.x == 0) a.base[a.n_seq] = total;
   if (g >= nw) return false;
   sh.u = (int)((uint64_t)g * n_units / nw);
   sh.end = (int)(((uint64_t)g + 1) * n_units / nw);
@@ -172,6 +174,68 @@ __device__ __forceinline__ bool sees(const AttnTree& a, const Seq& s, int j, int
   return at < 0 || (a.mask ? (words[at >> 5] >> (at & 31)) & 1 : at <= node);
 }
 
+// One (row, query head) alone, over the keys that it sees, NT at a time: a
+// thread a score, then a thread a dimension of every (NT / HD)-th value.  s_p: NT
+// floats in LDS, s_red: max(NT / 64, NT / HD).
+template <int HD, int NT>
+__device__ __forceinline__ void row_again(const AttnTree& a, const Seq& s, int b, int r, int hq, float* s_p, float* s_red) {
+  constexpr int PARTS = NT / HD;
+  const int t = threadIdx.x, h = hq / a.group, node = r - s.first, dkv = a.nkv * HD, d = t % HD, part = t / HD;
+  const uint32_t* words = a.mask + (int64_t)r * a.mask_words;
+  const int32_t* table = a.table + (int64_t)b * a.n_table;
+  const _Float16* q = a.q + ((int64_t)r * a.nq + hq) * HD;
+  float m = -INFINITY, l = 0.f, acc = 0.f;
+  for (int j0 = 0; j0 < s.keys; j0 += NT) {
+    const int j = j0 + t, slot = j < s.keys ? table[j >> a.cshift] : -1;
+    const bool on = (unsigned)slot < (unsigned)a.n_slots && sees(a, s, j, node, words);
+    float score = -INFINITY, top = -INFINITY;
+    if (on) {
+      const _Float16* k = reinterpret_cast<const _Float16*>(a.slab + slot * a.slot_bytes) + (int64_t)(j & (a.C - 1)) * dkv + h * HD;
+      float sum = 0.f;
+      for (int e = 0; e < HD; ++e) sum = __builtin_fmaf((float)k[e], (float)q[e], sum);
+      score = sum * a.scale_log2;
+      top = fmaxf(score, kLowest);
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+    __syncthreads();                   // the keys before have been read
+    if ((t & 63) == 0) s_red[t >> 6] = top;
+    __syncthreads();
+    float now = m;
+#pragma unroll
+    for (int x = 0; x < NT / 64; ++x) now = fmaxf(now, s_red[x]);
+    const float alpha = now == m ? 1.f : exp2_hw(m - now);
+    m = now;
+    s_p[t] = on ? exp2_hw(score - m) : -1.f;      // -1: not seen
+    l *= alpha;
+    acc *= alpha;
+    __syncthreads();
+    for (int k = part; k < NT; k += PARTS) {
+      const float p = s_p[k];
+      if (p == -1.f) continue;
+      const int jk = j0 + k;
+      const _Float16* v = reinterpret_cast<const _Float16*>(a.slab + table[jk >> a.cshift] * a.slot_bytes) + (int64_t)a.C * dkv +
+                          (int64_t)(h * HD + d) * a.C + (jk & (a.C - 1));
+      acc = __builtin_fmaf(p, (float)*v, acc);
+      l += p;
+    }
+  }
+  __syncthreads();
+  s_p[t] = acc;
+  if (d == 0) s_red[part] = l;
+  __syncthreads();
+  if (part == 0) {
+    float sum = 0.f, den = 0.f;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      sum += s_p[k * HD + d];
+      den += s_red[k];
+    }
+    a.out[((int64_t)r * a.nq + hq) * HD + d] = (_Float16)(m == -INFINITY ? 0.f : sum / den);
+  }
+  __syncthreads();
+}
+
 // Which of the eight keys from j on a node sees, of those before the end.
 __device__ __forceinline__ unsigned seen8(const AttnTree& a, const Seq& s, int j, int node, const uint32_t* words) {
   const int at = j - s.len;              // of the tree
@@ -215,7 +279,7 @@ __device__ __forceinline__ uint64_t seen64(const AttnTree& a, const Seq& s, int 
 // block (t: first or second product), so that the eight scores of a lane are
 // eight consecutive keys: its mask is eight bits, and the P operand meets one
 // 16-byte run of V^T.  The waves' sums meet in LDS at a piece's end.
-constexpr int kFewUnit = 128, kFewWaves = 4, kBlock = 32, kCols = 16, kFewWgs = 512;
+constexpr int kFewUnit = 128, kFewWaves = 4, kBlock = 32, kCols = 16;
 constexpr float kFewBias = 14.f;
 
 // Slots of a lane's K rows and of its V^T run in the block at key j0.
@@ -236,7 +300,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
   constexpr int KS = HD / 32;          // 32-wide dimension steps of a score product
   constexpr int DB = HD / 16;          // 16-dimension blocks of the output
   __shared__ float s_o[kFewWaves][DB][4][64];
-  __shared__ float s_ml[kFewWaves][2][R];
+  __shared__ float s_ml[kFewWaves][2][R], s_again[kFewWaves];
   __shared__ int s_red[kFewWaves], s_at[2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4, dkv = a.nkv * HD, g = blockIdx.x;
@@ -396,6 +460,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
         finite &= fabsf(acc[e]) < INFINITY;
       }
       const int bad = __syncthreads_or(!finite);
+      if (bad && p.t0 == 0 && p.t1 == s.units) {
+        for (int y = p.tile * R + nb * kCols, k = 0; k < kCols && y / a.group < s.nodes; ++k, ++y)
+          row_again<HD, 64 * kFewWaves>(a, s, sh.b, s.first + y / a.group, p.h * a.group + y % a.group, &s_o[0][0][0][0], s_again);
+        continue;
+      }
       if (i >= s.nodes) continue;
       const int64_t row = (int64_t)(s.first + i) * a.nq + head;
       if (p.t0 == 0 && p.t1 == s.units) {
@@ -405,7 +474,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
 #pragma unroll
         for (int e = 0; e < DPT; ++e) y[e] = (_Float16)(acc[e] * inv);
         *reinterpret_cast<out_vec*>(a.out + row * HD + dbase) = y;
-        if (dbase == 0) a.again[row] = bad;
       } else {
         const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * R + x;
         if (dbase == 0) a.ml[e0] = make_float2(bad ? NAN : mx, den);
@@ -431,49 +499,62 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
 // of tile t are formed; then P V of tile t while those of the second half are, and
 // the max of tile t + 1.  The running max is raised only where a tile exceeds it
 // by more than kSlack, so that sums are seldom scaled.
-constexpr int kTile = 64, kWideWaves = 8;      // keys of a tile; waves of a CU, two a SIMD
+// The loads run ST - 1 tiles (V^T) and ST tiles (K) ahead of their product in a
+// ring of ST tiles each, so that several are in flight whatever a step takes.
+// Slots come from a copy of the next kWindow tiles' stretch of the chunk table in
+// LDS: a read of the table between the loads would wait for all of them.
 constexpr float kSlack = 4.f, kWideBias = 11.f;
+constexpr int kWindow = 64;
 
 // LDS tiles are swizzled on 16-byte columns: row r's column c lies at c ^ r % 16
-// (K, 256-byte rows), c ^ (r / 2) % 8 (128-byte rows), so that neither the reads
-// of 32 rows' same column nor the writes of whole rows meet in a bank.
+// (256-byte rows), c ^ (r / 2) % 8 (128-byte rows), c ^ (r / 4) % 4 (64-byte rows),
+// so that neither the reads of 32 rows' same column nor the writes of whole rows
+// meet in a bank.
 template <int HALVES>
 __device__ __forceinline__ int swizzle(int r, int c) {
-  return HALVES == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7);
+  return HALVES == 128 ? c ^ (r & 15) : HALVES == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
 }
 template <int HALVES>
 __device__ __forceinline__ int tile_at(int r, int c) { return r * HALVES + swizzle<HALVES>(r, c) * 8; }
 
-template <int HD, int NW, bool SMALL>
-__global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wide_kernel(AttnTree a) {
-  constexpr int R = 32 * NW, UNIT = kTile;
-  constexpr int KC = HD / 8;                                   // 16-byte columns of a key
-  constexpr int STRETCHES = kTile * KC / 64;                   // of 1 KB, 64 lanes' 16 bytes, in a tile of K and of V^T
+// A wait that leaves the N youngest loads in flight.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
+}
+
+// NK: 32-key blocks of a tile.  SMALL: chunks of fewer tokens than a tile.
+template <int HD, int NW, int NK, int ST, bool SMALL>
+__global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
+  constexpr int R = 32 * NW, KT = 32 * NK, UNIT = KT;
+  constexpr int KC = HD / 8, VC = KT / 8;                      // 16-byte columns of a key, of a dimension
+  constexpr int STRETCHES = KT * KC / 64;                      // of 1 KB, 64 lanes' 16 bytes, in a tile of K and of V^T
   constexpr int PER = STRETCHES / NW;                          // of a wave
-  constexpr int TILE = kTile * HD;                             // halves
+  constexpr int TILE = KT * HD;                                // halves
   constexpr int KS = HD / 16, TN = HD / 32;
-  __shared__ __attribute__((aligned(16))) _Float16 lds[4 * TILE];      // K of two tiles, V^T of two
-  __shared__ int s_red[NW], s_at[2];
+  constexpr int AHEAD = (ST - 2) * 2 * PER;                    // loads that may be in flight when a step ends
+  __shared__ __attribute__((aligned(16))) _Float16 lds[2 * ST * TILE];      // the rings of K and of V^T
+  __shared__ int window[SMALL ? kWindow * KT / 8 + 1 : kWindow + 1];
+  __shared__ float s_again[NW];
+  int* s_at = reinterpret_cast<int*>(lds);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5, dkv = a.nkv * HD, g = blockIdx.x;
   Share sh;
-  if (!share_begin<R, UNIT, NW>(a, s_red, s_at, sh)) return;
+  if (!share_begin<R, UNIT, NW>(a, s_at + 2, s_at, sh)) return;
 
   // where the lane's 16 bytes of a stretch come from: stretch i NW + w holds
   // pieces 64 (i NW + w) + lane of the swizzled tile, so that from one i to the next
   // the key (K) or the dimension (V^T) goes on by a multiple of 8, and the column
   // stays as it is but for K of 16 columns and rows that are 8 apart
-  constexpr int K_STEP = NW * 64 / KC, V_STEP = NW * 8;
-  const int k_row = (w * 64 + lane) / KC, v_row = w * 8 + lane / 8;
+  constexpr int K_STEP = NW * 64 / KC, V_STEP = NW * 64 / VC;
+  const int k_row = (w * 64 + lane) / KC, v_row = (w * 64 + lane) / VC;
   const unsigned k_of = swizzle<HD>(k_row, lane % KC) * 16u;
-  const int v_key = swizzle<kTile>(v_row, lane % 8) * 8;       // the first of the eight keys
-  static_assert(STRETCHES % NW == 0 && V_STEP % 16 == 0 && K_STEP % 8 == 0, "columns of the stretches");
+  const int v_key = swizzle<KT>(v_row, lane % VC) * 8;         // the first of the eight keys
+  static_assert(STRETCHES % NW == 0 && V_STEP % 16 == 0 && K_STEP % 8 == 0 && (KC == 16 || K_STEP % 16 == 0), "columns of the stretches");
   typedef __attribute__((address_space(3))) void lds_void;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds);
-  auto k_buf = [&](int t) { return (t & 1) * TILE; };
-  auto v_buf = [&](int t) { return (2 + (t & 1)) * TILE; };
-  // 64 lanes' 16 bytes from base + at into LDS.  (The wait state lies between
-  // the write of M0 and the load that reads it.)
+  // 64 lanes' 16 bytes from base + at into LDS.  (The wait states lie between the
+  // writes of the base, by a vector instruction, and of M0, and the load that reads them.)
   auto fetch = [&](const uint8_t* base, unsigned at, int to) {
     const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds0 + to * 2);
     if constexpr (SMALL) {
@@ -482,7 +563,7 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     } else {
       const uint64_t b = (uint64_t)(uintptr_t)base;
       const uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(m0), "v"(at), "s"(u) : "memory");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(m0), "v"(at), "s"(u) : "memory");
     }
   };
 
@@ -490,11 +571,77 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
   while (sh.u < sh.end) {
     const Piece p = next_piece<R, UNIT>(a, sh, s);
     const int32_t* table = a.table + (int64_t)sh.b * a.n_table;
-    const int last = s.keys - 1;
+    const int last = s.keys - 1, t_end = p.t1;
     const int x = p.tile * R + w * 32 + col, node = x / a.group, head = p.h * a.group + x - node * a.group;
     const bool there = node < s.nodes;
     const bool active = (p.tile * R + w * 32) / a.group < s.nodes;      // of the wave
     const uint32_t* words = a.mask + (int64_t)(s.first + (there ? node : 0)) * a.mask_words;
+
+    // The table's stretch of tiles w0 .. w0 + kWindow - 1.
+    int w0 = p.t0, c0 = 0;
+    auto fill_window = [&](int t) {
+      w0 = t;
+      c0 = (t * KT) >> a.cshift;
+      const int n = min(((t + kWindow) * KT - 1) >> a.cshift, last >> a.cshift) - c0 + 1;
+      for (int i = threadIdx.x; i < n; i += 64 * NW) window[i] = table[c0 + i];
+      __syncthreads();
+    };
+    // The slot of key j of the window's tiles (keys past the last one: its slot).
+    auto slot_at = [&](int j) { return window[(min(j, last) >> a.cshift) - c0]; };
+    auto clean = [&](int slot) { return (unsigned)slot < (unsigned)a.n_slots ? slot : 0; };
+    // The slots of what the lane loads of a tile, read a step before they are used.
+    constexpr int KSLOTS = SMALL ? PER : 1;
+    int k_slot[KSLOTS], v_slot;
+    auto slots_of_k = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < KSLOTS; ++i) k_slot[i] = slot_at(t * KT + (SMALL ? k_row + i * K_STEP : 0));
+    };
+    auto slots_of_v = [&](int t) { v_slot = slot_at(t * KT + (SMALL ? v_key : 0)); };
+    auto load_k = [&](int t) {
+      const int j0 = (t * KT) & (a.C - 1), to = t % ST * TILE + w * 512;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int row = k_row + i * K_STEP, j = SMALL ? (j0 + row) & (a.C - 1) : j0 + row;
+        const unsigned of = K_STEP % 16 == 0 ? k_of : k_of ^ (i & 1) * 128u;
+        fetch(a.slab + (int64_t)clean(k_slot[i % KSLOTS]) * a.slot_bytes, (unsigned)j * (unsigned)dkv * 2u + p.h * HD * 2u + of, to + i * NW * 512);
+      }
+    };
+    auto load_v = [&](int t) {
+      const int j0 = (t * KT) & (a.C - 1), j = SMALL ? (j0 + v_key) & (a.C - 1) : j0 + v_key, to = (ST + t % ST) * TILE + w * 512;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        fetch(a.slab + (int64_t)clean(v_slot) * a.slot_bytes, ((unsigned)(dkv + p.h * HD + v_row + i * V_STEP) * (unsigned)a.C + (unsigned)j) * 2u,
+              to + i * NW * 512);
+    };
+    // Keys of tile t that are there, and zeros for the values of the others.
+    auto there64 = [&](int t) {
+      const int j = t * KT + lane;
+      return __ballot(lane >= KT || ((unsigned)slot_at(min(j, (w0 + kWindow) * KT - 1)) < (unsigned)a.n_slots && j < s.keys));
+    };
+    auto mend_v = [&](int t, uint64_t keys) {
+      const unsigned on = (unsigned)(keys >> v_key) & 0xFF;
+      if (on == 0xFF) return;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        f16x8* v = reinterpret_cast<f16x8*>(lds + (ST + t % ST) * TILE + (i * NW + w) * 512 + lane * 8);
+        f16x8 e = *v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = (on >> k) & 1 ? e[k] : (_Float16)0.f;
+        *v = e;
+      }
+    };
+
+    __syncthreads();                   // the piece before has been read
+    fill_window(p.t0);
+#pragma unroll
+    for (int i = 0; i < ST; ++i) {
+      if (p.t0 + i >= t_end) break;
+      slots_of_k(p.t0 + i);
+      load_k(p.t0 + i);
+      if (i + 1 == ST) break;
+      slots_of_v(p.t0 + i);
+      load_v(p.t0 + i);
+    }
     f16x8 q[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -508,66 +655,32 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
       for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    // Lane i holds the slot of key i of a tile.
-    auto slot_of = [&](int t) { return table[min(t * kTile + lane, last) >> a.cshift]; };
-    auto clean = [&](int slot) { return (unsigned)slot < (unsigned)a.n_slots ? slot : 0; };
-    auto load_k = [&](int t, int slots) {
-      const int at = clean(slots), j0 = (t * kTile) & (a.C - 1);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int row = k_row + i * K_STEP, j = SMALL ? (j0 + row) & (a.C - 1) : j0 + row;
-        const int slot = SMALL ? __shfl(at, row) : at;
-        const unsigned of = K_STEP % 16 == 0 || KC < 16 ? k_of : k_of ^ (i & 1) * 128u;
-        fetch(a.slab + (int64_t)slot * a.slot_bytes, (unsigned)j * (unsigned)dkv * 2u + p.h * HD * 2u + of, k_buf(t) + (i * NW + w) * 512);
-      }
-    };
-    auto load_v = [&](int t, int slots) {
-      const int at = clean(slots), j0 = (t * kTile) & (a.C - 1), j = SMALL ? (j0 + v_key) & (a.C - 1) : j0 + v_key;
-      const int slot = SMALL ? __shfl(at, v_key) : at;
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        fetch(a.slab + (int64_t)slot * a.slot_bytes,
-              ((unsigned)(dkv + p.h * HD + v_row + i * V_STEP) * (unsigned)a.C + (unsigned)j) * 2u, v_buf(t) + (i * NW + w) * 512);
-    };
-    // Keys of tile t that are there, and zeros for the values of the others.
-    auto there64 = [&](int t, int slots) { return __ballot((unsigned)slots < (unsigned)a.n_slots && t * kTile + lane < s.keys); };
-    auto mend_v = [&](int t, uint64_t keys) {
-      const unsigned on = (unsigned)(keys >> v_key) & 0xFF;
-      if (on == 0xFF) return;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        f16x8* v = reinterpret_cast<f16x8*>(lds + v_buf(t) + ((i * NW + w) * 64 + lane) * 8);
-        f16x8 e = *v;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] = (on >> k) & 1 ? e[k] : (_Float16)0.f;
-        *v = e;
-      }
-    };
-
     const int krow = (col & ~12) | ((col & 8) >> 1) | ((col & 4) << 1);
     auto k_frag = [&](const _Float16* k, int i) {        // of score product i
-      return *reinterpret_cast<const f16x8*>(&k[tile_at<HD>((i & 1) * 32 + krow, (i >> 1) * 2 + half)]);
+      return *reinterpret_cast<const f16x8*>(&k[tile_at<HD>(i % NK * 32 + krow, i / NK * 2 + half)]);
     };
     auto v_frag = [&](const _Float16* v, int grp, int t) {
-      return *reinterpret_cast<const f16x8*>(&v[tile_at<kTile>(t * 32 + col, grp * 2 + half)]);
+      return *reinterpret_cast<const f16x8*>(&v[tile_at<KT>(t * 32 + col, grp * 2 + half)]);
     };
     // Scores of tile t that do not count become -inf; keys: those that are there.
-    auto mask_scores = [&](f32x16 (&sc)[2], int t, uint64_t keys) {
-      const uint64_t on = keys & seen64(a, s, t * kTile, node, words);
-      const unsigned mine[2] = {(unsigned)(on >> (8 * half)), (unsigned)(on >> (32 + 8 * half))};
+    auto mask_scores = [&](f32x16 (&sc)[NK], int t, uint64_t keys) {
+      const uint64_t on = keys & seen64(a, s, t * KT, node, words) & (KT == 64 ? ~0ull : (1ull << KT) - 1);
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+      for (int kk = 0; kk < NK; ++kk) {
+        const unsigned mine = (unsigned)(on >> (32 * kk + 8 * half));
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float v = sc[kk][r];
-          sc[kk][r] = (mine[kk] >> (16 * (r >> 3) + (r & 7))) & 1 ? v : -INFINITY;
+          sc[kk][r] = (mine >> (16 * (r >> 3) + (r & 7))) & 1 ? v : -INFINITY;
         }
+      }
       return on != 0;
     };
-    // A tile with a key that counts raises the max to at least the lowest fp32
-    // value, so -inf means that none was seen.
-    auto raise_max = [&](float mx, bool some) {
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.scale_log2;
+    // The max of a column's scores is the lane's and lane ^ 32's.  A tile with a key
+    // that counts raises it to at least the lowest fp32 value, so -inf means that
+    // none was seen.
+    auto raise_max = [&](float mx, float other, bool some) {
+      mx = fmaxf(mx, other) * a.scale_log2;
       if (some) mx = fmaxf(mx, kLowest);
       const bool raise = mx > m + kSlack;
       if (__any(raise)) {
@@ -581,90 +694,138 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
           for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
       }
     };
-    f16x8 hi[4], lo[4];
-    auto weight = [&](const f32x16 (&sc)[2], int i, float base) {      // score i of 32
-      const float e = exp2_hw(__builtin_fmaf(sc[i >> 4][i & 15], a.scale_log2, -base));
-      l += e;
-      const _Float16 h = (_Float16)e;
-      hi[i >> 3][i & 7] = h;
-      lo[i >> 3][i & 7] = (_Float16)(e - (float)h);
+    f16x2 hi[8 * NK], lo[8 * NK];      // of two scores each, four to a P operand
+    float e0 = 0.f, e1 = 0.f, base = 0.f;
+    // The weights of scores 2 i and 2 i + 1 in four parts of about the same time
+    // (j = 4 i + part), so that they fit under products: the exponentials; their sum;
+    // their halves, lo = f16(e - hi) in one instruction each.  (Its inputs are a
+    // conversion's, not an exponential's or a product's, and a product may read it
+    // two wait states later.)
+    auto weigh = [&](const f32x16 (&sc)[NK], int j) {
+      const int i = j >> 2;
+      if ((j & 3) == 0) e0 = exp2_hw(__builtin_fmaf(sc[i >> 3][2 * (i & 7)], a.scale_log2, -base));
+      if ((j & 3) == 1) e1 = exp2_hw(__builtin_fmaf(sc[i >> 3][2 * (i & 7) + 1], a.scale_log2, -base));
+      if ((j & 3) == 2) {
+        l += e0;
+        l += e1;
+        asm volatile("" : "+v"(l));
+      }
+      if ((j & 3) == 3) {
+        hi[i] = f16x2{(_Float16)e0, (_Float16)e1};
+        asm volatile("v_fma_mixlo_f16 %0, %1, -1.0, %2 op_sel:[0,0,0] op_sel_hi:[1,0,0]\n\t"
+                     "v_fma_mixhi_f16 %0, %1, -1.0, %3 op_sel:[1,0,0] op_sel_hi:[1,0,0]\n\ts_nop 1"
+                     : "=&v"(lo[i]) : "v"(hi[i]), "v"(e0), "v"(e1));
+      }
+    };
+    // Product i of those before the last 16 keys' carries its share of the parts,
+    // so that a P operand is there when its products begin.
+    constexpr int PARTS = 32 * NK, CARRY = NK * KS + (2 * NK - 1) * 2 * TN;
+    auto carry = [&](const f32x16 (&sc)[NK], int i) {
+#pragma unroll
+      for (int j = i * PARTS / CARRY; j < (i + 1) * PARTS / CARRY; ++j) weigh(sc, j);
+    };
+    auto operand = [&](const f16x2* x, int grp) {
+      f16x8 y;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = x[4 * grp + k / 2][k & 1];
+      return y;
     };
 
-    const int t_end = p.t1;
-    int s1 = slot_of(min(p.t0 + 1, t_end - 1)), s2 = slot_of(min(p.t0 + 2, t_end - 1));
-    uint64_t keys;
-    f32x16 sa[2], sb[2];
+    f32x16 sa[NK], sb[NK];
     {
-      const int s0 = slot_of(p.t0);
-      load_k(p.t0, s0);
-      load_v(p.t0, s0);
-      if (p.t0 + 1 < t_end) load_k(p.t0 + 1, s1);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      keys = there64(p.t0, s0);
+      if (p.t0 + ST - 1 < t_end) wait_loads<AHEAD>(); else wait_loads<0>();
+      const uint64_t keys = there64(p.t0);
       if (~keys) mend_v(p.t0, keys);
       __syncthreads();
       if (active) {
 #pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {
+        for (int i = 0; i < NK * KS; ++i) {
           const f32x16 zero = {};
-          sa[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(lds + k_buf(p.t0), i), q[i >> 1], i < 2 ? zero : sa[i & 1], 0, 0, 0);
+          sa[i % NK] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(lds + p.t0 % ST * TILE, i), q[i / NK], i < NK ? zero : sa[i % NK], 0, 0, 0);
         }
         bool some = true;
-        if (~keys || p.t0 * kTile + kTile > s.len) some = mask_scores(sa, p.t0, keys);
+        if (~keys || p.t0 * KT + KT > s.len) some = mask_scores(sa, p.t0, keys);
         float mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, sa[i >> 4][i & 15]);
-        raise_max(mx, some);
+        for (int i = 0; i < 16 * NK; ++i) mx = fmaxf(mx, sa[i >> 4][i & 15]);
+        raise_max(mx, __shfl_xor(mx, 32), some);
       }
       __syncthreads();                 // K of the first tile has been read
     }
-    // Holds: K of tile t + 1 and V^T of tile t in LDS, the scores of tile t in sc.
-    auto step = [&](int t, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
-      const bool more = t + 1 < t_end;
-      int s3 = 0;
-      if (t + 2 < t_end) load_k(t + 2, s2);
-      if (more) load_v(t + 1, s1);
-      s3 = slot_of(min(t + 3, t_end - 1));
-      const uint64_t next_keys = there64(t + 1, s1);
+    uint64_t next_keys = 0;
+    auto look_ahead = [&](int t) {     // what step t needs of the table
+      if (t + ST - 1 < t_end) slots_of_v(t + ST - 1);
+      if (t + ST < t_end) slots_of_k(t + ST);
+      if (t + 1 < t_end) next_keys = there64(t + 1);
+    };
+    look_ahead(p.t0);
+    // Holds: K of tile t + 1 and V^T of tile t in LDS, the scores of tile t in
+    // sc.  Products and what is done under each are kept in this order by
+    // fences; fragments are read three products (K) and a pair of them (V^T) ahead.
+    auto step = [&](int t, f32x16 (&sc)[NK], f32x16 (&sn)[NK]) {
+      const bool more = t + 1 < t_end, full = t + ST < t_end;
+      const _Float16* kt = lds + (t + 1) % ST * TILE;
+      const _Float16* vt = lds + (ST + t % ST) * TILE;
+      f16x8 k0 = k_frag(kt, 0), k1 = k_frag(kt, 1), k2 = k_frag(kt, 2);
+      if (t + ST - 1 < t_end) load_v(t + ST - 1);
+      if (full) load_k(t + ST);
+      const uint64_t keys = next_keys;
+      const bool refill = full && t + 1 + ST >= w0 + kWindow;
+      if (!refill) look_ahead(t + 1);
       if (active) {
-        const float base = m == -INFINITY ? 0.f : m - kWideBias;
-        const _Float16* kt = lds + k_buf(t + 1);
-        const _Float16* vt = lds + v_buf(t);
+        base = m == -INFINITY ? 0.f : m - kWideBias;
+        f16x8 v0, v1;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 2 * KS; ++i) {
+        for (int i = 0; i < NK * KS; ++i) {
           const f32x16 zero = {};
-          sn[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(kt, i), q[i >> 1], i < 2 ? zero : sn[i & 1], 0, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 8 / KS; ++e) weight(sc, i * (8 / KS) + e, base);
+          const f16x8 k3 = i + 3 < NK * KS ? k_frag(kt, i + 3) : k2;
+          if (i == NK * KS - 3) v0 = v_frag(vt, 0, 0);
+          if (i == NK * KS - 2) v1 = v_frag(vt, 0, 1);
+          __builtin_amdgcn_sched_barrier(0);
+          sn[i % NK] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[i / NK], i < NK ? zero : sn[i % NK], 0, 0, 0);
+          k0 = k1;
+          k1 = k2;
+          k2 = k3;
+          carry(sc, i);
+          __builtin_amdgcn_sched_barrier(0);
         }
         bool some = true;
-        if (more && (~next_keys || (t + 1) * kTile + kTile > s.len)) some = mask_scores(sn, t + 1, next_keys);
-        float mx = -INFINITY;
+        if (more && (~keys || (t + 1) * KT + KT > s.len)) some = mask_scores(sn, t + 1, keys);
+        float mx = -INFINITY, other = -INFINITY;
+        constexpr int PAIRS = NK * TN;             // of V^T fragments: 16 keys, 32 dimensions each
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int grp = 0; grp < 4; ++grp)
+        for (int i = 0; i < PAIRS; ++i) {
+          const int grp = i / (TN / 2), d = i % (TN / 2) * 2, ng = (i + 1) / (TN / 2), nd = (i + 1) % (TN / 2) * 2;
+          const f16x8 v2 = i + 1 < PAIRS ? v_frag(vt, ng, nd) : v0, v3 = i + 1 < PAIRS ? v_frag(vt, ng, nd + 1) : v1;
 #pragma unroll
-          for (int i = 0; i < TN; ++i) {
-            const f16x8 v = v_frag(vt, grp, i);
-            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, hi[grp], o[i], 0, 0, 0);
-            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, lo[grp], o[i], 0, 0, 0);
-            if (grp < 2) {
+          for (int k = 0; k < 4; ++k) {
+            __builtin_amdgcn_sched_barrier(0);
+            o[d + (k & 1)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k & 1 ? v1 : v0, operand(k < 2 ? hi : lo, grp), o[d + (k & 1)], 0, 0, 0);
+            const int slot = 4 * i + k;
+            if (NK * KS + slot < CARRY) carry(sc, NK * KS + slot);
+            if (slot < 2 * NK * TN)                // the max of the next scores under the first half
 #pragma unroll
-              for (int e = 0; e < 8 / TN; ++e) weight(sc, 16 + (grp * TN + i) * (8 / TN) + e, base);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 16 / TN; ++e) {
-                const int k = ((grp - 2) * TN + i) * (16 / TN) + e;
-                mx = fmaxf(mx, sn[k >> 4][k & 15]);
+              for (int e = 0; e < 8 / TN; ++e) {
+                const int y = slot * (8 / TN) + e;
+                mx = fmaxf(mx, sn[y >> 4][y & 15]);
               }
-            }
+            if (slot == 2 * NK * TN) other = __shfl_xor(mx, 32);
+            __builtin_amdgcn_sched_barrier(0);
           }
-        if (more) raise_max(mx, some);
+          v0 = v2;
+          v1 = v3;
+        }
+        if (more) raise_max(mx, other, some);
       }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      if (more && ~next_keys) mend_v(t + 1, next_keys);
-      s1 = s2;
-      s2 = s3;
+      if (full) wait_loads<AHEAD>(); else wait_loads<0>();
+      if (more && ~keys) mend_v(t + 1, keys);
       __syncthreads();
+      if (refill) {
+        fill_window(t + 2);
+        look_ahead(t + 1);
+      }
     };
     int t = p.t0;
     for (; t + 1 < t_end; t += 2) {
@@ -679,10 +840,9 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     for (int t = 0; t < TN; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) finite &= fabsf(o[t][r]) < INFINITY;
-    const bool bad = __any(!finite);
-    if (!there) continue;
+    const bool whole = p.t0 == 0 && p.t1 == s.units;
     const int64_t row = (int64_t)(s.first + node) * a.nq + head;
-    if (p.t0 == 0 && p.t1 == s.units) {
+    if (there && whole) {
       const float inv = m == -INFINITY ? 0.f : 1.0f / l;
       _Float16* out = a.out + row * HD + 4 * half;
 #pragma unroll
@@ -691,147 +851,95 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
         for (int r = 0; r < 4; ++r)
           *reinterpret_cast<f16x4*>(out + t * 32 + 8 * r) = f16x4{(_Float16)(o[t][4 * r] * inv), (_Float16)(o[t][4 * r + 1] * inv),
                                                                   (_Float16)(o[t][4 * r + 2] * inv), (_Float16)(o[t][4 * r + 3] * inv)};
-      if (half == 0) a.again[row] = bad;
-    } else {
+    } else if (there) {
       const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * R + w * 32 + col;
-      if (half == 0) a.ml[e0] = make_float2(bad ? NAN : m, l);
+      if (half == 0) a.ml[e0] = make_float2(m, l);
+      if (!finite) a.ml[e0].x = NAN;
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           *reinterpret_cast<f32x4*>(a.part + e0 * HD + t * 32 + 8 * r + 4 * half) = f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]};
     }
+    if (whole && __syncthreads_or(there && !finite))
+      for (int y = p.tile * R, k = 0; k < R && y / a.group < s.nodes; ++k, ++y)
+        row_again<HD, 64 * NW>(a, s, sh.b, s.first + y / a.group, p.h * a.group + y % a.group, reinterpret_cast<float*>(lds), s_again);
   }
 }
 
 // ---- joining
-// One (row, query head) alone, over the keys that it sees, 256 at a time: a
-// thread a score, then a thread a dimension of every (256 / HD)-th value.
-template <int HD>
-__device__ __forceinline__ void row_again(const AttnTree& a, const Seq& s, int b, int r, int hq, float* s_p, float* s_red) {
-  constexpr int PARTS = 256 / HD;
-  const int t = threadIdx.x, h = hq / a.group, node = r - s.first, dkv = a.nkv * HD, d = t % HD, part = t / HD;
-  const uint32_t* words = a.mask + (int64_t)r * a.mask_words;
-  const int32_t* table = a.table + (int64_t)b * a.n_table;
-  const _Float16* q = a.q + ((int64_t)r * a.nq + hq) * HD;
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  for (int j0 = 0; j0 < s.keys; j0 += 256) {
-    const int j = j0 + t, slot = j < s.keys ? table[j >> a.cshift] : -1;
-    const bool on = (unsigned)slot < (unsigned)a.n_slots && sees(a, s, j, node, words);
-    float score = -INFINITY, top = -INFINITY;
-    if (on) {
-      const _Float16* k = reinterpret_cast<const _Float16*>(a.slab + slot * a.slot_bytes) + (int64_t)(j & (a.C - 1)) * dkv + h * HD;
-      float sum = 0.f;
-      for (int e = 0; e < HD; ++e) sum = __builtin_fmaf((float)k[e], (float)q[e], sum);
-      score = sum * a.scale_log2;
-      top = fmaxf(score, kLowest);
-    }
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-    __syncthreads();                   // the keys before have been read
-    if ((t & 63) == 0) s_red[t >> 6] = top;
-    __syncthreads();
-    const float now = fmaxf(fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])), m);
-    const float alpha = now == m ? 1.f : exp2_hw(m - now);
-    m = now;
-    s_p[t] = on ? exp2_hw(score - m) : -1.f;      // -1: not seen
-    l *= alpha;
-    acc *= alpha;
-    __syncthreads();
-    for (int k = part; k < 256; k += PARTS) {
-      const float p = s_p[k];
-      if (p == -1.f) continue;
-      const int jk = j0 + k;
-      const _Float16* v = reinterpret_cast<const _Float16*>(a.slab + table[jk >> a.cshift] * a.slot_bytes) + (int64_t)a.C * dkv +
-                          (int64_t)(h * HD + d) * a.C + (jk & (a.C - 1));
-      acc = __builtin_fmaf(p, (float)*v, acc);
-      l += p;
-    }
-  }
-  __syncthreads();
-  s_p[t] = acc;
-  if (d == 0) s_red[part] = l;
-  __syncthreads();
-  if (part == 0) {
-    float sum = 0.f, den = 0.f;
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
-      sum += s_p[k * HD + d];
-      den += s_red[k];
-    }
-    a.out[((int64_t)r * a.nq + hq) * HD + d] = (_Float16)(m == -INFINITY ? 0.f : sum / den);
-  }
-}
-
-// Joins the partials of one (row, query head): those of workgroups g0 .. g1.
-// Group pg of LPP lanes takes partials pg, pg + NG, ... with their own running
-// max, four dimensions a lane, and the groups meet in LDS; a partial's max, sum
-// and values come in one trip to memory.  What had sums that are not finite is
-// taken again.
+// Joins the partials of every (row, query head) that several shares met, g0 ..
+// g1.  TPR of a workgroup's threads take one: HD / 4 lanes a partial, four
+// dimensions each, AHEAD of them in one trip to memory, and the groups of lanes meet in
+// LDS.  Rows with sums that are not finite are taken again.
 template <int HD, int R, int UNIT>
 __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
-  constexpr int LPP = HD / 4, NG = 256 / LPP, AHEAD = 4;     // lanes per partial, partials at once
-  __shared__ float s_m[NG], s_l[NG];
-  __shared__ f32x4 s_acc[NG][LPP];
-  const int r = blockIdx.x / a.nq, hq = blockIdx.x % a.nq, h = hq / a.group;
-  const int b = a.row_seq[r];
-  if (b < 0) return;
-  const Seq s = seq_of<R, UNIT>(a, b);
-  const int n_units = a.base[a.n_seq] * a.nkv, x = (r - s.first) * a.group + hq - h * a.group, tile = x / R, c = x - tile * R;
-  const int t = threadIdx.x, dl = t % LPP, pg = t / LPP;
-  const int nw = shares(a, n_units), f0 = a.base[b] * a.nkv + (h * s.tiles + tile) * s.units;
-  const int g0 = share_of(f0, nw, n_units), n = share_of(f0 + s.units - 1, nw, n_units) - g0 + 1;
+  constexpr int TPR = R <= 32 ? 256 : 64, ROWS = 256 / TPR, LPP = HD / 4, NG = TPR / LPP, AHEAD = R <= 32 ? 4 : 8;
+  __shared__ float s_m[256 / LPP], s_l[256 / LPP];
+  __shared__ f32x4 s_acc[256 / LPP][LPP];
+  const int t = threadIdx.x, dl = t % LPP, group = t / LPP, pg = group % NG;
+  const int64_t first = (int64_t)blockIdx.x * ROWS, at = first + t / TPR, rows = (int64_t)a.m * a.nq;
+  const int total = a.base[a.n_seq] * a.nkv, nw = shares(a, total);
   bool again = false;
-  if (n == 1) {                                    // written whole
-    if (!a.again[blockIdx.x]) return;
-    again = true;
-  }
-  auto part = [&](int i) { return (int64_t)(2 * (g0 + i) + (i == 0)) * R + c; };
+  const int b = at < rows ? a.row_seq[at / a.nq] : -1;
+  int n = 0;
   float m = -INFINITY, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (n > 1)
-    for (int i0 = pg; i0 < n; i0 += AHEAD * NG) {
-      float2 ml[AHEAD];
-      f32x4 v[AHEAD];
+  if (b >= 0) {
+    const Seq s = seq_of<R, UNIT>(a, b);
+    const int r = (int)(at / a.nq), hq = (int)(at - (int64_t)r * a.nq), h = hq / a.group;
+    const int x = (r - s.first) * a.group + hq - h * a.group, tile = x / R, c = x - tile * R;
+    const int f0 = a.base[b] * a.nkv + (h * s.tiles + tile) * s.units;
+    const int g0 = share_of(f0, nw, total);
+    n = share_of(f0 + s.units - 1, nw, total) - g0 + 1;
+    auto part = [&](int i) { return (int64_t)(2 * (g0 + i) + (i == 0)) * R + c; };
+    if (n > 1)                         // else it is written whole
+      for (int i0 = pg; i0 < n; i0 += AHEAD * NG) {
+        float2 ml[AHEAD];
+        f32x4 v[AHEAD];
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const int64_t at = part(min(i0 + k * NG, n - 1));
-        ml[k] = a.ml[at];
-        v[k] = *reinterpret_cast<const f32x4*>(a.part + at * HD + dl * 4);
-      }
+        for (int k = 0; k < AHEAD; ++k) {
+          const int64_t y = part(min(i0 + k * NG, n - 1));
+          ml[k] = a.ml[y];
+          v[k] = *reinterpret_cast<const f32x4*>(a.part + y * HD + dl * 4);
+        }
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        if (i0 + k * NG >= n || ml[k].x == -INFINITY) continue;      // no key seen
-        again |= ml[k].x != ml[k].x;
-        const float top = fmaxf(m, ml[k].x), old = m == top ? 1.f : exp2_hw(m - top), wt = exp2_hw(ml[k].x - top);
-        m = top;
-        l = l * old + wt * ml[k].y;
-        acc = acc * old + v[k] * wt;
+        for (int k = 0; k < AHEAD; ++k) {
+          if (i0 + k * NG >= n || ml[k].x == -INFINITY) continue;      // no key seen
+          again |= ml[k].x != ml[k].x;
+          const float top = fmaxf(m, ml[k].x), old = m == top ? 1.f : exp2_hw(m - top), wt = exp2_hw(ml[k].x - top);
+          m = top;
+          l = l * old + wt * ml[k].y;
+          acc = acc * old + v[k] * wt;
+        }
       }
-    }
+  }
+  if (ROWS == 1 && n <= 1) return;
+  if (dl == 0) {
+    s_m[group] = m;
+    s_l[group] = l;
+  }
+  s_acc[group][dl] = acc;
   if (__syncthreads_or(again)) {
-    row_again<HD>(a, s, b, r, hq, reinterpret_cast<float*>(s_acc), s_m);
+    for (int k = 0; k < ROWS && first + k < rows; ++k) {
+      const int r = (int)((first + k) / a.nq), hq = (int)(first + k - (int64_t)r * a.nq), mine = a.row_seq[r];
+      if (mine >= 0) row_again<HD, 256>(a, seq_of<R, UNIT>(a, mine), mine, r, hq, reinterpret_cast<float*>(s_acc), s_m);
+    }
     return;
   }
-  if (dl == 0) {
-    s_m[pg] = m;
-    s_l[pg] = l;
-  }
-  s_acc[pg][dl] = acc;
-  __syncthreads();
-  if (pg == 0) {
+  if (pg == 0 && n > 1) {
     float top = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[i]);
+    for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[group + i]);
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
-      const float wt = s_m[i] == -INFINITY ? 0.f : exp2_hw(s_m[i] - top);
-      den += wt * s_l[i];
-      acc += s_acc[i][dl] * wt;
+      const float wt = s_m[group + i] == -INFINITY ? 0.f : exp2_hw(s_m[group + i] - top);
+      den += wt * s_l[group + i];
+      acc += s_acc[group + i][dl] * wt;
     }
     const float inv = top == -INFINITY ? 0.f : 1.0f / den;
-    *(reinterpret_cast<f16x4*>(a.out + (int64_t)blockIdx.x * HD) + dl) =
+    *(reinterpret_cast<f16x4*>(a.out + at * HD) + dl) =
         f16x4{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv), (_Float16)(acc[3] * inv)};
   }
 }
@@ -841,11 +949,18 @@ int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 // Columns of a tile for `cols` columns of an average sequence.
 int tile_cols(int64_t cols) { return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256; }
 
-int most_shares(int R) { return R <= 32 ? kFewWgs : 256 * kWideWaves * 32 / R > 512 ? 512 : 256 * kWideWaves * 32 / R; }
+// Shares: a workgroup for each that a CU holds.
+int most_shares(int R) { return R == 256 ? 256 : 512; }
+
+int least_units(int R) { return R <= 32 ? 1 : 8; }
+
+template <int HD, int R>
+struct WideShape {       // 32-key blocks of a tile, tiles of a ring
+  static constexpr int NK = 2, ST = R == 256 ? 3 : 2;
+};
 
 template <int HD, int R>
 void launch(const AttnTree& a, hipStream_t s) {
-  constexpr int UNIT = R <= 32 ? kFewUnit : kTile;
   const dim3 grid(a.wgs);
   if constexpr (R <= 32) {
     if (a.C < kBlock)
@@ -853,12 +968,14 @@ void launch(const AttnTree& a, hipStream_t s) {
     else
       hipLaunchKernelGGL((tree_few_kernel<HD, R / kCols, false>), grid, dim3(64 * kFewWaves), 0, s, a);
   } else {
-    if (a.C < kTile)
-      hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, true>), grid, dim3(2 * R), 0, s, a);
+    constexpr int NK = WideShape<HD, R>::NK, ST = WideShape<HD, R>::ST;
+    if (a.C < 32 * NK)
+      hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, NK, ST, true>), grid, dim3(2 * R), 0, s, a);
     else
-      hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, false>), grid, dim3(2 * R), 0, s, a);
+      hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, NK, ST, false>), grid, dim3(2 * R), 0, s, a);
   }
-  hipLaunchKernelGGL((tree_join_kernel<HD, R, UNIT>), dim3(a.m * a.nq), dim3(256), 0, s, a);
+  constexpr int UNIT = R <= 32 ? kFewUnit : 32 * WideShape<HD, R>::NK;
+  hipLaunchKernelGGL((tree_join_kernel<HD, R, UNIT>), dim3((unsigned)(((int64_t)a.m * a.nq * (R <= 32 ? 4 : 1) + 3) / 4)), dim3(256), 0, s, a);
 }
 
 template <int HD>
@@ -873,7 +990,7 @@ void launch(const AttnTree& a, int R, hipStream_t s) {
 }  // namespace
 
 int64_t attention_tree_units(int m, int n_seq, int n_table, int chunk_tokens, int nq, int nkv) {
-  const int64_t units = ((int64_t)n_table * chunk_tokens + kTile - 1) / kTile;
+  const int64_t units = ((int64_t)n_table * chunk_tokens + 31) / 32;
   const int64_t tiles = ((int64_t)m * (nq / nkv) + 15) / 16 + n_seq;
   return tiles * nkv * units;
 }
@@ -882,7 +999,7 @@ int64_t attention_tree_units(int m, int n_seq, int n_table, int chunk_tokens, in
 int64_t attention_tree_ws_bytes(int m, int n_seq, int nq, int nkv, int hd) {
   int64_t cols = 0;
   for (int R = 16; R <= tile_cols((int64_t)m * (nq / nkv)); R *= 2) cols = std::max<int64_t>(cols, (int64_t)2 * most_shares(R) * R);
-  return up256(((int64_t)n_seq + 1) * 4) + up256((int64_t)m * 4) + up256((int64_t)m * nq) + up256(cols * 8) + cols * hd * 4;
+  return up256(((int64_t)n_seq + 1) * 4) + up256((int64_t)m * 4) + up256(cols * 8) + cols * hd * 4;
 }
 
 void launch_attention_tree(AttnTree a, int hd, void* ws, hipStream_t s) {
@@ -892,11 +1009,10 @@ void launch_attention_tree(AttnTree a, int hd, void* ws, hipStream_t s) {
   p += up256(((int64_t)a.n_seq + 1) * 4);
   a.row_seq = reinterpret_cast<int32_t*>(p);
   p += up256((int64_t)a.m * 4);
-  a.again = p;
-  p += up256((int64_t)a.m * a.nq);
   a.ml = reinterpret_cast<float2*>(p);
   p += up256((int64_t)2 * most_shares(R) * R * 8);
   a.part = reinterpret_cast<float*>(p);
+  a.least = least_units(R);
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)hd);
   const int64_t most = attention_tree_units(a.m, a.n_seq, a.n_table, a.C, a.nq, a.nkv);
   a.wgs = most < most_shares(R) ? (int)most : most_shares(R);
