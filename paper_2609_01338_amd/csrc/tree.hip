@@ -9,11 +9,14 @@
 // whatever the depth, and the depth is their bits' number.
 //
 // Accept.  One wave walks from the root, 64 nodes in a look for the child that
-// holds the parent's choice.  Then the keys and values move: a thread owns 16
-// bytes of the key rows or one dimension of V^T for all of the branch, eight
-// places at a time, read before they are written.  Since path[i] >= i ascends,
-// what it has written (places up to i) is never what it still has to read (path[j]
-// > i for j > i), so nothing has to wait for another thread.
+// holds the parent's choice.  Then the keys and values move.  Of the keys a thread
+// owns 16 bytes of the rows for all of the branch, eight places at a time, read
+// before they are written.  Of V^T a value moves within a row of its own, a line of
+// memory for two bytes, so what counts is lines: four lanes own the 64 bytes
+// of a dimension that 32 places lie in, and write what changes of them as 16 bytes,
+// several layers at a time.  Since path[i] >= i ascends, what has been written (places
+// up to i) is never what is still to be read (path[j] > i for j > i), so nothing waits
+// for another wave.
 #include "mz_kernels.h"
 
 namespace mzk {
@@ -115,27 +118,47 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(TreePlan a) {
 }
 
 constexpr int kMoves = 8;        // places a thread reads before it writes
+constexpr int kLayers = 2;       // layers of V^T likewise
 
 __global__ __launch_bounds__(256) void tree_accept_kernel(TreeAccept a) {
   __shared__ int s_parent[kTreeNodes], s_token[kTreeNodes], s_choice[kTreeNodes], s_path[kTreeNodes];
-  __shared__ int s_n[2];
-  const int b = blockIdx.x % a.n_seq, slice = blockIdx.x / a.n_seq;
+  // (a sequence's slices follow each other, so that every XCD has some of all sequences)
+  const int slices = gridDim.x / a.n_seq, b = blockIdx.x / slices, slice = blockIdx.x - b * slices;
   int first;
   const int rows = tree_rows(a.row_off, b, a.m, first), n = min(rows, kTreeNodes), len = tree_len(a.lens, b);
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int p = a.parent ? a.parent[first + i] : i - 1;
-    s_parent[i] = p < i ? p : -1;
-    s_token[i] = a.token[first + i];
-    s_choice[i] = a.choice[first + i];
-  }
-  __syncthreads();
-  if (threadIdx.x < 64) {
-    const int lane = threadIdx.x;
-    int at = n > 0 ? 0 : -1, taken = 0, want = -1, moves = n;
+  const int lane = threadIdx.x & 63;
+  int at = n > 0 ? 0 : -1, taken = 0, want = -1, begin = n;      // begin: the first node that moves
+  auto take = [&] {
+    if (threadIdx.x == 0) s_path[taken] = at;
+    if (at != taken) begin = min(begin, taken);
+    ++taken;
+  };
+  if (n <= 64) {
+    // every wave walks by itself, a lane a node
+    const int i = first + min(lane, max(n - 1, 0));
+    int parent = -1, token = -1, choice = -1;
+    if (n > 0) {
+      parent = a.parent ? a.parent[i] : lane - 1;
+      token = a.token[i];
+      choice = a.choice[i];
+    }
+    if (lane >= n || parent >= lane) parent = -1;
     while (at >= 0) {
-      if (lane == 0) s_path[taken] = at;
-      if (at != taken) moves = min(moves, taken);
-      ++taken;
+      take();
+      want = __builtin_amdgcn_readlane(choice, at);
+      const uint64_t fits = want >= 0 ? __ballot(parent == at && token == want) : 0;
+      at = fits ? __builtin_ctzll(fits) : -1;
+    }
+  } else {
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const int p = a.parent ? a.parent[first + i] : i - 1;
+      s_parent[i] = p < i ? p : -1;
+      s_token[i] = a.token[first + i];
+      s_choice[i] = a.choice[first + i];
+    }
+    __syncthreads();
+    while (at >= 0) {
+      take();
       want = s_choice[at];
       int child = -1;
       if (want >= 0)
@@ -146,54 +169,33 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(TreeAccept a) {
         }
       at = child;
     }
-    if (lane == 0) {
-      s_n[0] = taken;
-      s_n[1] = moves;            // the first node that moves
-      if (slice == 0 && blockIdx.y == 0) {
-        a.accepted[b] = taken;
-        a.next[b] = want;
-        a.len_out[b] = len + taken;
-      }
-    }
+  }
+  if (slice == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    a.accepted[b] = taken;
+    a.next[b] = want;
+    a.len_out[b] = len + taken;
   }
   __syncthreads();
-  const int taken = s_n[0], begin = s_n[1];
   if (slice == 0 && blockIdx.y == 0)
     for (int i = threadIdx.x; i < rows; i += 256) a.path[first + i] = i < taken ? s_path[i] : -1;
   if (a.n_layers == 0 || begin >= taken) return;
-  // slots of the moves: from in s_parent, to in s_token, -1 where there is none
+  // slots that the moves come from in s_parent, -1 where there is none; that they go to in s_token
   const int32_t* table = a.table + (int64_t)b * a.n_table;
+  auto slot_at = [&](int pos) {
+    const int c = pos >> a.cshift, x = c < a.n_table ? table[c] : -1;
+    return (unsigned)x < (unsigned)a.n_slots ? x : -1;
+  };
   for (int i = begin + threadIdx.x; i < taken; i += 256) {
-    const int from = (len + s_path[i]) >> a.cshift, to = (len + i) >> a.cshift;
-    const int x = from < a.n_table ? table[from] : -1, y = to < a.n_table ? table[to] : -1;
-    const bool ok = (unsigned)x < (unsigned)a.n_slots && (unsigned)y < (unsigned)a.n_slots;
-    s_parent[i] = ok ? x : -1;
-    s_token[i] = y;
+    s_token[i] = slot_at(len + i);
+    s_parent[i] = s_token[i] >= 0 ? slot_at(len + s_path[i]) : -1;
   }
   __syncthreads();
-  const int item = slice * 256 + threadIdx.x, mask = a.C - 1;
-  if (item >= a.dkv + a.dkv / 8) return;
-  for (int layer = blockIdx.y; layer < a.n_layers; layer += gridDim.y) {
-    uint8_t* slab = a.slab + layer * a.layer_bytes;
-    if (item < a.dkv) {
-      uint8_t* v = slab + ((int64_t)a.dkv + item) * a.C * 2;
-      for (int i0 = begin; i0 < taken; i0 += kMoves) {
-        _Float16 x[kMoves];
-#pragma unroll
-        for (int e = 0; e < kMoves; ++e) {
-          const int i = min(i0 + e, taken - 1), from = s_parent[i];
-          if (from >= 0) x[e] = *reinterpret_cast<const _Float16*>(v + from * a.slot_bytes + ((len + s_path[i]) & mask) * 2);
-        }
-#pragma unroll
-        for (int e = 0; e < kMoves; ++e) {
-          const int i = i0 + e;
-          if (i < taken && s_parent[i] >= 0)
-            *reinterpret_cast<_Float16*>(v + s_token[i] * a.slot_bytes + ((len + i) & mask) * 2) = x[e];
-        }
-      }
-    } else {
-      uint8_t* k = slab + (item - a.dkv) * 16;
-      const int row = a.dkv * 2;
+  const int mask = a.C - 1, v_blocks = (a.dkv + 63) / 64, step = gridDim.y;
+  if (slice >= v_blocks) {
+    const int item = (slice - v_blocks) * 256 + threadIdx.x, row = a.dkv * 2;
+    if (item >= a.dkv / 8) return;
+    for (int layer = blockIdx.y; layer < a.n_layers; layer += step) {
+      uint8_t* k = a.slab + layer * a.layer_bytes + item * 16;
       for (int i0 = begin; i0 < taken; i0 += kMoves) {
         f16x8 x[kMoves];
 #pragma unroll
@@ -209,10 +211,46 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(TreeAccept a) {
         }
       }
     }
+    return;
+  }
+  // V^T: lane l of 4 has places pos .. pos + 7 of a dimension, in turns of 32
+  const int d = slice * 64 + threadIdx.x / 4;
+  if (d >= a.dkv) return;
+  const int64_t v_row = (int64_t)(a.dkv + d) * a.C * 2;
+  for (int at = (len + begin) & ~31; at < len + taken; at += 32) {
+    const int pos = at + (threadIdx.x & 3) * 8;
+    const int lo = max(pos, len + begin), hi = min(pos + 8, len + taken);      // places that change
+    const int to = lo < hi ? s_token[lo - len] : -1;
+    for (int l0 = blockIdx.y; l0 < a.n_layers; l0 += kLayers * step) {
+      f16x8 x[kLayers];
+#pragma unroll
+      for (int y = 0; y < kLayers; ++y) {
+        const int layer = l0 + y * step;
+        if (to >= 0 && layer < a.n_layers)
+          x[y] = *reinterpret_cast<const f16x8*>(a.slab + layer * a.layer_bytes + to * a.slot_bytes + v_row + (pos & mask) * 2);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = pos + e - len;
+        if (to < 0 || pos + e < lo || pos + e >= hi || s_parent[i] < 0) continue;
+        const int64_t from = s_parent[i] * a.slot_bytes + v_row + ((len + s_path[i]) & mask) * 2;
+#pragma unroll
+        for (int y = 0; y < kLayers; ++y) {
+          const int layer = l0 + y * step;
+          if (layer < a.n_layers) x[y][e] = *reinterpret_cast<const _Float16*>(a.slab + layer * a.layer_bytes + from);
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kLayers; ++y) {
+        const int layer = l0 + y * step;
+        if (to >= 0 && layer < a.n_layers)
+          *reinterpret_cast<f16x8*>(a.slab + layer * a.layer_bytes + to * a.slot_bytes + v_row + (pos & mask) * 2) = x[y];
+      }
+    }
   }
 }
 
-int accept_slices(int n_layers, int dkv) { return n_layers ? (dkv + dkv / 8 + 255) / 256 : 1; }
+int accept_slices(int n_layers, int dkv) { return n_layers ? (dkv + 63) / 64 + (dkv / 8 + 255) / 256 : 1; }
 
 }  // namespace
 
@@ -226,7 +264,7 @@ bool tree_accept_fits(int n_seq, int n_layers, int dkv) {
 
 void launch_tree_accept(const TreeAccept& a, hipStream_t s) {
   const int64_t blocks = (int64_t)a.n_seq * accept_slices(a.n_layers, a.dkv);
-  const int64_t most = blocks < 2048 ? 2048 / blocks : 1;
+  const int64_t most = blocks < 16384 ? 16384 / blocks : 1;
   const int layers = a.n_layers < 1 ? 1 : a.n_layers < most ? a.n_layers : (int)most;
   hipLaunchKernelGGL(tree_accept_kernel, dim3((unsigned)blocks, layers), dim3(256), 0, s, a);
 }
