@@ -119,8 +119,8 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_red, int* 
   const int n_units = total * a.nkv, nw = shares(a, n_units), g = blockIdx.x;
   if (g == 0 && threadIdx.x == 0) a.base[a.n_seq] = total;
   if (g >= nw) return false;
-  sh.u = (int)((uint64_t)g * n_units / nw);
-  sh.end = (int)(((uint64_t)g + 1) * n_units / nw);
+  sh.u = __builtin_amdgcn_readfirstlane((int)((uint64_t)g * n_units / nw));
+  sh.end = __builtin_amdgcn_readfirstlane((int)(((uint64_t)g + 1) * n_units / nw));
   auto here = [&](int b) {
     if (sh.u >= u_before * a.nkv && sh.u < (u_before + u_mine) * a.nkv) {
       s_at[0] = b;
@@ -553,18 +553,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
   static_assert(STRETCHES % NW == 0 && V_STEP % 16 == 0 && K_STEP % 8 == 0 && (KC == 16 || K_STEP % 16 == 0), "columns of the stretches");
   typedef __attribute__((address_space(3))) void lds_void;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds);
-  // 64 lanes' 16 bytes from base + at into LDS.  (The wait states lie between the
-  // writes of the base, by a vector instruction, and of M0, and the load that reads them.)
-  auto fetch = [&](const uint8_t* base, unsigned at, int to) {
-    const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds0 + to * 2);
-    if constexpr (SMALL) {
-      const uint8_t* from = base + at;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(m0), "v"(from) : "memory");
-    } else {
-      const uint64_t b = (uint64_t)(uintptr_t)base;
-      const uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(m0), "v"(at), "s"(u) : "memory");
-    }
+  // 64 lanes' 16 bytes from `from`, or from a base in scalar registers + at, into
+  // LDS.  (Wait states lie between the write of M0, and a vector instruction's of the
+  // base, and the load that reads them.)
+  auto fetch = [&](const uint8_t* from, int to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds0 + to * 2), "v"(from) : "memory");
+  };
+  auto fetch_from = [&](uint64_t base, unsigned at, int to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds0 + to * 2), "v"(at), "s"(base) : "memory");
   };
 
   Seq s = seq_of<R, UNIT>(a, sh.b);
@@ -589,34 +585,59 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
     // The slot of key j of the window's tiles (keys past the last one: its slot).
     auto slot_at = [&](int j) { return window[(min(j, last) >> a.cshift) - c0]; };
     auto clean = [&](int slot) { return (unsigned)slot < (unsigned)a.n_slots ? slot : 0; };
-    // The slots of what the lane loads of a tile, read a step before they are used.
+    // Slots are read a step before they are used: with SMALL those of what the lane
+    // loads, else the tile's, into scalar registers, q[i] that of tile t + 1 + i at step t.
     constexpr int KSLOTS = SMALL ? PER : 1;
-    int k_slot[KSLOTS], v_slot;
-    auto slots_of_k = [&](int t) {
-#pragma unroll
-      for (int i = 0; i < KSLOTS; ++i) k_slot[i] = slot_at(t * KT + (SMALL ? k_row + i * K_STEP : 0));
-    };
-    auto slots_of_v = [&](int t) { v_slot = slot_at(t * KT + (SMALL ? v_key : 0)); };
-    auto load_k = [&](int t) {
+    int k_slot[KSLOTS], v_slot = 0, q_slot[ST];
+    const unsigned k_lane = (unsigned)k_row * (unsigned)dkv * 2u + p.h * HD * 2u + k_of;
+    const unsigned v_lane = ((unsigned)(dkv + p.h * HD + v_row) * (unsigned)a.C + v_key) * 2u;
+    const uint64_t slab = (uint64_t)(uintptr_t)a.slab;
+    auto scalar_slot = [&](int t) { return __builtin_amdgcn_readfirstlane(slot_at(min(t, t_end - 1) * KT)); };
+    auto load_k = [&](int t, int slot) {
       const int j0 = (t * KT) & (a.C - 1), to = t % ST * TILE + w * 512;
+      const uint64_t base = slab + (uint64_t)clean(slot) * (uint64_t)a.slot_bytes + (unsigned)j0 * (unsigned)dkv * 2u;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int row = k_row + i * K_STEP, j = SMALL ? (j0 + row) & (a.C - 1) : j0 + row;
-        const unsigned of = K_STEP % 16 == 0 ? k_of : k_of ^ (i & 1) * 128u;
-        fetch(a.slab + (int64_t)clean(k_slot[i % KSLOTS]) * a.slot_bytes, (unsigned)j * (unsigned)dkv * 2u + p.h * HD * 2u + of, to + i * NW * 512);
+        if constexpr (SMALL) {
+          const int row = k_row + i * K_STEP;
+          const unsigned of = K_STEP % 16 == 0 ? k_of : k_of ^ (i & 1) * 128u;
+          fetch(a.slab + (int64_t)clean(k_slot[i]) * a.slot_bytes + ((unsigned)((j0 + row) & (a.C - 1)) * (unsigned)dkv * 2u + p.h * HD * 2u + of),
+                to + i * NW * 512);
+        } else {
+          fetch_from(base + (unsigned)(i * K_STEP) * (unsigned)dkv * 2u, K_STEP % 16 == 0 || i % 2 == 0 ? k_lane : (k_lane - k_of) + (k_of ^ 128u),
+                     to + i * NW * 512);
+        }
       }
     };
-    auto load_v = [&](int t) {
-      const int j0 = (t * KT) & (a.C - 1), j = SMALL ? (j0 + v_key) & (a.C - 1) : j0 + v_key, to = (ST + t % ST) * TILE + w * 512;
+    auto load_v = [&](int t, int slot) {
+      const int j0 = (t * KT) & (a.C - 1), to = (ST + t % ST) * TILE + w * 512;
+      const uint64_t base = slab + (uint64_t)clean(slot) * (uint64_t)a.slot_bytes + (unsigned)j0 * 2u;
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        fetch(a.slab + (int64_t)clean(v_slot) * a.slot_bytes, ((unsigned)(dkv + p.h * HD + v_row + i * V_STEP) * (unsigned)a.C + (unsigned)j) * 2u,
-              to + i * NW * 512);
+      for (int i = 0; i < PER; ++i) {
+        if constexpr (SMALL)
+          fetch(a.slab + (int64_t)clean(v_slot) * a.slot_bytes +
+                    ((unsigned)(dkv + p.h * HD + v_row + i * V_STEP) * (unsigned)a.C + (unsigned)((j0 + v_key) & (a.C - 1))) * 2u,
+                to + i * NW * 512);
+        else
+          fetch_from(base + (unsigned)(i * V_STEP) * (unsigned)a.C * 2u, v_lane, to + i * NW * 512);
+      }
     };
-    // Keys of tile t that are there, and zeros for the values of the others.
-    auto there64 = [&](int t) {
-      const int j = t * KT + lane;
-      return __ballot(lane >= KT || ((unsigned)slot_at(min(j, (w0 + kWindow) * KT - 1)) < (unsigned)a.n_slots && j < s.keys));
+    auto slots_of_k = [&](int t) {
+      if constexpr (SMALL)
+#pragma unroll
+        for (int i = 0; i < KSLOTS; ++i) k_slot[i] = slot_at(t * KT + k_row + i * K_STEP);
+    };
+    auto slots_of_v = [&](int t) {
+      if constexpr (SMALL) v_slot = slot_at(t * KT + v_key);
+    };
+    // Keys of tile t that are there (the last ones of 64 where a tile has fewer), and zeros for the values of the others.
+    auto there64 = [&](int t, int slot) -> uint64_t {
+      if constexpr (SMALL) {
+        const int j = t * KT + lane;
+        return __ballot(lane >= KT || ((unsigned)slot_at(min(j, (w0 + kWindow) * KT - 1)) < (unsigned)a.n_slots && j < s.keys));
+      } else {
+        return ((unsigned)slot < (unsigned)a.n_slots ? ones64(s.keys - t * KT) : 0) | (KT == 64 ? 0 : ~0ull << (KT & 63));
+      }
     };
     auto mend_v = [&](int t, uint64_t keys) {
       const unsigned on = (unsigned)(keys >> v_key) & 0xFF;
@@ -633,14 +654,17 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
 
     __syncthreads();                   // the piece before has been read
     fill_window(p.t0);
+    const int first_slot = SMALL ? 0 : scalar_slot(p.t0);
+#pragma unroll
+    for (int i = 0; i < ST; ++i) q_slot[i] = SMALL ? 0 : scalar_slot(p.t0 + 1 + i);
 #pragma unroll
     for (int i = 0; i < ST; ++i) {
       if (p.t0 + i >= t_end) break;
       slots_of_k(p.t0 + i);
-      load_k(p.t0 + i);
+      load_k(p.t0 + i, i ? q_slot[i - 1] : first_slot);
       if (i + 1 == ST) break;
       slots_of_v(p.t0 + i);
-      load_v(p.t0 + i);
+      load_v(p.t0 + i, i ? q_slot[i - 1] : first_slot);
     }
     f16x8 q[KS];
 #pragma unroll
@@ -734,7 +758,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
     f32x16 sa[NK], sb[NK];
     {
       if (p.t0 + ST - 1 < t_end) wait_loads<AHEAD>(); else wait_loads<0>();
-      const uint64_t keys = there64(p.t0);
+      const uint64_t keys = there64(p.t0, first_slot);
       if (~keys) mend_v(p.t0, keys);
       __syncthreads();
       if (active) {
@@ -753,12 +777,17 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
       __syncthreads();                 // K of the first tile has been read
     }
     uint64_t next_keys = 0;
+    int new_slot = 0;
     auto look_ahead = [&](int t) {     // what step t needs of the table
-      if (t + ST - 1 < t_end) slots_of_v(t + ST - 1);
-      if (t + ST < t_end) slots_of_k(t + ST);
-      if (t + 1 < t_end) next_keys = there64(t + 1);
+      if constexpr (SMALL) {
+        if (t + ST - 1 < t_end) slots_of_v(t + ST - 1);
+        if (t + ST < t_end) slots_of_k(t + ST);
+        if (t + 1 < t_end) next_keys = there64(t + 1, 0);
+      } else {
+        new_slot = slot_at(min(t + ST, t_end - 1) * KT);
+      }
     };
-    look_ahead(p.t0);
+    if constexpr (SMALL) look_ahead(p.t0);
     // Holds: K of tile t + 1 and V^T of tile t in LDS, the scores of tile t in
     // sc.  Products and what is done under each are kept in this order by
     // fences; fragments are read three products (K) and a pair of them (V^T) ahead.
@@ -767,9 +796,9 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
       const _Float16* kt = lds + (t + 1) % ST * TILE;
       const _Float16* vt = lds + (ST + t % ST) * TILE;
       f16x8 k0 = k_frag(kt, 0), k1 = k_frag(kt, 1), k2 = k_frag(kt, 2);
-      if (t + ST - 1 < t_end) load_v(t + ST - 1);
-      if (full) load_k(t + ST);
-      const uint64_t keys = next_keys;
+      if (t + ST - 1 < t_end) load_v(t + ST - 1, q_slot[ST - 2]);
+      if (full) load_k(t + ST, q_slot[ST - 1]);
+      const uint64_t keys = SMALL ? next_keys : there64(t + 1, q_slot[0]);
       const bool refill = full && t + 1 + ST >= w0 + kWindow;
       if (!refill) look_ahead(t + 1);
       if (active) {
@@ -825,6 +854,11 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
       if (refill) {
         fill_window(t + 2);
         look_ahead(t + 1);
+      }
+      if constexpr (!SMALL) {
+#pragma unroll
+        for (int i = 0; i + 1 < ST; ++i) q_slot[i] = q_slot[i + 1];
+        q_slot[ST - 1] = __builtin_amdgcn_readfirstlane(new_slot);
       }
     };
     int t = p.t0;
