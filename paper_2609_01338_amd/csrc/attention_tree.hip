@@ -31,6 +31,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr int kCus = 256, kShares = 512;      // most shares: two workgroups a CU
 constexpr float kLowest = -3.402823466e38f;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -53,8 +54,11 @@ __device__ __forceinline__ Seq seq_of(const AttnTree& a, int b) {
   return s;
 }
 
-// Shares of `total` units: as many as there are workgroups, but of a.least units at least.
-__device__ __forceinline__ int shares(const AttnTree& a, int total) { return max(1, min(a.wgs, total / a.least)); }
+// Shares of `total` units: as many as there are workgroups, but of a.least units
+// at least, or where those are too few for the CUs, of a.fewest.
+__device__ __forceinline__ int shares(const AttnTree& a, int total) {
+  return max(1, min(a.wgs, max(total / a.least, min(kCus, total / a.fewest))));
+}
 
 // The workgroup whose share [g total / nw, (g + 1) total / nw) holds unit u.
 __device__ __forceinline__ int share_of(int u, int nw, int total) {
@@ -84,23 +88,19 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& sum) {
 }
 
 // A workgroup's share [u, end) of the units, and the sequence that it begins
-// in, whose units begin at `first`.  The second kernel's tables on the way: the
-// units a KV head before every sequence, and the sequence of every row.
+// in, whose units begin at `first`.  On the way, for the second kernel, of every row
+// its sequence's first unit, units (0: none has the row), tiles and first row: each
+// workgroup writes those of some sequences.  s: NT + NW + 2 ints in LDS.
 struct Share {
   int u, end, b, first;
 };
 template <int R, int UNIT, int NW>
-__device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_red, int* s_at, Share& sh) {
+__device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_all, Share& sh) {
   constexpr int NT = 64 * NW;
-  for (int b = blockIdx.x; b <= a.n_seq; b += gridDim.x) {
-    if (b < a.n_seq) {
-      const Seq s = seq_of<R, UNIT>(a, b);
-      const int end = min(max(a.row_off[b + 1], s.first), a.m);
-      for (int r = s.first + threadIdx.x; r < end; r += NT) a.row_seq[r] = r - s.first < s.nodes ? b : -1;
-    } else {
-      const int before = min(max(a.row_off[0], 0), a.m), behind = min(max(a.row_off[a.n_seq], before), a.m);
-      for (int i = threadIdx.x; i < before + a.m - behind; i += NT) a.row_seq[i < before ? i : behind + i - before] = -1;
-    }
+  int *s_base = s_all, *s_red = s_all + NT, *s_at = s_red + NW;
+  if (blockIdx.x == gridDim.x - 1) {
+    const int before = min(max(a.row_off[0], 0), a.m), behind = min(max(a.row_off[a.n_seq], before), a.m);
+    for (int i = threadIdx.x; i < before + a.m - behind; i += NT) a.rows[i < before ? i : behind + i - before] = make_int4(0, 0, 0, 0);
   }
   int total = 0, u_mine = 0, u_before = 0;
   auto units = [&](int b) {
@@ -109,15 +109,22 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_red, int* 
     return s.tiles * s.units;
   };
   for (int b0 = 0; b0 < a.n_seq; b0 += NT) {
-    const int b = b0 + threadIdx.x;
-    u_mine = units(b);
+    u_mine = units(b0 + threadIdx.x);
     int sum;
     u_before = total + block_scan<NW>(u_mine, s_red, sum) - u_mine;
     total += sum;
-    if (blockIdx.x == 0 && b < a.n_seq) a.base[b] = u_before;
+    s_base[threadIdx.x] = u_before;
+    __syncthreads();
+    const int grid = gridDim.x, skip = (int)((blockIdx.x + (unsigned)grid - (unsigned)(b0 % grid)) % grid);
+    for (int b = b0 + skip; b < min(b0 + NT, a.n_seq); b += grid) {
+      const Seq s = seq_of<R, UNIT>(a, b);
+      const int end = min(max(a.row_off[b + 1], s.first), a.m);
+      for (int r = s.first + threadIdx.x; r < end; r += NT)
+        a.rows[r] = make_int4(s_base[b - b0] * a.nkv, r - s.first < s.nodes ? s.units : 0, s.tiles, s.first);
+    }
   }
   const int n_units = total * a.nkv, nw = shares(a, n_units), g = blockIdx.x;
-  if (g == 0 && threadIdx.x == 0) a.base[a.n_seq] = total;
+  if (g == 0 && threadIdx.x == 0) *a.total = n_units;
   if (g >= nw) return false;
   sh.u = __builtin_amdgcn_readfirstlane((int)((uint64_t)g * n_units / nw));
   sh.end = __builtin_amdgcn_readfirstlane((int)(((uint64_t)g + 1) * n_units / nw));
@@ -301,11 +308,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
   constexpr int DB = HD / 16;          // 16-dimension blocks of the output
   __shared__ float s_o[kFewWaves][DB][4][64];
   __shared__ float s_ml[kFewWaves][2][R], s_again[kFewWaves];
-  __shared__ int s_red[kFewWaves], s_at[2];
+  __shared__ int s_all[64 * kFewWaves + kFewWaves + 2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, lg = lane >> 4, dkv = a.nkv * HD, g = blockIdx.x;
   Share sh;
-  if (!share_begin<R, UNIT, kFewWaves>(a, s_red, s_at, sh)) return;
+  if (!share_begin<R, UNIT, kFewWaves>(a, s_all, sh)) return;
   Seq s = seq_of<R, UNIT>(a, sh.b);
   while (sh.u < sh.end) {
     const Piece p = next_piece<R, UNIT>(a, sh, s);
@@ -475,7 +482,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
         for (int e = 0; e < DPT; ++e) y[e] = (_Float16)(acc[e] * inv);
         *reinterpret_cast<out_vec*>(a.out + row * HD + dbase) = y;
       } else {
-        const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * R + x;
+        const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * a.cols + x;
         if (dbase == 0) a.ml[e0] = make_float2(bad ? NAN : mx, den);
 #pragma unroll
         for (int e = 0; e < DPT; e += 4)
@@ -525,7 +532,7 @@ __device__ __forceinline__ void wait_loads() {
 
 // NK: 32-key blocks of a tile.  SMALL: chunks of fewer tokens than a tile.
 template <int HD, int NW, int NK, int ST, bool SMALL>
-__global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
+__global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wide_kernel(AttnTree a) {
   constexpr int R = 32 * NW, KT = 32 * NK, UNIT = KT;
   constexpr int KC = HD / 8, VC = KT / 8;                      // 16-byte columns of a key, of a dimension
   constexpr int STRETCHES = KT * KC / 64;                      // of 1 KB, 64 lanes' 16 bytes, in a tile of K and of V^T
@@ -536,11 +543,10 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
   __shared__ __attribute__((aligned(16))) _Float16 lds[2 * ST * TILE];      // the rings of K and of V^T
   __shared__ int window[SMALL ? kWindow * KT / 8 + 1 : kWindow + 1];
   __shared__ float s_again[NW];
-  int* s_at = reinterpret_cast<int*>(lds);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5, dkv = a.nkv * HD, g = blockIdx.x;
   Share sh;
-  if (!share_begin<R, UNIT, NW>(a, s_at + 2, s_at, sh)) return;
+  if (!share_begin<R, UNIT, NW>(a, reinterpret_cast<int*>(lds), sh)) return;
 
   // where the lane's 16 bytes of a stretch come from: stretch i NW + w holds
   // pieces 64 (i NW + w) + lane of the swizzled tile, so that from one i to the next
@@ -652,6 +658,12 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
       }
     };
 
+    f16x8 q[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      q[ks] = f16x8{};
+      if (there) q[ks] = *reinterpret_cast<const f16x8*>(a.q + ((int64_t)(s.first + node) * a.nq + head) * HD + ks * 16 + half * 8);
+    }
     __syncthreads();                   // the piece before has been read
     fill_window(p.t0);
     const int first_slot = SMALL ? 0 : scalar_slot(p.t0);
@@ -665,12 +677,6 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
       if (i + 1 == ST) break;
       slots_of_v(p.t0 + i);
       load_v(p.t0 + i, i ? q_slot[i - 1] : first_slot);
-    }
-    f16x8 q[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      q[ks] = f16x8{};
-      if (there) q[ks] = *reinterpret_cast<const f16x8*>(a.q + ((int64_t)(s.first + node) * a.nq + head) * HD + ks * 16 + half * 8);
     }
     f32x16 o[TN];
 #pragma unroll
@@ -886,7 +892,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
           *reinterpret_cast<f16x4*>(out + t * 32 + 8 * r) = f16x4{(_Float16)(o[t][4 * r] * inv), (_Float16)(o[t][4 * r + 1] * inv),
                                                                   (_Float16)(o[t][4 * r + 2] * inv), (_Float16)(o[t][4 * r + 3] * inv)};
     } else if (there) {
-      const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * R + w * 32 + col;
+      const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * a.cols + w * 32 + col;
       if (half == 0) a.ml[e0] = make_float2(m, l);
       if (!finite) a.ml[e0].x = NAN;
 #pragma unroll
@@ -906,27 +912,25 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_wide_kernel(AttnTree a) {
 // g1.  TPR of a workgroup's threads take one: HD / 4 lanes a partial, four
 // dimensions each, AHEAD of them in one trip to memory, and the groups of lanes meet in
 // LDS.  Rows with sums that are not finite are taken again.
-template <int HD, int R, int UNIT>
+template <int HD, int R>
 __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   constexpr int TPR = R <= 32 ? 256 : 64, ROWS = 256 / TPR, LPP = HD / 4, NG = TPR / LPP, AHEAD = R <= 32 ? 4 : 8;
   __shared__ float s_m[256 / LPP], s_l[256 / LPP];
   __shared__ f32x4 s_acc[256 / LPP][LPP];
   const int t = threadIdx.x, dl = t % LPP, group = t / LPP, pg = group % NG;
   const int64_t first = (int64_t)blockIdx.x * ROWS, at = first + t / TPR, rows = (int64_t)a.m * a.nq;
-  const int total = a.base[a.n_seq] * a.nkv, nw = shares(a, total);
+  const int total = *a.total, nw = shares(a, total);
   bool again = false;
-  const int b = at < rows ? a.row_seq[at / a.nq] : -1;
+  const int r = (int)(min(at, rows - 1) / a.nq), hq = (int)(at - (int64_t)r * a.nq), h = hq / a.group;
+  const int4 row = a.rows[r];          // first unit, units, tiles, first row of its sequence
   int n = 0;
   float m = -INFINITY, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (b >= 0) {
-    const Seq s = seq_of<R, UNIT>(a, b);
-    const int r = (int)(at / a.nq), hq = (int)(at - (int64_t)r * a.nq), h = hq / a.group;
-    const int x = (r - s.first) * a.group + hq - h * a.group, tile = x / R, c = x - tile * R;
-    const int f0 = a.base[b] * a.nkv + (h * s.tiles + tile) * s.units;
-    const int g0 = share_of(f0, nw, total);
-    n = share_of(f0 + s.units - 1, nw, total) - g0 + 1;
-    auto part = [&](int i) { return (int64_t)(2 * (g0 + i) + (i == 0)) * R + c; };
+  if (at < rows && row.y) {
+    const int x = (r - row.w) * a.group + hq - h * a.group, tile = x / R, c = x - tile * R;
+    const int f0 = row.x + (h * row.z + tile) * row.y, g0 = share_of(f0, nw, total);
+    n = share_of(f0 + row.y - 1, nw, total) - g0 + 1;
+    auto part = [&](int i) { return (int64_t)(2 * (g0 + i) + (i == 0)) * a.cols + c; };
     if (n > 1)                         // else it is written whole
       for (int i0 = pg; i0 < n; i0 += AHEAD * NG) {
         float2 ml[AHEAD];
@@ -956,8 +960,11 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   s_acc[group][dl] = acc;
   if (__syncthreads_or(again)) {
     for (int k = 0; k < ROWS && first + k < rows; ++k) {
-      const int r = (int)((first + k) / a.nq), hq = (int)(first + k - (int64_t)r * a.nq), mine = a.row_seq[r];
-      if (mine >= 0) row_again<HD, 256>(a, seq_of<R, UNIT>(a, mine), mine, r, hq, reinterpret_cast<float*>(s_acc), s_m);
+      const int r = (int)((first + k) / a.nq), hq = (int)(first + k - (int64_t)r * a.nq);
+      if (!a.rows[r].y) continue;
+      int b = 0;                       // the row's sequence, the last that begins with it and has rows
+      while (b + 1 < a.n_seq && !(a.row_off[b] <= r && r < a.row_off[b + 1])) ++b;
+      row_again<HD, 256>(a, seq_of<R, 1>(a, b), b, r, hq, reinterpret_cast<float*>(s_acc), s_m);
     }
     return;
   }
@@ -981,17 +988,11 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
 // Columns of a tile for `cols` columns of an average sequence.
-int tile_cols(int64_t cols) { return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256; }
+int tile_cols(int64_t cols) { return cols <= 16 ? 16 : cols <= 32 ? 32 : 128; }
 
-// Shares: a workgroup for each that a CU holds.
-int most_shares(int R) { return R == 256 ? 256 : 512; }
+// Columns of a partial, of a call of `cols` columns a KV head in all.
+int part_cols(int R, int64_t cols) { return cols < R ? (int)cols : R; }
 
-int least_units(int R) { return R <= 32 ? 1 : 8; }
-
-template <int HD, int R>
-struct WideShape {       // 32-key blocks of a tile, tiles of a ring
-  static constexpr int NK = 2, ST = R == 256 ? 3 : 2;
-};
 
 template <int HD, int R>
 void launch(const AttnTree& a, hipStream_t s) {
@@ -1002,23 +1003,20 @@ void launch(const AttnTree& a, hipStream_t s) {
     else
       hipLaunchKernelGGL((tree_few_kernel<HD, R / kCols, false>), grid, dim3(64 * kFewWaves), 0, s, a);
   } else {
-    constexpr int NK = WideShape<HD, R>::NK, ST = WideShape<HD, R>::ST;
+    constexpr int NK = 2, ST = 2;
     if (a.C < 32 * NK)
       hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, NK, ST, true>), grid, dim3(2 * R), 0, s, a);
     else
       hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, NK, ST, false>), grid, dim3(2 * R), 0, s, a);
   }
-  constexpr int UNIT = R <= 32 ? kFewUnit : 32 * WideShape<HD, R>::NK;
-  hipLaunchKernelGGL((tree_join_kernel<HD, R, UNIT>), dim3((unsigned)(((int64_t)a.m * a.nq * (R <= 32 ? 4 : 1) + 3) / 4)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((tree_join_kernel<HD, R>), dim3((unsigned)(((int64_t)a.m * a.nq * (R <= 32 ? 4 : 1) + 3) / 4)), dim3(256), 0, s, a);
 }
 
 template <int HD>
 void launch(const AttnTree& a, int R, hipStream_t s) {
   if (R == 16) launch<HD, 16>(a, s);
   if (R == 32) launch<HD, 32>(a, s);
-  if (R == 64) launch<HD, 64>(a, s);
   if (R == 128) launch<HD, 128>(a, s);
-  if (R == 256) launch<HD, 256>(a, s);
 }
 
 }  // namespace
@@ -1031,25 +1029,26 @@ int64_t attention_tree_units(int m, int n_seq, int n_table, int chunk_tokens, in
 
 // Partials for the widest tile that fewer sequences of these rows may take, so that one workspace serves them too.
 int64_t attention_tree_ws_bytes(int m, int n_seq, int nq, int nkv, int hd) {
-  int64_t cols = 0;
-  for (int R = 16; R <= tile_cols((int64_t)m * (nq / nkv)); R *= 2) cols = std::max<int64_t>(cols, (int64_t)2 * most_shares(R) * R);
-  return up256(((int64_t)n_seq + 1) * 4) + up256((int64_t)m * 4) + up256(cols * 8) + cols * hd * 4;
+  const int64_t all = (int64_t)m * (nq / nkv), cols = (int64_t)2 * kShares * part_cols(tile_cols(all), all);
+  return 256 + up256((int64_t)m * 16) + up256(cols * 8) + cols * hd * 4;
 }
 
 void launch_attention_tree(AttnTree a, int hd, void* ws, hipStream_t s) {
   const int R = tile_cols(((int64_t)a.m + a.n_seq - 1) / a.n_seq * a.group);
+  a.cols = part_cols(R, (int64_t)a.m * a.group);
   uint8_t* p = reinterpret_cast<uint8_t*>(ws);
-  a.base = reinterpret_cast<int32_t*>(p);
-  p += up256(((int64_t)a.n_seq + 1) * 4);
-  a.row_seq = reinterpret_cast<int32_t*>(p);
-  p += up256((int64_t)a.m * 4);
+  a.total = reinterpret_cast<int32_t*>(p);
+  p += 256;
+  a.rows = reinterpret_cast<int4*>(p);
+  p += up256((int64_t)a.m * 16);
   a.ml = reinterpret_cast<float2*>(p);
-  p += up256((int64_t)2 * most_shares(R) * R * 8);
+  p += up256((int64_t)2 * kShares * a.cols * 8);
   a.part = reinterpret_cast<float*>(p);
-  a.least = least_units(R);
+  a.least = R <= 32 ? 1 : 8;
+  a.fewest = R <= 32 ? 1 : 3;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)hd);
   const int64_t most = attention_tree_units(a.m, a.n_seq, a.n_table, a.C, a.nq, a.nkv);
-  a.wgs = most < most_shares(R) ? (int)most : most_shares(R);
+  a.wgs = most < kShares ? (int)most : kShares;
   if (hd == 128)
     launch<128>(a, R, s);
   else

@@ -273,10 +273,12 @@ struct AttnTree {
   _Float16* out;
   int n_seq, m, mask_words, n_slots, n_table, C, cshift, nq, nkv, group;
   int64_t slot_bytes;
-  int32_t *base, *row_seq;   // [n_seq + 1] units a KV head of the sequences before, [m]
-  float2* ml;                // [2 wgs][columns of a tile] running max (NaN: sums that are not finite) and sum of a partial
-  float* part;               // [2 wgs][columns of a tile][hd]
-  int wgs, least;            // most workgroups that share the units, fewest units of a share
+  int32_t* total;            // units of all sequences and KV heads
+  int4* rows;                // [m] first unit, units (0: a row of no tree), tiles and first row of the row's sequence
+  float2* ml;                // [2 wgs][cols] running max (NaN: sums that are not finite) and sum of a partial
+  float* part;               // [2 wgs][cols][hd]
+  int wgs, least, fewest;    // most workgroups that share the units, fewest units of a share
+  int cols;                  // columns of a partial
   float scale_log2;
 };
 int64_t attention_tree_units(int m, int n_seq, int n_table, int chunk_tokens, int nq, int nkv);

@@ -468,6 +468,64 @@ def test_tree_attention_what_a_row_does_not_see(bad, C):
     tree_check(a, tree_run(a), f"{bad}")
 
 
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("C,n", [(8, 30), (64, 200), (64, 5000), (16, 4000)])
+def test_tree_attention_wide_trees_and_what_a_row_does_not_see(C, n, bad):
+    """The same for trees of many columns, alone in a workgroup's share and cut over several."""
+    a = tree_inputs([24, 9], [n, 7], C, 8, 1, 64, seed=C + n, mask="tree")
+    for b, node, half in ((0, 5, 1), (0, 17, 0), (1, 2, 1)):
+        at = a["lens"][b] + node
+        slot = a["table"][b, at // C]
+        if half:
+            a["slab"][slot].reshape(2, -1)[1].reshape(64, C)[3:40, at % C] = bad
+        else:
+            a["slab"][slot].reshape(2, -1)[0].reshape(C, 64)[at % C, 3] = bad
+    with np.errstate(invalid="ignore"):
+        ref, _, _ = tree_oracle(a)
+    hit = ~np.isfinite(ref[:33]).all(1)
+    assert hit.any() and not hit.all()
+    tree_check(a, tree_run(a), f"{bad}")
+
+
+@pytest.mark.parametrize("C", [8, 64, 256])
+def test_tree_attention_a_value_that_all_rows_see_is_infinite(C):
+    a = tree_inputs([24, 9], [700, 7], C, 8, 1, 64, seed=C, mask="any")
+    slot = a["table"][0, 300 // C]
+    a["slab"][slot].reshape(2, -1)[1].reshape(64, C)[11, 300 % C] = np.inf
+    tree_check(a, tree_run(a))
+
+
+@pytest.mark.parametrize("C", [8, 64, 512])
+def test_tree_attention_of_two_million_keys(C):
+    """Shares of more tiles than their copy of the chunk table holds at once."""
+    torch = torch_cuda()
+    n, t, nq, hd = 2200000, 3, 16, 64
+    chunks = (n + t + C - 1) // C
+    g = torch.Generator(device="cuda").manual_seed(C)
+    table = torch.randperm(chunks, device="cuda", generator=g).int()[None]
+    slab = torch.empty(chunks, 2, C * hd, device="cuda", dtype=torch.float16).normal_(generator=g)
+    q = torch.empty(t, nq * hd, device="cuda", dtype=torch.float16).normal_(generator=g)
+    off, lens = dev(np.array([0, t], np.int32)), dev(np.array([n], np.int32))
+    ws = torch.empty(mz.mz_attention_tree_workspace_bytes(t, 1, nq, 1, hd), device="cuda", dtype=torch.uint8)
+    out = full((t, nq * hd), 7.0, torch.float16)
+    mz.mz_attention_tree(ptr(q), t, ptr(off), ptr(lens), 1, ptr(slab), chunks, ptr(table), chunks, C, nq, 1, hd, ptr(ws), ws.numel(), ptr(out),
+                         stream())
+    at = table[0].long()
+    k = slab[at, 0].view(-1, hd)[:n + t].double()
+    v = slab[at, 1].view(-1, hd, C).transpose(1, 2).reshape(-1, hd)[:n + t].double()
+    s = q.view(-1, hd).double() @ k.T.contiguous() / 8
+    s.masked_fill_(torch.arange(n + t, device="cuda")[None, :] > n + torch.arange(t * nq, device="cuda")[:, None] // nq, -np.inf)
+    p = torch.softmax(s, 1)
+    ref = (p @ v).cpu().numpy().reshape(t, nq * hd)
+    # as tree_oracle's; a score is at most |q| |k| / 8, a share's sums have at most 8192 terms of a column, and 512 are joined
+    size = (p @ v.abs()).cpu().numpy().reshape(t, nq * hd)
+    part = float((q.view(-1, hd).double().norm(dim=1).max() * k.norm(dim=1).max()) / 8)
+    e = (hd + 4) * U32 * part + 4 * U32 * 2 * part + 4 * U32
+    bound = (2 * e + 2.0 ** -21 + 8 * (8192 / 32 + 512 + 64) * U32) * size * (1 + U16) + U16 * np.abs(ref) + TINY16 + n * 2.0 ** -34 * float(v.abs().max()) * \
+        float(p.max())
+    close(out, ref, bound, "out")
+
+
 def test_tree_attention_large_scores():
     tree_case([8, 3], [200, 31], 16, 4, 2, 64, seed=11, spread=30.0)
 
@@ -801,7 +859,7 @@ def test_pages_random(seed):
     pages_case(table, src, keep, None, n_slots, 0, C)
 
 
-@pytest.mark.parametrize("n_seq,wide,n_slots", [(1, 1, 1), (3, 5000, 20000), (1500, 7, 9000), (70, 300, 40000), (1100, 20, 16384)])
+@pytest.mark.parametrize("n_seq,wide,n_slots", [(1024, 20, 8192), (1025, 7, 8000), (64, 320, 8192), (64, 321, 8192), (64, 300, 8193), (4, 5121, 8000), (1, 1, 1), (3, 5000, 20000), (1500, 7, 9000), (70, 300, 40000), (1100, 20, 16384)])
 def test_pages_sizes(n_seq, wide, n_slots):
     rng = np.random.default_rng(n_seq)
     table, src, keep, room = pages_inputs(rng, n_seq, wide, n_slots, 8)
@@ -871,3 +929,114 @@ def test_copy_far_slots():
     mz.mz_kv_copy(ptr(copies), ptr(n), 2, ptr(slab), n_slots, 2, slab.stride(0) * 2, C, nkv, hd, stream())
     torch.cuda.synchronize()
     assert torch.equal(slab[:, [n_slots - 2, 2]], want)
+
+
+# ----------------------------------------------------------------------------- together
+
+def test_a_step_that_checks_drafted_trees():
+    """Pages, copies, rows, appending, attention and the branch in one graph, replayed over forks, trees and lengths that
+    change, against a cache that is kept token by token on the host."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(1)
+    layers, nq, nkv, hd, C, n_seq, m, n_table, n_slots, n_rope = 2, 8, 2, 64, 16, 4, 40, 8, 40, 200
+    dq, dkv, words, limit = nq * hd, nkv * hd, 1, 34
+    rope = rope_table(n_rope, hd)
+    z = lambda *shape, dtype=torch.int32: torch.zeros(shape, device="cuda", dtype=dtype)  # noqa: E731
+    table, src, keep, room, info = full((n_seq, n_table), -1), z(n_seq), z(n_seq), z(n_seq), z(4)
+    copies = z(n_seq + n_slots - limit, 4)
+    off, parent, token, choice, lens = z(n_seq + 1), z(m), z(m), z(m), z(n_seq)
+    seq, place, rpos, mask = z(m), z(m), z(m), z(m, words)
+    accepted, path, nxt, len_out = z(n_seq), z(m), z(n_seq), z(n_seq)
+    qkv, q_rot, out = z(layers, m, dq + 2 * dkv, dtype=torch.float32), z(layers, m, dq, dtype=torch.float16), z(layers, m, dq, dtype=torch.float16)
+    slab, d_rope = z(layers, n_slots, 2 * C * dkv, dtype=torch.float16), dev(rope)
+    pws = z(mz.mz_kv_pages_workspace_bytes(n_seq, n_table, n_slots), dtype=torch.uint8)
+    aws = z(mz.mz_attention_tree_workspace_bytes(m, n_seq, nq, nkv, hd), dtype=torch.uint8)
+    slab.fill_(float("nan"))
+
+    def step():
+        mz.mz_kv_pages(ptr(table), ptr(table), n_seq, n_table, n_slots, C, ptr(keep), ptr(copies), ptr(info), ptr(pws), pws.numel(), stream(),
+                       src_ptr=ptr(src), room_ptr=ptr(room), slot_limit=limit)
+        mz.mz_kv_copy(ptr(copies), ptr(info) + 8, copies.shape[0], ptr(slab), n_slots, layers, slab.stride(0) * 2, C, nkv, hd, stream())
+        mz.mz_tree_plan(ptr(off), ptr(lens), n_seq, m, stream(), parent_ptr=ptr(parent), seq_ptr=ptr(seq), place_ptr=ptr(place),
+                        rope_pos_ptr=ptr(rpos), mask_ptr=ptr(mask), mask_words=words)
+        for x in range(layers):
+            base = ptr(qkv[x])
+            mz.mz_kv_append_axes(m, base + dq * 4, base + (dq + dkv) * 4, ptr(seq), ptr(place), ptr(rpos), 1, [0] * (hd // 2), ptr(d_rope), n_rope,
+                                 ptr(slab[x]), n_slots, ptr(table), n_seq, n_table, C, nkv, hd, stream(), q_ptr=base, n_q=nq,
+                                 q_out_ptr=ptr(q_rot[x]), k_stride=dq + 2 * dkv, v_stride=dq + 2 * dkv, q_stride=dq + 2 * dkv)
+            mz.mz_attention_tree(ptr(q_rot[x]), m, ptr(off), ptr(lens), n_seq, ptr(slab[x]), n_slots, ptr(table), n_table, C, nq, nkv, hd,
+                                 ptr(aws), aws.numel(), ptr(out[x]), stream(), mask_ptr=ptr(mask), mask_words=words)
+        mz.mz_tree_accept(ptr(off), ptr(token), ptr(choice), ptr(lens), n_seq, m, ptr(accepted), ptr(path), ptr(nxt), ptr(len_out), stream(),
+                          parent_ptr=ptr(parent), slab_ptr=ptr(slab), n_slots=n_slots, n_layers=layers, layer_bytes=slab.stride(0) * 2,
+                          table_ptr=ptr(table), n_table=n_table, chunk_tokens=C, n_kv=nkv, head_dim=hd)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        step()
+    caches = [[np.zeros((0, 2 * dkv), np.float16)] * n_seq for _ in range(layers)]      # keys and values of every sequence
+    now = [0] * n_seq
+    deep = forked = 0
+    for turn in range(12):
+        sources = [b if turn < 2 or rng.random() < 0.6 else int(rng.integers(-1, n_seq)) for b in range(n_seq)]
+        kept = [now[s] if s >= 0 else 0 for s in sources]
+        kept = [int(rng.integers(0, k + 1)) if rng.random() < 0.2 else min(k, n_table * C - 20) for k in kept]
+        counts = [int(rng.integers(0, 11)) if b else 10 for b in range(n_seq)]
+        h_off = offsets(counts)
+        h_parent, h_token, h_choice = np.full(m, -1, np.int32), rng.integers(0, 2, m).astype(np.int32), rng.integers(0, 2, m).astype(np.int32)
+        for b, n in enumerate(counts):
+            h_parent[h_off[b]:h_off[b + 1]] = random_tree(rng, n)
+        h_qkv = rng.standard_normal((layers, m, dq + 2 * dkv)).astype(np.float32)
+        for x, v in ((src, sources), (keep, kept), (lens, kept), (room, counts), (off, h_off), (parent, h_parent), (token, h_token), (choice, h_choice),
+                     (qkv, h_qkv)):
+            x.copy_(dev(np.asarray(v, np.float32 if x is qkv else np.int32)))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert info.tolist()[0] == 0, "slots are missing"
+        forked += info.tolist()[2]
+        h_table = table.cpu().numpy()
+        plan = plan_oracle(h_off, h_parent, np.array(kept), m, words)
+        ways = accept_oracle(h_off, h_parent, h_token, h_choice, np.array(kept), m)
+        assert accepted.tolist() == ways[0].tolist() and len_out.tolist() == ways[3].tolist() and nxt.tolist() == ways[2].tolist()
+        deep = max(deep, int(ways[0].max()))
+        for x in range(layers):
+            halves = slab[x].cpu().numpy().reshape(n_slots, 2, -1)
+            got_q, got = q_rot[x].cpu().numpy(), out[x]
+            old, caches[x] = caches[x], []
+            rows = [np.zeros((0, 2 * dkv), np.float16)] * n_seq
+            for b in range(n_seq):
+                # keys of the branch as the append leaves them: read from the slab before the move would need another copy, so turn them here
+                part = []
+                for r in range(h_off[b], h_off[b + 1]):
+                    a = h_qkv[x, r, dq:dq + dkv].reshape(nkv, hd).astype(np.float64)
+                    c, s = rope[plan[2][r], :, 0].astype(np.float64), rope[plan[2][r], :, 1].astype(np.float64)
+                    y = np.concatenate([a[:, :hd // 2] * c - a[:, hd // 2:] * s, a[:, hd // 2:] * c + a[:, :hd // 2] * s], 1)
+                    part.append(np.concatenate([y.reshape(-1), h_qkv[x, r, dq + dkv:].astype(np.float16).astype(np.float64)]))
+                rows[b] = np.array(part).reshape(-1, 2 * dkv)
+                before = old[sources[b]][:kept[b]].astype(np.float64) if sources[b] >= 0 else np.zeros((0, 2 * dkv))
+                # the rows' outputs: the keys are at most half a step of f16 off, which moves a score by at most 2 U16 |q| |k|
+                for i in range(counts[b]):
+                    r = h_off[b] + i
+                    seen = [j for j in range(counts[b]) if plan[3][r, 0] >> j & 1]
+                    kv = np.concatenate([before, rows[b][seen]])
+                    for h in range(nq):
+                        kk, vv = kv[:, h // 4 * hd:][:, :hd], kv[:, dkv + h // 4 * hd:][:, :hd]
+                        q = got_q[r, h * hd:(h + 1) * hd].astype(np.float64)
+                        w = kk @ q / 8
+                        p = np.exp(w - w.max())
+                        p /= p.sum()
+                        e = 2 * U16 * (np.abs(kk) @ np.abs(q)).max() / 8 + 2.0 ** -18
+                        ref, size = p @ vv, p @ np.abs(vv)
+                        diff = np.abs(got[r, h * hd:(h + 1) * hd].double().cpu().numpy() - ref)
+                        assert (diff <= 2.1 * e * size + U16 * np.abs(ref) + TINY16).all(), (turn, x, b, i, h)
+                after = np.concatenate([before, rows[b][ways[4][b]]]) if ways[4][b] else before
+                # what the cache holds now, through the table
+                pos = np.arange(after.shape[0])
+                at = h_table[b, pos // C]
+                assert (at >= 0).all() and (at < limit).all()
+                held = np.concatenate([halves[at, 0].reshape(-1, C, dkv)[np.arange(pos.size), pos % C],
+                                       halves[at, 1].reshape(-1, dkv, C)[np.arange(pos.size), :, pos % C]], 1) if pos.size else np.zeros((0, 2 * dkv), np.float16)
+                assert (np.abs(held.astype(np.float64) - after) <= U16 * np.abs(after) * (1 + U16) + TINY16 + 8 * U32).all(), (turn, x, b)
+                caches[x].append(held)
+        now = [int(v) for v in ways[3]]
+    assert deep >= 3 and forked >= 3
