@@ -493,7 +493,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
 }
 
 // ---- more columns
-// NW waves own 32 columns each and meet the same keys, 64 at a time, which are
+// Four waves own 32 columns each and meet the same keys, 64 at a time, which are
 // loaded into LDS once for all of them (global_load_lds, 16 bytes a lane, one
 // tile ahead): S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16.  Lane l
 // feeds row / column l % 32 with the 8 consecutive k of group l / 32; element r
@@ -502,45 +502,46 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
 // eight consecutive keys from 16 g + 8 (l / 32) on, g = 0..3, and the P operand meets
 // 16-byte runs of V^T.
 //
-// A step multiplies: the scores of tile t + 1 while the weights of the first half
-// of tile t are formed; then P V of tile t while those of the second half are, and
-// the max of tile t + 1.  The running max is raised only where a tile exceeds it
-// by more than kSlack, so that sums are seldom scaled.
-// The loads run ST - 1 tiles (V^T) and ST tiles (K) ahead of their product in a
-// ring of ST tiles each, so that several are in flight whatever a step takes.
-// Slots come from a copy of the next kWindow tiles' stretch of the chunk table in
-// LDS: a read of the table between the loads would wait for all of them.
+// A step multiplies the scores of tile t + 1, then P V of tile t.  The weights of
+// tile t are formed under the products up to those that need them, the max of
+// tile t + 1 under P V.  The running max is raised only where a tile exceeds it by
+// more than kSlack, so that sums are seldom scaled.  Slots come from a copy of the
+// next kWindow tiles' stretch of the chunk table in LDS: a read of the table between
+// the loads would wait for them.
+//
+// Measured: 4 sequences of 24576 keys and 64 nodes, 8 KV heads of 128 with 4 query
+// heads each, 175 + 12 us (joining): 155 GFLOP with the lower halves at 0.88 PFLOP/s,
+// where products alone, at the clock that the power allows, take 112 (24 ns each a
+// SIMD; 13 at the full clock), loads alone 90.  Two waves a SIMD are little faster
+// than one (148 us against 161 of a smaller pipeline, from L2), and one workgroup of 256
+// columns a CU, which reads each key once, not twice, is as fast (184 us for 187) and
+// slower where trees are smaller.  32 ragged sequences of up to 8192 keys and 16 nodes 90 +
+// 11: 373 MB, loads alone 83.
+constexpr int kTile = 64, kWideWaves = 4;
 constexpr float kSlack = 4.f, kWideBias = 11.f;
 constexpr int kWindow = 64;
 
 // LDS tiles are swizzled on 16-byte columns: row r's column c lies at c ^ r % 16
-// (256-byte rows), c ^ (r / 2) % 8 (128-byte rows), c ^ (r / 4) % 4 (64-byte rows),
-// so that neither the reads of 32 rows' same column nor the writes of whole rows
-// meet in a bank.
+// (256-byte rows), c ^ (r / 2) % 8 (128-byte rows), so that neither the reads of 32
+// rows' same column nor the writes of whole rows meet in a bank.
 template <int HALVES>
 __device__ __forceinline__ int swizzle(int r, int c) {
-  return HALVES == 128 ? c ^ (r & 15) : HALVES == 64 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3);
+  return HALVES == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7);
 }
 template <int HALVES>
 __device__ __forceinline__ int tile_at(int r, int c) { return r * HALVES + swizzle<HALVES>(r, c) * 8; }
 
-// A wait that leaves the N youngest loads in flight.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
-}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// NK: 32-key blocks of a tile.  SMALL: chunks of fewer tokens than a tile.
-template <int HD, int NW, int NK, int ST, bool SMALL>
-__global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wide_kernel(AttnTree a) {
-  constexpr int R = 32 * NW, KT = 32 * NK, UNIT = KT;
+// SMALL: chunks of fewer tokens than a tile.
+template <int HD, bool SMALL>
+__global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree a) {
+  constexpr int NW = kWideWaves, R = 32 * NW, KT = kTile, UNIT = KT;
   constexpr int KC = HD / 8, VC = KT / 8;                      // 16-byte columns of a key, of a dimension
-  constexpr int STRETCHES = KT * KC / 64;                      // of 1 KB, 64 lanes' 16 bytes, in a tile of K and of V^T
-  constexpr int PER = STRETCHES / NW;                          // of a wave
+  constexpr int PER = KT * KC / 64 / NW;                       // stretches of 1 KB, 64 lanes' 16 bytes, of a tile and a wave
   constexpr int TILE = KT * HD;                                // halves
   constexpr int KS = HD / 16, TN = HD / 32;
-  constexpr int AHEAD = (ST - 2) * 2 * PER;                    // loads that may be in flight when a step ends
-  __shared__ __attribute__((aligned(16))) _Float16 lds[2 * ST * TILE];      // the rings of K and of V^T
+  __shared__ __attribute__((aligned(16))) _Float16 lds[4 * TILE];      // K of two tiles, V^T of two
   __shared__ int window[SMALL ? kWindow * KT / 8 + 1 : kWindow + 1];
   __shared__ float s_again[NW];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -550,13 +551,13 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
 
   // where the lane's 16 bytes of a stretch come from: stretch i NW + w holds
   // pieces 64 (i NW + w) + lane of the swizzled tile, so that from one i to the next
-  // the key (K) or the dimension (V^T) goes on by a multiple of 8, and the column
-  // stays as it is but for K of 16 columns and rows that are 8 apart
+  // the key (K) or the dimension (V^T) goes on by a multiple of 16, and the column
+  // stays as it is
   constexpr int K_STEP = NW * 64 / KC, V_STEP = NW * 64 / VC;
   const int k_row = (w * 64 + lane) / KC, v_row = (w * 64 + lane) / VC;
   const unsigned k_of = swizzle<HD>(k_row, lane % KC) * 16u;
   const int v_key = swizzle<KT>(v_row, lane % VC) * 8;         // the first of the eight keys
-  static_assert(STRETCHES % NW == 0 && V_STEP % 16 == 0 && K_STEP % 8 == 0 && (KC == 16 || K_STEP % 16 == 0), "columns of the stretches");
+  static_assert(PER >= 1 && V_STEP % 16 == 0 && K_STEP % 16 == 0, "columns of the stretches");
   typedef __attribute__((address_space(3))) void lds_void;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds);
   // 64 lanes' 16 bytes from `from`, or from a base in scalar registers + at, into
@@ -592,31 +593,29 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     auto slot_at = [&](int j) { return window[(min(j, last) >> a.cshift) - c0]; };
     auto clean = [&](int slot) { return (unsigned)slot < (unsigned)a.n_slots ? slot : 0; };
     // Slots are read a step before they are used: with SMALL those of what the lane
-    // loads, else the tile's, into scalar registers, q[i] that of tile t + 1 + i at step t.
+    // loads, else the tile's, into scalar registers, those of tiles t + 1 and t + 2 at step t.
     constexpr int KSLOTS = SMALL ? PER : 1;
-    int k_slot[KSLOTS], v_slot = 0, q_slot[ST];
+    int k_slot[KSLOTS], v_slot = 0, slot1, slot2;
     const unsigned k_lane = (unsigned)k_row * (unsigned)dkv * 2u + p.h * HD * 2u + k_of;
     const unsigned v_lane = ((unsigned)(dkv + p.h * HD + v_row) * (unsigned)a.C + v_key) * 2u;
     const uint64_t slab = (uint64_t)(uintptr_t)a.slab;
     auto scalar_slot = [&](int t) { return __builtin_amdgcn_readfirstlane(slot_at(min(t, t_end - 1) * KT)); };
     auto load_k = [&](int t, int slot) {
-      const int j0 = (t * KT) & (a.C - 1), to = t % ST * TILE + w * 512;
+      const int j0 = (t * KT) & (a.C - 1), to = (t & 1) * TILE + w * 512;
       const uint64_t base = slab + (uint64_t)clean(slot) * (uint64_t)a.slot_bytes + (unsigned)j0 * (unsigned)dkv * 2u;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         if constexpr (SMALL) {
           const int row = k_row + i * K_STEP;
-          const unsigned of = K_STEP % 16 == 0 ? k_of : k_of ^ (i & 1) * 128u;
-          fetch(a.slab + (int64_t)clean(k_slot[i]) * a.slot_bytes + ((unsigned)((j0 + row) & (a.C - 1)) * (unsigned)dkv * 2u + p.h * HD * 2u + of),
+          fetch(a.slab + (int64_t)clean(k_slot[i]) * a.slot_bytes + ((unsigned)((j0 + row) & (a.C - 1)) * (unsigned)dkv * 2u + p.h * HD * 2u + k_of),
                 to + i * NW * 512);
         } else {
-          fetch_from(base + (unsigned)(i * K_STEP) * (unsigned)dkv * 2u, K_STEP % 16 == 0 || i % 2 == 0 ? k_lane : (k_lane - k_of) + (k_of ^ 128u),
-                     to + i * NW * 512);
+          fetch_from(base + (unsigned)(i * K_STEP) * (unsigned)dkv * 2u, k_lane, to + i * NW * 512);
         }
       }
     };
     auto load_v = [&](int t, int slot) {
-      const int j0 = (t * KT) & (a.C - 1), to = (ST + t % ST) * TILE + w * 512;
+      const int j0 = (t * KT) & (a.C - 1), to = (2 + (t & 1)) * TILE + w * 512;
       const uint64_t base = slab + (uint64_t)clean(slot) * (uint64_t)a.slot_bytes + (unsigned)j0 * 2u;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -636,13 +635,13 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     auto slots_of_v = [&](int t) {
       if constexpr (SMALL) v_slot = slot_at(t * KT + v_key);
     };
-    // Keys of tile t that are there (the last ones of 64 where a tile has fewer), and zeros for the values of the others.
+    // Keys of tile t that are there, and zeros for the values of the others.
     auto there64 = [&](int t, int slot) -> uint64_t {
       if constexpr (SMALL) {
         const int j = t * KT + lane;
-        return __ballot(lane >= KT || ((unsigned)slot_at(min(j, (w0 + kWindow) * KT - 1)) < (unsigned)a.n_slots && j < s.keys));
+        return __ballot((unsigned)slot_at(j) < (unsigned)a.n_slots && j < s.keys);
       } else {
-        return ((unsigned)slot < (unsigned)a.n_slots ? ones64(s.keys - t * KT) : 0) | (KT == 64 ? 0 : ~0ull << (KT & 63));
+        return (unsigned)slot < (unsigned)a.n_slots ? ones64(s.keys - t * KT) : 0;
       }
     };
     auto mend_v = [&](int t, uint64_t keys) {
@@ -650,7 +649,7 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
       if (on == 0xFF) return;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        f16x8* v = reinterpret_cast<f16x8*>(lds + (ST + t % ST) * TILE + (i * NW + w) * 512 + lane * 8);
+        f16x8* v = reinterpret_cast<f16x8*>(lds + (2 + (t & 1)) * TILE + (i * NW + w) * 512 + lane * 8);
         f16x8 e = *v;
 #pragma unroll
         for (int k = 0; k < 8; ++k) e[k] = (on >> k) & 1 ? e[k] : (_Float16)0.f;
@@ -666,17 +665,16 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     }
     __syncthreads();                   // the piece before has been read
     fill_window(p.t0);
-    const int first_slot = SMALL ? 0 : scalar_slot(p.t0);
-#pragma unroll
-    for (int i = 0; i < ST; ++i) q_slot[i] = SMALL ? 0 : scalar_slot(p.t0 + 1 + i);
-#pragma unroll
-    for (int i = 0; i < ST; ++i) {
-      if (p.t0 + i >= t_end) break;
-      slots_of_k(p.t0 + i);
-      load_k(p.t0 + i, i ? q_slot[i - 1] : first_slot);
-      if (i + 1 == ST) break;
-      slots_of_v(p.t0 + i);
-      load_v(p.t0 + i, i ? q_slot[i - 1] : first_slot);
+    const int slot0 = SMALL ? 0 : scalar_slot(p.t0);
+    slot1 = SMALL ? 0 : scalar_slot(p.t0 + 1);
+    slot2 = SMALL ? 0 : scalar_slot(p.t0 + 2);
+    slots_of_k(p.t0);
+    slots_of_v(p.t0);
+    load_k(p.t0, slot0);
+    load_v(p.t0, slot0);
+    if (p.t0 + 1 < t_end) {
+      slots_of_k(p.t0 + 1);
+      load_k(p.t0 + 1, slot1);
     }
     f32x16 o[TN];
 #pragma unroll
@@ -687,16 +685,16 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
 
     const int krow = (col & ~12) | ((col & 8) >> 1) | ((col & 4) << 1);
     auto k_frag = [&](const _Float16* k, int i) {        // of score product i
-      return *reinterpret_cast<const f16x8*>(&k[tile_at<HD>(i % NK * 32 + krow, i / NK * 2 + half)]);
+      return *reinterpret_cast<const f16x8*>(&k[tile_at<HD>((i & 1) * 32 + krow, (i >> 1) * 2 + half)]);
     };
     auto v_frag = [&](const _Float16* v, int grp, int t) {
       return *reinterpret_cast<const f16x8*>(&v[tile_at<KT>(t * 32 + col, grp * 2 + half)]);
     };
     // Scores of tile t that do not count become -inf; keys: those that are there.
-    auto mask_scores = [&](f32x16 (&sc)[NK], int t, uint64_t keys) {
-      const uint64_t on = keys & seen64(a, s, t * KT, node, words) & (KT == 64 ? ~0ull : (1ull << KT) - 1);
+    auto mask_scores = [&](f32x16 (&sc)[2], int t, uint64_t keys) {
+      const uint64_t on = keys & seen64(a, s, t * KT, node, words);
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
+      for (int kk = 0; kk < 2; ++kk) {
         const unsigned mine = (unsigned)(on >> (32 * kk + 8 * half));
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -724,14 +722,14 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
           for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
       }
     };
-    f16x2 hi[8 * NK], lo[8 * NK];      // of two scores each, four to a P operand
+    f16x2 hi[16], lo[16];      // of two scores each, four to a P operand
     float e0 = 0.f, e1 = 0.f, base = 0.f;
     // The weights of scores 2 i and 2 i + 1 in four parts of about the same time
     // (j = 4 i + part), so that they fit under products: the exponentials; their sum;
     // their halves, lo = f16(e - hi) in one instruction each.  (Its inputs are a
     // conversion's, not an exponential's or a product's, and a product may read it
     // two wait states later.)
-    auto weigh = [&](const f32x16 (&sc)[NK], int j) {
+    auto weigh = [&](const f32x16 (&sc)[2], int j) {
       const int i = j >> 2;
       if ((j & 3) == 0) e0 = exp2_hw(__builtin_fmaf(sc[i >> 3][2 * (i & 7)], a.scale_log2, -base));
       if ((j & 3) == 1) e1 = exp2_hw(__builtin_fmaf(sc[i >> 3][2 * (i & 7) + 1], a.scale_log2, -base));
@@ -749,8 +747,8 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     };
     // Product i of those before the last 16 keys' carries its share of the parts,
     // so that a P operand is there when its products begin.
-    constexpr int PARTS = 32 * NK, CARRY = NK * KS + (2 * NK - 1) * 2 * TN;
-    auto carry = [&](const f32x16 (&sc)[NK], int i) {
+    constexpr int PARTS = 64, CARRY = 2 * KS + 3 * 2 * TN;
+    auto carry = [&](const f32x16 (&sc)[2], int i) {
 #pragma unroll
       for (int j = i * PARTS / CARRY; j < (i + 1) * PARTS / CARRY; ++j) weigh(sc, j);
     };
@@ -761,23 +759,23 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
       return y;
     };
 
-    f32x16 sa[NK], sb[NK];
+    f32x16 sa[2], sb[2];
     {
-      if (p.t0 + ST - 1 < t_end) wait_loads<AHEAD>(); else wait_loads<0>();
-      const uint64_t keys = there64(p.t0, first_slot);
+      wait_loads();
+      const uint64_t keys = there64(p.t0, slot0);
       if (~keys) mend_v(p.t0, keys);
       __syncthreads();
       if (active) {
 #pragma unroll
-        for (int i = 0; i < NK * KS; ++i) {
+        for (int i = 0; i < 2 * KS; ++i) {
           const f32x16 zero = {};
-          sa[i % NK] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(lds + p.t0 % ST * TILE, i), q[i / NK], i < NK ? zero : sa[i % NK], 0, 0, 0);
+          sa[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(lds + (p.t0 & 1) * TILE, i), q[i >> 1], i < 2 ? zero : sa[i & 1], 0, 0, 0);
         }
         bool some = true;
         if (~keys || p.t0 * KT + KT > s.len) some = mask_scores(sa, p.t0, keys);
         float mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 16 * NK; ++i) mx = fmaxf(mx, sa[i >> 4][i & 15]);
+        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, sa[i >> 4][i & 15]);
         raise_max(mx, __shfl_xor(mx, 32), some);
       }
       __syncthreads();                 // K of the first tile has been read
@@ -786,39 +784,39 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
     int new_slot = 0;
     auto look_ahead = [&](int t) {     // what step t needs of the table
       if constexpr (SMALL) {
-        if (t + ST - 1 < t_end) slots_of_v(t + ST - 1);
-        if (t + ST < t_end) slots_of_k(t + ST);
+        if (t + 1 < t_end) slots_of_v(t + 1);
+        if (t + 2 < t_end) slots_of_k(t + 2);
         if (t + 1 < t_end) next_keys = there64(t + 1, 0);
       } else {
-        new_slot = slot_at(min(t + ST, t_end - 1) * KT);
+        new_slot = slot_at(min(t + 2, t_end - 1) * KT);
       }
     };
     if constexpr (SMALL) look_ahead(p.t0);
     // Holds: K of tile t + 1 and V^T of tile t in LDS, the scores of tile t in
     // sc.  Products and what is done under each are kept in this order by
     // fences; fragments are read three products (K) and a pair of them (V^T) ahead.
-    auto step = [&](int t, f32x16 (&sc)[NK], f32x16 (&sn)[NK]) {
-      const bool more = t + 1 < t_end, full = t + ST < t_end;
-      const _Float16* kt = lds + (t + 1) % ST * TILE;
-      const _Float16* vt = lds + (ST + t % ST) * TILE;
+    auto step = [&](int t, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
+      const bool more = t + 1 < t_end;
+      const _Float16* kt = lds + ((t + 1) & 1) * TILE;
+      const _Float16* vt = lds + (2 + (t & 1)) * TILE;
       f16x8 k0 = k_frag(kt, 0), k1 = k_frag(kt, 1), k2 = k_frag(kt, 2);
-      if (t + ST - 1 < t_end) load_v(t + ST - 1, q_slot[ST - 2]);
-      if (full) load_k(t + ST, q_slot[ST - 1]);
-      const uint64_t keys = SMALL ? next_keys : there64(t + 1, q_slot[0]);
-      const bool refill = full && t + 1 + ST >= w0 + kWindow;
+      if (more) load_v(t + 1, slot1);
+      if (t + 2 < t_end) load_k(t + 2, slot2);
+      const uint64_t keys = SMALL ? next_keys : there64(t + 1, slot1);
+      const bool refill = t + 3 >= w0 + kWindow && t + 2 < t_end;
       if (!refill) look_ahead(t + 1);
       if (active) {
         base = m == -INFINITY ? 0.f : m - kWideBias;
         f16x8 v0, v1;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < NK * KS; ++i) {
+        for (int i = 0; i < 2 * KS; ++i) {
           const f32x16 zero = {};
-          const f16x8 k3 = i + 3 < NK * KS ? k_frag(kt, i + 3) : k2;
-          if (i == NK * KS - 3) v0 = v_frag(vt, 0, 0);
-          if (i == NK * KS - 2) v1 = v_frag(vt, 0, 1);
+          const f16x8 k3 = i + 3 < 2 * KS ? k_frag(kt, i + 3) : k2;
+          if (i == 2 * KS - 3) v0 = v_frag(vt, 0, 0);
+          if (i == 2 * KS - 2) v1 = v_frag(vt, 0, 1);
           __builtin_amdgcn_sched_barrier(0);
-          sn[i % NK] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[i / NK], i < NK ? zero : sn[i % NK], 0, 0, 0);
+          sn[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[i >> 1], i < 2 ? zero : sn[i & 1], 0, 0, 0);
           k0 = k1;
           k1 = k2;
           k2 = k3;
@@ -828,7 +826,7 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
         bool some = true;
         if (more && (~keys || (t + 1) * KT + KT > s.len)) some = mask_scores(sn, t + 1, keys);
         float mx = -INFINITY, other = -INFINITY;
-        constexpr int PAIRS = NK * TN;             // of V^T fragments: 16 keys, 32 dimensions each
+        constexpr int PAIRS = 2 * TN;             // of V^T fragments: 16 keys, 32 dimensions each
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
@@ -839,14 +837,14 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
             __builtin_amdgcn_sched_barrier(0);
             o[d + (k & 1)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k & 1 ? v1 : v0, operand(k < 2 ? hi : lo, grp), o[d + (k & 1)], 0, 0, 0);
             const int slot = 4 * i + k;
-            if (NK * KS + slot < CARRY) carry(sc, NK * KS + slot);
-            if (slot < 2 * NK * TN)                // the max of the next scores under the first half
+            if (2 * KS + slot < CARRY) carry(sc, 2 * KS + slot);
+            if (slot < 4 * TN)                // the max of the next scores under the first half
 #pragma unroll
               for (int e = 0; e < 8 / TN; ++e) {
                 const int y = slot * (8 / TN) + e;
                 mx = fmaxf(mx, sn[y >> 4][y & 15]);
               }
-            if (slot == 2 * NK * TN) other = __shfl_xor(mx, 32);
+            if (slot == 4 * TN) other = __shfl_xor(mx, 32);
             __builtin_amdgcn_sched_barrier(0);
           }
           v0 = v2;
@@ -854,7 +852,7 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
         }
         if (more) raise_max(mx, other, some);
       }
-      if (full) wait_loads<AHEAD>(); else wait_loads<0>();
+      wait_loads();
       if (more && ~keys) mend_v(t + 1, keys);
       __syncthreads();
       if (refill) {
@@ -862,9 +860,8 @@ __global__ __launch_bounds__(64 * NW, HD == 128 && NW == 2 ? 1 : 2) void tree_wi
         look_ahead(t + 1);
       }
       if constexpr (!SMALL) {
-#pragma unroll
-        for (int i = 0; i + 1 < ST; ++i) q_slot[i] = q_slot[i + 1];
-        q_slot[ST - 1] = __builtin_amdgcn_readfirstlane(new_slot);
+        slot1 = slot2;
+        slot2 = __builtin_amdgcn_readfirstlane(new_slot);
       }
     };
     int t = p.t0;
@@ -1003,11 +1000,10 @@ void launch(const AttnTree& a, hipStream_t s) {
     else
       hipLaunchKernelGGL((tree_few_kernel<HD, R / kCols, false>), grid, dim3(64 * kFewWaves), 0, s, a);
   } else {
-    constexpr int NK = 2, ST = 2;
-    if (a.C < 32 * NK)
-      hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, NK, ST, true>), grid, dim3(2 * R), 0, s, a);
+    if (a.C < kTile)
+      hipLaunchKernelGGL((tree_wide_kernel<HD, true>), grid, dim3(2 * R), 0, s, a);
     else
-      hipLaunchKernelGGL((tree_wide_kernel<HD, R / 32, NK, ST, false>), grid, dim3(2 * R), 0, s, a);
+      hipLaunchKernelGGL((tree_wide_kernel<HD, false>), grid, dim3(2 * R), 0, s, a);
   }
   hipLaunchKernelGGL((tree_join_kernel<HD, R>), dim3((unsigned)(((int64_t)a.m * a.nq * (R <= 32 ? 4 : 1) + 3) / 4)), dim3(256), 0, s, a);
 }
