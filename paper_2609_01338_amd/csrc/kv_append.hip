@@ -36,7 +36,12 @@ namespace {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kRotRows = 4;      // rows per thread of a rotating workgroup
+// Rows per thread of a rotating workgroup.  By axes fewer: a row has one more trip to
+// memory, and its registers keep waves away (4099 f16 rows of 12 + 2 + 2 heads of 128,
+// 3 axes: 12.6 us with 4, 11.2 with 2, 10.4 with 1; 32 + 8 + 8 heads, 1 axis 29.2, 26.8,
+// 24.7; fp32 rows of 12 + 2 + 2 13.1, 11.8, 12.3).
+template <typename T, bool AXES>
+constexpr int rot_rows() { return !AXES ? 4 : sizeof(T) == 4 ? 2 : 1; }
 constexpr int kValRows = 64;     // rows and dimensions of a value tile
 constexpr int kValDims = 64;
 
@@ -85,7 +90,7 @@ __device__ __forceinline__ bool row_ok_axes(const KvAppend& a, int s, int p, con
 
 template <typename T, bool AXES>
 __device__ __forceinline__ void rotate_rows(const KvAppend& a, int m, int t, int items) {
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, kRotRows = rot_rows<T, AXES>();
   typedef typename Vec<T>::raw raw;
   const int halfd = a.hd / 2, per_head = halfd / N;
   const int rg = t / items, item = t - rg * items;
@@ -259,6 +264,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppend a, int m, int i
   const int b = blockIdx.x;
   if (b < rot_blocks) {
     const int t = b * 256 + threadIdx.x;
+    constexpr int kRotRows = rot_rows<T, AXES>();
     if (t < (m + kRotRows - 1) / kRotRows * items) rotate_rows<T, AXES>(a, m, t, items);
     return;
   }
@@ -273,8 +279,9 @@ int append_items(int nq, int nkv, int hd) {
 
 }  // namespace
 
-bool kv_append_fits(int m, int nq, int nkv, int hd) {
-  const int64_t groups = ((int64_t)m + kRotRows - 1) / kRotRows;
+bool kv_append_fits(int m, int nq, int nkv, int hd, bool axes) {
+  const int rows = axes ? rot_rows<_Float16, true>() : rot_rows<float, false>();
+  const int64_t groups = ((int64_t)m + rows - 1) / rows;
   const int64_t tiles = ((int64_t)m + kValRows - 1) / kValRows * ((nkv * hd + kValDims - 1) / kValDims);
   const int64_t threads = groups * append_items<float>(nq, nkv, hd);
   return threads < (int64_t(1) << 31) && threads / 256 + 1 + tiles <= kMaxBlocks;
@@ -282,7 +289,8 @@ bool kv_append_fits(int m, int nq, int nkv, int hd) {
 
 void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s) {
   const int items = f32 ? append_items<float>(a.nq, a.nkv, a.hd) : append_items<_Float16>(a.nq, a.nkv, a.hd);
-  const int rot = ((m + kRotRows - 1) / kRotRows * items + 255) / 256;
+  const int rows = !a.rope_pos ? rot_rows<float, false>() : f32 ? rot_rows<float, true>() : rot_rows<_Float16, true>();
+  const int rot = ((m + rows - 1) / rows * items + 255) / 256;
   const int tiles = (m + kValRows - 1) / kValRows * ((a.nkv * a.hd + kValDims - 1) / kValDims);
   const dim3 grid(rot + tiles), block(256);
   if (f32 && a.rope_pos)

@@ -161,7 +161,7 @@ constexpr int64_t kMaxBlocks = (1 << 24) - 1;
 // the sequences' chunk tables, and the rows' queries rotated (see mz.h,
 // mz_kv_append).  q, k, v: rows of fp32 or f16, strides in elements; C = 1 <<
 // cshift; hd 32, 64 or 128; nq 0 leaves the queries out.  Every pointer and
-// row 16-byte aligned.  Only for kv_append_fits(m, ...).  With rope_pos
+// row 16-byte aligned.  Only for kv_append_fits(m, ..., with rope_pos).  With rope_pos
 // ([n_axes][m], mz_kv_append_axes) pair i turns by the position on the axis in
 // bits 4 (i % 16) .. + 3 of axis[i / 16] (15: it is not turned), and pos is the
 // place alone; axes_used has a bit for each axis that a pair names.
@@ -180,7 +180,7 @@ struct KvAppend {
   unsigned axes_used;
 };
 constexpr int kAxes = 4, kAxisNone = 15;
-bool kv_append_fits(int m, int nq, int nkv, int hd);
+bool kv_append_fits(int m, int nq, int nkv, int hd, bool axes);
 void launch_kv_append(const KvAppend& a, int m, bool f32, hipStream_t s);
 
 // Attention of one token of every sequence over its chunks (see mz.h,

@@ -2216,7 +2216,7 @@ static mz_status append_entry(const mz_kv_append_args* args, const mz_rope_axes*
     if (k.k_stride % step || k.v_stride % step || k.q_stride % step || !aligned16(a.k) || !aligned16(a.v) ||
         !aligned16(a.rope_cs) || !aligned16(a.slab) || (a.n_q_heads && (!aligned16(a.q) || !aligned16(a.q_out))))
       fail(MZ_EINVAL, "rows, rope_cs, slab and q_out must lie on 16-byte boundaries");
-    if (!mzk::kv_append_fits(m, a.n_q_heads, a.n_kv_heads, a.head_dim)) fail(MZ_EINVAL, "too many rows");
+    if (!mzk::kv_append_fits(m, a.n_q_heads, a.n_kv_heads, a.head_dim, with_axes)) fail(MZ_EINVAL, "too many rows");
     check_stream(stream);
     if (m == 0) return;
     k.q = a.q;

@@ -322,12 +322,13 @@ def tree_oracle(a, lens=None, off=None):
                     if on.any():
                         # the score's sum of hd exact products and its scale, the exponent, exp2 (1 ulp): e on each weight,
                         # once above and once below the line; 22 bits of a weight; sums of n terms in runs of 32 and the
-                        # factors of the running max; weights below 2^-38 of the largest lose their last bits
+                        # factors of the running max; the lower half of a weight is within 2^-25 of 2^11 times the largest at the least,
+                        # below its normal range: 2^-36
                         part = (np.abs(kk[on]) @ np.abs(x)).max() / np.sqrt(hd)
                         e = (hd + 4) * U32 * part + 4 * U32 * np.abs(s[on] - s[on].max()).max() + 4 * U32
                         size = p[on] @ np.abs(vv[on])
                         bound[r, h * hd:(h + 1) * hd] = (2 * e + 2.0 ** -21 + 8 * (len(s) / 32 + 64) * U32) * size * (1 + U16) + \
-                            U16 * np.abs(o) + TINY16 + len(s) * 2.0 ** -38 * np.abs(vv[on]).max(0)
+                            U16 * np.abs(o) + TINY16 + len(s) * 2.0 ** -36 * np.abs(vv[on]).max(0)
                 out[r, h * hd:(h + 1) * hd] = o
     return out, bound, wrote
 
