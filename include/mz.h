@@ -868,7 +868,8 @@ typedef struct {
  * the most rows and sequences serves fewer), any content, not shared by calls
  * in flight together (two graphs that may run at once need two).  Errors:
  * EINVAL for the above, a NULL pointer, more work than 2^31 blocks of 32 keys,
- * q, slab, workspace or out off 16-byte boundaries, or a short workspace. */
+ * q, slab, workspace or out off 16-byte boundaries, out or workspace in one
+ * another or in what is read, or a short workspace. */
 mz_status mz_attention_tree(const mz_attention_tree_args *args, void *workspace, int64_t workspace_bytes,
                             void *stream);
 
@@ -907,7 +908,7 @@ typedef struct {
  * other sequence holds the chunks that are written.  Layers held in other
  * allocations take a call each.  Lengths below 0 count as 0, above 2^30 as
  * 2^30; head_dim 32, 64 or 128; m at most 2^30, may be 0; n_seq at most 2^20;
- * chunks as for mz_kv_append.  Errors: EINVAL for the above, a NULL pointer,
+ * n_layers at most 4096; chunks as for mz_kv_append.  Errors: EINVAL for the above, a NULL pointer,
  * outputs that are one another or an input, slab or layer_bytes off 16-byte
  * boundaries, layers that overlap, too many layers and sequences for a launch. */
 mz_status mz_tree_accept(const mz_tree_accept_args *args, void *stream);
@@ -972,7 +973,7 @@ int64_t mz_kv_pages_workspace_bytes(int32_t n_seq, int32_t n_table, int32_t n_sl
  * chunk_tokens.  No slot that is copied to is in another entry.  Layers in
  * other allocations take a call each.  max_copies may be 0.  head_dim 32, 64 or
  * 128, chunk_tokens a power of two >= 8, a slot below 2^31 bytes.  Errors:
- * EINVAL for the above, n_layers below 1, a NULL pointer, copies, slab or
+ * EINVAL for the above, n_layers outside 1..4096, a NULL pointer, copies, slab or
  * layer_bytes off 16-byte boundaries, layers that overlap. */
 mz_status mz_kv_copy(const int32_t *copies, const int32_t *n_copies, int32_t max_copies, void *slab,
                      int32_t n_slots, int32_t n_layers, int64_t layer_bytes, int32_t chunk_tokens,

@@ -210,6 +210,7 @@ void launch_attention_batch(AttnBatch a, int hd, void* ws, hipStream_t s);
 // the calls on trees and pages.
 constexpr int kTreeNodes = 1024;
 constexpr int kTreeSeqs = 1 << 20;
+constexpr int kCacheLayers = 4096;
 
 // Rows of the trees of n_seq sequences (see mz.h, mz_tree_plan); any output may be null.
 struct TreePlan {

@@ -2419,7 +2419,9 @@ static int64_t check_layers(const void* slab, int32_t n_layers, int64_t layer_by
   const int64_t slot_bytes = (int64_t)chunk_tokens * n_kv * head_dim * 4;
   if (slot_bytes > INT32_MAX) fail(MZ_EINVAL, "a chunk slot exceeds 2^31 - 1 bytes");
   if (!aligned16(slab) || layer_bytes % 16) fail(MZ_EINVAL, "slab and layer_bytes must lie on 16-byte boundaries");
+  if (n_layers > mzk::kCacheLayers) fail(MZ_EINVAL, "n_layers must be at most %d", mzk::kCacheLayers);
   if (n_layers > 1 && layer_bytes < n_slots * slot_bytes) fail(MZ_EINVAL, "the layers overlap");
+  if (n_layers > 1 && layer_bytes > (int64_t)1 << 48) fail(MZ_EINVAL, "layer_bytes exceeds 2^48");
   return slot_bytes;
 }
 
@@ -2471,9 +2473,13 @@ mz_status mz_attention_tree(const mz_attention_tree_args* args, void* workspace,
       fail(MZ_EINVAL, "q, slab, workspace and out must lie on 16-byte boundaries");
     if (mzk::attention_tree_units(a.m, a.n_seq, a.n_table, a.chunk_tokens, nq, nkv) > INT32_MAX)
       fail(MZ_EINVAL, "m rows of n_seq sequences of n_table chunks are too many");
+    const int64_t rows = (int64_t)a.m * nq * a.head_dim * 2, need = a.m ? mzk::attention_tree_ws_bytes(a.m, a.n_seq, nq, nkv, a.head_dim) : 0;
+    if (workspace_bytes < need) fail(MZ_EINVAL, "workspace too small");
+    check_apart({{a.out, rows}, {workspace, need}},
+                {{a.q, rows}, {a.row_off, ((int64_t)a.n_seq + 1) * 4}, {a.lens, (int64_t)a.n_seq * 4}, {a.slab, a.n_slots * slot_bytes},
+                 {a.mask, (int64_t)a.m * a.mask_words * 4}, {a.table, (int64_t)a.n_seq * a.n_table * 4}});
     check_stream(stream);
     if (a.m == 0) return;
-    if (workspace_bytes < mzk::attention_tree_ws_bytes(a.m, a.n_seq, nq, nkv, a.head_dim)) fail(MZ_EINVAL, "workspace too small");
     mzk::AttnTree t{};
     t.q = reinterpret_cast<const _Float16*>(a.q);
     t.row_off = a.row_off;

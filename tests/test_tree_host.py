@@ -85,6 +85,25 @@ def test_attention_tree_refusals(bad, match):
     refused(mz.mz_attention_tree, **{**ATTENTION, **bad}, match=match)
 
 
+APART = {**ATTENTION, "q_ptr": 2 * P, "row_off_ptr": 3 * P, "lens_ptr": 4 * P, "slab_ptr": 100 * P, "table_ptr": 5 * P, "mask_ptr": 6 * P,
+         "out_ptr": 7 * P, "ws_ptr": 2000 * P}
+
+
+@pytest.mark.parametrize("bad,match", [
+    (dict(out_ptr=2 * P + 64), "overlaps an input"), (dict(out_ptr=4 * P), "overlaps an input"), (dict(out_ptr=6 * P), "overlaps an input"),
+    (dict(out_ptr=100 * P + 1024), "overlaps an input"), (dict(table_ptr=2004 * P), "overlaps an input"), (dict(ws_ptr=100 * P), "overlaps an input"),
+    (dict(ws_ptr=7 * P), "two outputs"), (dict(out_ptr=2000 * P + 256), "two outputs"),
+])
+def test_attention_tree_outputs_that_overlap(bad, match):
+    refused(mz.mz_attention_tree, **{**APART, **bad}, match=match)
+
+
+@pytest.mark.parametrize("bad,match", [(dict(n_layers=4097), "at most 4096"), (dict(layer_bytes=(1 << 48) + 16), "2^48")])
+def test_layers_that_are_too_many_or_far(bad, match):
+    refused(mz.mz_tree_accept, **{**ACCEPT, **bad}, match=match)
+    refused(mz.mz_kv_copy, **{**COPY, **bad}, match=match)
+
+
 def test_attention_tree_workspace():
     need = mz.mz_attention_tree_workspace_bytes(9, 3, 8, 2, 64)
     assert need > 0
