@@ -55,7 +55,11 @@ __device__ __forceinline__ Seq seq_of(const AttnTree& a, int b) {
 }
 
 // Shares of `total` units: as many as there are workgroups, but of a.least units
-// at least, or where those are too few for the CUs, of a.fewest.
+// at least, or where those are too few for the CUs, of a.fewest.  Each share costs
+// a start (10 us until its first tile is there) and fp32 partials: tiles of 128
+// columns want 8 units (8 ragged sequences of up to 4096 keys 40.8 us; at least 4:
+// 44.6; 8 of 26 nodes at 4096 keys 58, at least 12: 66), and 3 where one tree is all there
+// is (26 nodes at 2048 keys 15.5 us; 1: 16.4, 2: 17.0, 4: 19.3).
 __device__ __forceinline__ int shares(const AttnTree& a, int total) {
   return max(1, min(a.wgs, max(total / a.least, min(kCus, total / a.fewest))));
 }
@@ -286,6 +290,10 @@ __device__ __forceinline__ uint64_t seen64(const AttnTree& a, const Seq& s, int 
 // block (t: first or second product), so that the eight scores of a lane are
 // eight consecutive keys: its mask is eight bits, and the P operand meets one
 // 16-byte run of V^T.  The waves' sums meet in LDS at a piece's end.
+//
+// Bound by the chain of a share: offsets, table, keys, one trip to memory each, then
+// the waves' sums.  One tree of 7 nodes at 2048 keys, 8 KV heads of 64 with 4 query
+// heads each, 8.3 us, 2 MB of keys.
 constexpr int kFewUnit = 128, kFewWaves = 4, kBlock = 32, kCols = 16;
 constexpr float kFewBias = 14.f;
 
@@ -510,13 +518,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
 // the loads would wait for them.
 //
 // Measured: 4 sequences of 24576 keys and 64 nodes, 8 KV heads of 128 with 4 query
-// heads each, 175 + 12 us (joining): 155 GFLOP with the lower halves at 0.88 PFLOP/s,
-// where products alone, at the clock that the power allows, take 112 (24 ns each a
-// SIMD; 13 at the full clock), loads alone 90.  Two waves a SIMD are little faster
-// than one (148 us against 161 of a smaller pipeline, from L2), and one workgroup of 256
-// columns a CU, which reads each key once, not twice, is as fast (184 us for 187) and
-// slower where trees are smaller.  32 ragged sequences of up to 8192 keys and 16 nodes 90 +
-// 11: 373 MB, loads alone 83.
+// heads each, 167-190 us as the power allows: 155 GFLOP with the weights' lower halves,
+// 122 us at the rate of a large f16 product (the matrix units are busy 51 % of
+// the cycles, at 1.7 GHz), loads alone 90.  One workgroup of 256 columns a CU,
+// which reads each key once, not twice, takes as long (184 for 187), and longer where
+// trees are smaller (32 ragged 129 for 101).  32 ragged sequences of up to 8192 keys and 16
+// nodes 90: 373 MB, loads alone 83.
 constexpr int kTile = 64, kWideWaves = 4;
 constexpr float kSlack = 4.f, kWideBias = 11.f;
 constexpr int kWindow = 64;
@@ -878,6 +885,7 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
 #pragma unroll
       for (int r = 0; r < 16; ++r) finite &= fabsf(o[t][r]) < INFINITY;
     const bool whole = p.t0 == 0 && p.t1 == s.units;
+    const bool other_bad = __shfl_xor((int)!finite, 32);      // of the column's other dimensions
     const int64_t row = (int64_t)(s.first + node) * a.nq + head;
     if (there && whole) {
       const float inv = m == -INFINITY ? 0.f : 1.0f / l;
@@ -890,8 +898,8 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
                                                                   (_Float16)(o[t][4 * r + 2] * inv), (_Float16)(o[t][4 * r + 3] * inv)};
     } else if (there) {
       const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * a.cols + w * 32 + col;
-      if (half == 0) a.ml[e0] = make_float2(m, l);
-      if (!finite) a.ml[e0].x = NAN;
+      const bool both = finite && !other_bad;
+      if (half == 0) a.ml[e0] = make_float2(both ? m : NAN, l);
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -908,7 +916,9 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
 // Joins the partials of every (row, query head) that several shares met, g0 ..
 // g1.  TPR of a workgroup's threads take one: HD / 4 lanes a partial, four
 // dimensions each, AHEAD of them in one trip to memory, and the groups of lanes meet in
-// LDS.  Rows with sums that are not finite are taken again.
+// LDS.  Rows with sums that are not finite are taken again.  (4 sequences of 64 nodes,
+// 34 MB of partials, 11.6 us; a workgroup a row there, or one for each share's columns, is
+// slower.  Few rows of many shares want a workgroup each: 3.6-4.8 us for 7 nodes.)
 template <int HD, int R>
 __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   constexpr int TPR = R <= 32 ? 256 : 64, ROWS = 256 / TPR, LPP = HD / 4, NG = TPR / LPP, AHEAD = R <= 32 ? 4 : 8;
@@ -984,12 +994,21 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
 
 int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
-// Columns of a tile for `cols` columns of an average sequence.
+// Columns of a tile for `cols` columns of an average sequence.  Tiles of 16 and 32
+// start sooner, tiles of 128 share what they load and feed the matrix units better.
+// us, with tiles of 16 / 32 / 128, sequences x nodes at keys (columns):
+//   32 + 8 heads of 64:  1 x 7 at 2048 (28) 12.4 / 12.4 / 13.6, 8 x 7 at 4096 (28) 32.4 / 25.0 / 25.6,
+//     64 x 4 at 2048 (16) 112 / 114 / 110, 1 x 26 at 2048 (104) 17.2 / 16.7 / 15.7,
+//     1 x 60 at 8192 (240) 49.0 / 31.5 / 28.7
+//   12 + 2 heads of 128:  8 x 5 at 16384 (30) 25.6 / 27.5 / 31.5, 2 x 5 at 4096 (30) 13.1 / 14.7 / 21.5,
+//     8 ragged of 26 60.6 / 45.8 / 40.9
+//   32 + 8 heads of 128:  4 x 5 at 1000 (20) 16.2 / 16.6 / 21.1, 32 x 5 at 4096 (20) 168 / 119 / 112,
+//     16 x 8 at 4096 (32) 93.7 / 69.4 / 65.8, 8 x 26 at 4096 (104) 156 / 102 / 59,
+//     4 x 64 at 24576 (256) 708 / 388 / 188
 int tile_cols(int64_t cols) { return cols <= 16 ? 16 : cols <= 32 ? 32 : 128; }
 
 // Columns of a partial, of a call of `cols` columns a KV head in all.
 int part_cols(int R, int64_t cols) { return cols < R ? (int)cols : R; }
-
 
 template <int HD, int R>
 void launch(const AttnTree& a, hipStream_t s) {

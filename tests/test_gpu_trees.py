@@ -421,6 +421,15 @@ def test_tree_attention_padded_batch():
     tree_case(counts, lens, 16, 4, 2, 64, seed=6, mask="any")
 
 
+def test_tree_attention_many_sequences_of_wide_trees():
+    """More sequences than a workgroup has threads, most of them with as many rows as make wide tiles."""
+    rng = np.random.default_rng(7)
+    counts, lens = rng.integers(17, 40, 300), rng.integers(0, 90, 300)
+    counts[rng.integers(0, 300, 40)] = 0
+    tree_case(counts, lens, 16, 4, 2, 64, seed=60, mask="tree")
+    tree_case(counts, lens, 64, 4, 2, 64, seed=61, mask=None)
+
+
 def test_tree_attention_a_row_that_sees_nothing():
     a = tree_inputs([4, 3], [0, 0], 16, 4, 2, 64, seed=7, mask="any")
     a["mask"][:] = 0
