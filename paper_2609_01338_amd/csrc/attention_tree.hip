@@ -129,7 +129,7 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_all, Share
   }
   const int n_units = total * a.nkv, nw = shares(a, n_units), g = blockIdx.x;
   if (g == 0 && threadIdx.x == 0) *a.total = n_units;
-  if (g >= nw) return false;
+  if (g >= nw || n_units == 0) return false;      // (no units: no sequence to begin in)
   sh.u = __builtin_amdgcn_readfirstlane((int)((uint64_t)g * n_units / nw));
   sh.end = __builtin_amdgcn_readfirstlane((int)(((uint64_t)g + 1) * n_units / nw));
   auto here = [&](int b) {

@@ -413,6 +413,13 @@ def test_tree_attention_no_sequence_has_rows():
     tree_case([0, 0], [5, 9], 16, 4, 2, 64, seed=5, behind=4)
 
 
+def test_tree_attention_no_sequence_has_rows_after_other_work():
+    """Nor is anything of what a workgroup's LDS held before taken for a sequence: wide and few columns."""
+    for nq, nkv, hd, behind in ((4, 2, 64, 4), (16, 1, 128, 40), (32, 2, 64, 700)):
+        tree_case([3, 60, 1], [500, 90, 7], 16, nq, nkv, hd, seed=nq)
+        tree_case([0, 0, 0], [5, 9, 0], 16, nq, nkv, hd, seed=5, behind=behind)
+
+
 def test_tree_attention_padded_batch():
     """Few of many sequences have rows."""
     counts, lens = np.zeros(700, int), np.zeros(700, int)
