@@ -293,7 +293,7 @@ __device__ __forceinline__ uint64_t seen64(const AttnTree& a, const Seq& s, int 
 //
 // Bound by the chain of a share: offsets, table, keys, one trip to memory each, then
 // the waves' sums.  One tree of 7 nodes at 2048 keys, 8 KV heads of 64 with 4 query
-// heads each, 8.3 us, 2 MB of keys.
+// heads each, 8.3 us, 4.2 MB of keys and values.
 constexpr int kFewUnit = 128, kFewWaves = 4, kBlock = 32, kCols = 16;
 constexpr float kFewBias = 14.f;
 
