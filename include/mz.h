@@ -787,7 +787,8 @@ int64_t mz_logits_rules_workspace_bytes(int32_t m, int32_t vocab);
  * branch from the tokens of mz_logits_rules and moves its keys together.
  * The nodes of sequence b's tree are the rows row_off[b] .. row_off[b + 1] - 1
  * of m (device int32 [n_seq + 1]; the caller sees that they ascend within 0..m;
- * what lies outside is cut off, and nothing out of range is read or written).
+ * what lies outside is cut off, and nothing out of range is read or written;
+ * where they descend, mz_attention_tree writes no row).
  * Node i lies behind its parent (parent < i; any other entry makes it a root,
  * which sees nothing of the tree but itself) and, until a branch is taken, in
  * the cache at position lens[b] + i, whatever its depth.  A tree has at most

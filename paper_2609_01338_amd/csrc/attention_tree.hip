@@ -69,25 +69,28 @@ __device__ __forceinline__ int share_of(int u, int nw, int total) {
   return (int)((((uint64_t)u + 1) * nw - 1) / (unsigned)total);
 }
 
-// Inclusive sum over the 64 NW threads; sum: of all.
+// Inclusive sum over the 64 NW threads; sum: of all, below 0 where any of them is bad.
 template <int NW>
-__device__ __forceinline__ int block_scan(int v, int* red, int& sum) {
+__device__ __forceinline__ int block_scan(int v, bool bad, int* red, int& sum) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int u = __shfl_up(v, o);
     if (lane >= o) v += u;
   }
+  const bool any_bad = __any(bad);
   __syncthreads();
-  if (lane == 63) red[w] = v;
+  if (lane == 63) red[w] = any_bad ? -1 : v;
   __syncthreads();
-  int before = 0;
+  int before = 0, top = 0;
   sum = 0;
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
     if (i < w) before += red[i];
     sum += red[i];
+    top |= red[i];
   }
+  if (top < 0) sum = -1;
   return v + before;
 }
 
@@ -95,6 +98,10 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& sum) {
 // in, whose units begin at `first`.  On the way, for the second kernel, of every row
 // its sequence's first unit, units (0: none has the row), tiles and first row: each
 // workgroup writes those of some sequences.  s: NT + NW + 2 ints in LDS.
+//
+// The number of units fits 31 bits because the sequences' rows are m at most, which
+// holds for offsets that ascend only: with others the sums below could pass 31 bits,
+// and shares begin where no sequence is.  One pair that descends leaves no units at all.
 struct Share {
   int u, end, b, first;
 };
@@ -107,15 +114,21 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_all, Share
     for (int i = threadIdx.x; i < before + a.m - behind; i += NT) a.rows[i < before ? i : behind + i - before] = make_int4(0, 0, 0, 0);
   }
   int total = 0, u_mine = 0, u_before = 0;
+  bool bad = false;
   auto units = [&](int b) {
     if (b >= a.n_seq) return 0;
     const Seq s = seq_of<R, UNIT>(a, b);
+    bad |= min(max(a.row_off[b + 1], 0), a.m) < s.first;
     return s.tiles * s.units;
   };
   for (int b0 = 0; b0 < a.n_seq; b0 += NT) {
     u_mine = units(b0 + threadIdx.x);
     int sum;
-    u_before = total + block_scan<NW>(u_mine, s_red, sum) - u_mine;
+    u_before = total + block_scan<NW>(u_mine, bad, s_red, sum) - u_mine;
+    if (sum < 0) {
+      total = 0;
+      break;
+    }
     total += sum;
     s_base[threadIdx.x] = u_before;
     __syncthreads();
@@ -143,7 +156,7 @@ __device__ __forceinline__ bool share_begin(const AttnTree& a, int* s_all, Share
     for (int b0 = 0; b0 < a.n_seq; b0 += NT) {
       u_mine = units(b0 + threadIdx.x);
       int sum;
-      u_before = run + block_scan<NW>(u_mine, s_red, sum) - u_mine;
+      u_before = run + block_scan<NW>(u_mine, false, s_red, sum) - u_mine;
       here(b0 + threadIdx.x);
       run += sum;
     }
@@ -927,6 +940,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   const int t = threadIdx.x, dl = t % LPP, group = t / LPP, pg = group % NG;
   const int64_t first = (int64_t)blockIdx.x * ROWS, at = first + t / TPR, rows = (int64_t)a.m * a.nq;
   const int total = *a.total, nw = shares(a, total);
+  if (total == 0) return;              // (and rows is not filled, if offsets descend)
   bool again = false;
   const int r = (int)(min(at, rows - 1) / a.nq), hq = (int)(at - (int64_t)r * a.nq), h = hq / a.group;
   const int4 row = a.rows[r];          // first unit, units, tiles, first row of its sequence

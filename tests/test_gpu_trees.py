@@ -389,6 +389,30 @@ def test_tree_attention_lengths(n):
     tree_case([35, 5], [n, n + 3], 32, 2, 1, 128, seed=n + 1, mask="any")
 
 
+@pytest.mark.parametrize("nq,hd", [(2, 64), (16, 128)])
+def test_tree_attention_offsets_that_descend(nq, hd):
+    """Rows of several sequences at once, whose units would pass 31 bits: no row is written.  (No chunk has a slot,
+    so that nothing is to be read in any case.)"""
+    torch = torch_cuda()
+    m, C = 1024, 256
+    for n_seq, n_table, off in ((3, 4, [0, 5, 3, 8]), (3, 4, [0, 8, 8, 7]), (700, 4, [0] * 256 + [9, 8] + [9] * 443),
+                                (2048, 16384 // (nq // 2), [0, m] * 1024 + [0]), (300, 32768, [0, m] * 150 + [0])):
+        report("attention_tree", n_seq=n_seq, n_table=n_table, off=off[:8], nq=nq, hd=hd)
+        assert len(off) == n_seq + 1
+        table = full((n_seq, n_table), -1)
+        lens = full(n_seq, n_table * C - 100)
+        q, slab = full((m, nq * hd), 1.0, torch.float16), full((1, 2 * C * hd), 1.0, torch.float16)
+        need = mz.mz_attention_tree_workspace_bytes(m, n_seq, nq, 1, hd)
+        ws, out, d_off = torch.full((need // 4 + 1,), float("nan"), device="cuda"), full((m, nq * hd), 7.0, torch.float16), dev(np.array(off, np.int32))
+        mz.mz_attention_tree(ptr(q), m, ptr(d_off), ptr(lens), n_seq, ptr(slab), 1, ptr(table), n_table, C, nq, 1, hd, ptr(ws), need, ptr(out), stream())
+        torch.cuda.synchronize()
+        assert bool((out == 7).all())
+    d_off.copy_(dev(np.minimum(np.arange(n_seq + 1), m).astype(np.int32)))      # the same workspace, offsets that ascend: no key has a slot
+    mz.mz_attention_tree(ptr(q), m, ptr(d_off), ptr(lens), n_seq, ptr(slab), 1, ptr(table), n_table, C, nq, 1, hd, ptr(ws), need, ptr(out), stream())
+    torch.cuda.synchronize()
+    assert not bool(out[:n_seq].any()) and bool((out[n_seq:] == 7).all())      # (the rows behind are of no tree)
+
+
 @pytest.mark.parametrize("C", [8, 32, 256])
 def test_tree_attention_shared_by_many_workgroups(C):
     tree_case([3, 1, 5], [9000, 40, 6100], C, 4, 2, 64, seed=C)
