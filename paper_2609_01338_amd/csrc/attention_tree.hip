@@ -584,10 +584,10 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
   // LDS.  (Wait states lie between the write of M0, and a vector instruction's of the
   // base, and the load that reads them.)
   auto fetch = [&](const uint8_t* from, int to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds0 + to * 2), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds0 + to * 2), "v"(from) : "memory", "m0");
   };
   auto fetch_from = [&](uint64_t base, unsigned at, int to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds0 + to * 2), "v"(at), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds0 + to * 2), "v"(at), "s"(base) : "memory", "m0");
   };
 
   Seq s = seq_of<R, UNIT>(a, sh.b);

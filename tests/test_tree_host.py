@@ -3,7 +3,9 @@ host before anything is enqueued, so they need no GPU.  The device pointers are
 never followed."""
 
 import ctypes
+import glob
 import os
+import re
 
 import pytest
 
@@ -183,3 +185,16 @@ def test_copy_refusals(bad, match):
 
 def test_copy_of_nothing():
     mz.mz_kv_copy(**{**COPY, "max_copies": 0, "copies_ptr": 0, "n_copies_ptr": 0})
+
+
+def test_assembly_that_writes_m0_says_so():
+    """The compiler may hold a value of its own in M0 across a block that does not name it."""
+    seen = 0
+    for path in glob.glob(os.path.join(os.path.dirname(mz.__file__), "csrc", "*")):
+        with open(path) as f:
+            text = f.read()
+        for block in re.findall(r"\basm\b(?:\s+volatile)?\s*\(.*?\)\s*;", text, re.S):
+            if re.search(r"\bm0\s*,", block.split("::")[0]):
+                seen += 1
+                assert '"m0"' in block, (os.path.basename(path), block)
+    assert seen >= 6
