@@ -859,7 +859,9 @@ typedef struct {
  * outside 0..n_slots-1 is left out, a row that sees no key gets zeros, and rows
  * of no tree are not written.  What slots hold at keys that no row sees is
  * never used, and what a row does not see does not enter its output, be it NaN
- * or infinite.  Scores, sums and joins are fp32, and the softmax weights keep 22
+ * or infinite: such a key changes no bit of it, such a value that it is summed
+ * in another order, as are the rows that see either, one (row, head) after the
+ * other, which takes long.  Scores, sums and joins are fp32, and the softmax weights keep 22
  * bits for the product with the values.  head_dim 64 or 128, n_q_heads a
  * multiple of n_kv_heads with a group of at most 16, chunk_tokens a power of
  * two >= 8, n_table * chunk_tokens at most 2^30, a slot below 2^31 bytes, m *

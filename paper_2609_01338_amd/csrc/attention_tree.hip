@@ -16,8 +16,8 @@
 // output's only rounding to fewer bits is its own.  Both enter the same fp32
 // sums.  A weight of 0 removes what a node does not see, unless the value is
 // infinite or NaN: then sums that are not finite show it, and the columns that
-// they belong to are taken again, a (row, head) at a time, with fp32 products of
-// what the row sees alone.
+// they belong to, and no others, are taken again, a (row, head) at a time, with fp32
+// products of what the row sees alone.
 #include <algorithm>
 
 #include "mz_kernels.h"
@@ -487,15 +487,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
         for (int v = 0; v < kFewWaves; ++v) acc[e] += wt[v] * s_o[v][dim >> 4][dim & 3][((dim >> 2) & 3) * 16 + c];
         finite &= fabsf(acc[e]) < INFINITY;
       }
-      const int bad = __syncthreads_or(!finite);
-      if (bad && p.t0 == 0 && p.t1 == s.units) {
-        for (int y = p.tile * R + nb * kCols, k = 0; k < kCols && y / a.group < s.nodes; ++k, ++y)
-          row_again<HD, 64 * kFewWaves>(a, s, sh.b, s.first + y / a.group, p.h * a.group + y % a.group, &s_o[0][0][0][0], s_again);
-        continue;
-      }
-      if (i >= s.nodes) continue;
+      const bool whole = p.t0 == 0 && p.t1 == s.units;
+      bool bad = false;                // the column's sums
+      if (__syncthreads_or(!finite && i < s.nodes))
+        for (int y = p.tile * R + nb * kCols, k = 0; k < kCols && y / a.group < s.nodes; ++k, ++y) {
+          const int again = __syncthreads_or(!finite && c == k);
+          if (c == k) bad = again;
+          if (again && whole)
+            row_again<HD, 64 * kFewWaves>(a, s, sh.b, s.first + y / a.group, p.h * a.group + y % a.group, &s_o[0][0][0][0], s_again);
+        }
+      if (i >= s.nodes || (bad && whole)) continue;
       const int64_t row = (int64_t)(s.first + i) * a.nq + head;
-      if (p.t0 == 0 && p.t1 == s.units) {
+      if (whole) {
         typedef _Float16 out_vec __attribute__((ext_vector_type(DPT)));
         const float inv = mx == -INFINITY ? 0.f : 1.0f / den;
         out_vec y;
@@ -899,8 +902,9 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
       for (int r = 0; r < 16; ++r) finite &= fabsf(o[t][r]) < INFINITY;
     const bool whole = p.t0 == 0 && p.t1 == s.units;
     const bool other_bad = __shfl_xor((int)!finite, 32);      // of the column's other dimensions
+    const bool bad = !finite || other_bad;
     const int64_t row = (int64_t)(s.first + node) * a.nq + head;
-    if (there && whole) {
+    if (there && whole && !bad) {
       const float inv = m == -INFINITY ? 0.f : 1.0f / l;
       _Float16* out = a.out + row * HD + 4 * half;
 #pragma unroll
@@ -909,19 +913,19 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
         for (int r = 0; r < 4; ++r)
           *reinterpret_cast<f16x4*>(out + t * 32 + 8 * r) = f16x4{(_Float16)(o[t][4 * r] * inv), (_Float16)(o[t][4 * r + 1] * inv),
                                                                   (_Float16)(o[t][4 * r + 2] * inv), (_Float16)(o[t][4 * r + 3] * inv)};
-    } else if (there) {
+    } else if (there && !whole) {
       const int64_t e0 = (int64_t)(2 * g + (p.t0 == 0)) * a.cols + w * 32 + col;
-      const bool both = finite && !other_bad;
-      if (half == 0) a.ml[e0] = make_float2(both ? m : NAN, l);
+      if (half == 0) a.ml[e0] = make_float2(bad ? NAN : m, l);
 #pragma unroll
       for (int t = 0; t < TN; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           *reinterpret_cast<f32x4*>(a.part + e0 * HD + t * 32 + 8 * r + 4 * half) = f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]};
     }
-    if (whole && __syncthreads_or(there && !finite))
+    if (whole && __syncthreads_or(there && bad))
       for (int y = p.tile * R, k = 0; k < R && y / a.group < s.nodes; ++k, ++y)
-        row_again<HD, 64 * NW>(a, s, sh.b, s.first + y / a.group, p.h * a.group + y % a.group, reinterpret_cast<float*>(lds), s_again);
+        if (__syncthreads_or(bad && w * 32 + col == k))
+          row_again<HD, 64 * NW>(a, s, sh.b, s.first + y / a.group, p.h * a.group + y % a.group, reinterpret_cast<float*>(lds), s_again);
   }
 }
 
@@ -979,17 +983,11 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
     s_l[group] = l;
   }
   s_acc[group][dl] = acc;
-  if (__syncthreads_or(again)) {
-    for (int k = 0; k < ROWS && first + k < rows; ++k) {
-      const int r = (int)((first + k) / a.nq), hq = (int)(first + k - (int64_t)r * a.nq);
-      if (!a.rows[r].y) continue;
-      int b = 0;                       // the row's sequence, the last that begins with it and has rows
-      while (b + 1 < a.n_seq && !(a.row_off[b] <= r && r < a.row_off[b + 1])) ++b;
-      row_again<HD, 256>(a, seq_of<R, 1>(a, b), b, r, hq, reinterpret_cast<float*>(s_acc), s_m);
-    }
-    return;
-  }
-  if (pg == 0 && n > 1) {
+  unsigned bad = 0;                    // a bit for each of the rows that are taken again
+  if (__syncthreads_or(again))
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) bad |= (unsigned)(__syncthreads_or(again && t / TPR == k) != 0) << k;
+  if (pg == 0 && n > 1 && !((bad >> (t / TPR)) & 1)) {
     float top = -INFINITY, den = 0.f;
 #pragma unroll
     for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[group + i]);
@@ -1003,6 +1001,15 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
     const float inv = top == -INFINITY ? 0.f : 1.0f / den;
     *(reinterpret_cast<f16x4*>(a.out + at * HD) + dl) =
         f16x4{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv), (_Float16)(acc[3] * inv)};
+  }
+  if (!bad) return;
+  __syncthreads();                     // the others' sums have been read
+  for (int k = 0; k < ROWS; ++k) {
+    if (!((bad >> k) & 1)) continue;
+    const int r = (int)((first + k) / a.nq), hq = (int)(first + k - (int64_t)r * a.nq);
+    int b = 0;                         // the row's sequence, the last that begins with it and has rows
+    while (b + 1 < a.n_seq && !(a.row_off[b] <= r && r < a.row_off[b + 1])) ++b;
+    row_again<HD, 256>(a, seq_of<R, 1>(a, b), b, r, hq, reinterpret_cast<float*>(s_acc), s_m);
   }
 }
 

@@ -528,6 +528,27 @@ def test_tree_attention_wide_trees_and_what_a_row_does_not_see(C, n, bad):
     tree_check(a, tree_run(a), f"{bad}")
 
 
+@pytest.mark.parametrize("counts,lens,nq,nkv,hd,C", [
+    ([12, 5], [40, 7], 4, 2, 64, 16), ([12, 5], [40, 7], 12, 2, 128, 64), ([6, 5], [9000, 40], 4, 2, 64, 64), ([9, 3], [5000, 40], 6, 2, 128, 8),
+    ([24, 9], [30, 7], 8, 1, 64, 8), ([40, 20], [200, 7], 4, 2, 64, 64), ([40, 30], [5000, 7], 4, 2, 64, 64), ([21, 9], [4000, 7], 6, 1, 128, 16)])
+def test_tree_attention_bits_of_rows_that_do_not_see_a_key_of_nan(counts, lens, nq, nkv, hd, C):
+    """A key of NaN changes the rows that see it, in its head, and not a bit of the others: few and many columns, alone in
+    a workgroup's share and cut over several."""
+    a = tree_inputs(counts, lens, C, nq, nkv, hd, seed=C + nq, mask="tree")
+    clean = tree_run(a).cpu().numpy()
+    sees = np.zeros((len(a["q"]), nq), bool)
+    for b, node in ((0, 3), (1, 2)):
+        at = a["lens"][b] + node
+        a["slab"][a["table"][b, at // C]].reshape(2, -1)[0].reshape(C, nkv * hd)[at % C, 3] = np.nan
+        sees[a["off"][b]:a["off"][b + 1], :nq // nkv] = ((a["mask"][a["off"][b]:a["off"][b + 1], 0] >> node) & 1)[:, None].astype(bool)
+    got = tree_run(a)
+    tree_check(a, got)
+    got, sees = got.cpu().numpy(), np.repeat(sees, hd, 1)
+    assert sees.any() and not sees[:a["off"][-1], :(nq // nkv) * hd].all()
+    assert np.isnan(got[sees]).all()
+    assert np.array_equal(got[~sees].view(np.uint16), clean[~sees].view(np.uint16))
+
+
 @pytest.mark.parametrize("C", [8, 64, 256])
 def test_tree_attention_a_value_that_all_rows_see_is_infinite(C):
     a = tree_inputs([24, 9], [700, 7], C, 8, 1, 64, seed=C, mask="any")
