@@ -97,7 +97,8 @@ __device__ __forceinline__ int block_scan(int v, bool bad, int* red, int& sum) {
 // A workgroup's share [u, end) of the units, and the sequence that it begins
 // in, whose units begin at `first`.  On the way, for the second kernel, of every row
 // its sequence's first unit, units (0: none has the row), tiles and first row: each
-// workgroup writes those of some sequences.  s: NT + NW + 2 ints in LDS.
+// workgroup writes those of some sequences.  (Every workgroup looks through all sequences:
+// 1.6 ms for 2^18 of them, nearly all without rows.)  s: NT + NW + 2 ints in LDS.
 //
 // The number of units fits 31 bits because the sequences' rows are m at most, which
 // holds for offsets that ascend only: with others the sums below could pass 31 bits,
@@ -935,7 +936,8 @@ __global__ __launch_bounds__(64 * kWideWaves, 2) void tree_wide_kernel(AttnTree 
 // dimensions each, AHEAD of them in one trip to memory, and the groups of lanes meet in
 // LDS.  Rows with sums that are not finite are taken again.  (4 sequences of 64 nodes,
 // 34 MB of partials, 11.6 us; a workgroup a row there, or one for each share's columns, is
-// slower.  Few rows of many shares want a workgroup each: 3.6-4.8 us for 7 nodes.)
+// slower.  Few rows of many shares want a workgroup each: 3.6-4.8 us for 7 nodes.  A row
+// finds its sequence by halves: 8 of 2^18 sequences with infinite values 40 -> 3 ms.)
 template <int HD, int R>
 __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   constexpr int TPR = R <= 32 ? 256 : 64, ROWS = 256 / TPR, LPP = HD / 4, NG = TPR / LPP, AHEAD = R <= 32 ? 4 : 8;
@@ -1007,8 +1009,14 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   for (int k = 0; k < ROWS; ++k) {
     if (!((bad >> k) & 1)) continue;
     const int r = (int)((first + k) / a.nq), hq = (int)(first + k - (int64_t)r * a.nq);
-    int b = 0;                         // the row's sequence, the last that begins with it and has rows
-    while (b + 1 < a.n_seq && !(a.row_off[b] <= r && r < a.row_off[b + 1])) ++b;
+    int b = 0;                         // the row's sequence: the last that begins at or before it
+    for (int behind = a.n_seq; behind - b > 1;) {
+      const int mid = (b + behind) >> 1;
+      if (a.row_off[mid] <= r)
+        b = mid;
+      else
+        behind = mid;
+    }
     row_again<HD, 256>(a, seq_of<R, 1>(a, b), b, r, hq, reinterpret_cast<float*>(s_acc), s_m);
   }
 }

@@ -489,6 +489,21 @@ def test_tree_attention_chunks_without_a_slot():
         tree_check(a, tree_run(a), f"chunks of {C}")
 
 
+@pytest.mark.parametrize("nq,nkv", [(4, 2), (16, 1)])
+def test_tree_attention_of_many_sequences_with_infinite_values(nq, nkv):
+    """Rows cut over several shares, far behind in a batch of which few sequences have rows, are taken again."""
+    counts, lens = np.zeros(150000, int), np.zeros(150000, int)
+    for b, t, n in ((0, 2, 100), (3, 5, 6000), (70001, 1, 9000), (149998, 4, 8000), (149999, 1, 70)):
+        counts[b], lens[b] = t, n
+    a = tree_inputs(counts, lens, 256, nq, nkv, 64, seed=64, mask="tree")
+    for b, at, d in ((3, 17, 2), (70001, 8999, 5), (149998, 4000, 60), (149998, 8001, 9)):
+        a["slab"][a["table"][b, at // 256]].reshape(2, -1)[1].reshape(-1, 256)[d, at % 256] = np.inf
+    report("attention_tree", n_seq=len(lens), nq=nq, nkv=nkv)
+    out = tree_run(a)
+    tree_check(a, out)
+    assert np.isinf(out.cpu().numpy()[:13]).sum() >= 5 * nq // nkv
+
+
 @pytest.mark.parametrize("C", [8, 64])
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 def test_tree_attention_what_a_row_does_not_see(bad, C):
