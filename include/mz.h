@@ -795,7 +795,8 @@ int64_t mz_logits_rules_workspace_bytes(int32_t m, int32_t vocab);
  * 1024 nodes where its parents or a mask are given, and at most 32 mask_words
  * with a mask; the rows of further nodes count as rows of no tree.  Without
  * parents and mask the nodes are a chain, of any length: drafts without
- * branches, or the next piece of every prompt.  Offsets, parents, lengths and
+ * branches, or the next piece of every prompt (of which mz_tree_accept looks at
+ * the first 1024 nodes).  Offsets, parents, lengths and
  * tables are read on the device, as for the calls above, and what is said there
  * about graphs, streams and allocation holds here too. */
 
@@ -903,7 +904,11 @@ typedef struct {
  * token that was taken before the step), then, as long as there is one, the
  * lowest child whose token is its parent's choice.  With the choice of a greedy
  * or of a sampled token (mz_logits_rules) at every node, the tokens that are
- * kept are what the model would have produced one at a time.  Then position
+ * kept are what the model would have produced one at a time.  A call looks at
+ * the first 1024 nodes of a tree, of a chain without parents too, so accepted
+ * is 1024 at most; next then is the last one's choice, and of a longer chain a
+ * call with row_off 1024 further on and lens = len_out takes what follows, if
+ * its first token is next.  Then position
  * lens[b] + path[i] of the cache moves to lens[b] + i, keys and values, in each
  * layer, so that the sequence goes on at len_out.  All other positions stay as
  * they are; a move from or to a chunk without a slot (an entry outside

@@ -9,15 +9,16 @@
 // whatever the depth, and the depth is their bits' number.  It is bound by its launch:
 // 2.1 us for one tree of 7 nodes, 3.0 for 64 trees of 61.
 //
-// Accept.  One wave walks from the root, 64 nodes in a look for the child that
-// holds the parent's choice.  Then the keys and values move.  Of the keys a thread
-// owns 16 bytes of the rows for all of the branch, eight places at a time, read
-// before they are written.  Of V^T a value moves within a row of its own, a line of
-// memory for two bytes, so what counts is lines: four lanes own the 64 bytes
-// of a dimension that 32 places lie in, and write what changes of them as 16 bytes,
-// several layers at a time.  Since path[i] >= i ascends, what has been written (places
-// up to i) is never what is still to be read (path[j] > i for j > i), so nothing waits
-// for another wave.
+// Accept.  One wave walks from the root, 64 nodes in a look for the child that holds
+// the parent's choice, among the first 1024 nodes, whose parents, tokens and choices
+// LDS holds (of a longer chain the next call takes the rest).  Then the keys and
+// values move.  Of the keys a thread owns 16 bytes of the rows for all of the branch,
+// eight places at a time, read before they are written.  Of V^T a value moves within
+// a row of its own, a line of memory for two bytes, so what counts is lines: four
+// lanes own the 64 bytes of a dimension that 32 places lie in, and write what
+// changes of them as 16 bytes, several layers at a time.  Since path[i] >= i ascends,
+// what has been written (places up to i) is never what is still to be read (path[j]
+// > i for j > i), so nothing waits for another wave.
 //
 // The branches of 64 trees of 61 nodes in 32 layers of 8 KV heads of 128 take 69 us:
 // the walk 15, reading 4, and writing 1.2 million lines of V^T, of which 2 bytes change,

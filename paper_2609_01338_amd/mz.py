@@ -615,7 +615,7 @@ def mz_tree_accept(row_off_ptr: int, token_ptr: int, choice_ptr: int, lens_ptr: 
                    path_ptr: int, next_ptr: int, len_out_ptr: int, stream: Optional[int] = None, parent_ptr: int = 0,
                    slab_ptr: int = 0, n_slots: int = 0, n_layers: int = 0, layer_bytes: int = 0, table_ptr: int = 0,
                    n_table: int = 0, chunk_tokens: int = 0, n_kv: int = 0, head_dim: int = 0) -> None:
-    """Without layers (n_layers 0) the branches are taken and nothing is moved."""
+    """Without layers (n_layers 0) the branches are taken and nothing is moved.  At most 1024 nodes of a sequence are looked at."""
     a = mz_tree_accept_args(n_seq, m, row_off_ptr, parent_ptr, token_ptr, choice_ptr, lens_ptr, accepted_ptr, path_ptr, next_ptr,
                             len_out_ptr, n_layers, n_slots, slab_ptr, layer_bytes, table_ptr, n_table, chunk_tokens, n_kv, head_dim)
     _check(lib().mz_tree_accept(ctypes.byref(a), stream), None)

@@ -763,6 +763,35 @@ def test_accept_chains():
     accept_case([1100], [7], 64, 1, 32, 1, seed=3, tree=False, vocab=1)
 
 
+@pytest.mark.parametrize("n,miss", [(1023, None), (1024, None), (1025, None), (2500, None), (2500, 1022), (2500, 1023), (2500, 1024), (5000, 3000)])
+def test_accept_chains_of_more_nodes_than_a_call_takes(n, miss):
+    """A call takes the first 1024 nodes, calls on the rest what follows: together the whole branch; miss: the node whose
+    choice is not the next one's token."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(n)
+    token = rng.integers(0, 1000, n).astype(np.int32)
+    choice = np.append(token[1:], 5).astype(np.int32)
+    if miss is not None:
+        choice[miss] = (choice[miss] + 1) % 1000
+    whole = n if miss is None else miss + 1
+    d_token, d_choice, lens, at, total = dev(token), dev(choice), dev(np.array([77], np.int32)), 0, 0
+    while True:
+        report("accept", n=n, miss=miss, at=at)
+        accepted, path, nxt, len_out, off = full(1), full(n), full(1), full(1), dev(np.array([at, n], np.int32))
+        mz.mz_tree_accept(ptr(off), ptr(d_token), ptr(d_choice), ptr(lens), 1, n, ptr(accepted), ptr(path), ptr(nxt), ptr(len_out), stream())
+        torch.cuda.synchronize()
+        count = min(whole - at, 1024)
+        want = np.full(n, -1)
+        want[:at] = 7      # rows before the chain are left as they are
+        want[at:at + count] = np.arange(count)
+        assert accepted.tolist() == [count] and nxt.tolist() == [choice[at + count - 1]] and len_out.tolist() == [77 + at + count]
+        assert np.array_equal(path.cpu().numpy(), want)
+        total, lens, at = total + count, len_out, at + count
+        if at == n or nxt.item() != token[at]:
+            break
+    assert total == whole
+
+
 def test_accept_moves_a_long_branch():
     """A branch of more places than a thread holds at once, every place moved by one."""
     n = 40
