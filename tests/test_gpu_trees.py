@@ -641,6 +641,118 @@ def test_tree_attention_far_slots():
     tree_check(a, tree_run(a, d))
 
 
+# The same for trees of so many columns that tiles of 128 are taken: (nq, nkv, hd).
+WIDE_HEADS = [(8, 1, 64), (12, 2, 128), (32, 2, 64)]
+
+
+def wide_inputs(counts, lens, C, heads, **kw):
+    """tree_inputs whose average sequence has more than 32 columns: rows and heads of a KV head."""
+    a = tree_inputs(counts, lens, C, *heads, **kw)
+    assert -(-len(a["q"]) // len(counts)) * (heads[0] // heads[1]) > 32
+    return a
+
+
+@pytest.mark.parametrize("heads", WIDE_HEADS)
+@pytest.mark.parametrize("C", [8, 32, 64, 256])
+def test_wide_trees_chunks_without_a_slot(C, heads):
+    """Missing first, middle, last and neighbouring chunks, the trees' own, and all of a sequence; one share and many."""
+    for n, seed in ((300, 70), (700, 71), (6000, 72)):
+        a = wide_inputs([24, 9, 5], [n, 100, 2], C, heads, seed=seed + C, mask="any")
+        a["table"][0, [0, n // 2 // C, n // 2 // C + 1, n // C]] = (-1, 1 << 30, a["slab"].shape[0], -(1 << 31))
+        a["table"][1, 70 // C] = -3
+        a["table"][2] = -7
+        out = tree_run(a)
+        tree_check(a, out, f"chunks of {C}, {n} keys")
+        assert not out[33:38].any()
+
+
+@pytest.mark.parametrize("heads", WIDE_HEADS)
+@pytest.mark.parametrize("C", [16, 64])
+def test_wide_trees_lengths_out_of_range(C, heads):
+    a = wide_inputs([24, 13, 2], [220, 0, 460], C, heads, seed=73, mask="any", extra_table=0)
+    wide = a["table"].shape[1]
+    for b in (0, 2):      # tables of full chunks
+        a["table"][b] = np.arange(wide) % a["slab"].shape[0]
+    a["table"][1] = np.where((a["table"][1] >= 0) & (a["table"][1] < a["slab"].shape[0]), a["table"][1], 0)
+    a["slab"], top = np.nan_to_num(a["slab"]), wide * C
+    for lens in ([-5, 0, 60], [top, 0, top - 1], [(1 << 31) - 1, -(1 << 31), top + 1], [top - 9, top - 64, top - 65]):
+        a["lens"] = np.array(lens, np.int32)
+        tree_check(a, tree_run(a), f"lengths {lens}")
+
+
+@pytest.mark.parametrize("C", [16, 64])
+@pytest.mark.parametrize("heads", [(8, 1, 128), (32, 2, 64)])
+def test_wide_trees_far_slots(C, heads):
+    """Slots past 2^32 bytes of the slab."""
+    torch = torch_cuda()
+    a = wide_inputs([25, 9], [1500, 64], C, heads, seed=74, mask="any")
+    n_slots = (1 << 32) // (C * heads[1] * heads[2] * 4) + a["slab"].shape[0] + 9
+    slab = torch.full((n_slots, 2 * C * heads[1] * heads[2]), float("nan"), device="cuda", dtype=torch.float16)
+    far = n_slots - a["slab"].shape[0]
+    slab[far:] = dev(a["slab"])
+    table = a["table"].copy()
+    for b in range(2):
+        c = (int(a["lens"][b]) + (25, 9)[b] + C - 1) // C
+        table[b, :c] += far
+    tree_check(a, tree_run(a, dict(q=dev(a["q"]), off=dev(a["off"]), lens=dev(a["lens"]), slab=slab, table=dev(table), mask=dev(a["mask"]))))
+
+
+@pytest.mark.parametrize("heads", WIDE_HEADS)
+@pytest.mark.parametrize("C", [16, 128])
+def test_wide_trees_large_scores(C, heads):
+    a = wide_inputs([24, 13], [500, 31], C, heads, seed=75, spread=30.0)
+    tree_check(a, tree_run(a))
+
+
+@pytest.mark.parametrize("counts,lens,heads", [([7, 2], [900, 30], (4, 2, 64)), ([24, 13], [900, 30], (8, 1, 64)), ([24, 13], [900, 5000], (12, 2, 128))])
+@pytest.mark.parametrize("way", ["up", "down", "steps", "one at the end"])
+def test_tree_attention_scores_that_rise_along_the_keys(counts, lens, heads, way):
+    """The largest score grows by less and by more than what a running maximum may fall behind, or comes last."""
+    C = 32
+    a = tree_inputs(counts, lens, C, *heads, seed=76, mask=None)
+    nq, nkv, hd = heads
+    a["q"][:] = np.random.default_rng(77).uniform(0.5, 1.0, a["q"].shape)
+    dkv = nkv * hd
+    for b, n in enumerate(np.array(lens) + counts):
+        j = np.arange(n)
+        high = {"up": j / n, "down": 1 - j / n, "steps": (j // 70) % 5 / 5 + (j // 350) / 20, "one at the end": (j == n - 1) * 1.0}[way] * 12 / np.sqrt(hd)
+        for i, slot in enumerate(a["table"][b, :(n + C - 1) // C]):
+            t = min(C, n - i * C)
+            a["slab"][slot].reshape(2, -1)[0].reshape(C, dkv)[:t] = high[i * C:i * C + t, None]
+    tree_check(a, tree_run(a))
+
+
+@pytest.mark.parametrize("counts,lens,heads", [([6, 3], [400, 31], (4, 2, 64)), ([3, 2], [700, 31], (4, 1, 128)),
+                                               ([24, 13], [300, 31], (8, 1, 64)), ([24, 13], [900, 31], (8, 1, 128)), ([33], [2000], (8, 1, 128))])
+@pytest.mark.parametrize("C", [16, 64, 256])
+def test_tree_attention_lower_halves_of_the_weights(C, counts, lens, heads):
+    """Two kinds of keys in turn, with values of 1 and -1: a weight's rounding to f16 is the same for all keys of a kind and stays
+    in the sum.  The same sums with weights of f16 lie outside of the bound, which so holds the further bits."""
+    a = tree_inputs(counts, lens, C, *heads, seed=78, mask=None, behind=0)
+    (nq, nkv, hd), rng = heads, np.random.default_rng(79)
+    kinds = (rng.standard_normal((2, nkv * hd)) * 0.05).astype(np.float16)
+    for b, n in enumerate(np.array(lens) + counts):
+        for i, slot in enumerate(a["table"][b, :(n + C - 1) // C]):
+            t = min(C, n - i * C)
+            k, v = a["slab"][slot].reshape(2, -1)
+            k.reshape(C, -1)[:t] = kinds[np.arange(t) % 2]
+            v.reshape(-1, C)[:, :t] = np.where(np.arange(t) % 2 == 0, 1.0, -1.0)
+    ref, bound, _ = tree_oracle(a)
+    tree_check(a, tree_run(a))
+    worst = 0.0
+    for b, n in enumerate(lens):
+        for i in range(counts[b]):
+            r = a["off"][b] + i
+            for h in range(nq):
+                x, g = a["q"][r, h * hd:(h + 1) * hd].astype(np.float64), h // (nq // nkv) * hd
+                s = kinds[:, g:g + hd].astype(np.float64) @ x / np.sqrt(hd)
+                w, times = 2.0 ** 11 * np.exp(s - s.max()), np.array([(n + i + 2) // 2, (n + i + 1) // 2])
+                out = float(w.astype(np.float16).astype(np.float64) @ (times * [1, -1]) / (w @ times))
+                worst = max(worst, abs(out - ref[r, h * hd]) / bound[r, h * hd])
+    report("lower halves", worst=round(worst, 2))
+    assert worst > 1.5
+
+
 def test_tree_attention_captured_graph():
     """One graph over changing trees and lengths; its workspace holds the last replay's partials."""
     torch = torch_cuda()
