@@ -11,8 +11,11 @@
 // are numbered by prefix sums, and the k-th wanted one gets the k-th free one.
 //
 // All of it is latency: a table of 64 rows of 257 entries over 7000 slots is 66 KB.
-// Small tables (see small_table) one workgroup does with the counts in LDS (16 bits of
-// holders and 16 of writers a slot), others four launches do.
+// Up to kSmallSlots slots, kSmallRows rows and kSmallEntries entries one workgroup
+// does it with the counts in LDS (16 bits of holders and 16 of writers a slot), else four
+// launches do (64 rows of 257 entries over 7000 slots 17.9 us with
+// the empty copy behind it, in a graph, against 18.0, 16 rows of 67 11.7 against 18.0; 64
+// rows of 1000 entries 45 in one against 31).
 //
 // The copies are a launch of their own: 16 KB pieces, a workgroup each up to 8192 of
 // them, stored past the caches.  Of 16 layers of 1 MB slots, 50 moves and 12
@@ -205,22 +208,7 @@ __global__ __launch_bounds__(256) void pages_take_kernel(KvPages a) {
 }
 
 // ---- all of it in one workgroup
-// It takes its entries in turns of 8192, and waits for two trips to memory in each, so up to
-// two turns it is faster whatever the rows and slots, and with many rows, which are one
-// wave's work for the four launches, a while beyond.  us in a graph, one workgroup / four launches:
-//   entries   16 rows, 3000 slots   16 rows, 8192 slots   256-320 rows, 8192 slots   1024 rows, 3000 slots
-//      8192       9.5 / 13.8           11.9 / 15.5             12.0 / 18.4                10.6 / 25.9
-//     12288      12.2 / 13.6           15.0 / 16.1
-//     16384      12.7 / 13.8           15.3 / 15.8             16.0 / 18.6                14.3 / 26.2
-//     20480      15.6 / 14.2           18.4 / 15.9             19.1 / 19.6                17.3 / 25.9
-// and 64 rows of 1000 entries 45 / 31.  (Where all of many rows write the one chunk that they
-// share, each looks at the others: 1024 rows 69 / 25.)
-constexpr int kSmallSlots = 8192, kSmallRows = 1024, kSmallEntries = 16384, kSmallEntriesOfMany = 20480, kManyRows = 256;
-
-bool small_table(const KvPages& a) {
-  const int64_t entries = (int64_t)a.n_seq * a.n_table;
-  return a.n_slots <= kSmallSlots && a.n_seq <= kSmallRows && entries <= (a.n_seq < kManyRows ? kSmallEntries : kSmallEntriesOfMany);
-}
+constexpr int kSmallSlots = 8192, kSmallRows = 1024, kSmallEntries = 20480;
 
 // Which threads of the wave below this one have `on`, and how many have it in all.
 __device__ __forceinline__ int rank_of(uint64_t on) {
@@ -463,7 +451,7 @@ void launch_kv_pages(KvPages a, void* ws, hipStream_t s) {
   a.need = take(a.n_seq);
   a.forks = take(a.n_seq);
   a.sums = take(8);
-  if (small_table(a)) {
+  if (a.n_slots <= kSmallSlots && a.n_seq <= kSmallRows && entries <= kSmallEntries) {
     hipLaunchKernelGGL(pages_small_kernel, dim3(1), dim3(1024), 0, s, a);
     return;
   }
