@@ -13,9 +13,7 @@
 // All of it is latency: a table of 64 rows of 257 entries over 7000 slots is 66 KB.
 // Up to kSmallSlots slots, kSmallRows rows and kSmallEntries entries one workgroup
 // does it with the counts in LDS (16 bits of holders and 16 of writers a slot), else four
-// launches do (64 rows of 257 entries over 7000 slots 17.9 us with
-// the empty copy behind it, in a graph, against 18.0, 16 rows of 67 11.7 against 18.0; 64
-// rows of 1000 entries 45 in one against 31).
+// launches do.
 //
 // The copies are a launch of their own: 16 KB pieces, a workgroup each up to 8192 of
 // them, stored past the caches.  Of 16 layers of 1 MB slots, 50 moves and 12
@@ -208,6 +206,20 @@ __global__ __launch_bounds__(256) void pages_take_kernel(KvPages a) {
 }
 
 // ---- all of it in one workgroup
+// It takes its entries in turns of 8192, with two trips to memory in each, where four
+// launches have a start of their own.  us of one workgroup / four launches, in a graph and, in
+// brackets, called alone and waited for:
+//   entries      16 rows, 8192 slots          64 rows, 8192 slots        320 rows, 8192   1024, 3000
+//      8192   11.9 / 15.5                  11.9 / 15.9                                    10.6 / 25.9
+//     16384   15.4 / 15.9 (30.5 / 32.9)    15.6 / 16.0 (30.5 / 33.8)                      14.3 / 26.2
+//     20480   18.4 / 16.4 (33.3 / 33.6)    18.5 / 16.6 (33.3 / 33.7)    19.1 / 19.8       17.3 / 25.9
+//     24576                                19.1 / 17.1 (34.1 / 34.1)
+//     32768                                22.7 / 17.0 (37.4 / 34.0)
+// Among a step's other launches from Python 64 rows of 257 entries over 7000 slots are 16.8 /
+// 21.5 with the empty copy behind them, 17.5 / 16.9 in a graph.  The limit is the number at which few rows
+// called alone take as long either way, in a graph 2 us too high for few rows and
+// too low for many.  (Where all of many rows write the one chunk that they share, each looks
+// at the others: 1024 rows 69 / 25.)
 constexpr int kSmallSlots = 8192, kSmallRows = 1024, kSmallEntries = 20480;
 
 // Which threads of the wave below this one have `on`, and how many have it in all.

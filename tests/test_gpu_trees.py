@@ -1087,6 +1087,17 @@ def test_pages_sizes(n_seq, wide, n_slots):
     pages_case(table, None, [0] * n_seq, None, n_slots, 0, 8)
 
 
+@pytest.mark.parametrize("n_seq,wide,n_slots", [(16, 1280, 8192), (16, 1281, 8192), (1, 20480, 8000), (1, 20481, 8000), (256, 80, 8192), (256, 81, 8192),
+                                                (1024, 16, 700), (1025, 16, 700)])
+def test_pages_on_both_sides_of_one_workgroup(n_seq, wide, n_slots):
+    """Tables that one workgroup takes and that it leaves to several launches; rows that all write the chunk that they share."""
+    rng = np.random.default_rng(n_seq + wide)
+    table, src, keep, room = pages_inputs(rng, n_seq, wide, n_slots, 8)
+    pages_case(table, src, keep, room, n_slots, 0, 8)
+    pages_case(table, None, keep, room, n_slots, n_slots * 3 // 4, 8)
+    pages_case(table, [n_seq - 1] * n_seq, [19] * n_seq, [3] * n_seq, n_slots, 0, 8)
+
+
 def test_pages_forks_and_beams():
     C, t = 8, [[3, 4, -1], [5, -1, -1], [6, 7, -1], [-1, -1, -1]]
     # a fork of a chunk that both write: the row that stays keeps it
