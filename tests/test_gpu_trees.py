@@ -461,6 +461,17 @@ def test_tree_attention_many_sequences_of_wide_trees():
     tree_case(counts, lens, 64, 4, 2, 64, seed=61, mask=None)
 
 
+@pytest.mark.parametrize("nq,nkv,hd", [(4, 2, 64), (2, 2, 64), (8, 1, 128)])
+@pytest.mark.parametrize("rest", [1, 0])
+def test_tree_attention_a_piece_beside_many_short_sequences(rest, nq, nkv, hd):
+    """Tiles go by the average of the rows, far from any sequence's own."""
+    rng = np.random.default_rng(nq + rest)
+    counts, lens = np.full(40, rest), rng.integers(0, 500, 40)
+    counts[[7, 39]], lens[[7, 39]] = (130, 40), (900, 0)
+    tree_case(counts, lens, 16, nq, nkv, hd, seed=80, mask=None)
+    tree_case(counts, lens, 64, nq, nkv, hd, seed=81, mask="tree")
+
+
 def test_tree_attention_a_row_that_sees_nothing():
     a = tree_inputs([4, 3], [0, 0], 16, 4, 2, 64, seed=7, mask="any")
     a["mask"][:] = 0
