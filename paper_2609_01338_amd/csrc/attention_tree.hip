@@ -56,8 +56,9 @@ __device__ __forceinline__ Seq seq_of(const AttnTree& a, int b) {
 
 // Shares of `total` units: as many as there are workgroups, but of a.least units
 // at least, or where those are too few for the CUs, of a.fewest.  Each share costs
-// a start (10 us until its first tile is there) and fp32 partials: tiles of 128
-// columns want 8 units (8 ragged sequences of up to 4096 keys 40.8 us; at least 4:
+// a start and fp32 partials (32 ragged sequences: offsets and shares are known 3.9 us
+// after the launch, queries, table and first tile are there after 9.7, its scores after
+// 10.7): tiles of 128 columns want 8 units (8 ragged sequences of up to 4096 keys 40.8 us; at least 4:
 // 44.6; 8 of 26 nodes at 4096 keys 58, at least 12: 66), and 3 where one tree is all there
 // is (26 nodes at 2048 keys 15.5 us; 1: 16.4, 2: 17.0, 4: 19.3).
 __device__ __forceinline__ int shares(const AttnTree& a, int total) {
@@ -535,9 +536,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void tree_few_kernel(AttnTree a)
 // the loads would wait for them.
 //
 // Measured: 4 sequences of 24576 keys and 64 nodes, 8 KV heads of 128 with 4 query
-// heads each, 167-190 us as the power allows: 155 GFLOP with the weights' lower halves,
-// 122 us at the rate of a large f16 product (the matrix units are busy 51 % of
-// the cycles, at 1.7 GHz), loads alone 90.  One workgroup of 256 columns a CU,
+// heads each, 170 us call after call, 164-212 as the clock goes where a profiler lies
+// between the calls: 155 GFLOP with the weights' lower halves, 122 us at the rate of a
+// large f16 product (the matrix units are busy 51 % of the cycles, at 1.7 GHz), loads
+// alone 90.  (The last step of a piece multiplies scores that nobody uses, one
+// tile's K Q^T in 8 or more.)  All 256 registers are taken; 20 bytes a lane (SMALL: 56)
+// go to scratch before a piece's loop and come back after it.  One workgroup of 256 columns a CU,
 // which reads each key once, not twice, takes as long (184 for 187), and longer where
 // trees are smaller (32 ragged 129 for 101).  32 ragged sequences of up to 8192 keys and 16
 // nodes 90: 373 MB, loads alone 83.
@@ -1034,6 +1038,15 @@ int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 //   32 + 8 heads of 128:  4 x 5 at 1000 (20) 16.2 / 16.6 / 21.1, 32 x 5 at 4096 (20) 168 / 119 / 112,
 //     16 x 8 at 4096 (32) 93.7 / 69.4 / 65.8, 8 x 26 at 4096 (104) 156 / 102 / 59,
 //     4 x 64 at 24576 (256) 708 / 388 / 188
+// (So not every average gets its fastest tile: 2-12 % are lost at 20-32 columns, one way
+// or the other.)  What the rule does not see is how unlike the trees are; a prompt's
+// piece beside sequences of one row takes narrow tiles and reads its own keys once for
+// each of them (columns of the average; us again with 16 / 32 / 128):
+//   32 + 8 heads of 128:  256 rows beside 63 of 1 at 4096 (20) 349 / 288 / 246,
+//     512 beside 127 ragged to 8192 (20) 571 / 514 / 471
+//   32 + 8 heads of 64:  256 beside 63 at 4096 (20) 179 / 158 / 169
+//   32 + 8 heads of 128, beside sequences of no row:  256 and 63 at 4096 (16) 141 / 95 / 57,
+//     512 and 127 at 8192 (16) 504 / 270 / 133
 int tile_cols(int64_t cols) { return cols <= 16 ? 16 : cols <= 32 ? 32 : 128; }
 
 // Columns of a partial, of a call of `cols` columns a KV head in all.

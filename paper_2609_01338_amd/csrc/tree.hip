@@ -20,11 +20,13 @@
 // what has been written (places up to i) is never what is still to be read (path[j]
 // > i for j > i), so nothing waits for another wave.
 //
-// The branches of 64 trees of 61 nodes in 32 layers of 8 KV heads of 128 take 69 us:
-// the walk 15, reading 4, and writing 1.2 million lines of V^T, of which 2 bytes change,
-// 51.  Whole 64-byte lines are no faster than the 16 bytes.  So many lines want
-// all channels and many waves: 16384 workgroups (2048: 139), a sequence's slices on all
-// XCDs (on one: 87).  One tree of 7 nodes in 16 layers of 8 KV heads of 64 takes 4.3 us.
+// The branches of 64 trees of 61 nodes in 32 layers of 8 KV heads of 128 take 69 us.
+// A launch that ends behind the walk, which each of 16320 workgroups does for itself,
+// takes 15, one behind the slots 17, one that writes no V^T 46: reading 1.2 million lines
+// (160 MB) takes 28 and writing as many, of which 2 bytes change (42 MB), 24.  Both
+// are 43 at the rate of a large copy.  Whole 64-byte lines are no faster than the 16
+// bytes.  So many lines want all channels and many waves: 16384 workgroups (2048: 139), a
+// sequence's slices on all XCDs (on one: 87).  One tree of 7 nodes in 16 layers of 8 KV heads of 64 takes 4.3 us.
 #include "mz_kernels.h"
 
 namespace mzk {
