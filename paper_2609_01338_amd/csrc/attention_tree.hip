@@ -950,14 +950,13 @@ __global__ __launch_bounds__(256) void tree_join_kernel(AttnTree a) {
   const int t = threadIdx.x, dl = t % LPP, group = t / LPP, pg = group % NG;
   const int64_t first = (int64_t)blockIdx.x * ROWS, at = first + t / TPR, rows = (int64_t)a.m * a.nq;
   const int total = *a.total, nw = shares(a, total);
-  if (total == 0) return;              // (and rows is not filled, if offsets descend)
   bool again = false;
   const int r = (int)(min(at, rows - 1) / a.nq), hq = (int)(at - (int64_t)r * a.nq), h = hq / a.group;
   const int4 row = a.rows[r];          // first unit, units, tiles, first row of its sequence
   int n = 0;
   float m = -INFINITY, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (at < rows && row.y) {
+  if (at < rows && row.y && total > 0) {      // (no units: rows is not filled where offsets descend)
     const int x = (r - row.w) * a.group + hq - h * a.group, tile = x / R, c = x - tile * R;
     const int f0 = row.x + (h * row.z + tile) * row.y, g0 = share_of(f0, nw, total);
     n = share_of(f0 + row.y - 1, nw, total) - g0 + 1;
